@@ -290,6 +290,120 @@ int sage_attn_debug_qk(const sage_attn_args* args, int b, int h, int q_tile, int
 int sage_attn_debug_mfma_fp8(const uint8_t* a_codes, const uint8_t* b_codes, const float* c_in,
                              float* d_out, void* stream);
 
+/* ------------------------------------------------------------------------------------------------------------------
+ * Operators around the attention calls of a serving program: rotary positions of Q and K, 16-bit attention of a batch that
+ * shares a prefix, the attention weight that each key of a cache has received, and the eviction of the others.  The conventions at
+ * the head of this file hold for them too; d is 64, 128 or 256 and tensors are fp16 or bf16 throughout.  None of them allocates,
+ * synchronises or keeps anything between calls, so all can be captured into a graph; results do not depend on the order in
+ * which workgroups run.
+ *
+ * kv_lens (device, [B] int32, or NULL): how many leading tokens of each sequence's cache are in use, cut to 0 .. N_kv; NULL = N_kv
+ * for all.  Tokens behind them are not read as keys or values - whatever they hold, also NaN, changes nothing - and their
+ * places in an output stay as they were.  Under a causal mask query r of N sees key t iff t <= r + max(len - N, 0). */
+
+/* Rotary positions.  Channel pair i of the first rot_dim channels of every row is turned by the angle
+ * (position + offset) * inv_freq[i] and multiplied by scale:  (x, y) -> scale (x cos - y sin, x sin + y cos);  the others are copied.
+ * Angles are computed in 64 bits.  inverse: by the negative angle - with the same scale, the gradient of the forward rotation.
+ * In place is allowed (q_out = q and / or k_out = k, then with the same strides); other overlaps are not. */
+enum { SAGE_ROPE_PLAIN = 0, SAGE_ROPE_LINEAR = 1, SAGE_ROPE_BASE = 2, SAGE_ROPE_PARTS = 3 };
+typedef struct sage_rope_args {
+  const void* q;            /* device, [B, H, N, d] or [B, N, H, d]; rows are aligned to 2 bytes at least (16 is fastest) */
+  const void* k;            /* device, [B, H_kv, N, d] or [B, N, H_kv, d]; NULL: q only */
+  void* q_out;
+  void* k_out;              /* NULL iff k is */
+  int B, H, H_kv, N, d;
+  int rot_dim;              /* even, 2 .. d */
+  int dtype, layout;        /* SAGE_DT_*, SAGE_LAYOUT_* */
+  int interleaved;          /* 0: pair i is channels (i, i + rot_dim / 2); 1: channels (2 i, 2 i + 1) */
+  int inverse;
+  float scale;              /* 0 means 1 */
+  const double* inv_freq;   /* device, [rot_dim / 2]: radians per position, e.g. from sage_rope_frequencies */
+  const int* positions;     /* device, or NULL: token n stands at n.  positions[b * positions_stride + n] */
+  long long positions_stride;  /* 0: the same for every sequence */
+  long long offset;         /* added to every position */
+  /* Strides of batch, head and token in elements, for views - slices of a fused projection, rows of a cache; all 0: contiguous in
+     `layout`.  The channels of a row are contiguous, and no two rows of an output overlap. */
+  long long q_strides[3], k_strides[3], q_out_strides[3], k_out_strides[3];
+  void* stream;
+} sage_rope_args;
+int sage_rope(const sage_rope_args* args);
+
+/* Writes the rot_dim / 2 frequencies base^(-2 i / rot_dim) to inv_freq, on the HOST, for contexts `factor` times longer than
+ * the model was trained for:  SAGE_ROPE_LINEAR: all divided by factor;  SAGE_ROPE_BASE: base times
+ * factor^(rot_dim / (rot_dim - 2)), which keeps the fastest and divides the slowest by factor;  SAGE_ROPE_PARTS: those that make
+ * `high` turns or more in original_length tokens are kept, those that make `low` or fewer divided by factor, between them
+ * the weights move linearly with the turns.  factor >= 1.  Unused numbers are not looked at. */
+int sage_rope_frequencies(int rot_dim, double base, int scaling, double factor, double original_length, double low, double high,
+                          double* inv_freq);
+
+/* Attention of N new queries per sequence over keys and values that all sequences of the batch share - a system prompt, a
+ * document - followed by each sequence's own:  out = softmax(sm_scale Q [K_prefix; K]^T) [V_prefix; V].  Nothing is quantized: K and V
+ * are read as they are, scores, softmax and sums are FP32, P is rounded to the 16-bit type for its product with V.  The prefix
+ * is read once for the whole batch.  Meant for decode steps and short chunks of queries.  Every query sees the whole prefix; `causal`
+ * masks the own keys (see above).  A query without any key gets zeros and lse = -inf. */
+typedef struct sage_attn_shared_prefix_args {
+  const void* q;            /* device, [B, H, N, d] or [B, N, H, d] */
+  const void* k_prefix;     /* device, [H_kv, N_prefix, d] or [N_prefix, H_kv, d]; not read if N_prefix = 0 */
+  const void* v_prefix;
+  const void* k;            /* device, [B, H_kv, N_kv, d] or [B, N_kv, H_kv, d]; not read if N_kv = 0 */
+  const void* v;
+  void* out;                /* device, like q */
+  const int* kv_lens;
+  float* lse;               /* device, [B, H, N] f32, or NULL: natural-log-sum-exp of a row's scaled scores */
+  int B, H, H_kv, N, N_prefix, N_kv, d;
+  int causal;
+  float sm_scale;           /* <= 0 means 1/sqrt(d) */
+  int dtype, layout;
+  void* workspace;          /* device, 256-byte aligned */
+  size_t workspace_bytes;
+  void* stream;
+} sage_attn_shared_prefix_args;
+size_t sage_attn_shared_prefix_workspace_bytes(const sage_attn_shared_prefix_args* args);   /* 0 if the arguments are invalid */
+int sage_attn_shared_prefix(const sage_attn_shared_prefix_args* args);
+
+/* The attention weight that each key has received from N queries of the heads that read it:
+ *   weights[b, j, t] = weights_in[b, j, t] + sum over heads h of KV head j, queries r that see t of exp(sm_scale <q_r, k_t> - lse[b, h, r])
+ * with the log-sum-exp that an attention call returned (over these keys and any others).  Sums are FP32, in a fixed order.  Added up
+ * over the steps of a generation it is what sage_cache_evict goes by. */
+typedef struct sage_attn_key_weights_args {
+  const void* q;            /* device, [B, H, N, d] or [B, N, H, d] */
+  const void* k;            /* device, [B, H_kv, N_kv, d] or [B, N_kv, H_kv, d] */
+  const float* lse;         /* device, [B, H, N] f32.  A query whose lse is -inf saw no key: it adds nothing */
+  const float* weights_in;  /* device, [B, H_kv, N_kv] f32, or NULL: zeros.  May be `weights` */
+  float* weights;           /* device, [B, H_kv, N_kv] f32 */
+  const int* kv_lens;
+  int B, H, H_kv, N, N_kv, d;
+  int causal;
+  float sm_scale;           /* <= 0 means 1/sqrt(d) */
+  int dtype, layout;
+  void* workspace;          /* device, 256-byte aligned; may be NULL where the size is 0 */
+  size_t workspace_bytes;
+  void* stream;
+} sage_attn_key_weights_args;
+size_t sage_attn_key_weights_workspace_bytes(const sage_attn_key_weights_args* args);   /* 0: none is needed, or the arguments are invalid */
+int sage_attn_key_weights(const sage_attn_key_weights_args* args);
+
+/* Eviction from a cache.  Of each sequence and KV head the first `sink` tokens in use, the last `recent` and, of those between,
+ * the ones with the largest weights are kept, N_keep in all (all of them if no more than N_keep are in use): ties go to the lowest
+ * index, a NaN counts as less than any weight.  Kept tokens keep their order and go to the front of the outputs.  The outputs
+ * overlap neither the inputs nor each other. */
+typedef struct sage_cache_evict_args {
+  const void* k;            /* device, [B, H_kv, N_kv, d] or [B, N_kv, H_kv, d] */
+  const void* v;
+  const float* weights;     /* device, [B, H_kv, N_kv] f32, e.g. from sage_attn_key_weights */
+  const int* kv_lens;
+  void* k_out;              /* device, [B, H_kv, N_keep, d] or [B, N_keep, H_kv, d] */
+  void* v_out;
+  float* weights_out;       /* device, [B, H_kv, N_keep] f32, or NULL */
+  int* kept;                /* device, [B, H_kv, N_keep] int32: which tokens, ascending */
+  int* lens_out;            /* device, [B] int32: min(len, N_keep) */
+  int B, H_kv, N_kv, N_keep, d;
+  int sink, recent;         /* sink + recent <= N_keep */
+  int dtype, layout;
+  void* stream;
+} sage_cache_evict_args;
+int sage_cache_evict(const sage_cache_evict_args* args);
+
 const char* sage_status_string(int status);
 
 #ifdef __cplusplus

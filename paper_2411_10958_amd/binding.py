@@ -57,6 +57,34 @@ class sage_quant_out(ctypes.Structure):
                                               "v_scale", "k_mean", "q_mean", "delta_s", "v_mean")]
 
 
+class sage_rope_args(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("q", "k", "q_out", "k_out")] + \
+               [(n, ctypes.c_int) for n in ("B", "H", "H_kv", "N", "d", "rot_dim", "dtype", "layout", "interleaved", "inverse")] + \
+               [("scale", ctypes.c_float), ("inv_freq", ctypes.c_void_p), ("positions", ctypes.c_void_p),
+                ("positions_stride", ctypes.c_longlong), ("offset", ctypes.c_longlong)] + \
+               [(n, ctypes.c_longlong * 3) for n in ("q_strides", "k_strides", "q_out_strides", "k_out_strides")] + [("stream", ctypes.c_void_p)]
+
+
+class sage_attn_shared_prefix_args(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("q", "k_prefix", "v_prefix", "k", "v", "out", "kv_lens", "lse")] + \
+               [(n, ctypes.c_int) for n in ("B", "H", "H_kv", "N", "N_prefix", "N_kv", "d", "causal")] + \
+               [("sm_scale", ctypes.c_float), ("dtype", ctypes.c_int), ("layout", ctypes.c_int), ("workspace", ctypes.c_void_p),
+                ("workspace_bytes", ctypes.c_size_t), ("stream", ctypes.c_void_p)]
+
+
+class sage_attn_key_weights_args(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("q", "k", "lse", "weights_in", "weights", "kv_lens")] + \
+               [(n, ctypes.c_int) for n in ("B", "H", "H_kv", "N", "N_kv", "d", "causal")] + \
+               [("sm_scale", ctypes.c_float), ("dtype", ctypes.c_int), ("layout", ctypes.c_int), ("workspace", ctypes.c_void_p),
+                ("workspace_bytes", ctypes.c_size_t), ("stream", ctypes.c_void_p)]
+
+
+class sage_cache_evict_args(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("k", "v", "weights", "kv_lens", "k_out", "v_out", "weights_out", "kept", "lens_out")] + \
+               [(n, ctypes.c_int) for n in ("B", "H_kv", "N_kv", "N_keep", "d", "sink", "recent", "dtype", "layout")] + \
+               [("stream", ctypes.c_void_p)]
+
+
 def lib_path():
     """The in-tree library; SAGEATTN_LIB may name another build of the same sources."""
     return os.environ.get("SAGEATTN_LIB") or os.path.join(_PKG, "libsageattn.so")
@@ -93,6 +121,14 @@ def load_library():
         lib.sage_attn_debug_qk.argtypes = [P(sage_attn_args)] + [ctypes.c_int] * 4 + [ctypes.c_void_p]
         lib.sage_attn_debug_mfma_fp8.restype = ctypes.c_int
         lib.sage_attn_debug_mfma_fp8.argtypes = [ctypes.c_void_p] * 5
+        for name in ("sage_rope", "sage_attn_shared_prefix", "sage_attn_key_weights", "sage_cache_evict"):
+            getattr(lib, name).restype = ctypes.c_int
+            getattr(lib, name).argtypes = [P(globals()[name + "_args"])]
+        for name in ("sage_attn_shared_prefix", "sage_attn_key_weights"):
+            getattr(lib, name + "_workspace_bytes").restype = ctypes.c_size_t
+            getattr(lib, name + "_workspace_bytes").argtypes = [P(globals()[name + "_args"])]
+        lib.sage_rope_frequencies.restype = ctypes.c_int
+        lib.sage_rope_frequencies.argtypes = [ctypes.c_int, ctypes.c_double, ctypes.c_int] + [ctypes.c_double] * 4 + [ctypes.c_void_p]
         lib.sage_status_string.restype = ctypes.c_char_p
         lib.sage_status_string.argtypes = [ctypes.c_int]
         _LIB = lib
@@ -372,3 +408,278 @@ def sage_attn_debug_mfma_fp8(a_codes, b_codes, c_in):
     _check(load_library().sage_attn_debug_mfma_fp8(_ptr(a_codes), _ptr(b_codes), _ptr(c_in), _ptr(d), s),
            "sage_attn_debug_mfma_fp8")
     return d
+
+
+# ---- operators around the attention calls: rotary positions, a shared prefix, key weights, eviction ----
+
+SAGE_ROPE_PLAIN, SAGE_ROPE_LINEAR, SAGE_ROPE_BASE, SAGE_ROPE_PARTS = 0, 1, 2, 3
+_ROPE_SCALINGS = {"plain": 0, "linear": 1, "base": 2, "parts": 3, 0: 0, 1: 1, 2: 2, 3: 3}
+
+
+def _need(name, t, device, dtype, shape=None, dims=None, contiguous=True):
+    """Raises unless t is a tensor of that kind on that GPU.  shape: exact; dims: its number of dimensions."""
+    if not t.is_cuda or t.device != device:
+        raise ValueError(f"{name} must be on {device}, like q or k")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    if dims is not None and t.dim() != dims:
+        raise ValueError(f"{name} must have {dims} dimensions, got {t.dim()}")
+    if contiguous and not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+
+
+def _address(t):
+    return 0 if t is None else t.data_ptr()
+
+
+def _call(name, args, device):
+    """One entry point with its argument structure, on the device of its tensors."""
+    f = getattr(load_library(), name)
+    if torch.cuda.current_device() == device.index:
+        status = f(ctypes.byref(args))
+    else:
+        with torch.cuda.device(device):
+            status = f(ctypes.byref(args))
+    if status != 0:
+        raise SageError(status, name)
+
+
+def _raw_stream(stream, device):
+    return _current_raw_stream(device.index) if stream is None else stream.cuda_stream
+
+
+def _own_workspace(name, args, device, workspace, stream):
+    """Points args at `workspace`, or at a new one.  The result has to live until the call is enqueued."""
+    if workspace is None:
+        need = int(getattr(load_library(), name + "_workspace_bytes")(ctypes.byref(args)))
+        if need == 0:
+            return None
+        workspace = torch.empty(need, dtype=torch.uint8, device=device)
+        if stream is not None:
+            workspace.record_stream(stream)      # allocated on the current stream, used on another one
+    elif not workspace.is_cuda or workspace.device != device or not workspace.is_contiguous():
+        raise ValueError(f"workspace must be a contiguous tensor on {device}")
+    args.workspace, args.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    return workspace
+
+
+def _sizes(x, layout):
+    """B, heads, tokens, d of a 4-D tensor."""
+    return (x.shape[0], x.shape[2], x.shape[1], x.shape[3]) if layout else tuple(x.shape)
+
+
+def _shape_of(layout, B, heads, tokens, d):
+    return (B, tokens, heads, d) if layout else (B, heads, tokens, d)
+
+
+def sage_rope_frequencies(rot_dim, base=10000.0, scaling="plain", factor=1.0, original_length=0.0, low=1.0, high=32.0, device=None):
+    """The rot_dim / 2 frequencies, in radians per position, for sage_rope: a float64 tensor on `device` (None: the current GPU).
+    scaling: "plain"; for contexts `factor` times longer than trained for, "linear" (all divided by it), "base" (the base raised so that
+    the slowest is divided by it) or "parts" (those that turn `high` times or more in original_length tokens kept, `low` times or fewer
+    divided, linear between)."""
+    out = (ctypes.c_double * max(int(rot_dim) // 2, 1))()
+    _check(load_library().sage_rope_frequencies(int(rot_dim), float(base), _ROPE_SCALINGS[scaling], float(factor), float(original_length),
+                                                float(low), float(high), ctypes.cast(out, ctypes.c_void_p)), "sage_rope_frequencies")
+    return torch.tensor(list(out), dtype=torch.float64, device="cuda" if device is None else device)
+
+
+def sage_rope(q, k=None, inv_freq=None, positions=None, offset=0, interleaved=False, inverse=False, scale=1.0, layout="HND", q_out=None,
+              k_out=None, stream=None):
+    """Rotary positions of q and k in one launch: the first 2 * len(inv_freq) channels of every row are turned, the others copied.
+    q [B, H, N, d], k [B, H_kv, N, d] or None (layout "HND"; tokens outside heads with "NHD"), or packed [tokens, heads, d] with positions
+    [tokens].  Any strides will do while the channels are contiguous.  positions: int32 [N] or [B, N] (None: 0 .. N - 1), `offset` is
+    added.  inverse turns back; with the same scale that is the gradient.  q_out, k_out may be q and k.  Returns q_out, or
+    (q_out, k_out)."""
+    if inv_freq is None:
+        raise ValueError("inv_freq is needed (see sage_rope_frequencies)")
+    dtype, device = _dtype_code(q), q.device
+    if not q.is_cuda or q.dim() not in (3, 4):
+        raise ValueError("q must be a 4-D, or packed 3-D, GPU tensor")
+    nhd = _LAYOUTS[layout]
+    packed = q.dim() == 3
+    if packed:
+        nhd = 1
+    _need("inv_freq", inv_freq, device, torch.float64, dims=1)
+    a = sage_rope_args()
+    pairs = [("q", q, q_out, a.q_strides, a.q_out_strides)]
+    if k is not None:
+        _need("k", k, device, q.dtype, dims=q.dim(), contiguous=False)
+        pairs.append(("k", k, k_out, a.k_strides, a.k_out_strides))
+    elif k_out is not None:
+        raise ValueError("k_out without k")
+    outs = []
+    for name, x, y, xs, ys in pairs:
+        if y is None:
+            y = torch.empty(x.shape, dtype=x.dtype, device=device)
+            if stream is not None:
+                y.record_stream(stream)
+        else:
+            _need(name + "_out", y, device, q.dtype, shape=x.shape, contiguous=False)
+        outs.append(y)
+        for t, st in ((x, xs), (y, ys)):
+            s = t.stride()
+            if s[-1] != 1:
+                raise ValueError(f"{name}: the channels of a row must be contiguous")
+            if packed:
+                s = (0,) + s[:-1]
+            st[0], st[1], st[2] = (s[0], s[2], s[1]) if nhd else s[:3]
+    B, H, N, d = _sizes(q.unsqueeze(0) if packed else q, nhd)
+    Bk, Hkv, Nk, dk = _sizes(k.unsqueeze(0) if packed else k, nhd) if k is not None else (B, 0, N, d)
+    if (Bk, Nk, dk) != (B, N, d):
+        raise ValueError("k shape does not match q")
+    if positions is not None:
+        _need("positions", positions, device, torch.int32)
+        if tuple(positions.shape) not in ((N,), (B, N)):
+            raise ValueError(f"positions must have shape ({N},) or ({B}, {N}), got {tuple(positions.shape)}")
+        a.positions, a.positions_stride = positions.data_ptr(), N if positions.dim() == 2 else 0
+    elif packed:
+        raise ValueError("a packed batch needs positions")
+    if q.numel() == 0:
+        raise ValueError("q is empty")
+    a.q, a.k, a.q_out, a.k_out = q.data_ptr(), _address(k), outs[0].data_ptr(), outs[1].data_ptr() if k is not None else 0
+    a.B, a.H, a.H_kv, a.N, a.d, a.rot_dim, a.dtype, a.layout = B, H, Hkv, N, d, 2 * inv_freq.numel(), dtype, nhd
+    a.interleaved, a.inverse, a.scale, a.inv_freq, a.offset = int(bool(interleaved)), int(bool(inverse)), float(scale), inv_freq.data_ptr(), int(offset)
+    a.stream = _raw_stream(stream, device)
+    _call("sage_rope", a, device)
+    return outs[0] if k is None else tuple(outs)
+
+
+def _shared_prefix_args(q, k_prefix, v_prefix, k, v, kv_lens, out, causal, sm_scale, layout, stream):
+    dtype, device, nhd = _dtype_code(q), q.device, _LAYOUTS[layout]
+    _need("q", q, device, q.dtype, dims=4)
+    B, H, N, d = _sizes(q, nhd)
+    a = sage_attn_shared_prefix_args()
+    if (k_prefix is None) != (v_prefix is None) or (k is None) != (v is None) or (k is None and k_prefix is None):
+        raise ValueError("a prefix, own keys and values, or both are needed, each with its values")
+    Hkv = None
+    if k_prefix is not None:
+        _need("k_prefix", k_prefix, device, q.dtype, dims=3)
+        _need("v_prefix", v_prefix, device, q.dtype, shape=k_prefix.shape)
+        P, Hkv, dp = (k_prefix.shape[0], k_prefix.shape[1], k_prefix.shape[2]) if nhd else (k_prefix.shape[1], k_prefix.shape[0], k_prefix.shape[2])
+        if dp != d:
+            raise ValueError("the prefix does not match q")
+        a.k_prefix, a.v_prefix, a.N_prefix = k_prefix.data_ptr(), v_prefix.data_ptr(), P
+    if k is not None:
+        _need("k", k, device, q.dtype, dims=4)
+        _need("v", v, device, q.dtype, shape=k.shape)
+        Bk, Hk, Nk, dk = _sizes(k, nhd)
+        if (Bk, dk) != (B, d) or (Hkv is not None and Hk != Hkv):
+            raise ValueError("k does not match q or the prefix")
+        Hkv = Hk
+        a.k, a.v, a.N_kv = k.data_ptr(), v.data_ptr(), Nk
+    if kv_lens is not None:
+        _need("kv_lens", kv_lens, device, torch.int32, shape=(B,))
+        a.kv_lens = kv_lens.data_ptr()
+    if out is not None:
+        _need("out", out, device, q.dtype, shape=q.shape)
+        a.out = out.data_ptr()
+    a.q = q.data_ptr()
+    a.B, a.H, a.H_kv, a.N, a.d, a.causal, a.sm_scale, a.dtype, a.layout = B, H, Hkv, N, d, int(bool(causal)), float(sm_scale), dtype, nhd
+    a.stream = _raw_stream(stream, device)
+    return a
+
+
+def sage_attn_shared_prefix_workspace_bytes(args):
+    return int(load_library().sage_attn_shared_prefix_workspace_bytes(ctypes.byref(args)))
+
+
+def sage_attn_shared_prefix(q, k_prefix, v_prefix, k=None, v=None, kv_lens=None, out=None, causal=True, sm_scale=0.0, layout="HND",
+                            return_lse=False, workspace=None, stream=None):
+    """16-bit attention of q [B, H, N, d] over a prefix [H_kv, P, d] that all sequences share (None: none), then over each
+    sequence's own k, v [B, H_kv, N_kv, d] (None: none), of which the first kv_lens (int32 [B]; None: all) are in use.  Layout "NHD":
+    tokens outside heads in all of them.  causal masks the own keys, aligned to the last query and key in use.  Returns out, or
+    (out, lse) with lse float32 [B, H, N]."""
+    if out is None:
+        out = torch.empty_like(q)
+        if stream is not None:
+            out.record_stream(stream)
+    a = _shared_prefix_args(q, k_prefix, v_prefix, k, v, kv_lens, out, causal, sm_scale, layout, stream)
+    lse = None
+    if return_lse:
+        lse = torch.empty((a.B, a.H, a.N), dtype=torch.float32, device=q.device)
+        if stream is not None:
+            lse.record_stream(stream)
+        a.lse = lse.data_ptr()
+    keep = _own_workspace("sage_attn_shared_prefix", a, q.device, workspace, stream)
+    _call("sage_attn_shared_prefix", a, q.device)
+    del keep
+    return (out, lse) if return_lse else out
+
+
+def sage_attn_key_weights_workspace_bytes(args):
+    return int(load_library().sage_attn_key_weights_workspace_bytes(ctypes.byref(args)))
+
+
+def sage_attn_key_weights(q, k, lse, weights_in=None, weights=None, kv_lens=None, causal=True, sm_scale=0.0, layout="HND", workspace=None,
+                          stream=None):
+    """What each key of k [B, H_kv, N_kv, d] has received of the attention of q [B, H, N, d] with log-sum-exp lse (float32 [B, H, N], as the
+    attention calls return it), summed over the queries of its KV head and added to weights_in.  Returns weights, float32
+    [B, H_kv, N_kv]; may be weights_in.  Entries behind kv_lens keep what they hold (zeros if the result is allocated here)."""
+    dtype, device, nhd = _dtype_code(q), q.device, _LAYOUTS[layout]
+    _need("q", q, device, q.dtype, dims=4)
+    _need("k", k, device, q.dtype, dims=4)
+    B, H, N, d = _sizes(q, nhd)
+    Bk, Hkv, Nk, dk = _sizes(k, nhd)
+    if (Bk, dk) != (B, d):
+        raise ValueError("k does not match q")
+    _need("lse", lse, device, torch.float32, shape=(B, H, N))
+    a = sage_attn_key_weights_args()
+    shape = (B, Hkv, Nk)
+    if weights_in is not None:
+        _need("weights_in", weights_in, device, torch.float32, shape=shape)
+        a.weights_in = weights_in.data_ptr()
+    if kv_lens is not None:
+        _need("kv_lens", kv_lens, device, torch.int32, shape=(B,))
+        a.kv_lens = kv_lens.data_ptr()
+    if weights is None:
+        weights = torch.zeros(shape, dtype=torch.float32, device=device) if kv_lens is not None else torch.empty(shape, dtype=torch.float32, device=device)
+        if stream is not None:
+            weights.record_stream(stream)
+    else:
+        _need("weights", weights, device, torch.float32, shape=shape)
+    a.q, a.k, a.lse, a.weights = q.data_ptr(), k.data_ptr(), lse.data_ptr(), weights.data_ptr()
+    a.B, a.H, a.H_kv, a.N, a.N_kv, a.d, a.causal, a.sm_scale, a.dtype, a.layout = B, H, Hkv, N, Nk, d, int(bool(causal)), float(sm_scale), dtype, nhd
+    a.stream = _raw_stream(stream, device)
+    keep = _own_workspace("sage_attn_key_weights", a, device, workspace, stream)
+    _call("sage_attn_key_weights", a, device)
+    del keep
+    return weights
+
+
+def sage_cache_evict(k, v, weights, n_keep, sink=0, recent=0, kv_lens=None, layout="HND", k_out=None, v_out=None, weights_out=None, kept=None,
+                     lens_out=None, stream=None):
+    """Cuts a cache k, v [B, H_kv, N_kv, d] to n_keep tokens per KV head: the first `sink` and the last `recent` of those in use
+    (kv_lens, int32 [B]; None: all) and the ones of largest weight (float32 [B, H_kv, N_kv]) between.  Returns (k_out, v_out,
+    weights_out, kept, lens_out): the rows kept, in their order, their weights, which they were (int32 [B, H_kv, n_keep]) and how many
+    (int32 [B]); what stands behind them keeps what it held (zeros where the output is allocated here)."""
+    dtype, device, nhd = _dtype_code(k), k.device, _LAYOUTS[layout]
+    _need("k", k, device, k.dtype, dims=4)
+    _need("v", v, device, k.dtype, shape=k.shape)
+    B, Hkv, Nk, d = _sizes(k, nhd)
+    n_keep = int(n_keep)
+    if n_keep < 1:
+        raise ValueError("n_keep must be at least 1")
+    _need("weights", weights, device, torch.float32, shape=(B, Hkv, Nk))
+    if kv_lens is not None:
+        _need("kv_lens", kv_lens, device, torch.int32, shape=(B,))
+    make = torch.zeros if kv_lens is not None or n_keep > Nk else torch.empty
+    rows, per = _shape_of(nhd, B, Hkv, n_keep, d), (B, Hkv, n_keep)
+    outs = []
+    for name, t, shape, dt in (("k_out", k_out, rows, k.dtype), ("v_out", v_out, rows, k.dtype), ("weights_out", weights_out, per, torch.float32),
+                               ("kept", kept, per, torch.int32), ("lens_out", lens_out, (B,), torch.int32)):
+        if t is None:
+            t = make(shape, dtype=dt, device=device)
+            if stream is not None:
+                t.record_stream(stream)
+        else:
+            _need(name, t, device, dt, shape=shape)
+        outs.append(t)
+    a = sage_cache_evict_args()
+    a.k, a.v, a.weights, a.kv_lens = k.data_ptr(), v.data_ptr(), weights.data_ptr(), _address(kv_lens)
+    a.k_out, a.v_out, a.weights_out, a.kept, a.lens_out = (t.data_ptr() for t in outs)
+    a.B, a.H_kv, a.N_kv, a.N_keep, a.d, a.sink, a.recent, a.dtype, a.layout = B, Hkv, Nk, n_keep, d, int(sink), int(recent), dtype, nhd
+    a.stream = _raw_stream(stream, device)
+    _call("sage_cache_evict", a, device)
+    return tuple(outs)

@@ -5,7 +5,8 @@ import sys
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
-SOURCES = ["sage_api.hip", "sage_prologue.hip", "sage_attn_kernel.hip", "sage_attn_raw.hip"]
+SOURCES = ["sage_api.hip", "sage_prologue.hip", "sage_attn_kernel.hip", "sage_attn_raw.hip", "sage_rope.hip",
+           "sage_attn_shared.hip", "sage_key_weights.hip", "sage_cache.hip"]
 LIB = os.path.join(PKG, "libsageattn.so")
 
 HIPCC_FLAGS = [

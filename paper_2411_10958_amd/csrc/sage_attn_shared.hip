@@ -1,0 +1,373 @@
+// 16-bit attention of a batch whose sequences share a prefix of keys and values (sage_attn_shared_prefix).
+//
+// O = softmax(kappa [Q Kp^T, Q Ko^T]) [Vp; Vo]: the prefix's keys are the same for every sequence, so the rows of one
+// product over them are the queries of all sequences and of all query heads of a KV head (B G N rows, G = H / H_kv), and the
+// prefix is read once instead of B times.  A sequence's own keys meet only its own G N rows.  The two parts, and chunks
+// of their keys, are independent workgroups of one launch; each leaves (m, l, O) under its own running maximum (Sec. 2.1, Eq. 1)
+// and a second kernel merges them: O = sum_i 2^(m_i - m) O_i / sum_i 2^(m_i - m) l_i.
+//
+// With few rows this reads the cache and nothing else bounds it, so K and V stay in the 16 bits they are kept in: quantizing them
+// on the way would cost vector instructions for nothing.  P is rounded to the type of V for the second product (half a step, 2^-9
+// of a weight with bf16, which averages out over the keys; the output is rounded to the same type); scores, the running
+// maximum, the sum and O are FP32.
+#include "sage_attn.h"
+#include "sage_ops.h"
+
+#include <algorithm>
+#include <cmath>
+
+namespace sage {
+namespace {
+
+constexpr int SH_ROWS = 128;     // query rows of a workgroup: 32 per wavefront
+constexpr int SH_KEYS = 64;      // keys of a tile
+
+struct SharedParams {
+  const unsigned short *q, *kp, *vp, *ko, *vo;
+  unsigned short* out;
+  float* lse;
+  const int* lens;
+  float *part_o, *part_ml;       // [partial][row][d], [partial][row][2]: see part_row
+  TensorMap qm, pm, om;          // of q and out; of the prefix; of the own caches
+  int B, H, Hkv, G, N, P, Nk;
+  int causal;
+  float kappa;                   // sm_scale log2(e)
+  int Sp, So;                    // key chunks of the prefix and of the own keys
+  int rtp, rto;                  // row tiles of the prefix (of B G N rows) and of the own keys (of G N rows)
+  int n_prefix;                  // workgroups of the prefix; those of the own keys follow
+};
+
+// Where partial result `s` of a row is kept: the prefix's chunks first, then the own ones.  Rows are numbered (KV head, batch, head of
+// the group, query), partials of one row are a chunk apart.
+__device__ __forceinline__ size_t part_row(const SharedParams& p, int s, int hkv, long long i) {
+  const size_t rows = (size_t)p.B * p.G * p.N;
+  return ((size_t)s * p.Hkv + hkv) * rows + i;
+}
+
+__device__ __forceinline__ int own_len(const SharedParams& p, int b) { return p.lens ? min(max(p.lens[b], 0), p.Nk) : p.Nk; }
+
+template <int D> constexpr int shared_occupancy() { return D == 64 ? 4 : D == 128 ? 2 : 1; }
+
+template <int D, bool BF16>
+__global__ void __launch_bounds__(256, shared_occupancy<D>()) k_shared(const SharedParams p) {
+  constexpr int NP = D / 8;                       // 16-byte pieces of a row
+  constexpr int KS = D / 16;                      // contraction steps of the score product
+  constexpr int CT = D / 32;                      // channel tiles of the output
+  constexpr int TILE = SH_KEYS * NP;              // pieces of a K (or V) tile
+  __shared__ v4i s_kv[2][2 * TILE];               // [stage][K, V]
+  const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
+  const int col = lane & 31, half = lane >> 5;
+
+  // ---- which rows and keys
+  int id = blockIdx.x, hkv, b = 0, rt, s;
+  const bool prefix = id < p.n_prefix;
+  if (prefix) {                                   // row tiles of one chunk side by side: they read the same keys
+    rt = id % p.rtp; id /= p.rtp;
+    hkv = id % p.Hkv; s = id / p.Hkv;
+  } else {
+    id -= p.n_prefix;
+    rt = id % p.rto; id /= p.rto;
+    hkv = id % p.Hkv; id /= p.Hkv;
+    b = id % p.B; s = id / p.B;
+  }
+  const int GN = p.G * p.N;
+  const long long rows = prefix ? (long long)p.B * GN : GN;
+  const long long r0 = (long long)rt * SH_ROWS;
+  const int nr = (int)min((long long)SH_ROWS, rows - r0);     // rows of this workgroup
+  const int nk = prefix ? p.P : own_len(p, b);
+  const int tiles = (nk + SH_KEYS - 1) / SH_KEYS, S = prefix ? p.Sp : p.So;
+  const int per = (tiles + S - 1) / S;
+  const int j0 = min(s * per, tiles), j1 = min(j0 + per, tiles);
+  const int sp = prefix ? s : p.Sp + s;
+  const long long i0 = prefix ? r0 : (long long)b * GN + r0;  // first row in the numbering of part_row
+
+  // Wavefronts: 32 rows each; with fewer than 65 rows, two share rows and take every other 32 keys
+  const int WK = nr <= 64 ? 2 : 1;
+  const int kg = WK == 2 ? wave & 1 : 0, rg = WK == 2 ? wave >> 1 : wave;
+  const bool active = rg * 32 < nr;
+
+  if (j0 >= j1) {                                 // no keys: a partial result that the merge skips
+    for (int i = t; i < nr; i += 256) {
+      float* ml = p.part_ml + part_row(p, sp, hkv, i0 + i) * 2;
+      ml[0] = -INFINITY;
+      ml[1] = 0.0f;
+    }
+    return;
+  }
+
+  // ---- my row's query as the B operand, and how many keys it sees
+  const int row = min(rg * 32 + col, nr - 1);
+  const long long i = i0 + row;
+  const int rb = (int)(i / GN), rgn = (int)(i - (long long)rb * GN), rg_h = rgn / p.N, rn = rgn - rg_h * p.N;
+  const size_t qrow = row_offset(p.qm, head_offset(p.qm, (unsigned)(rb * p.H + hkv * p.G + rg_h)), rn);
+  v4i q[KS];
+#pragma unroll
+  for (int st = 0; st < KS; ++st) q[st] = *reinterpret_cast<const v4i*>(p.q + qrow + 16 * st + 8 * half);
+  const int coff = max(nk - p.N, 0);
+  const int vis = prefix || !p.causal ? nk : min(coff + rn + 1, nk);
+  const int vis_all = prefix || !p.causal ? nk : min(coff + 1, nk);       // keys that every query sees
+
+  // ---- copies of a tile: rows behind the last key repeat it, so that masked places hold finite values where the keys do
+  const TensorMap& m = prefix ? p.pm : p.om;
+  const size_t head = head_offset(m, prefix ? (unsigned)hkv : (unsigned)(b * p.Hkv + hkv));
+  const char* gk = uniform_ptr(reinterpret_cast<const char*>((prefix ? p.kp : p.ko) + head));
+  const char* gv = uniform_ptr(reinterpret_cast<const char*>((prefix ? p.vp : p.vo) + head));
+  const unsigned lds0 = (unsigned)(size_t)(__attribute__((address_space(3))) char*)&s_kv[0][0];
+  const unsigned step = (unsigned)m.sn * 2;       // bytes from token to token
+  auto copy = [&](int j, int stage) {
+    const size_t at = (size_t)j * SH_KEYS * m.sn * 2;
+    const int last = nk - 1 - j * SH_KEYS;
+#pragma unroll
+    for (int x = 0; x < TILE / 256; ++x) {
+      const int pc = (x * 4 + wave) * 64 + lane, r = pc / NP, c = (pc % NP) ^ swizzle<D>(r);
+      const unsigned off = (unsigned)min(r, last) * step + (unsigned)c * 16;
+      const unsigned to = lds0 + (unsigned)(stage * 2 * TILE + (x * 4 + wave) * 64) * 16;
+      dma_b128(gk + at, off, to);
+      dma_b128(gv + at, off, to + TILE * 16);
+    }
+  };
+
+  v16f o[CT];
+#pragma unroll
+  for (int c = 0; c < CT; ++c)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) o[c][v] = 0.0f;
+  float mx = -INFINITY, l = 0.0f;                 // running maximum (of both halves) and this half's sum
+
+  copy(j0, 0);
+  for (int j = j0; j < j1; ++j) {
+    const int stage = (j - j0) & 1;
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();                 // tile j is there, and nobody reads the other stage any more
+    asm volatile("" ::: "memory");
+    if (j + 1 < j1) copy(j + 1, stage ^ 1);
+    if (!active) continue;
+    const v4i* tk = &s_kv[stage][0];
+    const v4i* tv = &s_kv[stage][TILE];
+    for (int sub = kg; sub < 2; sub += WK) {
+      const int key0 = j * SH_KEYS + 32 * sub;
+      if (key0 >= nk) break;
+      // S^T = K Q^T.  Operand row rho = 8g + 4h + r takes key 16 (g / 2) + 8h + 4 (g % 2) + r: half h of the lanes then has
+      // keys 8h + 0..7 and 16 + 8h + 0..7 of its query, in the order in which the second product wants them.
+      const int rho = col, kr = 32 * sub + 16 * (rho >> 4) + 8 * ((rho >> 2) & 1) + 4 * ((rho >> 3) & 1) + (rho & 3);
+      v16f sc;
+#pragma unroll
+      for (int v = 0; v < 16; ++v) sc[v] = 0.0f;
+#pragma unroll
+      for (int st = 0; st < KS; ++st) sc = mfma16<BF16>(tk[row_piece<D>(kr, 2 * st + half)], q[st], sc);
+      if (key0 + 32 > vis_all) {
+#pragma unroll
+        for (int v = 0; v < 16; ++v) sc[v] = key0 + 16 * (v >> 3) + 8 * half + (v & 7) < vis ? sc[v] : -INFINITY;
+      }
+      float top = sc[0];
+#pragma unroll
+      for (int v = 1; v < 16; ++v) top = fmaxf(top, sc[v]);
+      top = half_max(top) * p.kappa;
+      const float m_new = fmaxf(mx, top);
+      const float base = m_new == -INFINITY ? 0.0f : m_new;       // (no key seen yet: every weight 2^-inf)
+      if (__ballot(m_new > mx) != 0) {
+        const float alpha = __builtin_amdgcn_exp2f(mx - base);
+        l *= alpha;
+#pragma unroll
+        for (int c = 0; c < CT; ++c)
+#pragma unroll
+          for (int v = 0; v < 16; ++v) o[c][v] *= alpha;
+        mx = m_new;
+      }
+      float e[16];
+#pragma unroll
+      for (int v = 0; v < 16; ++v) e[v] = __builtin_amdgcn_exp2f(__fmaf_rn(sc[v], p.kappa, -base));
+      float sum = 0.0f;
+#pragma unroll
+      for (int v = 0; v < 16; ++v) sum += e[v];
+      l += sum;
+      v4i pb[2];
+#pragma unroll
+      for (int v = 0; v < 16; v += 2) pb[v >> 3][(v & 7) >> 1] = (int)pack16x2<BF16>(e[v], e[v + 1]);
+      // O^T += V^T P^T: a transposed read gives lane l channel l % 16 of the four keys whose rows its group of 16 lanes point at
+      const int g16 = lane & 15, ch = 16 * ((lane >> 4) & 1) + 4 * (g16 & 3);
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks) {
+        const int vr = 32 * sub + 16 * ks + 8 * half + (g16 >> 2);
+#pragma unroll
+        for (int c = 0; c < CT; ++c) {
+          typedef short v4s __attribute__((ext_vector_type(4)));
+          typedef __attribute__((address_space(3))) v4s* lds_v4s;
+          const int pc = (32 * c + ch) >> 3, in = ch & 4;
+          const short* a0 = reinterpret_cast<const short*>(&tv[row_piece<D>(vr, pc)]) + in;
+          const short* a1 = reinterpret_cast<const short*>(&tv[row_piece<D>(vr + 4, pc)]) + in;
+          const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s)a0);
+          const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s)a1);
+          const v8s a = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+          o[c] = mfma16<BF16>(__builtin_bit_cast(v4i, a), pb[ks], o[c]);
+        }
+      }
+    }
+  }
+  l = half_sum(l);
+
+  // ---- the two key groups of the same rows into one
+  if (WK == 2) {
+    float* x = reinterpret_cast<float*>(&s_kv[0][0]) + rg * 32 * (D + 2);
+    __syncthreads();
+    if (active && kg == 1) {
+#pragma unroll
+      for (int c = 0; c < CT; ++c)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) x[(16 * c + v) * 64 + lane] = o[c][v];
+      if (half == 0) {
+        x[32 * D + 2 * col] = mx;
+        x[32 * D + 2 * col + 1] = l;
+      }
+    }
+    __syncthreads();
+    if (kg == 1) return;
+    if (active) {
+      const float m1 = x[32 * D + 2 * col], l1 = x[32 * D + 2 * col + 1];
+      const float m_new = fmaxf(mx, m1), base = m_new == -INFINITY ? 0.0f : m_new;
+      const float a0 = __builtin_amdgcn_exp2f(mx - base), a1 = __builtin_amdgcn_exp2f(m1 - base);
+      l = l * a0 + l1 * a1;
+      mx = m_new;
+#pragma unroll
+      for (int c = 0; c < CT; ++c)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) o[c][v] = o[c][v] * a0 + x[(16 * c + v) * 64 + lane] * a1;
+    }
+  }
+  if (!active || rg * 32 + col >= nr) return;
+  const size_t pr = part_row(p, sp, hkv, i);
+  if (half == 0) {
+    p.part_ml[pr * 2] = mx;
+    p.part_ml[pr * 2 + 1] = l;
+  }
+  float* po = p.part_o + pr * D + 4 * half;
+#pragma unroll
+  for (int c = 0; c < CT; ++c)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const v4f y = {o[c][4 * g], o[c][4 * g + 1], o[c][4 * g + 2], o[c][4 * g + 3]};
+      *reinterpret_cast<v4f*>(po + 32 * c + 8 * g) = y;
+    }
+}
+
+// The partial results of a row into its output: D / 4 threads per row, four channels each.  Scores that are NaN leave their
+// mark in the sum, whatever the maximum.
+template <int D, bool BF16>
+__global__ void __launch_bounds__(256) k_shared_merge(const SharedParams p) {
+  constexpr int TPR = D / 4;
+  const long long rows = (long long)p.B * p.G * p.N;
+  const long long id = (long long)blockIdx.x * (256 / TPR) + threadIdx.x / TPR;
+  if (id >= rows * p.Hkv) return;
+  const int c = 4 * (threadIdx.x % TPR);
+  const int hkv = (int)(id / rows);
+  const long long i = id - hkv * rows;
+  const int GN = p.G * p.N, b = (int)(i / GN), rgn = (int)(i - (long long)b * GN), g = rgn / p.N, n = rgn - g * p.N;
+  const int S = p.Sp + p.So;
+  float m = -INFINITY;
+  for (int s = 0; s < S; ++s) m = fmaxf(m, p.part_ml[part_row(p, s, hkv, i) * 2]);
+  float l = 0.0f;
+  v4f acc = {0.0f, 0.0f, 0.0f, 0.0f};
+  for (int s = 0; s < S; ++s) {
+    const size_t pr = part_row(p, s, hkv, i);
+    const float ms = p.part_ml[pr * 2], ls = p.part_ml[pr * 2 + 1];
+    if (ms == -INFINITY && ls == 0.0f) continue;  // (no key of this chunk is seen: O may not even be there)
+    const float w = __builtin_amdgcn_exp2f(ms - m);
+    l = __fmaf_rn(w, ls, l);
+    const v4f x = *reinterpret_cast<const v4f*>(p.part_o + pr * D + c);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) acc[k] = __fmaf_rn(w, x[k], acc[k]);
+  }
+  const int h = hkv * p.G + g;
+  const bool none = m == -INFINITY && l == 0.0f;  // no key at all: zeros
+  const float inv = none ? 0.0f : __fdiv_rn(1.0f, l);
+  if (p.lse && c == 0) p.lse[((size_t)b * p.H + h) * p.N + n] = none ? -INFINITY : LN2 * (m + __builtin_amdgcn_logf(l));
+  unsigned short* y = p.out + row_offset(p.qm, head_offset(p.qm, (unsigned)(b * p.H + h)), n) + c;
+  *reinterpret_cast<uint2*>(y) = make_uint2(pack16x2<BF16>(acc[0] * inv, acc[1] * inv), pack16x2<BF16>(acc[2] * inv, acc[3] * inv));
+}
+
+// Key chunks: so many that the workgroups fill the places of the chip, each with at least four tiles.
+void choose_chunks(SharedParams* p, int d) {
+  const long long tp = (p->P + SH_KEYS - 1) / SH_KEYS, to = (p->Nk + SH_KEYS - 1) / SH_KEYS;
+  const long long np = (long long)p->Hkv * p->rtp, no = (long long)p->B * p->Hkv * p->rto;
+  const long long places = 256LL * (d == 64 ? 4 : d == 128 ? 2 : 1);
+  long long per = std::max(4LL, (np * tp + no * to + places - 1) / places);
+  p->Sp = (int)std::min(256LL, (tp + per - 1) / per);
+  p->So = (int)std::min(256LL, (to + per - 1) / per);
+}
+
+int shared_params(const sage_attn_shared_prefix_args* a, SharedParams* p, bool need_io) {
+  if (!a || a->B <= 0 || a->H <= 0 || a->H_kv <= 0 || a->N <= 0 || a->N_prefix < 0 || a->N_kv < 0) return SAGE_ERR_INVALID_ARG;
+  if (a->H % a->H_kv != 0) return SAGE_ERR_INVALID_ARG;
+  if (a->d != 64 && a->d != 128 && a->d != 256) return SAGE_ERR_UNSUPPORTED;
+  if (a->dtype != SAGE_DT_FP16 && a->dtype != SAGE_DT_BF16) return SAGE_ERR_UNSUPPORTED;
+  if (a->layout != SAGE_LAYOUT_HND && a->layout != SAGE_LAYOUT_NHD) return SAGE_ERR_UNSUPPORTED;
+  if (a->N > MAX_TOKENS || a->N_prefix > MAX_TOKENS || a->N_kv > MAX_TOKENS || (long long)a->B * a->H > 65535) return SAGE_ERR_UNSUPPORTED;
+  if (need_io) {
+    if (!a->q || !a->out || (a->N_prefix > 0 && (!a->k_prefix || !a->v_prefix)) || (a->N_kv > 0 && (!a->k || !a->v))) return SAGE_ERR_INVALID_ARG;
+    if ((((uintptr_t)a->q | (uintptr_t)a->out | (uintptr_t)a->k_prefix | (uintptr_t)a->v_prefix | (uintptr_t)a->k | (uintptr_t)a->v) & 15u) != 0)
+      return SAGE_ERR_INVALID_ARG;
+    if ((((uintptr_t)a->lse | (uintptr_t)a->kv_lens) & 3u) != 0) return SAGE_ERR_INVALID_ARG;
+  }
+  p->q = (const unsigned short*)a->q; p->kp = (const unsigned short*)a->k_prefix; p->vp = (const unsigned short*)a->v_prefix;
+  p->ko = (const unsigned short*)a->k; p->vo = (const unsigned short*)a->v; p->out = (unsigned short*)a->out;
+  p->lse = a->lse; p->lens = a->kv_lens;
+  p->B = a->B; p->H = a->H; p->Hkv = a->H_kv; p->G = a->H / a->H_kv; p->N = a->N; p->P = a->N_prefix; p->Nk = a->N_kv;
+  p->causal = a->causal != 0;
+  p->kappa = (a->sm_scale > 0.0f ? a->sm_scale : (float)(1.0 / std::sqrt((double)a->d))) * LOG2E;
+  const int nhd = a->layout == SAGE_LAYOUT_NHD;
+  p->qm = make_tensor_map(nhd, a->H, a->N, a->d);
+  p->pm = make_tensor_map(nhd, a->H_kv, a->N_prefix, a->d);
+  p->om = make_tensor_map(nhd, a->H_kv, a->N_kv, a->d);
+  const long long gn = (long long)p->G * p->N, rows = gn * p->B;
+  if (rows > (1LL << 30)) return SAGE_ERR_UNSUPPORTED;
+  p->rtp = (int)((rows + SH_ROWS - 1) / SH_ROWS);
+  p->rto = (int)((gn + SH_ROWS - 1) / SH_ROWS);
+  choose_chunks(p, a->d);
+  const long long np = (long long)p->Sp * p->Hkv * p->rtp, no = (long long)p->So * p->B * p->Hkv * p->rto;
+  if (np + no > 0x7fffffffLL || rows * p->Hkv > 0x7fffffffLL) return SAGE_ERR_UNSUPPORTED;
+  p->n_prefix = (int)np;
+  return SAGE_OK;
+}
+
+size_t part_rows(const SharedParams& p) { return (size_t)(p.Sp + p.So) * p.Hkv * p.B * p.G * p.N; }
+
+template <int D, bool BF16> hipError_t launch_shared(const SharedParams& p, hipStream_t s) {
+  const long long own = (long long)p.So * p.B * p.Hkv * p.rto, blocks = p.n_prefix + own;
+  if (blocks > 0) {
+    k_shared<D, BF16><<<(unsigned)blocks, 256, 0, s>>>(p);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  const long long rows = (long long)p.B * p.G * p.N * p.Hkv;
+  k_shared_merge<D, BF16><<<(unsigned)((rows + 256 / (D / 4) - 1) / (256 / (D / 4))), 256, 0, s>>>(p);
+  return hipGetLastError();
+}
+
+}  // namespace
+}  // namespace sage
+
+using namespace sage;
+
+extern "C" size_t sage_attn_shared_prefix_workspace_bytes(const sage_attn_shared_prefix_args* a) {
+  SharedParams p;
+  if (shared_params(a, &p, false) != SAGE_OK) return 0;
+  const size_t rows = part_rows(p);
+  return align256(align256(rows * 2 * sizeof(float)) + rows * a->d * sizeof(float)) + 256;
+}
+
+extern "C" int sage_attn_shared_prefix(const sage_attn_shared_prefix_args* a) {
+  SharedParams p;
+  int st = shared_params(a, &p, true);
+  if (st != SAGE_OK) return st;
+  if (!a->workspace || a->workspace_bytes < sage_attn_shared_prefix_workspace_bytes(a) || ((uintptr_t)a->workspace & 255u) != 0)
+    return SAGE_ERR_WORKSPACE;
+  p.part_ml = (float*)a->workspace;
+  p.part_o = (float*)((char*)a->workspace + align256(part_rows(p) * 2 * sizeof(float)));
+  const hipStream_t s = (hipStream_t)a->stream;
+  const bool bf16 = a->dtype == SAGE_DT_BF16;
+  hipError_t e;
+  if (a->d == 64) e = bf16 ? launch_shared<64, true>(p, s) : launch_shared<64, false>(p, s);
+  else if (a->d == 128) e = bf16 ? launch_shared<128, true>(p, s) : launch_shared<128, false>(p, s);
+  else e = bf16 ? launch_shared<256, true>(p, s) : launch_shared<256, false>(p, s);
+  return op_status(e);
+}

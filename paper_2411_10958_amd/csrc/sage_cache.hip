@@ -1,0 +1,196 @@
+// Eviction from a key / value cache (sage_cache_evict).
+#include "sage_attn.h"
+#include "sage_ops.h"
+
+#include <algorithm>
+
+namespace sage {
+namespace {
+
+struct EvictParams {
+  const unsigned short *k, *v;
+  const float* w;
+  const int* lens;
+  unsigned short *k_out, *v_out;
+  float* w_out;
+  int *kept, *lens_out;
+  int Hkv, N, keep, sink, recent;
+  TensorMap in, out;
+};
+
+// A weight as an unsigned number of the same order: NaN below everything, -0 with +0.
+__device__ __forceinline__ unsigned order_of(float w) {
+  const unsigned u = __float_as_uint(w + 0.0f);
+  const unsigned k = (u >> 31) ? ~u : u | 0x80000000u;
+  return w == w ? k : 0u;
+}
+
+constexpr int SEL_THREADS = 1024, SEL_WAVES = SEL_THREADS / 64;
+
+// Which tokens stay, one workgroup per sequence and KV head: the m-th largest weight between sink and recent, one digit of 8 bits
+// at a time by counting, then one pass in order that keeps what is larger and the first of what equals it.
+__global__ void __launch_bounds__(SEL_THREADS) k_evict_select(const EvictParams p) {
+  __shared__ unsigned s_hist[256];
+  __shared__ unsigned s_pick[2];
+  __shared__ unsigned s_gt[SEL_WAVES], s_eq[SEL_WAVES];
+  const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+  const int b = blockIdx.x / p.Hkv;
+  const int len = p.lens ? min(max(p.lens[b], 0), p.N) : p.N;
+  const float* w = p.w + (size_t)blockIdx.x * p.N;
+  int* kept = p.kept + (size_t)blockIdx.x * p.keep;
+  float* w_out = p.w_out ? p.w_out + (size_t)blockIdx.x * p.keep : nullptr;
+  if (t == 0 && blockIdx.x % p.Hkv == 0) p.lens_out[b] = min(len, p.keep);
+  if (len <= p.keep) {
+    for (int i = t; i < len; i += SEL_THREADS) {
+      kept[i] = i;
+      if (w_out) w_out[i] = w[i];
+    }
+    return;
+  }
+  const int c0 = p.sink, n = len - p.recent - p.sink, m = p.keep - p.sink - p.recent;     // n > m >= 0 tokens to choose from
+  for (int i = t; i < p.sink + p.recent; i += SEL_THREADS) {
+    const int from = i < p.sink ? i : len - p.recent + (i - p.sink), to = i < p.sink ? i : p.keep - p.recent + (i - p.sink);
+    kept[to] = from;
+    if (w_out) w_out[to] = w[from];
+  }
+  if (m == 0) return;
+  unsigned prefix = 0, need = (unsigned)m;
+  for (int shift = 24; shift >= 0; shift -= 8) {
+    if (t < 256) s_hist[t] = 0;
+    __syncthreads();
+    const unsigned mask = shift == 24 ? 0u : ~0u << (shift + 8);
+    for (int i = t; i < n; i += SEL_THREADS) {
+      const unsigned u = order_of(w[c0 + i]);
+      if ((u & mask) == prefix) atomicAdd(&s_hist[(u >> shift) & 255], 1u);
+    }
+    __syncthreads();
+    if (wave == 0) {            // lane l holds digits 255 - 4 l .. 252 - 4 l: from the largest down
+      unsigned c[4], sum = 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) { c[i] = s_hist[255 - 4 * lane - i]; sum += c[i]; }
+      unsigned upto = sum;
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const unsigned x = __shfl_up(upto, o);
+        if (lane >= o) upto += x;
+      }
+      unsigned before = upto - sum;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (before < need && before + c[i] >= need) { s_pick[0] = 255 - 4 * lane - i; s_pick[1] = before; }
+        before += c[i];
+      }
+    }
+    __syncthreads();
+    prefix |= s_pick[0] << shift;
+    need -= s_pick[1];
+  }
+  // wavefront w has the tokens of its own stretch, 64 at a time
+  const int seg = ((n + SEL_WAVES - 1) / SEL_WAVES + 63) / 64 * 64;
+  const int i0 = min(wave * seg, n), i1 = min(i0 + seg, n);
+  unsigned gt = 0, eq = 0;
+  for (int i = i0; i < i1; i += 64) {
+    const unsigned u = i + lane < i1 ? order_of(w[c0 + i + lane]) : 0u;
+    gt += (unsigned)__popcll(__ballot(i + lane < i1 && u > prefix));
+    eq += (unsigned)__popcll(__ballot(i + lane < i1 && u == prefix));
+  }
+  if (lane == 0) { s_gt[wave] = gt; s_eq[wave] = eq; }
+  __syncthreads();
+  unsigned above = 0, ties = 0;
+  for (int i = 0; i < wave; ++i) { above += s_gt[i]; ties += s_eq[i]; }
+  const unsigned long long below = (1ull << lane) - 1;
+  for (int i = i0; i < i1; i += 64) {
+    const bool in = i + lane < i1;
+    const float x = in ? w[c0 + i + lane] : 0.0f;
+    const unsigned u = order_of(x);
+    const unsigned long long bg = __ballot(in && u > prefix), be = __ballot(in && u == prefix);
+    const unsigned tie = ties + (unsigned)__popcll(be & below);
+    if (in && (u > prefix || (u == prefix && tie < need))) {
+      const unsigned to = (unsigned)p.sink + above + (unsigned)__popcll(bg & below) + min(tie, need);
+      kept[to] = c0 + i + lane;
+      if (w_out) w_out[to] = x;
+    }
+    above += (unsigned)__popcll(bg);
+    ties += (unsigned)__popcll(be);
+  }
+}
+
+// The rows of the kept tokens: a thread moves 16 bytes of K and of V of GU tokens.  Grid: (pieces of the kept tokens, heads).
+constexpr int GU = 4;
+template <int D> __global__ void __launch_bounds__(256) k_evict_rows(const EvictParams p) {
+  constexpr int P = D / 8, TOK = 256 / P;
+  const int b = blockIdx.y / p.Hkv;
+  const int len = p.lens ? min(max(p.lens[b], 0), p.N) : p.N, there = min(len, p.keep);
+  const int first = blockIdx.x * (TOK * GU) + threadIdx.x / P;
+  if (first >= there) return;
+  const int c = 8 * (threadIdx.x % P);
+  const int* kept = p.kept + (size_t)blockIdx.y * p.keep;
+  const size_t hi = head_offset(p.in, blockIdx.y) + c, ho = head_offset(p.out, blockIdx.y) + c;
+  int from[GU];
+#pragma unroll
+  for (int i = 0; i < GU; ++i) from[i] = kept[min(first + i * TOK, there - 1)];
+  v4i a[GU], x[GU];
+#pragma unroll
+  for (int i = 0; i < GU; ++i) {
+    const size_t at = row_offset(p.in, hi, from[i]);
+    a[i] = *reinterpret_cast<const v4i*>(p.k + at);
+    x[i] = *reinterpret_cast<const v4i*>(p.v + at);
+  }
+#pragma unroll
+  for (int i = 0; i < GU; ++i) {
+    if (first + i * TOK < there) {
+      const size_t at = row_offset(p.out, ho, first + i * TOK);
+      *reinterpret_cast<v4i*>(p.k_out + at) = a[i];
+      *reinterpret_cast<v4i*>(p.v_out + at) = x[i];
+    }
+  }
+}
+
+struct Span { const void* at; size_t bytes; };
+bool overlap(const Span& a, const Span& b) {
+  const uintptr_t x = (uintptr_t)a.at, y = (uintptr_t)b.at;
+  return a.at && b.at && x < y + b.bytes && y < x + a.bytes;
+}
+
+}  // namespace
+}  // namespace sage
+
+using namespace sage;
+
+extern "C" int sage_cache_evict(const sage_cache_evict_args* a) {
+  if (!a || a->B <= 0 || a->H_kv <= 0 || a->N_kv <= 0 || a->N_keep <= 0 || a->sink < 0 || a->recent < 0) return SAGE_ERR_INVALID_ARG;
+  if ((long long)a->sink + a->recent > a->N_keep) return SAGE_ERR_INVALID_ARG;
+  if (!a->k || !a->v || !a->weights || !a->k_out || !a->v_out || !a->kept || !a->lens_out) return SAGE_ERR_INVALID_ARG;
+  if (a->d != 64 && a->d != 128 && a->d != 256) return SAGE_ERR_UNSUPPORTED;
+  if (a->dtype != SAGE_DT_FP16 && a->dtype != SAGE_DT_BF16) return SAGE_ERR_UNSUPPORTED;
+  if (a->layout != SAGE_LAYOUT_HND && a->layout != SAGE_LAYOUT_NHD) return SAGE_ERR_UNSUPPORTED;
+  if (a->N_kv > MAX_TOKENS || a->N_keep > MAX_TOKENS || (long long)a->B * a->H_kv > 65535) return SAGE_ERR_UNSUPPORTED;
+  if ((((uintptr_t)a->k | (uintptr_t)a->v | (uintptr_t)a->k_out | (uintptr_t)a->v_out) & 15u) != 0) return SAGE_ERR_INVALID_ARG;
+  if ((((uintptr_t)a->weights | (uintptr_t)a->weights_out | (uintptr_t)a->kept | (uintptr_t)a->lens_out | (uintptr_t)a->kv_lens) & 3u) != 0)
+    return SAGE_ERR_INVALID_ARG;
+  const size_t heads = (size_t)a->B * a->H_kv, rows = heads * a->N_kv, out_rows = heads * a->N_keep;
+  const Span in[4] = {{a->k, rows * a->d * 2}, {a->v, rows * a->d * 2}, {a->weights, rows * 4}, {a->kv_lens, (size_t)a->B * 4}};
+  const Span out[5] = {{a->k_out, out_rows * a->d * 2}, {a->v_out, out_rows * a->d * 2}, {a->weights_out, out_rows * 4}, {a->kept, out_rows * 4},
+                       {a->lens_out, (size_t)a->B * 4}};
+  for (int i = 0; i < 5; ++i) {
+    for (const Span& s : in) if (overlap(out[i], s)) return SAGE_ERR_INVALID_ARG;
+    for (int j = 0; j < i; ++j) if (overlap(out[i], out[j])) return SAGE_ERR_INVALID_ARG;
+  }
+  EvictParams p;
+  p.k = (const unsigned short*)a->k; p.v = (const unsigned short*)a->v; p.w = a->weights; p.lens = a->kv_lens;
+  p.k_out = (unsigned short*)a->k_out; p.v_out = (unsigned short*)a->v_out; p.w_out = a->weights_out; p.kept = a->kept; p.lens_out = a->lens_out;
+  p.Hkv = a->H_kv; p.N = a->N_kv; p.keep = a->N_keep; p.sink = a->sink; p.recent = a->recent;
+  const int nhd = a->layout == SAGE_LAYOUT_NHD;
+  p.in = make_tensor_map(nhd, a->H_kv, a->N_kv, a->d);
+  p.out = make_tensor_map(nhd, a->H_kv, a->N_keep, a->d);
+  const hipStream_t s = (hipStream_t)a->stream;
+  k_evict_select<<<(unsigned)heads, SEL_THREADS, 0, s>>>(p);
+  int st = op_status(hipGetLastError());
+  if (st != SAGE_OK) return st;
+  const int per = 256 / (a->d / 8) * GU;
+  const dim3 grid((unsigned)((std::min(a->N_keep, a->N_kv) + per - 1) / per), (unsigned)heads);
+  if (a->d == 64) k_evict_rows<64><<<grid, 256, 0, s>>>(p);
+  else if (a->d == 128) k_evict_rows<128><<<grid, 256, 0, s>>>(p);
+  else k_evict_rows<256><<<grid, 256, 0, s>>>(p);
+  return op_status(hipGetLastError());
+}

@@ -1,0 +1,49 @@
+// Shared by the operators around attention (sage_rope.hip, sage_attn_shared.hip, sage_cache.hip).
+#pragma once
+#include "sage_attn_core.h"
+
+namespace sage {
+
+// The status of a launch: argument errors are found before it, so what is left is HIP's.  The error is cleared.
+inline int op_status(hipError_t e) {
+  if (e == hipSuccess) return 0;
+  (void)hipGetLastError();
+  return -4;      // SAGE_ERR_HIP
+}
+
+// 16-bit products on the matrix unit, 32 x 32 x 16: lane l supplies row (A) or column (B) l % 32 and contraction slots
+// 8 (l / 32) + 0..7; accumulator v of lane l is row 8 (v / 4) + 4 (l / 32) + v % 4, column l % 32.
+typedef short v8s __attribute__((ext_vector_type(8)));
+template <bool BF16> __device__ __forceinline__ v16f mfma16(v4i a, v4i b, v16f c) {
+  if constexpr (BF16) {
+    typedef __bf16 v8b __attribute__((ext_vector_type(8)));
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8b, a), __builtin_bit_cast(v8b, b), c, 0, 0, 0);
+  } else {
+    typedef _Float16 v8h __attribute__((ext_vector_type(8)));
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(v8h, a), __builtin_bit_cast(v8h, b), c, 0, 0, 0);
+  }
+}
+
+// Sum / maximum of a value over the two halves of the wavefront, in both.
+__device__ __forceinline__ float half_sum(float x) {
+  const unsigned u = __float_as_uint(x);
+  const auto sw = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  return __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
+}
+__device__ __forceinline__ float half_max(float x) {
+  const unsigned u = __float_as_uint(x);
+  const auto sw = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  return fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
+}
+
+// Rows of D 16-bit values in LDS, D / 8 pieces of 16 bytes each, as an LDS-DMA lays them down: piece c of row r stands at
+// piece c ^ swizzle(r) of the row.  Without it, the same piece of the rows that a matrix operand takes together would fall on the
+// same banks (a row is a multiple of 128 bytes).  The low two row bits go to piece bits 2 and 3 because a transposed read takes four
+// consecutive pieces of each of rows 4i .. 4i + 3 together.
+template <int D> __device__ __forceinline__ int swizzle(int r) {
+  if constexpr (D == 64) return ((r >> 1) & 1) << 2 | ((r >> 2) & 3);
+  return (r & 3) << 2 | ((r >> 2) & 3);
+}
+template <int D> __device__ __forceinline__ int row_piece(int r, int c) { return r * (D / 8) + (c ^ swizzle<D>(r)); }
+
+}  // namespace sage

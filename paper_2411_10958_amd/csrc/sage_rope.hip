@@ -1,0 +1,271 @@
+// Rotary positions of queries and keys (sage_rope) and their frequencies (sage_rope_frequencies).
+//
+// Channel pair i of the first `rot` channels is turned by the angle p f_i: (a, b) -> scale (a cos - b sin, b cos + a sin), the
+// pair being channels (i, i + rot/2) or (2i, 2i + 1).  Nothing but bytes moves this: every value is read and written once, 4 bytes.
+// A thread owns 2 VW channels of a token - VW pairs in either style - works their angles out once and then walks over heads, so the
+// FP64 product and the sine and cosine are shared by all of them.  Angles are taken in 64 bits (position 10^6 times the fastest
+// frequency in FP32 would be off by 0.03 rad), reduced to a fraction of a turn there, and their sine and cosine in FP32.
+#include "sage_attn.h"
+#include "sage_ops.h"
+
+#include <algorithm>
+#include <cmath>
+
+namespace sage {
+namespace {
+
+struct RopeTensor {
+  const unsigned short* x;
+  unsigned short* y;
+  long long xb, xh, xn, yb, yh, yn;      // strides of batch, head and token, in elements
+  int heads;
+};
+struct RopeParams {
+  RopeTensor q, k;                       // k.heads = 0 without keys
+  const double* inv_freq;
+  const int* positions;                  // null: the token's index
+  long long pos_sb, offset, total;       // total: units of all tokens
+  int N, d, rot, units, turned, hchunk;  // units per token, the first `turned` of which are rotated, the others copied
+  float scale, sign;
+};
+
+template <int VW> struct Vec;
+template <> struct Vec<8> { typedef uint4 type; };
+template <> struct Vec<4> { typedef uint2 type; };
+template <> struct Vec<1> { typedef unsigned short type; };
+
+template <bool BF16, int VW> __device__ __forceinline__ void unpack(const typename Vec<VW>::type& v, float (&f)[VW]) {
+  if constexpr (VW == 1) {
+    f[0] = load16<BF16>(v);
+  } else {
+    const unsigned* u = reinterpret_cast<const unsigned*>(&v);
+#pragma unroll
+    for (int i = 0; i < VW / 2; ++i) {
+      f[2 * i] = load16<BF16>((unsigned short)u[i]);
+      f[2 * i + 1] = load16<BF16>((unsigned short)(u[i] >> 16));
+    }
+  }
+}
+template <bool BF16, int VW> __device__ __forceinline__ typename Vec<VW>::type pack(const float (&f)[VW]) {
+  typename Vec<VW>::type v;
+  if constexpr (VW == 1) {
+    v = (unsigned short)pack16x2<BF16>(f[0], 0.0f);
+  } else {
+    unsigned* u = reinterpret_cast<unsigned*>(&v);
+#pragma unroll
+    for (int i = 0; i < VW / 2; ++i) u[i] = pack16x2<BF16>(f[2 * i], f[2 * i + 1]);
+  }
+  return v;
+}
+
+// One vector pair (channels c0.., c1..) of one head; INTER: element 2i, 2i + 1 of the two vectors laid end to end are a pair.
+template <bool BF16, int VW, bool INTER>
+__device__ __forceinline__ void turn(typename Vec<VW>::type& v0, typename Vec<VW>::type& v1, const float (&c)[VW], const float (&s)[VW]) {
+  float x[2 * VW], y[2 * VW], lo[VW], hi[VW];
+  unpack<BF16, VW>(v0, lo);
+  unpack<BF16, VW>(v1, hi);
+#pragma unroll
+  for (int i = 0; i < VW; ++i) { x[i] = lo[i]; x[VW + i] = hi[i]; }
+#pragma unroll
+  for (int i = 0; i < VW; ++i) {
+    const int a = INTER ? 2 * i : i, b = INTER ? 2 * i + 1 : VW + i;
+    y[a] = __fmaf_rn(x[a], c[i], -__fmul_rn(x[b], s[i]));
+    y[b] = __fmaf_rn(x[b], c[i], __fmul_rn(x[a], s[i]));
+  }
+#pragma unroll
+  for (int i = 0; i < VW; ++i) { lo[i] = y[i]; hi[i] = y[VW + i]; }
+  v0 = pack<BF16, VW>(lo);
+  v1 = pack<BF16, VW>(hi);
+}
+
+// Grid: (units of all tokens / 256, pieces of the heads).
+template <bool BF16, int VW, bool INTER>
+__global__ void __launch_bounds__(256) k_rope(const RopeParams p) {
+  const long long id = (long long)blockIdx.x * 256 + threadIdx.x;
+  if (id >= p.total) return;
+  const long long tok = id / p.units;
+  const int unit = (int)(id - tok * p.units);
+  const long long b = tok / p.N;
+  const int n = (int)(tok - b * p.N);
+  const bool turned = unit < p.turned;
+  float c[VW], s[VW];
+  int c0, c1;
+  if (turned) {
+    c0 = INTER ? 2 * VW * unit : VW * unit;
+    c1 = INTER ? c0 + VW : c0 + p.rot / 2;
+    const double at = (double)((p.positions ? (long long)p.positions[b * p.pos_sb + n] : (long long)n) + p.offset);
+#pragma unroll
+    for (int i = 0; i < VW; ++i) {
+      const double turns = at * p.inv_freq[VW * unit + i] * 0.15915494309189533577;      // 1 / (2 pi)
+      const float x = 2.0f * (float)(turns - rint(turns));
+      float si, co;
+      sincospif(x, &si, &co);
+      c[i] = __fmul_rn(co, p.scale);
+      s[i] = __fmul_rn(si, p.sign);
+    }
+  } else {                           // (what is left of a row is a multiple of two vectors too)
+    c0 = p.rot + (unit - p.turned) * 2 * VW;
+    c1 = c0 + VW;
+  }
+  const int h0 = blockIdx.y * p.hchunk, h1 = min(h0 + p.hchunk, p.q.heads + p.k.heads);
+  typedef typename Vec<VW>::type V;
+  constexpr int HU = 4;              // heads whose loads are in flight together
+  auto run = [&](const RopeTensor& t, int ha, int hb) {
+    const unsigned short* x = t.x + b * t.xb + (long long)n * t.xn;
+    unsigned short* y = t.y + b * t.yb + (long long)n * t.yn;
+    for (int h = ha; h < hb; h += HU) {
+      V v0[HU], v1[HU];
+#pragma unroll
+      for (int i = 0; i < HU; ++i) {
+        const unsigned short* r = x + (long long)min(h + i, hb - 1) * t.xh;
+        v0[i] = *reinterpret_cast<const V*>(r + c0);
+        v1[i] = *reinterpret_cast<const V*>(r + c1);
+      }
+#pragma unroll
+      for (int i = 0; i < HU; ++i) {
+        if (h + i >= hb) break;
+        if (turned) turn<BF16, VW, INTER>(v0[i], v1[i], c, s);
+        unsigned short* r = y + (long long)(h + i) * t.yh;
+        *reinterpret_cast<V*>(r + c0) = v0[i];
+        *reinterpret_cast<V*>(r + c1) = v1[i];
+      }
+    }
+  };
+  if (h0 < p.q.heads) run(p.q, h0, min(h1, p.q.heads));
+  if (h1 > p.q.heads) run(p.k, max(h0 - p.q.heads, 0), h1 - p.q.heads);
+}
+
+// Strides of one tensor, as given or contiguous in `layout`; false if they are not usable.
+bool tensor_strides(const long long* given, int layout, int heads, int N, int d, long long (&st)[3]) {
+  if (given[0] == 0 && given[1] == 0 && given[2] == 0) {
+    const TensorMap m = make_tensor_map(layout, heads, N, d);
+    st[0] = m.sb; st[1] = m.sh; st[2] = m.sn;
+    return true;
+  }
+  for (int i = 0; i < 3; ++i) {
+    if (given[i] < 0) return false;
+    st[i] = given[i];
+  }
+  return true;
+}
+
+// Whether no two rows of a tensor share a value: in the order of their strides, each extent steps over all that lies inside it.
+// (Rows of an output that did would be written by several threads.)
+bool rows_apart(const long long (&st)[3], long long B, long long heads, long long N, long long d) {
+  const long long extent[3] = {B, heads, N};
+  int at[3] = {0, 1, 2};
+  std::sort(at, at + 3, [&](int i, int j) { return st[i] < st[j]; });
+  long long span = d;
+  for (int i : at) {
+    if (extent[i] == 1) continue;
+    if (st[i] < span) return false;
+    span += st[i] * (extent[i] - 1);
+  }
+  return true;
+}
+
+template <bool BF16, int VW>
+void launch(const RopeParams& p, bool inter, dim3 grid, hipStream_t s) {
+  if (inter) k_rope<BF16, VW, true><<<grid, 256, 0, s>>>(p);
+  else k_rope<BF16, VW, false><<<grid, 256, 0, s>>>(p);
+}
+
+}  // namespace
+}  // namespace sage
+
+using namespace sage;
+
+extern "C" int sage_rope(const sage_rope_args* a) {
+  if (!a) return SAGE_ERR_INVALID_ARG;
+  const bool keys = a->k != nullptr;
+  if (a->B <= 0 || a->H <= 0 || a->N <= 0 || a->rot_dim <= 0 || (keys ? a->H_kv <= 0 : a->k_out != nullptr)) return SAGE_ERR_INVALID_ARG;
+  if (!a->q || !a->q_out || (keys && !a->k_out) || !a->inv_freq) return SAGE_ERR_INVALID_ARG;
+  if (a->d != 64 && a->d != 128 && a->d != 256) return SAGE_ERR_UNSUPPORTED;
+  if (a->rot_dim % 2 != 0 || a->rot_dim > a->d) return SAGE_ERR_UNSUPPORTED;
+  if (a->dtype != SAGE_DT_FP16 && a->dtype != SAGE_DT_BF16) return SAGE_ERR_UNSUPPORTED;
+  if (a->layout != SAGE_LAYOUT_HND && a->layout != SAGE_LAYOUT_NHD) return SAGE_ERR_UNSUPPORTED;
+  if (a->N > MAX_TOKENS || a->B > 65535 || a->H > 65535 || a->H_kv > 65535) return SAGE_ERR_UNSUPPORTED;
+  if ((a->interleaved & ~1) != 0 || (a->inverse & ~1) != 0) return SAGE_ERR_UNSUPPORTED;
+  if ((((uintptr_t)a->q | (uintptr_t)a->k | (uintptr_t)a->q_out | (uintptr_t)a->k_out) & 1u) != 0) return SAGE_ERR_INVALID_ARG;
+  if (((uintptr_t)a->inv_freq & 7u) != 0 || ((uintptr_t)a->positions & 3u) != 0 || a->positions_stride < 0) return SAGE_ERR_INVALID_ARG;
+  if (!std::isfinite(a->scale)) return SAGE_ERR_INVALID_ARG;
+
+  RopeParams p;
+  long long st[4][3];
+  const long long* given[4] = {a->q_strides, a->k_strides, a->q_out_strides, a->k_out_strides};
+  for (int i = 0; i < 4; ++i) {
+    const int heads = (i & 1) ? a->H_kv : a->H;
+    if ((i & 1) && !keys) { st[i][0] = st[i][1] = st[i][2] = 0; continue; }
+    if (!tensor_strides(given[i], a->layout, heads, a->N, a->d, st[i])) return SAGE_ERR_INVALID_ARG;
+    if (i >= 2 && !rows_apart(st[i], a->B, heads, a->N, a->d)) return SAGE_ERR_INVALID_ARG;
+  }
+  for (int i = 0; i < 2; ++i) {          // in place: the same rows, or a thread would overwrite what another has still to read
+    const bool same = i == 0 ? a->q == a->q_out : keys && a->k == a->k_out;
+    const int heads = i == 0 ? a->H : a->H_kv;
+    if (same && ((a->B > 1 && st[i][0] != st[i + 2][0]) || (heads > 1 && st[i][1] != st[i + 2][1]) || (a->N > 1 && st[i][2] != st[i + 2][2])))
+      return SAGE_ERR_INVALID_ARG;
+  }
+  auto tensor = [&](const void* x, void* y, int i, int heads) {
+    RopeTensor t;
+    t.x = (const unsigned short*)x; t.y = (unsigned short*)y;
+    t.xb = st[i][0]; t.xh = st[i][1]; t.xn = st[i][2];
+    t.yb = st[i + 2][0]; t.yh = st[i + 2][1]; t.yn = st[i + 2][2];
+    t.heads = heads;
+    return t;
+  };
+  p.q = tensor(a->q, a->q_out, 0, a->H);
+  p.k = tensor(a->k, a->k_out, 1, keys ? a->H_kv : 0);
+  p.inv_freq = a->inv_freq; p.positions = a->positions; p.pos_sb = a->positions_stride; p.offset = a->offset;
+  p.N = a->N; p.d = a->d; p.rot = a->rot_dim;
+  p.scale = a->scale == 0.0f ? 1.0f : a->scale;
+  p.sign = a->inverse ? -p.scale : p.scale;
+
+  // Widest access that every row allows: both halves of a pair's vectors start at a multiple of it.
+  unsigned long long bits = (uintptr_t)a->q / 2 | (uintptr_t)a->q_out / 2 | (uintptr_t)a->k / 2 | (uintptr_t)a->k_out / 2;
+  for (auto& s : st) bits |= (unsigned long long)(s[0] | s[1] | s[2]);
+  bits |= (unsigned long long)(a->rot_dim / 2);
+  const int vw = (bits & 7) == 0 ? 8 : (bits & 3) == 0 ? 4 : 1;
+  p.turned = a->rot_dim / 2 / vw;
+  // (in place, what is not turned stays where it is)
+  const bool in_place = a->q == a->q_out && (!keys || a->k == a->k_out);
+  p.units = p.turned + (in_place ? 0 : (a->d - a->rot_dim) / (2 * vw));
+  p.total = (long long)a->B * a->N * p.units;
+  const long long blocks = (p.total + 255) / 256;
+  if (blocks > 0x7fffffffLL) return SAGE_ERR_UNSUPPORTED;
+  // Heads are divided over workgroups only until there are eight of these per CU: each pays for the angles again.
+  const int heads = p.q.heads + p.k.heads;
+  long long pieces = (2048 + blocks - 1) / blocks;
+  if (pieces > heads) pieces = heads;
+  p.hchunk = (int)((heads + pieces - 1) / pieces);
+  const dim3 grid((unsigned)blocks, (unsigned)((heads + p.hchunk - 1) / p.hchunk));
+  const hipStream_t s = (hipStream_t)a->stream;
+  const bool inter = a->interleaved != 0;
+  if (a->dtype == SAGE_DT_BF16) {
+    if (vw == 8) launch<true, 8>(p, inter, grid, s); else if (vw == 4) launch<true, 4>(p, inter, grid, s); else launch<true, 1>(p, inter, grid, s);
+  } else {
+    if (vw == 8) launch<false, 8>(p, inter, grid, s); else if (vw == 4) launch<false, 4>(p, inter, grid, s); else launch<false, 1>(p, inter, grid, s);
+  }
+  return op_status(hipGetLastError());
+}
+
+extern "C" int sage_rope_frequencies(int rot_dim, double base, int scaling, double factor, double original_length, double low, double high,
+                                     double* inv_freq) {
+  if (!inv_freq || rot_dim <= 0 || rot_dim % 2 != 0 || !(base > 1.0) || !std::isfinite(base)) return SAGE_ERR_INVALID_ARG;
+  if (scaling < SAGE_ROPE_PLAIN || scaling > SAGE_ROPE_PARTS) return SAGE_ERR_UNSUPPORTED;
+  if (scaling != SAGE_ROPE_PLAIN && (!(factor >= 1.0) || !std::isfinite(factor))) return SAGE_ERR_INVALID_ARG;
+  if (scaling == SAGE_ROPE_PARTS && (!(original_length > 0.0) || !std::isfinite(original_length) || !(low < high) || !std::isfinite(low) || !std::isfinite(high)))
+    return SAGE_ERR_INVALID_ARG;
+  if (scaling == SAGE_ROPE_BASE && rot_dim == 2) return SAGE_ERR_UNSUPPORTED;      // (one frequency, which no base moves)
+  if (scaling == SAGE_ROPE_BASE) base *= std::pow(factor, (double)rot_dim / (rot_dim - 2));
+  for (int i = 0; i < rot_dim / 2; ++i) {
+    double f = std::pow(base, -2.0 * i / rot_dim);
+    if (scaling == SAGE_ROPE_LINEAR) f /= factor;
+    if (scaling == SAGE_ROPE_PARTS) {
+      const double turns = original_length * f / 6.283185307179586477;
+      const double keep = std::fmin(std::fmax((turns - low) / (high - low), 0.0), 1.0);
+      f *= keep + (1.0 - keep) / factor;
+    }
+    inv_freq[i] = f;
+  }
+  return SAGE_OK;
+}
