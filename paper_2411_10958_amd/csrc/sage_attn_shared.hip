@@ -127,6 +127,15 @@ __global__ void __launch_bounds__(256, shared_occupancy<D>()) k_shared(const Sha
     }
   };
 
+  // The first tile is on its way while the queries come; the wait for them is one for it too, since loads are counted in order.  From
+  // there on two tiles are in flight.
+  copy(j0, 0);
+#pragma unroll
+  for (int st = 0; st < KS; ++st)
+#pragma unroll
+    for (int x = 0; x < 4; ++x) use_now(q[st][x]);
+  if (j0 + 1 < j1) copy(j0 + 1, 1);
+
   v16f o[CT];
 #pragma unroll
   for (int c = 0; c < CT; ++c)
@@ -134,17 +143,16 @@ __global__ void __launch_bounds__(256, shared_occupancy<D>()) k_shared(const Sha
     for (int v = 0; v < 16; ++v) o[c][v] = 0.0f;
   float mx = -INFINITY, l = 0.0f;                 // running maximum (of both halves) and this half's sum
 
-  copy(j0, 0);
+  constexpr int PER_TILE = 2 * (TILE / 256);       // copies of a tile that a wavefront starts
   for (int j = j0; j < j1; ++j) {
     const int stage = (j - j0) & 1;
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-    __builtin_amdgcn_s_barrier();                 // tile j is there, and nobody reads the other stage any more
+    if (j + 1 < j1) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(PER_TILE) : "memory");
+    else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();                 // tile j is there
     asm volatile("" ::: "memory");
-    if (j + 1 < j1) copy(j + 1, stage ^ 1);
-    if (!active) continue;
     const v4i* tk = &s_kv[stage][0];
     const v4i* tv = &s_kv[stage][TILE];
-    for (int sub = kg; sub < 2; sub += WK) {
+    for (int sub = active ? kg : 2; sub < 2; sub += WK) {
       const int key0 = j * SH_KEYS + 32 * sub;
       if (key0 >= nk) break;
       // S^T = K Q^T.  Operand row rho = 8g + 4h + r takes key 16 (g / 2) + 8h + 4 (g % 2) + r: half h of the lanes then has
@@ -203,6 +211,12 @@ __global__ void __launch_bounds__(256, shared_occupancy<D>()) k_shared(const Sha
         }
       }
     }
+    if (j + 2 < j1) {                             // the next tile but one takes this one's place when all have read it
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+      copy(j + 2, stage);
+    }
   }
   l = half_sum(l);
 
@@ -250,33 +264,67 @@ __global__ void __launch_bounds__(256, shared_occupancy<D>()) k_shared(const Sha
     }
 }
 
-// The partial results of a row into its output: D / 4 threads per row, four channels each.  Scores that are NaN leave their
-// mark in the sum, whatever the maximum.
+// The partial results of a row into its output, a wavefront per row: lane s looks at partial results s, s + 64, .. for the
+// maximum and the weights; then D / 4 lanes take four channels each of every GRP-th partial result, MERGE_LOADS of them in flight.  Bound by
+// the two trips to memory, not by bytes.  Scores that are NaN leave their mark in the sum, whatever the maximum.
+constexpr int MERGE_LOADS = 8, MERGE_PER_LANE = 4;
+constexpr int MAX_PARTS = 64 * MERGE_PER_LANE;
 template <int D, bool BF16>
 __global__ void __launch_bounds__(256) k_shared_merge(const SharedParams p) {
-  constexpr int TPR = D / 4;
+  constexpr int LPR = D / 4, GRP = 64 / LPR;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const long long rows = (long long)p.B * p.G * p.N;
-  const long long id = (long long)blockIdx.x * (256 / TPR) + threadIdx.x / TPR;
+  const long long id = (long long)blockIdx.x * 4 + wave;
   if (id >= rows * p.Hkv) return;
-  const int c = 4 * (threadIdx.x % TPR);
   const int hkv = (int)(id / rows);
   const long long i = id - hkv * rows;
   const int GN = p.G * p.N, b = (int)(i / GN), rgn = (int)(i - (long long)b * GN), g = rgn / p.N, n = rgn - g * p.N;
-  const int S = p.Sp + p.So;
-  float m = -INFINITY;
-  for (int s = 0; s < S; ++s) m = fmaxf(m, p.part_ml[part_row(p, s, hkv, i) * 2]);
-  float l = 0.0f;
-  v4f acc = {0.0f, 0.0f, 0.0f, 0.0f};
-  for (int s = 0; s < S; ++s) {
-    const size_t pr = part_row(p, s, hkv, i);
-    const float ms = p.part_ml[pr * 2], ls = p.part_ml[pr * 2 + 1];
-    if (ms == -INFINITY && ls == 0.0f) continue;  // (no key of this chunk is seen: O may not even be there)
-    const float w = __builtin_amdgcn_exp2f(ms - m);
-    l = __fmaf_rn(w, ls, l);
-    const v4f x = *reinterpret_cast<const v4f*>(p.part_o + pr * D + c);
+  const int S = p.Sp + p.So, c = 4 * (lane % LPR), grp = lane / LPR;
+  float ms[MERGE_PER_LANE], w[MERGE_PER_LANE], m = -INFINITY, l = 0.0f;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) acc[k] = __fmaf_rn(w, x[k], acc[k]);
+  for (int x = 0; x < MERGE_PER_LANE; ++x) {
+    ms[x] = -INFINITY; w[x] = 0.0f;
+    if (64 * x + lane < S) {
+      const float2 ml = *reinterpret_cast<const float2*>(p.part_ml + part_row(p, 64 * x + lane, hkv, i) * 2);
+      ms[x] = ml.x; w[x] = ml.y;
+    }
+    m = fmaxf(m, ms[x]);
   }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
+#pragma unroll
+  for (int x = 0; x < MERGE_PER_LANE; ++x) {
+    const float ls = w[x];
+    w[x] = ms[x] == -INFINITY && ls == 0.0f ? -1.0f : __builtin_amdgcn_exp2f(ms[x] - m);    // (-1: no key is seen: O may not even be there)
+    if (w[x] != -1.0f) l = __fmaf_rn(w[x], ls, l);
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) l += __shfl_xor(l, o);
+  v4f acc = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+  for (int x = 0; x < MERGE_PER_LANE; ++x) {
+    const int end = min(S - 64 * x, 64);
+    for (int s0 = 0; s0 < end; s0 += GRP * MERGE_LOADS) {
+      v4f o4[MERGE_LOADS];
+      float ws[MERGE_LOADS];
+#pragma unroll
+      for (int k = 0; k < MERGE_LOADS; ++k) {
+        const int s = s0 + k * GRP + grp;
+        ws[k] = __shfl(w[x], s & 63);
+        ws[k] = s < end ? ws[k] : -1.0f;
+        o4[k] = *reinterpret_cast<const v4f*>(p.part_o + part_row(p, 64 * x + min(s, end - 1), hkv, i) * D + c);
+      }
+#pragma unroll
+      for (int k = 0; k < MERGE_LOADS; ++k)
+#pragma unroll
+        for (int y = 0; y < 4; ++y) acc[y] = ws[k] == -1.0f ? acc[y] : __fmaf_rn(ws[k], o4[k][y], acc[y]);
+    }
+  }
+#pragma unroll
+  for (int o = LPR; o < 64; o <<= 1)
+#pragma unroll
+    for (int y = 0; y < 4; ++y) acc[y] += __shfl_xor(acc[y], o);
+  if (grp != 0) return;
   const int h = hkv * p.G + g;
   const bool none = m == -INFINITY && l == 0.0f;  // no key at all: zeros
   const float inv = none ? 0.0f : __fdiv_rn(1.0f, l);
@@ -291,8 +339,8 @@ void choose_chunks(SharedParams* p, int d) {
   const long long np = (long long)p->Hkv * p->rtp, no = (long long)p->B * p->Hkv * p->rto;
   const long long places = 256LL * (d == 64 ? 4 : d == 128 ? 2 : 1);
   long long per = std::max(4LL, (np * tp + no * to + places - 1) / places);
-  p->Sp = (int)std::min(256LL, (tp + per - 1) / per);
-  p->So = (int)std::min(256LL, (to + per - 1) / per);
+  p->Sp = (int)std::min((long long)MAX_PARTS / 2, (tp + per - 1) / per);
+  p->So = (int)std::min((long long)MAX_PARTS / 2, (to + per - 1) / per);
 }
 
 int shared_params(const sage_attn_shared_prefix_args* a, SharedParams* p, bool need_io) {
@@ -339,7 +387,7 @@ template <int D, bool BF16> hipError_t launch_shared(const SharedParams& p, hipS
     if (e != hipSuccess) return e;
   }
   const long long rows = (long long)p.B * p.G * p.N * p.Hkv;
-  k_shared_merge<D, BF16><<<(unsigned)((rows + 256 / (D / 4) - 1) / (256 / (D / 4))), 256, 0, s>>>(p);
+  k_shared_merge<D, BF16><<<(unsigned)((rows + 3) / 4), 256, 0, s>>>(p);
   return hipGetLastError();
 }
 
