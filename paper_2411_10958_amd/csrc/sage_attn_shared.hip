@@ -15,12 +15,16 @@
 
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 namespace sage {
 namespace {
 
-constexpr int SH_ROWS = 128;     // query rows of a workgroup: 32 per wavefront
 constexpr int SH_KEYS = 64;      // keys of a tile
+// Wavefronts of a workgroup, 32 query rows each.  Two wavefronts share a SIMD where 128 rows do (one's vector work runs beside
+// the other's products); 256-wide heads, whose two tiles of K and V fill the LDS of a CU, need eight in one workgroup for that.
+template <int D> constexpr int shared_waves() { return D == 256 ? 8 : 4; }
+constexpr int shared_rows(int d) { return d == 256 ? 256 : 128; }
 
 struct SharedParams {
   const unsigned short *q, *kp, *vp, *ko, *vo;
@@ -46,24 +50,31 @@ __device__ __forceinline__ size_t part_row(const SharedParams& p, int s, int hkv
 
 __device__ __forceinline__ int own_len(const SharedParams& p, int b) { return p.lens ? min(max(p.lens[b], 0), p.Nk) : p.Nk; }
 
-template <int D> constexpr int shared_occupancy() { return D == 64 ? 4 : D == 128 ? 2 : 1; }
+template <int D> constexpr int shared_occupancy() { return D == 64 ? 3 : 2; }   // wavefronts per SIMD
 
 template <int D, bool BF16>
-__global__ void __launch_bounds__(256, shared_occupancy<D>()) k_shared(const SharedParams p) {
+__global__ void __launch_bounds__(64 * shared_waves<D>(), shared_occupancy<D>()) k_shared(const SharedParams p) {
   constexpr int NP = D / 8;                       // 16-byte pieces of a row
   constexpr int KS = D / 16;                      // contraction steps of the score product
   constexpr int CT = D / 32;                      // channel tiles of the output
   constexpr int TILE = SH_KEYS * NP;              // pieces of a K (or V) tile
-  __shared__ v4i s_kv[2][2 * TILE];               // [stage][K, V]
+  constexpr int W = shared_waves<D>(), ROWS = 32 * W;
+  __shared__ __align__(1024) v4i s_kv[2][2 * TILE];     // [stage][K, V]
+  __shared__ float s_ml[shared_waves<D>() / 2][64];     // maxima and sums of the second key group
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
   const int col = lane & 31, half = lane >> 5;
 
   // ---- which rows and keys
   int id = blockIdx.x, hkv, b = 0, rt, s;
   const bool prefix = id < p.n_prefix;
-  if (prefix) {                                   // row tiles of one chunk side by side: they read the same keys
-    rt = id % p.rtp; id /= p.rtp;
-    hkv = id % p.Hkv; s = id / p.Hkv;
+  if (prefix) {
+    // The row tiles of a chunk read the same keys: they are 8 apart, since workgroups go to the 8 XCDs in turn and each has a cache
+    // of its own.  (The last chunks, fewer than 8, have theirs side by side.)
+    const int chunks = p.Sp * p.Hkv, full = chunks / 8 * 8 * p.rtp;
+    const int grp = id < full ? id / (8 * p.rtp) : chunks / 8, wide = id < full ? 8 : chunks % 8, in = id - grp * 8 * p.rtp;
+    rt = in / wide;
+    const int chunk = grp * 8 + in % wide;
+    hkv = chunk % p.Hkv; s = chunk / p.Hkv;
   } else {
     id -= p.n_prefix;
     rt = id % p.rto; id /= p.rto;
@@ -72,8 +83,8 @@ __global__ void __launch_bounds__(256, shared_occupancy<D>()) k_shared(const Sha
   }
   const int GN = p.G * p.N;
   const long long rows = prefix ? (long long)p.B * GN : GN;
-  const long long r0 = (long long)rt * SH_ROWS;
-  const int nr = (int)min((long long)SH_ROWS, rows - r0);     // rows of this workgroup
+  const long long r0 = (long long)rt * ROWS;
+  const int nr = (int)min((long long)ROWS, rows - r0);     // rows of this workgroup
   const int nk = prefix ? p.P : own_len(p, b);
   const int tiles = (nk + SH_KEYS - 1) / SH_KEYS, S = prefix ? p.Sp : p.So;
   const int per = (tiles + S - 1) / S;
@@ -81,13 +92,13 @@ __global__ void __launch_bounds__(256, shared_occupancy<D>()) k_shared(const Sha
   const int sp = prefix ? s : p.Sp + s;
   const long long i0 = prefix ? r0 : (long long)b * GN + r0;  // first row in the numbering of part_row
 
-  // Wavefronts: 32 rows each; with fewer than 65 rows, two share rows and take every other 32 keys
-  const int WK = nr <= 64 ? 2 : 1;
+  // Wavefronts: 32 rows each; where half of them do for the rows, two share rows and take every other 32 keys
+  const int WK = nr <= ROWS / 2 ? 2 : 1;
   const int kg = WK == 2 ? wave & 1 : 0, rg = WK == 2 ? wave >> 1 : wave;
   const bool active = rg * 32 < nr;
 
   if (j0 >= j1) {                                 // no keys: a partial result that the merge skips
-    for (int i = t; i < nr; i += 256) {
+    for (int i = t; i < nr; i += 64 * W) {
       float* ml = p.part_ml + part_row(p, sp, hkv, i0 + i) * 2;
       ml[0] = -INFINITY;
       ml[1] = 0.0f;
@@ -118,10 +129,10 @@ __global__ void __launch_bounds__(256, shared_occupancy<D>()) k_shared(const Sha
     const size_t at = (size_t)j * SH_KEYS * m.sn * 2;
     const int last = nk - 1 - j * SH_KEYS;
 #pragma unroll
-    for (int x = 0; x < TILE / 256; ++x) {
-      const int pc = (x * 4 + wave) * 64 + lane, r = pc / NP, c = (pc % NP) ^ swizzle<D>(r);
+    for (int x = 0; x < TILE / (64 * W); ++x) {
+      const int pc = (x * W + wave) * 64 + lane, r = pc / NP, c = (pc % NP) ^ swizzle<D>(r);
       const unsigned off = (unsigned)min(r, last) * step + (unsigned)c * 16;
-      const unsigned to = lds0 + (unsigned)(stage * 2 * TILE + (x * 4 + wave) * 64) * 16;
+      const unsigned to = lds0 + (unsigned)(stage * 2 * TILE + (x * W + wave) * 64) * 16;
       dma_b128(gk + at, off, to);
       dma_b128(gv + at, off, to + TILE * 16);
     }
@@ -143,73 +154,98 @@ __global__ void __launch_bounds__(256, shared_occupancy<D>()) k_shared(const Sha
     for (int v = 0; v < 16; ++v) o[c][v] = 0.0f;
   float mx = -INFINITY, l = 0.0f;                 // running maximum (of both halves) and this half's sum
 
-  constexpr int PER_TILE = 2 * (TILE / 256);       // copies of a tile that a wavefront starts
+  // Where my operands start in a tile.  A row's first byte has its low bits zero and the swizzle of a row repeats every 16 rows, so a
+  // step to another piece of a row is one exclusive or and a step of 16 or 32 rows an offset: no address is kept over the loop.
+  // K: row of key 16 (g / 2) + 8h + 4 (g % 2) + r for operand row 8g + 4h + r, piece 2 st + half.  V: row 8 half + (l % 16) / 4 - the
+  // transposed read gives lane l channel l % 16 of the four keys whose rows its group of 16 lanes point at - and, for
+  // the upper four keys, four rows on, where the swizzle differs in its lowest bit.
+  constexpr unsigned ROW = D * 2;
+  typedef __attribute__((address_space(3))) const v4i* lds_v4i;
+  typedef short v4s __attribute__((ext_vector_type(4)));
+  typedef __attribute__((address_space(3))) v4s* lds_v4s;
+  const int kr = 16 * (col >> 4) + 8 * ((col >> 2) & 1) + 4 * ((col >> 3) & 1) + (col & 3), vr = 8 * half + ((lane & 15) >> 2);
+  const int vc = 16 * ((lane >> 4) & 1) + 4 * (lane & 3);                  // first channel that my lane points at
+  const unsigned k_at = (unsigned)row_piece<D>(kr, half) * 16, v_at = (unsigned)row_piece<D>(vr, vc >> 3) * 16 + (vc & 4) * 2;
+
+  // NS times 32 keys of a tile, from the sub0-th on: scores, weights and their product with V
+  auto tile_keys = [&](auto ns, unsigned stage0, int tile0, int sub0) __attribute__((always_inline)) {
+    constexpr int NS = decltype(ns)::value;
+    const int key0 = tile0 + 32 * sub0;
+    // S^T = K Q^T: with the rows as above, half h of the lanes has keys 8h + 0..7 and 16 + 8h + 0..7 of its query, in the order in
+    // which the second product wants them
+    const unsigned ka = stage0 + 32 * sub0 * ROW + k_at, va = stage0 + TILE * 16 + 32 * sub0 * ROW + v_at;
+    v16f sc[NS];
+#pragma unroll
+    for (int y = 0; y < NS; ++y)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) sc[y][v] = 0.0f;
+#pragma unroll
+    for (int st = 0; st < KS; ++st)
+#pragma unroll
+      for (int y = 0; y < NS; ++y) sc[y] = mfma16<BF16>(*(lds_v4i)((ka ^ (32 * st)) + 32 * y * ROW), q[st], sc[y]);
+    if (key0 + 32 * NS > vis_all) {
+#pragma unroll
+      for (int y = 0; y < NS; ++y)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) sc[y][v] = key0 + 32 * y + 16 * (v >> 3) + 8 * half + (v & 7) < vis ? sc[y][v] : -INFINITY;
+    }
+    float top = -INFINITY;
+#pragma unroll
+    for (int v = 0; v < 16; ++v)
+#pragma unroll
+      for (int y = 0; y < NS; ++y) top = fmaxf(top, sc[y][v]);
+    top = half_max(top) * p.kappa;
+    const float m_new = fmaxf(mx, top);
+    const float base = m_new == -INFINITY ? 0.0f : m_new;       // (no key seen yet: every weight 2^-inf)
+    if (__ballot(m_new > mx) != 0) {
+      const float alpha = __builtin_amdgcn_exp2f(mx - base);
+      l *= alpha;
+#pragma unroll
+      for (int c = 0; c < CT; ++c)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) o[c][v] *= alpha;
+      mx = m_new;
+    }
+    float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    v4i pb[NS][2];
+#pragma unroll
+    for (int y = 0; y < NS; ++y)
+#pragma unroll
+      for (int v = 0; v < 16; v += 2) {
+        const float e0 = __builtin_amdgcn_exp2f(__fmaf_rn(sc[y][v], p.kappa, -base));
+        const float e1 = __builtin_amdgcn_exp2f(__fmaf_rn(sc[y][v + 1], p.kappa, -base));
+        sum[v & 2] += e0;
+        sum[(v & 2) + 1] += e1;
+        pb[y][v >> 3][(v & 7) >> 1] = (int)pack16x2<BF16>(e0, e1);
+      }
+    l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+    // O^T += V^T P^T
+#pragma unroll
+    for (int y = 0; y < NS; ++y)
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks) {
+#pragma unroll
+        for (int c = 0; c < CT; ++c) {
+          const unsigned rows = (32 * y + 16 * ks) * ROW;
+          const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s)((va ^ (64 * c)) + rows));
+          const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s)((va ^ (64 * c + 16)) + rows + 4 * ROW));
+          const v8s a = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+          o[c] = mfma16<BF16>(__builtin_bit_cast(v4i, a), pb[y][ks], o[c]);
+        }
+      }
+  };
+
+  constexpr int PER_TILE = 2 * (TILE / (64 * W));       // copies of a tile that a wavefront starts
   for (int j = j0; j < j1; ++j) {
     const int stage = (j - j0) & 1;
     if (j + 1 < j1) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(PER_TILE) : "memory");
     else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();                 // tile j is there
     asm volatile("" ::: "memory");
-    const v4i* tk = &s_kv[stage][0];
-    const v4i* tv = &s_kv[stage][TILE];
-    for (int sub = active ? kg : 2; sub < 2; sub += WK) {
-      const int key0 = j * SH_KEYS + 32 * sub;
-      if (key0 >= nk) break;
-      // S^T = K Q^T.  Operand row rho = 8g + 4h + r takes key 16 (g / 2) + 8h + 4 (g % 2) + r: half h of the lanes then has
-      // keys 8h + 0..7 and 16 + 8h + 0..7 of its query, in the order in which the second product wants them.
-      const int rho = col, kr = 32 * sub + 16 * (rho >> 4) + 8 * ((rho >> 2) & 1) + 4 * ((rho >> 3) & 1) + (rho & 3);
-      v16f sc;
-#pragma unroll
-      for (int v = 0; v < 16; ++v) sc[v] = 0.0f;
-#pragma unroll
-      for (int st = 0; st < KS; ++st) sc = mfma16<BF16>(tk[row_piece<D>(kr, 2 * st + half)], q[st], sc);
-      if (key0 + 32 > vis_all) {
-#pragma unroll
-        for (int v = 0; v < 16; ++v) sc[v] = key0 + 16 * (v >> 3) + 8 * half + (v & 7) < vis ? sc[v] : -INFINITY;
-      }
-      float top = sc[0];
-#pragma unroll
-      for (int v = 1; v < 16; ++v) top = fmaxf(top, sc[v]);
-      top = half_max(top) * p.kappa;
-      const float m_new = fmaxf(mx, top);
-      const float base = m_new == -INFINITY ? 0.0f : m_new;       // (no key seen yet: every weight 2^-inf)
-      if (__ballot(m_new > mx) != 0) {
-        const float alpha = __builtin_amdgcn_exp2f(mx - base);
-        l *= alpha;
-#pragma unroll
-        for (int c = 0; c < CT; ++c)
-#pragma unroll
-          for (int v = 0; v < 16; ++v) o[c][v] *= alpha;
-        mx = m_new;
-      }
-      float e[16];
-#pragma unroll
-      for (int v = 0; v < 16; ++v) e[v] = __builtin_amdgcn_exp2f(__fmaf_rn(sc[v], p.kappa, -base));
-      float sum = 0.0f;
-#pragma unroll
-      for (int v = 0; v < 16; ++v) sum += e[v];
-      l += sum;
-      v4i pb[2];
-#pragma unroll
-      for (int v = 0; v < 16; v += 2) pb[v >> 3][(v & 7) >> 1] = (int)pack16x2<BF16>(e[v], e[v + 1]);
-      // O^T += V^T P^T: a transposed read gives lane l channel l % 16 of the four keys whose rows its group of 16 lanes point at
-      const int g16 = lane & 15, ch = 16 * ((lane >> 4) & 1) + 4 * (g16 & 3);
-#pragma unroll
-      for (int ks = 0; ks < 2; ++ks) {
-        const int vr = 32 * sub + 16 * ks + 8 * half + (g16 >> 2);
-#pragma unroll
-        for (int c = 0; c < CT; ++c) {
-          typedef short v4s __attribute__((ext_vector_type(4)));
-          typedef __attribute__((address_space(3))) v4s* lds_v4s;
-          const int pc = (32 * c + ch) >> 3, in = ch & 4;
-          const short* a0 = reinterpret_cast<const short*>(&tv[row_piece<D>(vr, pc)]) + in;
-          const short* a1 = reinterpret_cast<const short*>(&tv[row_piece<D>(vr + 4, pc)]) + in;
-          const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s)a0);
-          const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s)a1);
-          const v8s a = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-          o[c] = mfma16<BF16>(__builtin_bit_cast(v4i, a), pb[ks], o[c]);
-        }
-      }
+    const unsigned at = lds0 + (unsigned)stage * (2 * TILE * 16);
+    if (active) {
+      if (D < 256 && WK == 1 && j * SH_KEYS + 32 < nk) tile_keys(std::integral_constant<int, 2>{}, at, j * SH_KEYS, 0);
+      else for (int sub = kg; sub < 2 && j * SH_KEYS + 32 * sub < nk; sub += WK) tile_keys(std::integral_constant<int, 1>{}, at, j * SH_KEYS, sub);
     }
     if (j + 2 < j1) {                             // the next tile but one takes this one's place when all have read it
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -222,7 +258,7 @@ __global__ void __launch_bounds__(256, shared_occupancy<D>()) k_shared(const Sha
 
   // ---- the two key groups of the same rows into one
   if (WK == 2) {
-    float* x = reinterpret_cast<float*>(&s_kv[0][0]) + rg * 32 * (D + 2);
+    float* x = reinterpret_cast<float*>(&s_kv[0][0]) + rg * 32 * D;
     __syncthreads();
     if (active && kg == 1) {
 #pragma unroll
@@ -230,14 +266,14 @@ __global__ void __launch_bounds__(256, shared_occupancy<D>()) k_shared(const Sha
 #pragma unroll
         for (int v = 0; v < 16; ++v) x[(16 * c + v) * 64 + lane] = o[c][v];
       if (half == 0) {
-        x[32 * D + 2 * col] = mx;
-        x[32 * D + 2 * col + 1] = l;
+        s_ml[rg][2 * col] = mx;
+        s_ml[rg][2 * col + 1] = l;
       }
     }
     __syncthreads();
     if (kg == 1) return;
     if (active) {
-      const float m1 = x[32 * D + 2 * col], l1 = x[32 * D + 2 * col + 1];
+      const float m1 = s_ml[rg][2 * col], l1 = s_ml[rg][2 * col + 1];
       const float m_new = fmaxf(mx, m1), base = m_new == -INFINITY ? 0.0f : m_new;
       const float a0 = __builtin_amdgcn_exp2f(mx - base), a1 = __builtin_amdgcn_exp2f(m1 - base);
       l = l * a0 + l1 * a1;
@@ -337,7 +373,7 @@ __global__ void __launch_bounds__(256) k_shared_merge(const SharedParams p) {
 void choose_chunks(SharedParams* p, int d) {
   const long long tp = (p->P + SH_KEYS - 1) / SH_KEYS, to = (p->Nk + SH_KEYS - 1) / SH_KEYS;
   const long long np = (long long)p->Hkv * p->rtp, no = (long long)p->B * p->Hkv * p->rto;
-  const long long places = 256LL * (d == 64 ? 4 : d == 128 ? 2 : 1);
+  const long long places = 256LL * (d == 64 ? 3 : d == 128 ? 2 : 1);
   long long per = std::max(4LL, (np * tp + no * to + places - 1) / places);
   p->Sp = (int)std::min((long long)MAX_PARTS / 2, (tp + per - 1) / per);
   p->So = (int)std::min((long long)MAX_PARTS / 2, (to + per - 1) / per);
@@ -368,8 +404,9 @@ int shared_params(const sage_attn_shared_prefix_args* a, SharedParams* p, bool n
   p->om = make_tensor_map(nhd, a->H_kv, a->N_kv, a->d);
   const long long gn = (long long)p->G * p->N, rows = gn * p->B;
   if (rows > (1LL << 30)) return SAGE_ERR_UNSUPPORTED;
-  p->rtp = (int)((rows + SH_ROWS - 1) / SH_ROWS);
-  p->rto = (int)((gn + SH_ROWS - 1) / SH_ROWS);
+  const int per = shared_rows(a->d);
+  p->rtp = (int)((rows + per - 1) / per);
+  p->rto = (int)((gn + per - 1) / per);
   choose_chunks(p, a->d);
   const long long np = (long long)p->Sp * p->Hkv * p->rtp, no = (long long)p->So * p->B * p->Hkv * p->rto;
   if (np + no > 0x7fffffffLL || rows * p->Hkv > 0x7fffffffLL) return SAGE_ERR_UNSUPPORTED;
@@ -382,7 +419,7 @@ size_t part_rows(const SharedParams& p) { return (size_t)(p.Sp + p.So) * p.Hkv *
 template <int D, bool BF16> hipError_t launch_shared(const SharedParams& p, hipStream_t s) {
   const long long own = (long long)p.So * p.B * p.Hkv * p.rto, blocks = p.n_prefix + own;
   if (blocks > 0) {
-    k_shared<D, BF16><<<(unsigned)blocks, 256, 0, s>>>(p);
+    k_shared<D, BF16><<<(unsigned)blocks, 64 * shared_waves<D>(), 0, s>>>(p);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
