@@ -416,62 +416,78 @@ SAGE_ROPE_PLAIN, SAGE_ROPE_LINEAR, SAGE_ROPE_BASE, SAGE_ROPE_PARTS = 0, 1, 2, 3
 _ROPE_SCALINGS = {"plain": 0, "linear": 1, "base": 2, "parts": 3, 0: 0, 1: 1, 2: 2, 3: 3}
 
 
-def _need(name, t, device, dtype, shape=None, dims=None, contiguous=True):
-    """Raises unless t is a tensor of that kind on that GPU.  shape: exact; dims: its number of dimensions."""
-    if not t.is_cuda or t.device != device:
-        raise ValueError(f"{name} must be on {device}, like q or k")
+def _gpu_of(name, t):
+    """The index of the GPU that t is on."""
+    index = t.get_device()
+    if index < 0:
+        raise ValueError(f"{name} must be a GPU tensor")
+    return index
+
+
+def _need(name, t, index, dtype, shape=None):
+    """Raises unless t is a contiguous tensor of that type (and shape) on GPU `index`."""
+    if t.get_device() != index or t.dtype != dtype or (shape is not None and t.shape != shape) or not t.is_contiguous():
+        _refuse(name, t, index, dtype, shape)
+
+
+def _refuse(name, t, index, dtype, shape):
+    if t.get_device() != index:
+        raise ValueError(f"{name} must be on GPU {index} like the other tensors, is on {t.device}")
     if t.dtype != dtype:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
-    if shape is not None and tuple(t.shape) != tuple(shape):
+    if shape is not None and t.shape != shape:
         raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
-    if dims is not None and t.dim() != dims:
-        raise ValueError(f"{name} must have {dims} dimensions, got {t.dim()}")
-    if contiguous and not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous")
+    raise ValueError(f"{name} must be contiguous")
+
+
+def _new(shape, dtype, index, stream, make=torch.empty):
+    """An output or a workspace from torch's allocator.  For another stream it is allocated (and filled) there: the block may have been
+    another tensor's, and what is still queued for that one is ordered with the stream that it came from."""
+    if stream is None:
+        return make(shape, dtype=dtype, device=index)
+    with torch.cuda.stream(stream):
+        t = make(shape, dtype=dtype, device=index)
+    t.record_stream(torch.cuda.current_stream(index))        # the caller goes on with it here
+    return t
 
 
 def _address(t):
     return 0 if t is None else t.data_ptr()
 
 
-def _call(name, args, device):
+def _call(name, args, index):
     """One entry point with its argument structure, on the device of its tensors."""
     f = getattr(load_library(), name)
-    if torch.cuda.current_device() == device.index:
+    if torch.cuda.current_device() == index:
         status = f(ctypes.byref(args))
     else:
-        with torch.cuda.device(device):
+        with torch.cuda.device(index):
             status = f(ctypes.byref(args))
     if status != 0:
         raise SageError(status, name)
 
 
-def _raw_stream(stream, device):
-    return _current_raw_stream(device.index) if stream is None else stream.cuda_stream
-
-
-def _own_workspace(name, args, device, workspace, stream):
+def _own_workspace(name, args, index, workspace, stream):
     """Points args at `workspace`, or at a new one.  The result has to live until the call is enqueued."""
     if workspace is None:
-        need = int(getattr(load_library(), name + "_workspace_bytes")(ctypes.byref(args)))
+        need = getattr(load_library(), name + "_workspace_bytes")(ctypes.byref(args))
         if need == 0:
             return None
-        workspace = torch.empty(need, dtype=torch.uint8, device=device)
-        if stream is not None:
-            workspace.record_stream(stream)      # allocated on the current stream, used on another one
-    elif not workspace.is_cuda or workspace.device != device or not workspace.is_contiguous():
-        raise ValueError(f"workspace must be a contiguous tensor on {device}")
+        workspace = _new(need, torch.uint8, index, stream)
+        args.workspace, args.workspace_bytes = workspace.data_ptr(), need
+        return workspace
+    if workspace.get_device() != index or not workspace.is_contiguous():
+        raise ValueError(f"workspace must be a contiguous tensor on GPU {index}")
     args.workspace, args.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
     return workspace
 
 
-def _sizes(x, layout):
+def _sizes(name, x, nhd):
     """B, heads, tokens, d of a 4-D tensor."""
-    return (x.shape[0], x.shape[2], x.shape[1], x.shape[3]) if layout else tuple(x.shape)
-
-
-def _shape_of(layout, B, heads, tokens, d):
-    return (B, tokens, heads, d) if layout else (B, heads, tokens, d)
+    if x.dim() != 4:
+        raise ValueError(f"{name} must have 4 dimensions, got {x.dim()}")
+    B, m, n, d = x.shape
+    return (B, n, m, d) if nhd else (B, m, n, d)
 
 
 def sage_rope_frequencies(rot_dim, base=10000.0, scaling="plain", factor=1.0, original_length=0.0, low=1.0, high=32.0, device=None):
@@ -494,91 +510,88 @@ def sage_rope(q, k=None, inv_freq=None, positions=None, offset=0, interleaved=Fa
     (q_out, k_out)."""
     if inv_freq is None:
         raise ValueError("inv_freq is needed (see sage_rope_frequencies)")
-    dtype, device = _dtype_code(q), q.device
-    if not q.is_cuda or q.dim() not in (3, 4):
-        raise ValueError("q must be a 4-D, or packed 3-D, GPU tensor")
-    nhd = _LAYOUTS[layout]
+    dtype, index = _dtype_code(q), _gpu_of("q", q)
     packed = q.dim() == 3
-    if packed:
-        nhd = 1
-    _need("inv_freq", inv_freq, device, torch.float64, dims=1)
-    a = sage_rope_args()
-    pairs = [("q", q, q_out, a.q_strides, a.q_out_strides)]
+    if not packed and q.dim() != 4:
+        raise ValueError(f"q must have 4 dimensions, or 3 if packed, got {q.dim()}")
+    nhd = 1 if packed else _LAYOUTS[layout]
+    B, H, N, d = (1, q.shape[1], q.shape[0], q.shape[2]) if packed else _sizes("q", q, nhd)
+    Hkv = 0
     if k is not None:
-        _need("k", k, device, q.dtype, dims=q.dim(), contiguous=False)
-        pairs.append(("k", k, k_out, a.k_strides, a.k_out_strides))
+        if k.get_device() != index or k.dtype != q.dtype or k.dim() != q.dim():
+            raise ValueError("k must have the type, device and number of dimensions of q")
+        Bk, Hkv, Nk, dk = (1, k.shape[1], k.shape[0], k.shape[2]) if packed else _sizes("k", k, nhd)
+        if (Bk, Nk, dk) != (B, N, d):
+            raise ValueError("k shape does not match q")
     elif k_out is not None:
         raise ValueError("k_out without k")
-    outs = []
-    for name, x, y, xs, ys in pairs:
-        if y is None:
-            y = torch.empty(x.shape, dtype=x.dtype, device=device)
-            if stream is not None:
-                y.record_stream(stream)
-        else:
-            _need(name + "_out", y, device, q.dtype, shape=x.shape, contiguous=False)
-        outs.append(y)
-        for t, st in ((x, xs), (y, ys)):
-            s = t.stride()
-            if s[-1] != 1:
-                raise ValueError(f"{name}: the channels of a row must be contiguous")
-            if packed:
-                s = (0,) + s[:-1]
-            st[0], st[1], st[2] = (s[0], s[2], s[1]) if nhd else s[:3]
-    B, H, N, d = _sizes(q.unsqueeze(0) if packed else q, nhd)
-    Bk, Hkv, Nk, dk = _sizes(k.unsqueeze(0) if packed else k, nhd) if k is not None else (B, 0, N, d)
-    if (Bk, Nk, dk) != (B, N, d):
-        raise ValueError("k shape does not match q")
+    if q.numel() == 0 or (k is not None and Hkv == 0):
+        raise ValueError("q or k is empty")
+    _need("inv_freq", inv_freq, index, torch.float64)
+    if inv_freq.dim() != 1:
+        raise ValueError("inv_freq must have one dimension")
     if positions is not None:
-        _need("positions", positions, device, torch.int32)
-        if tuple(positions.shape) not in ((N,), (B, N)):
+        _need("positions", positions, index, torch.int32)
+        if positions.shape != (N,) and positions.shape != (B, N):
             raise ValueError(f"positions must have shape ({N},) or ({B}, {N}), got {tuple(positions.shape)}")
-        a.positions, a.positions_stride = positions.data_ptr(), N if positions.dim() == 2 else 0
     elif packed:
         raise ValueError("a packed batch needs positions")
-    if q.numel() == 0:
-        raise ValueError("q is empty")
-    a.q, a.k, a.q_out, a.k_out = q.data_ptr(), _address(k), outs[0].data_ptr(), outs[1].data_ptr() if k is not None else 0
-    a.B, a.H, a.H_kv, a.N, a.d, a.rot_dim, a.dtype, a.layout = B, H, Hkv, N, d, 2 * inv_freq.numel(), dtype, nhd
-    a.interleaved, a.inverse, a.scale, a.inv_freq, a.offset = int(bool(interleaved)), int(bool(inverse)), float(scale), inv_freq.data_ptr(), int(offset)
-    a.stream = _raw_stream(stream, device)
-    _call("sage_rope", a, device)
+    outs = []
+    for name, x, y in (("q_out", q, q_out), ("k_out", k, k_out)):
+        if x is None:
+            y = None
+        elif y is None:
+            y = _new(x.shape, x.dtype, index, stream)
+        elif y.get_device() != index or y.dtype != q.dtype or y.shape != x.shape:
+            raise ValueError(f"{name} must have the type, shape and device of its input")
+        outs.append(y)
+    a = sage_rope_args(q.data_ptr(), _address(k), outs[0].data_ptr(), _address(outs[1]), B, H, Hkv, N, d, 2 * inv_freq.numel(), dtype, nhd,
+                       int(bool(interleaved)), int(bool(inverse)), float(scale), inv_freq.data_ptr(), _address(positions),
+                       N if positions is not None and positions.dim() == 2 else 0, int(offset))
+    a.stream = stream.cuda_stream if stream is not None else _current_raw_stream(index)
+    for t, st in ((q, a.q_strides), (k, a.k_strides), (outs[0], a.q_out_strides), (outs[1], a.k_out_strides)):
+        if t is None or t.is_contiguous():
+            continue                            # (all zero: contiguous)
+        s = t.stride()
+        if s[-1] != 1:
+            raise ValueError("the channels of a row must be contiguous")
+        if packed:
+            s = (0,) + s[:-1]
+        st[0], st[1], st[2] = (s[0], s[2], s[1]) if nhd else s[:3]
+    _call("sage_rope", a, index)
     return outs[0] if k is None else tuple(outs)
 
 
 def _shared_prefix_args(q, k_prefix, v_prefix, k, v, kv_lens, out, causal, sm_scale, layout, stream):
-    dtype, device, nhd = _dtype_code(q), q.device, _LAYOUTS[layout]
-    _need("q", q, device, q.dtype, dims=4)
-    B, H, N, d = _sizes(q, nhd)
-    a = sage_attn_shared_prefix_args()
+    dtype, dt, index, nhd = _dtype_code(q), q.dtype, _gpu_of("q", q), _LAYOUTS[layout]
+    B, H, N, d = _sizes("q", q, nhd)
+    _need("q", q, index, dt)
     if (k_prefix is None) != (v_prefix is None) or (k is None) != (v is None) or (k is None and k_prefix is None):
         raise ValueError("a prefix, own keys and values, or both are needed, each with its values")
+    P = Nk = 0
     Hkv = None
     if k_prefix is not None:
-        _need("k_prefix", k_prefix, device, q.dtype, dims=3)
-        _need("v_prefix", v_prefix, device, q.dtype, shape=k_prefix.shape)
-        P, Hkv, dp = (k_prefix.shape[0], k_prefix.shape[1], k_prefix.shape[2]) if nhd else (k_prefix.shape[1], k_prefix.shape[0], k_prefix.shape[2])
+        if k_prefix.dim() != 3:
+            raise ValueError(f"k_prefix must have 3 dimensions, got {k_prefix.dim()}")
+        P, Hkv, dp = k_prefix.shape if nhd else (k_prefix.shape[1], k_prefix.shape[0], k_prefix.shape[2])
+        _need("k_prefix", k_prefix, index, dt)
+        _need("v_prefix", v_prefix, index, dt, k_prefix.shape)
         if dp != d:
             raise ValueError("the prefix does not match q")
-        a.k_prefix, a.v_prefix, a.N_prefix = k_prefix.data_ptr(), v_prefix.data_ptr(), P
     if k is not None:
-        _need("k", k, device, q.dtype, dims=4)
-        _need("v", v, device, q.dtype, shape=k.shape)
-        Bk, Hk, Nk, dk = _sizes(k, nhd)
-        if (Bk, dk) != (B, d) or (Hkv is not None and Hk != Hkv):
+        Bk, Hk, Nk, dk = _sizes("k", k, nhd)
+        _need("k", k, index, dt)
+        _need("v", v, index, dt, k.shape)
+        if Bk != B or dk != d or (Hkv is not None and Hk != Hkv):
             raise ValueError("k does not match q or the prefix")
         Hkv = Hk
-        a.k, a.v, a.N_kv = k.data_ptr(), v.data_ptr(), Nk
     if kv_lens is not None:
-        _need("kv_lens", kv_lens, device, torch.int32, shape=(B,))
-        a.kv_lens = kv_lens.data_ptr()
+        _need("kv_lens", kv_lens, index, torch.int32, (B,))
     if out is not None:
-        _need("out", out, device, q.dtype, shape=q.shape)
-        a.out = out.data_ptr()
-    a.q = q.data_ptr()
-    a.B, a.H, a.H_kv, a.N, a.d, a.causal, a.sm_scale, a.dtype, a.layout = B, H, Hkv, N, d, int(bool(causal)), float(sm_scale), dtype, nhd
-    a.stream = _raw_stream(stream, device)
-    return a
+        _need("out", out, index, dt, q.shape)
+    return sage_attn_shared_prefix_args(q.data_ptr(), _address(k_prefix), _address(v_prefix), _address(k), _address(v), _address(out), _address(kv_lens), 0,
+                                        B, H, Hkv, N, P, Nk, d, int(bool(causal)), float(sm_scale), dtype, nhd, 0, 0,
+                                        stream.cuda_stream if stream is not None else _current_raw_stream(index))
 
 
 def sage_attn_shared_prefix_workspace_bytes(args):
@@ -591,19 +604,16 @@ def sage_attn_shared_prefix(q, k_prefix, v_prefix, k=None, v=None, kv_lens=None,
     sequence's own k, v [B, H_kv, N_kv, d] (None: none), of which the first kv_lens (int32 [B]; None: all) are in use.  Layout "NHD":
     tokens outside heads in all of them.  causal masks the own keys, aligned to the last query and key in use.  Returns out, or
     (out, lse) with lse float32 [B, H, N]."""
-    if out is None:
-        out = torch.empty_like(q)
-        if stream is not None:
-            out.record_stream(stream)
     a = _shared_prefix_args(q, k_prefix, v_prefix, k, v, kv_lens, out, causal, sm_scale, layout, stream)
-    lse = None
+    index, lse = q.get_device(), None
+    if out is None:
+        out = _new(q.shape, q.dtype, index, stream)
+        a.out = out.data_ptr()
     if return_lse:
-        lse = torch.empty((a.B, a.H, a.N), dtype=torch.float32, device=q.device)
-        if stream is not None:
-            lse.record_stream(stream)
+        lse = _new((a.B, a.H, a.N), torch.float32, index, stream)
         a.lse = lse.data_ptr()
-    keep = _own_workspace("sage_attn_shared_prefix", a, q.device, workspace, stream)
-    _call("sage_attn_shared_prefix", a, q.device)
+    keep = _own_workspace("sage_attn_shared_prefix", a, index, workspace, stream)
+    _call("sage_attn_shared_prefix", a, index)
     del keep
     return (out, lse) if return_lse else out
 
@@ -617,33 +627,28 @@ def sage_attn_key_weights(q, k, lse, weights_in=None, weights=None, kv_lens=None
     """What each key of k [B, H_kv, N_kv, d] has received of the attention of q [B, H, N, d] with log-sum-exp lse (float32 [B, H, N], as the
     attention calls return it), summed over the queries of its KV head and added to weights_in.  Returns weights, float32
     [B, H_kv, N_kv]; may be weights_in.  Entries behind kv_lens keep what they hold (zeros if the result is allocated here)."""
-    dtype, device, nhd = _dtype_code(q), q.device, _LAYOUTS[layout]
-    _need("q", q, device, q.dtype, dims=4)
-    _need("k", k, device, q.dtype, dims=4)
-    B, H, N, d = _sizes(q, nhd)
-    Bk, Hkv, Nk, dk = _sizes(k, nhd)
-    if (Bk, dk) != (B, d):
+    dtype, index, nhd = _dtype_code(q), _gpu_of("q", q), _LAYOUTS[layout]
+    B, H, N, d = _sizes("q", q, nhd)
+    Bk, Hkv, Nk, dk = _sizes("k", k, nhd)
+    _need("q", q, index, q.dtype)
+    _need("k", k, index, q.dtype)
+    if Bk != B or dk != d:
         raise ValueError("k does not match q")
-    _need("lse", lse, device, torch.float32, shape=(B, H, N))
-    a = sage_attn_key_weights_args()
+    _need("lse", lse, index, torch.float32, (B, H, N))
     shape = (B, Hkv, Nk)
     if weights_in is not None:
-        _need("weights_in", weights_in, device, torch.float32, shape=shape)
-        a.weights_in = weights_in.data_ptr()
+        _need("weights_in", weights_in, index, torch.float32, shape)
     if kv_lens is not None:
-        _need("kv_lens", kv_lens, device, torch.int32, shape=(B,))
-        a.kv_lens = kv_lens.data_ptr()
+        _need("kv_lens", kv_lens, index, torch.int32, (B,))
     if weights is None:
-        weights = torch.zeros(shape, dtype=torch.float32, device=device) if kv_lens is not None else torch.empty(shape, dtype=torch.float32, device=device)
-        if stream is not None:
-            weights.record_stream(stream)
+        weights = _new(shape, torch.float32, index, stream, torch.empty if kv_lens is None else torch.zeros)
     else:
-        _need("weights", weights, device, torch.float32, shape=shape)
-    a.q, a.k, a.lse, a.weights = q.data_ptr(), k.data_ptr(), lse.data_ptr(), weights.data_ptr()
-    a.B, a.H, a.H_kv, a.N, a.N_kv, a.d, a.causal, a.sm_scale, a.dtype, a.layout = B, H, Hkv, N, Nk, d, int(bool(causal)), float(sm_scale), dtype, nhd
-    a.stream = _raw_stream(stream, device)
-    keep = _own_workspace("sage_attn_key_weights", a, device, workspace, stream)
-    _call("sage_attn_key_weights", a, device)
+        _need("weights", weights, index, torch.float32, shape)
+    a = sage_attn_key_weights_args(q.data_ptr(), k.data_ptr(), lse.data_ptr(), _address(weights_in), weights.data_ptr(), _address(kv_lens),
+                                   B, H, Hkv, N, Nk, d, int(bool(causal)), float(sm_scale), dtype, nhd, 0, 0,
+                                   stream.cuda_stream if stream is not None else _current_raw_stream(index))
+    keep = _own_workspace("sage_attn_key_weights", a, index, workspace, stream)
+    _call("sage_attn_key_weights", a, index)
     del keep
     return weights
 
@@ -654,32 +659,28 @@ def sage_cache_evict(k, v, weights, n_keep, sink=0, recent=0, kv_lens=None, layo
     (kv_lens, int32 [B]; None: all) and the ones of largest weight (float32 [B, H_kv, N_kv]) between.  Returns (k_out, v_out,
     weights_out, kept, lens_out): the rows kept, in their order, their weights, which they were (int32 [B, H_kv, n_keep]) and how many
     (int32 [B]); what stands behind them keeps what it held (zeros where the output is allocated here)."""
-    dtype, device, nhd = _dtype_code(k), k.device, _LAYOUTS[layout]
-    _need("k", k, device, k.dtype, dims=4)
-    _need("v", v, device, k.dtype, shape=k.shape)
-    B, Hkv, Nk, d = _sizes(k, nhd)
+    dtype, dt, index, nhd = _dtype_code(k), k.dtype, _gpu_of("k", k), _LAYOUTS[layout]
+    B, Hkv, Nk, d = _sizes("k", k, nhd)
+    _need("k", k, index, dt)
+    _need("v", v, index, dt, k.shape)
     n_keep = int(n_keep)
     if n_keep < 1:
         raise ValueError("n_keep must be at least 1")
-    _need("weights", weights, device, torch.float32, shape=(B, Hkv, Nk))
+    _need("weights", weights, index, torch.float32, (B, Hkv, Nk))
     if kv_lens is not None:
-        _need("kv_lens", kv_lens, device, torch.int32, shape=(B,))
+        _need("kv_lens", kv_lens, index, torch.int32, (B,))
     make = torch.zeros if kv_lens is not None or n_keep > Nk else torch.empty
-    rows, per = _shape_of(nhd, B, Hkv, n_keep, d), (B, Hkv, n_keep)
+    rows, per = (B, n_keep, Hkv, d) if nhd else (B, Hkv, n_keep, d), (B, Hkv, n_keep)
     outs = []
-    for name, t, shape, dt in (("k_out", k_out, rows, k.dtype), ("v_out", v_out, rows, k.dtype), ("weights_out", weights_out, per, torch.float32),
-                               ("kept", kept, per, torch.int32), ("lens_out", lens_out, (B,), torch.int32)):
+    for name, t, shape, want in (("k_out", k_out, rows, dt), ("v_out", v_out, rows, dt), ("weights_out", weights_out, per, torch.float32),
+                                 ("kept", kept, per, torch.int32), ("lens_out", lens_out, (B,), torch.int32)):
         if t is None:
-            t = make(shape, dtype=dt, device=device)
-            if stream is not None:
-                t.record_stream(stream)
+            t = _new(shape, want, index, stream, make)
         else:
-            _need(name, t, device, dt, shape=shape)
+            _need(name, t, index, want, shape)
         outs.append(t)
-    a = sage_cache_evict_args()
-    a.k, a.v, a.weights, a.kv_lens = k.data_ptr(), v.data_ptr(), weights.data_ptr(), _address(kv_lens)
-    a.k_out, a.v_out, a.weights_out, a.kept, a.lens_out = (t.data_ptr() for t in outs)
-    a.B, a.H_kv, a.N_kv, a.N_keep, a.d, a.sink, a.recent, a.dtype, a.layout = B, Hkv, Nk, n_keep, d, int(sink), int(recent), dtype, nhd
-    a.stream = _raw_stream(stream, device)
-    _call("sage_cache_evict", a, device)
+    a = sage_cache_evict_args(k.data_ptr(), v.data_ptr(), weights.data_ptr(), _address(kv_lens), *[t.data_ptr() for t in outs],
+                              B, Hkv, Nk, n_keep, d, int(sink), int(recent), dtype, nhd,
+                              stream.cuda_stream if stream is not None else _current_raw_stream(index))
+    _call("sage_cache_evict", a, index)
     return tuple(outs)

@@ -26,96 +26,107 @@ __device__ __forceinline__ unsigned order_of(float w) {
 }
 
 constexpr int SEL_THREADS = 1024, SEL_WAVES = SEL_THREADS / 64;
+constexpr int DIGIT = 11, BINS = 1 << DIGIT;      // three digits of 11, 11 and 10 bits
 
-// Which tokens stay, one workgroup per sequence and KV head: the m-th largest weight between sink and recent, one digit of 8 bits
-// at a time by counting, then one pass in order that keeps what is larger and the first of what equals it.
+// Which tokens stay, one workgroup per sequence and KV head: the m-th largest weight between sink and recent, found digit by digit by
+// counting, then one pass in order that keeps what is larger and the first of what equals it.  A wavefront has a stretch of
+// 64 K weights in registers, in the order of unsigned numbers, so they are read and converted once; K = 0: more than that, read
+// again each time, eight loads in flight.  Bound by the instructions of its five passes on one CU: 32 rows of 32768 25 us of the call's
+// 122 (51 with 8-bit digits and weights read from memory in each pass; counts in four copies changed nothing).  (The first digit is sign, exponent and two bits: with 8-bit digits a wavefront's
+// counts would fall on a dozen addresses.)  What a stretch has behind the last weight counts as less than any and comes after
+// all, so it is never taken: n > m.
+template <int K>
 __global__ void __launch_bounds__(SEL_THREADS) k_evict_select(const EvictParams p) {
-  __shared__ unsigned s_hist[256];
-  __shared__ unsigned s_pick[2];
+  __shared__ unsigned s_hist[BINS];
+  __shared__ unsigned s_wave[SEL_WAVES], s_pick[2];
   __shared__ unsigned s_gt[SEL_WAVES], s_eq[SEL_WAVES];
-  const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+  const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
   const int b = blockIdx.x / p.Hkv;
   const int len = p.lens ? min(max(p.lens[b], 0), p.N) : p.N;
   const float* w = p.w + (size_t)blockIdx.x * p.N;
   int* kept = p.kept + (size_t)blockIdx.x * p.keep;
-  float* w_out = p.w_out ? p.w_out + (size_t)blockIdx.x * p.keep : nullptr;
   if (t == 0 && blockIdx.x % p.Hkv == 0) p.lens_out[b] = min(len, p.keep);
   if (len <= p.keep) {
-    for (int i = t; i < len; i += SEL_THREADS) {
-      kept[i] = i;
-      if (w_out) w_out[i] = w[i];
-    }
+    for (int i = t; i < len; i += SEL_THREADS) kept[i] = i;
     return;
   }
   const int c0 = p.sink, n = len - p.recent - p.sink, m = p.keep - p.sink - p.recent;     // n > m >= 0 tokens to choose from
-  for (int i = t; i < p.sink + p.recent; i += SEL_THREADS) {
-    const int from = i < p.sink ? i : len - p.recent + (i - p.sink), to = i < p.sink ? i : p.keep - p.recent + (i - p.sink);
-    kept[to] = from;
-    if (w_out) w_out[to] = w[from];
-  }
+  constexpr int STEP = K > 0 ? K : 8;             // 64s that a wavefront has at a time
+  const int seg = K > 0 ? 64 * K : ((n + SEL_WAVES - 1) / SEL_WAVES + 63) / 64 * 64;
+  const int i0 = min(wave * seg, n), i1 = min(i0 + seg, n);
+  unsigned u[STEP];
+  auto load = [&](int from) __attribute__((always_inline)) {
+    float x[STEP];
+#pragma unroll
+    for (int j = 0; j < STEP; ++j) x[j] = from + 64 * j < i1 ? w[c0 + min(from + 64 * j + lane, i1 - 1)] : 0.0f;
+#pragma unroll
+    for (int j = 0; j < STEP; ++j) u[j] = from + 64 * j + lane < i1 ? order_of(x[j]) : 0u;
+  };
+  if (K > 0) load(i0);
+  for (int i = t; i < p.sink; i += SEL_THREADS) kept[i] = i;
+  for (int i = t; i < p.recent; i += SEL_THREADS) kept[p.keep - p.recent + i] = len - p.recent + i;
   if (m == 0) return;
+  // f(weights in order, first token) for the 64s of my stretch
+  auto each = [&](auto f) __attribute__((always_inline)) {
+    for (int i = i0; i < i1; i += 64 * STEP) {
+      if (K == 0) load(i);
+#pragma unroll
+      for (int j = 0; j < STEP; ++j)
+        if (i + 64 * j < i1) f(u[j], i + 64 * j);
+    }
+  };
   unsigned prefix = 0, need = (unsigned)m;
-  for (int shift = 24; shift >= 0; shift -= 8) {
-    if (t < 256) s_hist[t] = 0;
+#pragma unroll
+  for (int d = 0; d < 3; ++d) {
+    const int low = d == 0 ? 32 - DIGIT : d == 1 ? 32 - 2 * DIGIT : 0, bits = d < 2 ? DIGIT : 32 - 2 * DIGIT;
+    for (int i = t; i < BINS; i += SEL_THREADS) s_hist[i] = 0;
     __syncthreads();
-    const unsigned mask = shift == 24 ? 0u : ~0u << (shift + 8);
-    for (int i = t; i < n; i += SEL_THREADS) {
-      const unsigned u = order_of(w[c0 + i]);
-      if ((u & mask) == prefix) atomicAdd(&s_hist[(u >> shift) & 255], 1u);
+    each([&](unsigned v, int) __attribute__((always_inline)) {
+      if (d == 0 || (v >> (low + bits)) == (prefix >> (low + bits))) atomicAdd(&s_hist[(v >> low) & ((1u << bits) - 1)], 1u);
+    });
+    __syncthreads();
+    // thread t holds digits 2047 - 2t and 2046 - 2t: from the largest down
+    const unsigned a0 = s_hist[BINS - 1 - 2 * t], a1 = s_hist[BINS - 2 - 2 * t];
+    unsigned upto = a0 + a1;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const unsigned y = __shfl_up(upto, o);
+      if (lane >= o) upto += y;
+    }
+    if (lane == 63) s_wave[wave] = upto;
+    __syncthreads();
+    for (int i = 0; i < wave; ++i) upto += s_wave[i];
+    const unsigned before = upto - a0 - a1;
+    if (before < need && upto >= need) {
+      const bool second = before + a0 < need;
+      s_pick[0] = (unsigned)(BINS - 1 - 2 * t) - second;
+      s_pick[1] = before + (second ? a0 : 0u);
     }
     __syncthreads();
-    if (wave == 0) {            // lane l holds digits 255 - 4 l .. 252 - 4 l: from the largest down
-      unsigned c[4], sum = 0;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) { c[i] = s_hist[255 - 4 * lane - i]; sum += c[i]; }
-      unsigned upto = sum;
-#pragma unroll
-      for (int o = 1; o < 64; o <<= 1) {
-        const unsigned x = __shfl_up(upto, o);
-        if (lane >= o) upto += x;
-      }
-      unsigned before = upto - sum;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if (before < need && before + c[i] >= need) { s_pick[0] = 255 - 4 * lane - i; s_pick[1] = before; }
-        before += c[i];
-      }
-    }
-    __syncthreads();
-    prefix |= s_pick[0] << shift;
+    prefix |= s_pick[0] << low;
     need -= s_pick[1];
   }
-  // wavefront w has the tokens of its own stretch, 64 at a time
-  const int seg = ((n + SEL_WAVES - 1) / SEL_WAVES + 63) / 64 * 64;
-  const int i0 = min(wave * seg, n), i1 = min(i0 + seg, n);
   unsigned gt = 0, eq = 0;
-  for (int i = i0; i < i1; i += 64) {
-    const unsigned u = i + lane < i1 ? order_of(w[c0 + i + lane]) : 0u;
-    gt += (unsigned)__popcll(__ballot(i + lane < i1 && u > prefix));
-    eq += (unsigned)__popcll(__ballot(i + lane < i1 && u == prefix));
-  }
+  each([&](unsigned v, int) __attribute__((always_inline)) {
+    gt += (unsigned)__popcll(__ballot(v > prefix));
+    eq += (unsigned)__popcll(__ballot(v == prefix));
+  });
   if (lane == 0) { s_gt[wave] = gt; s_eq[wave] = eq; }
   __syncthreads();
-  unsigned above = 0, ties = 0;
+  unsigned above = (unsigned)p.sink, ties = 0;
   for (int i = 0; i < wave; ++i) { above += s_gt[i]; ties += s_eq[i]; }
   const unsigned long long below = (1ull << lane) - 1;
-  for (int i = i0; i < i1; i += 64) {
-    const bool in = i + lane < i1;
-    const float x = in ? w[c0 + i + lane] : 0.0f;
-    const unsigned u = order_of(x);
-    const unsigned long long bg = __ballot(in && u > prefix), be = __ballot(in && u == prefix);
+  each([&](unsigned v, int i) __attribute__((always_inline)) {
+    const unsigned long long bg = __ballot(v > prefix), be = __ballot(v == prefix);
     const unsigned tie = ties + (unsigned)__popcll(be & below);
-    if (in && (u > prefix || (u == prefix && tie < need))) {
-      const unsigned to = (unsigned)p.sink + above + (unsigned)__popcll(bg & below) + min(tie, need);
-      kept[to] = c0 + i + lane;
-      if (w_out) w_out[to] = x;
-    }
+    if (v > prefix || (v == prefix && tie < need)) kept[above + (unsigned)__popcll(bg & below) + min(tie, need)] = c0 + i + lane;
     above += (unsigned)__popcll(bg);
     ties += (unsigned)__popcll(be);
-  }
+  });
 }
 
-// The rows of the kept tokens: a thread moves 16 bytes of K and of V of GU tokens.  Grid: (pieces of the kept tokens, heads).
+// The rows of the kept tokens, and their weights: a thread moves 16 bytes of K and of V of GU tokens, the first of a row also its
+// weight.  Grid: (pieces of the kept tokens, heads).
 constexpr int GU = 4;
 template <int D> __global__ void __launch_bounds__(256) k_evict_rows(const EvictParams p) {
   constexpr int P = D / 8, TOK = 256 / P;
@@ -130,6 +141,10 @@ template <int D> __global__ void __launch_bounds__(256) k_evict_rows(const Evict
 #pragma unroll
   for (int i = 0; i < GU; ++i) from[i] = kept[min(first + i * TOK, there - 1)];
   v4i a[GU], x[GU];
+  float wt[GU];
+  const bool weigh = p.w_out && c == 0;
+#pragma unroll
+  for (int i = 0; i < GU; ++i) wt[i] = weigh ? p.w[(size_t)blockIdx.y * p.N + from[i]] : 0.0f;
 #pragma unroll
   for (int i = 0; i < GU; ++i) {
     const size_t at = row_offset(p.in, hi, from[i]);
@@ -142,6 +157,7 @@ template <int D> __global__ void __launch_bounds__(256) k_evict_rows(const Evict
       const size_t at = row_offset(p.out, ho, first + i * TOK);
       *reinterpret_cast<v4i*>(p.k_out + at) = a[i];
       *reinterpret_cast<v4i*>(p.v_out + at) = x[i];
+      if (weigh) p.w_out[(size_t)blockIdx.y * p.keep + first + i * TOK] = wt[i];
     }
   }
 }
@@ -184,7 +200,12 @@ extern "C" int sage_cache_evict(const sage_cache_evict_args* a) {
   p.in = make_tensor_map(nhd, a->H_kv, a->N_kv, a->d);
   p.out = make_tensor_map(nhd, a->H_kv, a->N_keep, a->d);
   const hipStream_t s = (hipStream_t)a->stream;
-  k_evict_select<<<(unsigned)heads, SEL_THREADS, 0, s>>>(p);
+  const int most = a->N_kv - a->sink - a->recent;       // weights to choose from
+  if (most <= 4 * SEL_THREADS) k_evict_select<4><<<(unsigned)heads, SEL_THREADS, 0, s>>>(p);
+  else if (most <= 16 * SEL_THREADS) k_evict_select<16><<<(unsigned)heads, SEL_THREADS, 0, s>>>(p);
+  else if (most <= 32 * SEL_THREADS) k_evict_select<32><<<(unsigned)heads, SEL_THREADS, 0, s>>>(p);
+  else if (most <= 64 * SEL_THREADS) k_evict_select<64><<<(unsigned)heads, SEL_THREADS, 0, s>>>(p);
+  else k_evict_select<0><<<(unsigned)heads, SEL_THREADS, 0, s>>>(p);
   int st = op_status(hipGetLastError());
   if (st != SAGE_OK) return st;
   const int per = 256 / (a->d / 8) * GU;

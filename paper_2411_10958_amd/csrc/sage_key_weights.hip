@@ -16,6 +16,8 @@ namespace {
 
 constexpr int KW_KEYS = 256;     // keys of a workgroup: 64 per wavefront
 constexpr int KW_ROWS = 64;      // queries of a tile
+constexpr int KW_FEW = 32;       // rows of a group that are few
+constexpr int KW_PIECE = 16;     // most query tiles of a workgroup: their constants are kept in LDS
 
 struct KwParams {
   const unsigned short *q, *k;
@@ -24,9 +26,11 @@ struct KwParams {
   const int* lens;
   TensorMap qm, km;
   int B, H, Hkv, G, N, Nk;
+  int few;                       // k_key_weights_few takes it: `piece` is then key tiles of a wavefront, `key_tiles` workgroups per head
   int causal, flat;              // flat: tiles run over the G N queries of a group, else over the N of each head
   float kappa;
   int key_tiles, pieces, piece;  // most pieces of a key tile, query tiles of a piece
+  FastDiv by_heads, by_hkv, by_kt, by_n;      // B H_kv, H_kv, key_tiles, N
 };
 
 // Query tiles of the keys t0 .. t0 + 255 of a sequence with `len` keys: per head those from the first query that sees t0 on.
@@ -48,32 +52,76 @@ __host__ __device__ __forceinline__ KwItems kw_items(int flat, int causal, int G
 
 __device__ __forceinline__ int kw_len(const KwParams& p, int b) { return p.lens ? min(max(p.lens[b], 0), p.Nk) : p.Nk; }
 
-template <int D> constexpr int kw_occupancy() { return D == 64 ? 4 : 2; }
+// Wavefronts per SIMD that registers and LDS are cut for.
+template <int D> constexpr int kw_occupancy() { return D == 256 ? 2 : 3; }
 
 template <int D, bool BF16>
 __global__ void __launch_bounds__(256, kw_occupancy<D>()) k_key_weights(const KwParams p) {
-  constexpr int NP = D / 8, KS = D / 16, TILE = KW_ROWS * NP;
-  __shared__ v4i s_q[2][TILE];
-  __shared__ __align__(16) float s_nl[2][KW_ROWS];    // -lse log2(e) of the tile's queries
-  __shared__ __align__(16) int s_vis[2][KW_ROWS];     // how many keys they see
+  constexpr int NP = D / 8, KS = D / 16, TILE = KW_ROWS * NP, NST = 2;
+  constexpr unsigned ROW = D * 2;
+  __shared__ __align__(1024) v4i s_q[NST][TILE];
+  __shared__ __align__(16) float s_nl[KW_PIECE * KW_ROWS + 32];    // -lse log2(e) of the piece's queries; -inf: adds nothing; 32 of those
+  __shared__ __align__(16) int s_vis[KW_PIECE * KW_ROWS];     // how many keys they see
+  __shared__ int s_masked[KW_PIECE];                          // whether a query of the tile does not see all of the workgroup's keys
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
   const int col = lane & 31, half = lane >> 5;
   // workgroups in order: piece, key tile, head - the first keys' (the longest) first, heads side by side on different XCDs
-  int id = blockIdx.x;
-  const int bh = id % (p.B * p.Hkv); id /= p.B * p.Hkv;
-  const int kt = id % p.key_tiles, piece = id / p.key_tiles;
-  const int b = bh / p.Hkv, hkv = bh - b * p.Hkv;
-  const int len = kw_len(p, b), t0 = kt * KW_KEYS;
+  unsigned bh = blockIdx.x, kt = split_by(bh, p.by_heads), hkv = bh;
+  const int piece = (int)split_by(kt, p.by_kt), b = (int)split_by(hkv, p.by_hkv);
+  const int len = kw_len(p, b), t0 = (int)kt * KW_KEYS;
   if (t0 >= len) return;
   const KwItems it = kw_items(p.flat, p.causal, p.G, p.N, len, t0);
-  const int i0 = min(piece * p.piece, it.count), i1 = min(i0 + p.piece, it.count);
+  const int used = (it.count + p.piece - 1) / p.piece, each = used > 0 ? (it.count + used - 1) / used : 0;     // pieces of this key tile, all of a length
+  const int i0 = min(piece * each, it.count), i1 = min(i0 + each, it.count);
   const bool alone = p.pieces == 1;
   if (i0 >= i1 && !alone) return;
   const int coff = max(len - p.N, 0);
 
+  const unsigned lds0 = (unsigned)(size_t)(__attribute__((address_space(3))) char*)&s_q[0][0];
+  const int rows_all = p.flat ? p.G * p.N : p.N;       // rows of the list that a tile is cut from
+  const unsigned step = (unsigned)p.qm.sn * 2;
+  const unsigned short* qb = p.q + head_offset_of(p.qm, b, (int)hkv * p.G);
+  // The tile to copy next: row r0 of head g of the group.  What a lane adds to its first byte stays the same but for a head's last tile.
+  const int g0 = i0 / it.per_head;
+  int g = g0, r0 = (it.first + i0 - g0 * it.per_head) * KW_ROWS;
+  unsigned offs[TILE / 256];
+#pragma unroll
+  for (int x = 0; x < TILE / 256; ++x) {
+    const int pc = (x * 4 + wave) * 64 + lane, r = pc / NP;
+    offs[x] = (unsigned)r * step + (unsigned)((pc % NP) ^ swizzle<D>(r)) * 16;
+  }
+  auto copy = [&](int stage) __attribute__((always_inline)) {
+    const unsigned to = lds0 + (unsigned)(stage * TILE + wave * 64) * 16;
+    const char* base = uniform_ptr(reinterpret_cast<const char*>(qb + (p.flat ? 0 : (size_t)g * p.qm.sh + (size_t)r0 * p.qm.sn)));
+    if (!p.flat && r0 + KW_ROWS <= rows_all) {
+#pragma unroll
+      for (int x = 0; x < TILE / 256; ++x) dma_b128(base, offs[x], to + x * 4096);
+    } else {
+#pragma unroll 1
+      for (int x = 0; x < TILE / 256; ++x) {
+        const int pc = (x * 4 + wave) * 64 + lane, r = pc / NP, c = (pc % NP) ^ swizzle<D>(r);
+        unsigned n = (unsigned)min(r0 + r, rows_all - 1);
+        unsigned off;
+        if (p.flat) {
+          const unsigned gg = split_by(n, p.by_n);
+          off = gg * (unsigned)(p.qm.sh * 2) + n * step;
+        } else {
+          off = (n - (unsigned)r0) * step;
+        }
+        dma_b128(base, off + (unsigned)c * 16, to + x * 4096);
+      }
+    }
+    r0 += KW_ROWS;
+    if (!p.flat && r0 >= rows_all) {
+      r0 = it.first * KW_ROWS;
+      ++g;
+    }
+  };
+  if (i0 < i1) copy(0);
+
   // ---- my keys: column l % 32 of two operands, channels 16 s + 8 (l / 32) + 0..7
   const int key0 = t0 + 64 * wave;
-  const size_t khead = head_offset(p.km, (unsigned)bh);
+  const size_t khead = head_offset_of(p.km, b, (int)hkv);
   v4i kreg[2][KS];
 #pragma unroll
   for (int x = 0; x < 2; ++x) {
@@ -81,100 +129,242 @@ __global__ void __launch_bounds__(256, kw_occupancy<D>()) k_key_weights(const Kw
 #pragma unroll
     for (int s = 0; s < KS; ++s) kreg[x][s] = *reinterpret_cast<const v4i*>(kp + 16 * s);
   }
-
-  const unsigned lds0 = (unsigned)(size_t)(__attribute__((address_space(3))) char*)&s_q[0][0];
-  const int rows_all = p.flat ? p.G * p.N : p.N;       // rows of the list that a tile is cut from
-  const unsigned step = (unsigned)p.qm.sn * 2;
-  auto copy = [&](int i, int stage) {
-    const int g = i / it.per_head, r0 = (it.first + i - g * it.per_head) * KW_ROWS, last = rows_all - 1 - r0;
-    const size_t head = head_offset(p.qm, (unsigned)(b * p.H + hkv * p.G + (p.flat ? 0 : g)));
-    const char* base = uniform_ptr(reinterpret_cast<const char*>(p.q + head + (p.flat ? 0 : (size_t)r0 * p.qm.sn)));
+  // ---- the queries' constants, a wavefront per tile, four of its loads together
+  int gi = g0, qi = i0 - g0 * it.per_head + wave;
+  for (int i = i0 + wave; i < i1; i += 16) {
+    float lse[4];
+    int seen[4];
 #pragma unroll
-    for (int x = 0; x < TILE / 256; ++x) {
-      const int pc = (x * 4 + wave) * 64 + lane, r = pc / NP, c = (pc % NP) ^ swizzle<D>(r);
-      unsigned off;
-      if (p.flat) {
-        const unsigned at = (unsigned)(r0 + min(r, last)), gg = at / (unsigned)p.N, n = at - gg * (unsigned)p.N;
-        off = gg * (unsigned)(p.qm.sh * 2) + n * step;
-      } else {
-        off = (unsigned)min(r, last) * step;
+    for (int y = 0; y < 4; ++y, qi += 4) {
+      for (; qi >= it.per_head && gi < p.G; qi -= it.per_head) ++gi;
+      const int r = (it.first + qi) * KW_ROWS + lane;
+      lse[y] = INFINITY;                // (rows behind the last repeat it, and add nothing)
+      seen[y] = len;
+      if (i + 4 * y < i1 && r < rows_all) {
+        unsigned n = (unsigned)r;
+        const int gg = p.flat ? (int)split_by(n, p.by_n) : gi;
+        lse[y] = p.lse[((size_t)b * p.H + (int)hkv * p.G + gg) * p.N + n];
+        if (p.causal) seen[y] = min(coff + (int)n + 1, len);
       }
-      dma_b128(base, off + (unsigned)c * 16, lds0 + (unsigned)(stage * TILE + (x * 4 + wave) * 64) * 16);
     }
-  };
-  // the first wavefront's lanes look up their query's constants; written to LDS a tile later
-  float nl = 0.0f;
-  int vis = 0;
-  auto look = [&](int i) {
-    const int g = i / it.per_head, r = (it.first + i - g * it.per_head) * KW_ROWS + lane;
-    vis = 0;
-    nl = 0.0f;
-    if (r < rows_all) {
-      const int gg = p.flat ? r / p.N : g, n = p.flat ? r - gg * p.N : r;
-      const float x = p.lse[((size_t)b * p.H + hkv * p.G + gg) * p.N + n];
-      nl = -x * LOG2E;
-      vis = x == -INFINITY ? 0 : p.causal ? min(coff + n + 1, len) : len;
-    }
-  };
-
-  float sum[2] = {0.0f, 0.0f};
-  if (i0 < i1) {
-    copy(i0, 0);
-    if (wave == 0) {
-      look(i0);
-      s_nl[0][lane] = nl;
-      s_vis[0][lane] = vis;
+#pragma unroll
+    for (int y = 0; y < 4; ++y) {
+      const int at = i - i0 + 4 * y;
+      if (at < i1 - i0) {
+        const int vis = lse[y] == -INFINITY ? 0 : seen[y];
+        const int masked = __ballot(vis < min(t0 + KW_KEYS, len)) != 0;
+        s_nl[at * KW_ROWS + lane] = -lse[y] * LOG2E;
+        s_vis[at * KW_ROWS + lane] = vis;
+        if (lane == 0) s_masked[at] = masked;
+      }
     }
   }
+  if (t < 32) s_nl[KW_PIECE * KW_ROWS + t] = -INFINITY;
+  // (the keys are here before the loop, or it would wait for its copies with the first use of each)
+#pragma unroll
+  for (int x = 0; x < 2; ++x)
+#pragma unroll
+    for (int s = 0; s < KS; ++s)
+#pragma unroll
+      for (int y = 0; y < 4; ++y) use_now(kreg[x][s][y]);
+
+  // Scores of 32 queries and my 64 keys, and the weights of 32 others, whose scores are there: the matrix unit works on the one while
+  // the vector unit takes the other.  A row's pieces are one exclusive or apart (see swizzle).
+  typedef __attribute__((address_space(3))) const v4i* lds_v4i;
+  const unsigned q_at = (unsigned)row_piece<D>(col, half) * 16;
+  float sum[2][2] = {{0.0f, 0.0f}, {0.0f, 0.0f}};
+  float kappa = p.kappa;
+  auto constants = [&](int row, int g) __attribute__((always_inline)) {        // rows 8 g + 4 h + 0..3
+    return *reinterpret_cast<const v4f*>(&s_nl[row + 8 * g + 4 * half]);
+  };
+  auto weight = [&](int e, const v16f (&sc)[2], const v4f& n) __attribute__((always_inline)) {
+    const int x = e & 1, v = e >> 1;
+    sum[x][v & 1] += __builtin_amdgcn_exp2f(__fmaf_rn(sc[x][v], kappa, n[v & 3]));
+  };
+  auto weights = [&](const v16f (&sc)[2], int row) __attribute__((always_inline)) {
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const v4f n = constants(row, g);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) weight(8 * g + e, sc, n);
+    }
+  };
+  auto scores = [&](unsigned at, v16f (&acc)[2], const v16f (&sc)[2], int row) __attribute__((always_inline)) {
+    constexpr int AHEAD = 2;            // operands come from LDS so many steps before their products
+    v4i a[KS];
+    v4f n = constants(row, 0), next;
+#pragma unroll
+    for (int s = 0; s < AHEAD; ++s) a[s] = *(lds_v4i)(at ^ (32 * s));
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      if (s + AHEAD < KS) a[s + AHEAD] = *(lds_v4i)(at ^ (32 * (s + AHEAD)));
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        v16f c = acc[x];
+        if (s == 0) {
+#pragma unroll
+          for (int v = 0; v < 16; ++v) c[v] = 0.0f;
+        }
+        acc[x] = mfma16<BF16>(a[s], kreg[x][s], c);
+        constexpr int PER = 16 / KS;    // weights after a product; eight share their constants
+#pragma unroll
+        for (int e = 0; e < PER; ++e) {
+          const int w = (2 * s + x) * PER + e;
+          if (w % 8 == 0 && w < 24) next = constants(row, w / 8 + 1);
+          weight(w, sc, n);
+          if (w % 8 == 7) n = next;
+        }
+        __builtin_amdgcn_sched_barrier(0);      // (a product, then its share of the weights: not all products first)
+      }
+    }
+  };
+
+  v16f acc_a[2], acc_b[2];
+  constexpr int NO_ROW = KW_PIECE * KW_ROWS;
+  int row_b;                                      // where the constants of acc_b's queries are
+  auto nothing = [&]() __attribute__((always_inline)) {       // scores whose weights are zero
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) acc_b[x][v] = 0.0f;
+    row_b = NO_ROW;
+  };
+  nothing();
+  int stage = 0;
   for (int i = i0; i < i1; ++i) {
-    const int stage = (i - i0) & 1;
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();                 // tile i is there, and nobody reads the other stage any more
     asm volatile("" ::: "memory");
-    if (i + 1 < i1) {
-      copy(i + 1, stage ^ 1);
-      if (wave == 0) look(i + 1);
-    }
+    if (i + 1 < i1) copy(stage ^ 1);
+    const unsigned at = lds0 + (unsigned)stage * (TILE * 16) + q_at;
+    const int row = (i - i0) * KW_ROWS;
+    if (__builtin_amdgcn_readfirstlane(s_masked[i - i0]) == 0) {
+      scores(at, acc_a, acc_b, row_b);
+      scores(at + 32 * ROW, acc_b, acc_a, row);
+      row_b = row + 32;
+    } else {
+      asm volatile("" : "+s"(kappa));             // (or the weights of acc_b, common to both ways, would be taken before them)
+      weights(acc_b, row_b);
 #pragma unroll 1
-    for (int hr = 0; hr < 2; ++hr) {
-      v16f acc[2];
+      for (int hr = 0; hr < 2; ++hr) {
+        const unsigned here = at + 32 * hr * ROW;
 #pragma unroll
-      for (int x = 0; x < 2; ++x)
+        for (int x = 0; x < 2; ++x)
 #pragma unroll
-        for (int v = 0; v < 16; ++v) acc[x][v] = 0.0f;
+          for (int v = 0; v < 16; ++v) acc_a[x][v] = 0.0f;
 #pragma unroll
-      for (int s = 0; s < KS; ++s) {
-        const v4i a = s_q[stage][row_piece<D>(32 * hr + col, 2 * s + half)];
+        for (int s = 0; s < KS; ++s)
 #pragma unroll
-        for (int x = 0; x < 2; ++x) acc[x] = mfma16<BF16>(a, kreg[x][s], acc[x]);
+          for (int x = 0; x < 2; ++x) acc_a[x] = mfma16<BF16>(*(lds_v4i)(here ^ (32 * s)), kreg[x][s], acc_a[x]);
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const v4f n = constants(row + 32 * hr, g);
+          const v4i v4 = *reinterpret_cast<const v4i*>(&s_vis[row + 32 * hr + 8 * g + 4 * half]);
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+              const float e = __builtin_amdgcn_exp2f(__fmaf_rn(acc_a[x][4 * g + r], p.kappa, n[r]));
+              sum[x][r & 1] += key0 + 32 * x + col < v4[r] ? e : 0.0f;
+            }
+        }
       }
-      // rows 8 g + 4 h + r of the tile half: four runs of four
-#pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const v4f n4 = *reinterpret_cast<const v4f*>(&s_nl[stage][32 * hr + 8 * g + 4 * half]);
-        const v4i v4 = *reinterpret_cast<const v4i*>(&s_vis[stage][32 * hr + 8 * g + 4 * half]);
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-#pragma unroll
-          for (int x = 0; x < 2; ++x) {
-            const float e = __builtin_amdgcn_exp2f(__fmaf_rn(acc[x][4 * g + r], p.kappa, n4[r]));
-            sum[x] += key0 + 32 * x + col < v4[r] ? e : 0.0f;
-          }
-      }
+      nothing();
     }
-    if (i + 1 < i1 && wave == 0) {
-      s_nl[stage ^ 1][lane] = nl;
-      s_vis[stage ^ 1][lane] = vis;
-    }
+    stage ^= 1;
   }
+  weights(acc_b, row_b);
 #pragma unroll
   for (int x = 0; x < 2; ++x) {
-    const float y = half_sum(sum[x]);
+    const float y = half_sum(sum[x][0] + sum[x][1]);
     const int key = key0 + 32 * x + col;
     if (half == x && key < len) {
-      const size_t at = (size_t)bh * p.Nk + key;
+      const size_t at = ((size_t)b * p.Hkv + hkv) * p.Nk + key;
       if (alone) p.w[at] = (p.w_in ? p.w_in[at] : 0.0f) + y;
       else p.part[(size_t)piece * p.B * p.Hkv * p.Nk + at] = y;
+    }
+  }
+}
+
+// Few queries (a group's rows fit one operand): nothing but the keys is read to speak of, and each of them once.  The queries stay in
+// registers, and a wavefront walks over tiles of 32 keys that go from memory to registers, one tile ahead; no LDS, no
+// barrier, and rows that are not there are paid for in products that nobody waits for.
+template <int D, bool BF16>
+__global__ void __launch_bounds__(256, D == 256 ? 2 : 3) k_key_weights_few(const KwParams p) {
+  constexpr int KS = D / 16;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int col = lane & 31, half = lane >> 5;
+  unsigned bh = blockIdx.x;
+  const int chunk = (int)split_by(bh, p.by_heads);
+  unsigned hkv = bh;
+  const int b = (int)split_by(hkv, p.by_hkv);
+  const int len = kw_len(p, b), rows = p.G * p.N, coff = max(len - p.N, 0);
+  const int tiles = (len + 31) / 32, j0 = chunk * 4 * p.piece + wave, j1 = min(j0 + 4 * p.piece, tiles);
+  if (j0 >= j1) return;
+  const unsigned short* kb = p.k + head_offset_of(p.km, b, (int)hkv) + 8 * half;
+  const size_t wb = (size_t)bh * p.Nk;
+  struct Keys { v4i k[KS]; float w; };
+  auto load = [&](Keys& x, int j) __attribute__((always_inline)) {
+    const int key = min(32 * j + col, len - 1);
+    const unsigned short* at = kb + (size_t)key * p.km.sn;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) x.k[s] = *reinterpret_cast<const v4i*>(at + 16 * s);
+    x.w = p.w_in ? p.w_in[wb + key] : 0.0f;
+  };
+  Keys ka, kc;
+  load(ka, j0);
+  // ---- the queries: row l % 32 of the operand, and the constants of the rows of my accumulators (8 g + 4 h + r)
+  v4i q[KS];
+  {
+    unsigned n = (unsigned)min(col, rows - 1);
+    const int g = (int)split_by(n, p.by_n);
+    const unsigned short* at = p.q + head_offset_of(p.qm, b, (int)hkv * p.G + g) + (size_t)n * p.qm.sn + 8 * half;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) q[s] = *reinterpret_cast<const v4i*>(at + 16 * s);
+  }
+  float mine = INFINITY;                          // lse of row `lane`
+  if (lane < rows) {
+    unsigned n = (unsigned)lane;
+    const int g = (int)split_by(n, p.by_n);
+    mine = p.lse[((size_t)b * p.H + (int)hkv * p.G + g) * p.N + n];
+  }
+  const bool blind = __ballot(mine == -INFINITY) != 0;      // (a row that saw nothing: whatever its scores, it adds nothing)
+  const int sees_all = blind ? 0 : p.causal ? min(coff + 1, len) : len;
+  float nl[16];
+#pragma unroll
+  for (int v = 0; v < 16; ++v) nl[v] = -__shfl(mine, 8 * (v >> 2) + 4 * half + (v & 3)) * LOG2E;
+
+  auto tile = [&](const Keys& k, int j) __attribute__((always_inline)) {
+    v16f acc;
+#pragma unroll
+    for (int v = 0; v < 16; ++v) acc[v] = 0.0f;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) acc = mfma16<BF16>(q[s], k.k[s], acc);
+    const int key = 32 * j + col;
+    float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (32 * j + 32 <= sees_all) {
+#pragma unroll
+      for (int v = 0; v < 16; ++v) sum[v & 3] += __builtin_amdgcn_exp2f(__fmaf_rn(acc[v], p.kappa, nl[v]));
+    } else {
+#pragma unroll
+      for (int v = 0; v < 16; ++v) {
+        unsigned n = (unsigned)min(8 * (v >> 2) + 4 * half + (v & 3), rows - 1);
+        (void)split_by(n, p.by_n);
+        // (an lse of -inf or a row that is not there has +inf or -inf here)
+        const bool see = fabsf(nl[v]) < INFINITY || nl[v] != nl[v];
+        const float e = __builtin_amdgcn_exp2f(__fmaf_rn(acc[v], p.kappa, nl[v]));
+        sum[v & 3] += see && key < (p.causal ? min(coff + (int)n + 1, len) : len) ? e : 0.0f;
+      }
+    }
+    const float y = half_sum((sum[0] + sum[1]) + (sum[2] + sum[3]));
+    if (half == 0 && key < len) p.w[wb + key] = k.w + y;
+  };
+  for (int j = j0; j < j1; j += 8) {
+    if (j + 4 < j1) load(kc, j + 4);
+    tile(ka, j);
+    if (j + 4 < j1) {
+      if (j + 8 < j1) load(ka, j + 8);
+      tile(kc, j + 4);
     }
   }
 }
@@ -188,7 +378,13 @@ __global__ void __launch_bounds__(256) k_key_weights_sum(const KwParams p) {
   const int n = (it.count + p.piece - 1) / p.piece;
   const size_t at = (size_t)bh * p.Nk + key, step = (size_t)p.B * p.Hkv * p.Nk;
   float y = 0.0f;
-  for (int i = 0; i < n; ++i) y += p.part[i * step + at];
+  for (int i0 = 0; i0 < n; i0 += 8) {             // eight loads in flight, added in order
+    float x[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = p.part[(size_t)min(i0 + i, n - 1) * step + at];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y += i0 + i < n ? x[i] : 0.0f;
+  }
   p.w[at] = (p.w_in ? p.w_in[at] : 0.0f) + y;
 }
 
@@ -223,10 +419,29 @@ int kw_params(const sage_attn_key_weights_args* a, KwParams* p, bool need_io) {
     most = std::max(most, c);
   }
   p->key_tiles = (int)kts;
-  p->piece = (int)std::min<long long>(most, std::max(16LL, (heads * all + 2047) / 2048));
+  p->by_heads = fast_div((unsigned)heads); p->by_hkv = fast_div((unsigned)a->H_kv); p->by_kt = fast_div((unsigned)kts); p->by_n = fast_div((unsigned)a->N);
+  // As many tiles as give 1024 workgroups, 2 to 16: what a workgroup does before its first tile costs as much as three to six, but
+  // with fewer of them the last ones run alone.  Us, tiles of a workgroup: 66 k tiles (8192 causal queries, 32 heads of 128) 4 / 8 / 16 / 32
+  // 339 / 306 / 296 / 293, 17 k 103 / 94 / 93 / 97, 9 k (not causal) 52 / 49 / 53 / 60, 1.2 k 24 / 28 / 46 / 64, 96 (2 / 4 / 8) 15 / 19 / 24; of 256
+  // channels 8 k 73 / 69 / 73; of 64 33 k 134 / 119 / 116 / 120.
+  p->piece = (int)std::min<long long>(std::min(most, KW_PIECE), std::max(2LL, (heads * all + 1023) / 1024));
   p->pieces = (most + p->piece - 1) / p->piece;
-  if (heads * kts * p->pieces > 0x7fffffffLL) return SAGE_ERR_UNSUPPORTED;
+  // (With two operands, 33 to 64 rows, the registers leave two wavefronts per SIMD: 64 rows on 16 caches of 6000 keys 23.6 us, with tiles 13.6.)
+  p->few = (long long)p->G * a->N <= KW_FEW;
+  if (p->few) {                  // tiles of 32 keys per wavefront: until there are 12 wavefronts per CU
+    const long long tiles = (a->N_kv + 31) / 32;
+    p->pieces = 1;
+    p->piece = (int)std::max(1LL, std::min(64LL, heads * tiles / (256 * 12)));
+    p->key_tiles = (int)((tiles + 4 * p->piece - 1) / (4 * p->piece));
+  }
+  if (heads * p->key_tiles * p->pieces > 0x7fffffffLL) return SAGE_ERR_UNSUPPORTED;
   return SAGE_OK;
+}
+
+template <int D, bool BF16> hipError_t launch_kw(const KwParams& p, unsigned blocks, hipStream_t s) {
+  if (!p.few) k_key_weights<D, BF16><<<blocks, 256, 0, s>>>(p);
+  else k_key_weights_few<D, BF16><<<blocks, 256, 0, s>>>(p);
+  return hipGetLastError();
 }
 
 size_t kw_bytes(const KwParams& p) { return p.pieces == 1 ? 0 : align256((size_t)p.pieces * p.B * p.Hkv * p.Nk * sizeof(float)); }
@@ -250,10 +465,10 @@ extern "C" int sage_attn_key_weights(const sage_attn_key_weights_args* a) {
   const hipStream_t s = (hipStream_t)a->stream;
   const unsigned blocks = (unsigned)((long long)p.B * p.Hkv * p.key_tiles * p.pieces);
   const bool bf16 = a->dtype == SAGE_DT_BF16;
-  if (a->d == 64) { if (bf16) k_key_weights<64, true><<<blocks, 256, 0, s>>>(p); else k_key_weights<64, false><<<blocks, 256, 0, s>>>(p); }
-  else if (a->d == 128) { if (bf16) k_key_weights<128, true><<<blocks, 256, 0, s>>>(p); else k_key_weights<128, false><<<blocks, 256, 0, s>>>(p); }
-  else { if (bf16) k_key_weights<256, true><<<blocks, 256, 0, s>>>(p); else k_key_weights<256, false><<<blocks, 256, 0, s>>>(p); }
-  st = op_status(hipGetLastError());
+  const hipError_t e = a->d == 64 ? (bf16 ? launch_kw<64, true>(p, blocks, s) : launch_kw<64, false>(p, blocks, s))
+                     : a->d == 128 ? (bf16 ? launch_kw<128, true>(p, blocks, s) : launch_kw<128, false>(p, blocks, s))
+                                   : (bf16 ? launch_kw<256, true>(p, blocks, s) : launch_kw<256, false>(p, blocks, s));
+  st = op_status(e);
   if (st != SAGE_OK || p.pieces == 1) return st;
   k_key_weights_sum<<<dim3((unsigned)p.key_tiles, (unsigned)(p.B * p.Hkv)), 256, 0, s>>>(p);
   return op_status(hipGetLastError());

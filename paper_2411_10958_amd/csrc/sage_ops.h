@@ -11,6 +11,9 @@ inline int op_status(hipError_t e) {
   return -4;      // SAGE_ERR_HIP
 }
 
+// Element offset of head h of batch b.
+__device__ __forceinline__ size_t head_offset_of(const TensorMap& m, int b, int h) { return (size_t)b * m.sb + (size_t)h * m.sh; }
+
 // 16-bit products on the matrix unit, 32 x 32 x 16: lane l supplies row (A) or column (B) l % 32 and contraction slots
 // 8 (l / 32) + 0..7; accumulator v of lane l is row 8 (v / 4) + 4 (l / 32) + v % 4, column l % 32.
 typedef short v8s __attribute__((ext_vector_type(8)));
@@ -22,6 +25,33 @@ template <bool BF16> __device__ __forceinline__ v16f mfma16(v4i a, v4i b, v16f c
     typedef _Float16 v8h __attribute__((ext_vector_type(8)));
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(v8h, a), __builtin_bit_cast(v8h, b), c, 0, 0, 0);
   }
+}
+
+// Division by a number that the host knows (numerators and divisors below 2^31): a product's high half and two shifts, where the
+// instruction sequence for an unknown divisor has some thirty.  With l = ceil(log2 d) and m = floor(2^32 (2^l - d) / d) + 1,
+// floor(n / d) = (t + (n - t >> s1)) >> s2 for t = the high half of m n, s1 = min(l, 1), s2 = max(l - 1, 0).
+struct FastDiv {
+  unsigned d, m, s1, s2;
+};
+inline FastDiv fast_div(unsigned d) {
+  unsigned l = 0;
+  while (l < 32 && (1ull << l) < d) ++l;
+  FastDiv f;
+  f.d = d;
+  f.m = (unsigned)(((1ull << 32) * ((1ull << l) - d)) / d + 1);
+  f.s1 = l < 1 ? l : 1;
+  f.s2 = l > 1 ? l - 1 : 0;
+  return f;
+}
+__device__ __forceinline__ unsigned div_by(unsigned n, const FastDiv& f) {
+  const unsigned t = (unsigned)(((unsigned long long)f.m * n) >> 32);
+  return (t + ((n - t) >> f.s1)) >> f.s2;
+}
+// Quotient; n becomes the remainder.
+__device__ __forceinline__ unsigned split_by(unsigned& n, const FastDiv& f) {
+  const unsigned q = div_by(n, f);
+  n -= q * f.d;
+  return q;
 }
 
 // Sum / maximum of a value over the two halves of the wavefront, in both.
