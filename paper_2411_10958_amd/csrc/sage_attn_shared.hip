@@ -39,6 +39,8 @@ struct SharedParams {
   int Sp, So;                    // key chunks of the prefix and of the own keys
   int rtp, rto;                  // row tiles of the prefix (of B G N rows) and of the own keys (of G N rows)
   int n_prefix;                  // workgroups of the prefix; those of the own keys follow
+  int full;                      // of them, those of whole groups of 8 chunks
+  FastDiv by_group, by_rtp, by_hkv, by_rto, by_b, by_gn, by_n, by_rows;      // 8 rtp, rtp, H_kv, rto, B, G N, N, B G N
 };
 
 // Where partial result `s` of a row is kept: the prefix's chunks first, then the own ones.  Rows are numbered (KV head, batch, head of
@@ -65,32 +67,36 @@ __global__ void __launch_bounds__(64 * shared_waves<D>(), shared_occupancy<D>())
   const int col = lane & 31, half = lane >> 5;
 
   // ---- which rows and keys
-  int id = blockIdx.x, hkv, b = 0, rt, s;
-  const bool prefix = id < p.n_prefix;
+  unsigned id = blockIdx.x, hkv, b = 0, rt, s;
+  const bool prefix = (int)id < p.n_prefix;
   if (prefix) {
     // The row tiles of a chunk read the same keys: they are 8 apart, since workgroups go to the 8 XCDs in turn and each has a cache
-    // of its own.  (The last chunks, fewer than 8, have theirs side by side.)
-    const int chunks = p.Sp * p.Hkv, full = chunks / 8 * 8 * p.rtp;
-    const int grp = id < full ? id / (8 * p.rtp) : chunks / 8, wide = id < full ? 8 : chunks % 8, in = id - grp * 8 * p.rtp;
-    rt = in / wide;
-    const int chunk = grp * 8 + in % wide;
-    hkv = chunk % p.Hkv; s = chunk / p.Hkv;
+    // of its own.  (The last chunks, fewer than 8, have a chunk's side by side.)
+    if ((int)id < p.full) {
+      const unsigned group = split_by(id, p.by_group);
+      s = group * 8 + id % 8;
+      rt = id / 8;
+    } else {
+      rt = id - (unsigned)p.full;
+      const unsigned before = div_by((unsigned)p.full, p.by_rtp);
+      s = before + split_by(rt, p.by_rtp);
+    }
+    hkv = s;
+    s = split_by(hkv, p.by_hkv);
   } else {
-    id -= p.n_prefix;
-    rt = id % p.rto; id /= p.rto;
-    hkv = id % p.Hkv; id /= p.Hkv;
-    b = id % p.B; s = id / p.B;
+    rt = id - (unsigned)p.n_prefix;
+    hkv = split_by(rt, p.by_rto);
+    b = split_by(hkv, p.by_hkv);
+    s = split_by(b, p.by_b);
   }
-  const int GN = p.G * p.N;
-  const long long rows = prefix ? (long long)p.B * GN : GN;
-  const long long r0 = (long long)rt * ROWS;
-  const int nr = (int)min((long long)ROWS, rows - r0);     // rows of this workgroup
-  const int nk = prefix ? p.P : own_len(p, b);
+  const int GN = p.G * p.N, rows = prefix ? p.B * GN : GN, r0 = (int)rt * ROWS;
+  const int nr = min(ROWS, rows - r0);            // rows of this workgroup
+  const int nk = prefix ? p.P : own_len(p, (int)b);
   const int tiles = (nk + SH_KEYS - 1) / SH_KEYS, S = prefix ? p.Sp : p.So;
   const int per = (tiles + S - 1) / S;
-  const int j0 = min(s * per, tiles), j1 = min(j0 + per, tiles);
-  const int sp = prefix ? s : p.Sp + s;
-  const long long i0 = prefix ? r0 : (long long)b * GN + r0;  // first row in the numbering of part_row
+  const int j0 = min((int)s * per, tiles), j1 = min(j0 + per, tiles);
+  const int sp = (int)s + (prefix ? 0 : p.Sp);
+  const int i0 = prefix ? r0 : (int)b * GN + r0;  // first row in the numbering of part_row
 
   // Wavefronts: 32 rows each; where half of them do for the rows, two share rows and take every other 32 keys
   const int WK = nr <= ROWS / 2 ? 2 : 1;
@@ -99,7 +105,7 @@ __global__ void __launch_bounds__(64 * shared_waves<D>(), shared_occupancy<D>())
 
   if (j0 >= j1) {                                 // no keys: a partial result that the merge skips
     for (int i = t; i < nr; i += 64 * W) {
-      float* ml = p.part_ml + part_row(p, sp, hkv, i0 + i) * 2;
+      float* ml = p.part_ml + part_row(p, sp, (int)hkv, i0 + i) * 2;
       ml[0] = -INFINITY;
       ml[1] = 0.0f;
     }
@@ -108,36 +114,51 @@ __global__ void __launch_bounds__(64 * shared_waves<D>(), shared_occupancy<D>())
 
   // ---- my row's query as the B operand, and how many keys it sees
   const int row = min(rg * 32 + col, nr - 1);
-  const long long i = i0 + row;
-  const int rb = (int)(i / GN), rgn = (int)(i - (long long)rb * GN), rg_h = rgn / p.N, rn = rgn - rg_h * p.N;
-  const size_t qrow = row_offset(p.qm, head_offset(p.qm, (unsigned)(rb * p.H + hkv * p.G + rg_h)), rn);
+  const int i = i0 + row;
+  unsigned rn = (unsigned)i;
+  const unsigned rb = split_by(rn, p.by_gn), rh = split_by(rn, p.by_n);
+  const size_t qrow = row_offset(p.qm, head_offset_of(p.qm, (int)rb, (int)(hkv * p.G + rh)), (int)rn);
   v4i q[KS];
 #pragma unroll
   for (int st = 0; st < KS; ++st) q[st] = *reinterpret_cast<const v4i*>(p.q + qrow + 16 * st + 8 * half);
   const int coff = max(nk - p.N, 0);
-  const int vis = prefix || !p.causal ? nk : min(coff + rn + 1, nk);
+  const int vis = prefix || !p.causal ? nk : min(coff + (int)rn + 1, nk);
   const int vis_all = prefix || !p.causal ? nk : min(coff + 1, nk);       // keys that every query sees
 
   // ---- copies of a tile: rows behind the last key repeat it, so that masked places hold finite values where the keys do
   const TensorMap& m = prefix ? p.pm : p.om;
-  const size_t head = head_offset(m, prefix ? (unsigned)hkv : (unsigned)(b * p.Hkv + hkv));
+  const size_t head = head_offset_of(m, (int)b, (int)hkv);
   const char* gk = uniform_ptr(reinterpret_cast<const char*>((prefix ? p.kp : p.ko) + head));
   const char* gv = uniform_ptr(reinterpret_cast<const char*>((prefix ? p.vp : p.vo) + head));
   const unsigned lds0 = (unsigned)(size_t)(__attribute__((address_space(3))) char*)&s_kv[0][0];
   const unsigned step = (unsigned)m.sn * 2;       // bytes from token to token
-  auto copy = [&](int j, int stage) {
-    const size_t at = (size_t)j * SH_KEYS * m.sn * 2;
-    const int last = nk - 1 - j * SH_KEYS;
+  constexpr int COPIES = TILE / (64 * W);         // of a tile of K (or V), by a wavefront
+  unsigned offs[COPIES];
 #pragma unroll
-    for (int x = 0; x < TILE / (64 * W); ++x) {
-      const int pc = (x * W + wave) * 64 + lane, r = pc / NP, c = (pc % NP) ^ swizzle<D>(r);
-      const unsigned off = (unsigned)min(r, last) * step + (unsigned)c * 16;
-      const unsigned to = lds0 + (unsigned)(stage * 2 * TILE + (x * W + wave) * 64) * 16;
-      dma_b128(gk + at, off, to);
-      dma_b128(gv + at, off, to + TILE * 16);
+  for (int x = 0; x < COPIES; ++x) {
+    const int pc = (x * W + wave) * 64 + lane, r = pc / NP;
+    offs[x] = (unsigned)r * step + (unsigned)((pc % NP) ^ swizzle<D>(r)) * 16;
+  }
+  auto copy = [&](int j, int stage) __attribute__((always_inline)) {
+    const size_t at = (size_t)j * SH_KEYS * m.sn * 2;
+    const unsigned to = lds0 + (unsigned)(stage * 2 * TILE + wave * 64) * 16;
+    const int last = nk - 1 - j * SH_KEYS;
+    if (last >= SH_KEYS - 1) {
+#pragma unroll
+      for (int x = 0; x < COPIES; ++x) {
+        dma_b128(gk + at, offs[x], to + x * (W * 1024));
+        dma_b128(gv + at, offs[x], to + TILE * 16 + x * (W * 1024));
+      }
+    } else {
+#pragma unroll 1
+      for (int x = 0; x < COPIES; ++x) {
+        const int pc = (x * W + wave) * 64 + lane, r = pc / NP, c = (pc % NP) ^ swizzle<D>(r);
+        const unsigned off = (unsigned)min(r, last) * step + (unsigned)c * 16;
+        dma_b128(gk + at, off, to + x * (W * 1024));
+        dma_b128(gv + at, off, to + TILE * 16 + x * (W * 1024));
+      }
     }
   };
-
   // The first tile is on its way while the queries come; the wait for them is one for it too, since loads are counted in order.  From
   // there on two tiles are in flight.
   copy(j0, 0);
@@ -235,7 +256,7 @@ __global__ void __launch_bounds__(64 * shared_waves<D>(), shared_occupancy<D>())
       }
   };
 
-  constexpr int PER_TILE = 2 * (TILE / (64 * W));       // copies of a tile that a wavefront starts
+  constexpr int PER_TILE = 2 * COPIES;            // copies of a tile that a wavefront starts
   for (int j = j0; j < j1; ++j) {
     const int stage = (j - j0) & 1;
     if (j + 1 < j1) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(PER_TILE) : "memory");
@@ -285,7 +306,7 @@ __global__ void __launch_bounds__(64 * shared_waves<D>(), shared_occupancy<D>())
     }
   }
   if (!active || rg * 32 + col >= nr) return;
-  const size_t pr = part_row(p, sp, hkv, i);
+  const size_t pr = part_row(p, sp, (int)hkv, i);
   if (half == 0) {
     p.part_ml[pr * 2] = mx;
     p.part_ml[pr * 2 + 1] = l;
@@ -309,12 +330,12 @@ template <int D, bool BF16>
 __global__ void __launch_bounds__(256) k_shared_merge(const SharedParams p) {
   constexpr int LPR = D / 4, GRP = 64 / LPR;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const long long rows = (long long)p.B * p.G * p.N;
-  const long long id = (long long)blockIdx.x * 4 + wave;
-  if (id >= rows * p.Hkv) return;
-  const int hkv = (int)(id / rows);
-  const long long i = id - hkv * rows;
-  const int GN = p.G * p.N, b = (int)(i / GN), rgn = (int)(i - (long long)b * GN), g = rgn / p.N, n = rgn - g * p.N;
+  unsigned row = blockIdx.x * 4 + (unsigned)wave;
+  if (row >= (unsigned)(p.B * p.G * p.N * p.Hkv)) return;
+  const int hkv = (int)split_by(row, p.by_rows);
+  const long long i = row;
+  unsigned n = row;
+  const int b = (int)split_by(n, p.by_gn), g = (int)split_by(n, p.by_n);
   const int S = p.Sp + p.So, c = 4 * (lane % LPR), grp = lane / LPR;
   float ms[MERGE_PER_LANE], w[MERGE_PER_LANE], m = -INFINITY, l = 0.0f;
 #pragma unroll
@@ -365,18 +386,25 @@ __global__ void __launch_bounds__(256) k_shared_merge(const SharedParams p) {
   const bool none = m == -INFINITY && l == 0.0f;  // no key at all: zeros
   const float inv = none ? 0.0f : __fdiv_rn(1.0f, l);
   if (p.lse && c == 0) p.lse[((size_t)b * p.H + h) * p.N + n] = none ? -INFINITY : LN2 * (m + __builtin_amdgcn_logf(l));
-  unsigned short* y = p.out + row_offset(p.qm, head_offset(p.qm, (unsigned)(b * p.H + h)), n) + c;
+  unsigned short* y = p.out + row_offset(p.qm, head_offset_of(p.qm, b, h), (int)n) + c;
   *reinterpret_cast<uint2*>(y) = make_uint2(pack16x2<BF16>(acc[0] * inv, acc[1] * inv), pack16x2<BF16>(acc[2] * inv, acc[3] * inv));
 }
 
-// Key chunks: so many that the workgroups fill the places of the chip, each with at least four tiles.
-void choose_chunks(SharedParams* p, int d) {
+// Tiles of a key chunk.  The chip has room for 256, 512 or 768 workgroups (of 256, 128, 64 channels), and each has its start to pay
+// for, so 512 / d tiles at least.  A workgroup of the prefix takes an even share of all tiles - it has up to 128 rows of partial
+// results to leave - and where it has few rows and is bound by reading, so many that there is one to a CU.  The own keys of a
+// sequence have few rows, and lengths that the host does not know: they are cut finer, 12 tiles at most, so that the chip fills up to
+// the end.  Us, an even share for both / this: 64 sequences of up to 4096 tokens over 32768, 128 channels 174 / 162;
+// 1 of 300 over 32768 33.4 / 31.5; 4 of 2000 over 100000 88.8 / 86.1; 32 of 3000 over 200 50.9 / 49.3.
+void choose_chunks(SharedParams* p, int d, long long rows) {
   const long long tp = (p->P + SH_KEYS - 1) / SH_KEYS, to = (p->Nk + SH_KEYS - 1) / SH_KEYS;
-  const long long np = (long long)p->Hkv * p->rtp, no = (long long)p->B * p->Hkv * p->rto;
-  const long long places = 256LL * (d == 64 ? 3 : d == 128 ? 2 : 1);
-  long long per = std::max(4LL, (np * tp + no * to + places - 1) / places);
-  p->Sp = (int)std::min((long long)MAX_PARTS / 2, (tp + per - 1) / per);
-  p->So = (int)std::min((long long)MAX_PARTS / 2, (to + per - 1) / per);
+  const long long prefix = (long long)p->Hkv * p->rtp * tp, own = (long long)p->B * p->Hkv * p->rto * to;
+  const long long places = 256LL * (d == 64 ? 3 : d == 128 ? 2 : 1), least = 512 / d;
+  long long share = (prefix + own + places - 1) / places;
+  if (rows <= 64) share = std::max(share, (prefix + 255) / 256);
+  const long long pp = std::max(least, share), po = std::max(least, std::min(12LL, (own + places - 1) / places));
+  p->Sp = (int)std::min((long long)MAX_PARTS / 2, (tp + pp - 1) / pp);
+  p->So = (int)std::min((long long)MAX_PARTS / 2, (to + po - 1) / po);
 }
 
 int shared_params(const sage_attn_shared_prefix_args* a, SharedParams* p, bool need_io) {
@@ -407,10 +435,13 @@ int shared_params(const sage_attn_shared_prefix_args* a, SharedParams* p, bool n
   const int per = shared_rows(a->d);
   p->rtp = (int)((rows + per - 1) / per);
   p->rto = (int)((gn + per - 1) / per);
-  choose_chunks(p, a->d);
+  choose_chunks(p, a->d, rows);
   const long long np = (long long)p->Sp * p->Hkv * p->rtp, no = (long long)p->So * p->B * p->Hkv * p->rto;
   if (np + no > 0x7fffffffLL || rows * p->Hkv > 0x7fffffffLL) return SAGE_ERR_UNSUPPORTED;
   p->n_prefix = (int)np;
+  p->full = p->Sp * a->H_kv / 8 * 8 * p->rtp;
+  p->by_group = fast_div(8u * p->rtp); p->by_rtp = fast_div(p->rtp); p->by_hkv = fast_div(a->H_kv); p->by_rto = fast_div(p->rto);
+  p->by_b = fast_div(a->B); p->by_gn = fast_div((unsigned)gn); p->by_n = fast_div(a->N); p->by_rows = fast_div((unsigned)rows);
   return SAGE_OK;
 }
 
