@@ -506,8 +506,8 @@ def sage_rope(q, k=None, inv_freq=None, positions=None, offset=0, interleaved=Fa
     """Rotary positions of q and k in one launch: the first 2 * len(inv_freq) channels of every row are turned, the others copied.
     q [B, H, N, d], k [B, H_kv, N, d] or None (layout "HND"; tokens outside heads with "NHD"), or packed [tokens, heads, d] with positions
     [tokens].  Any strides will do while the channels are contiguous.  positions: int32 [N] or [B, N] (None: 0 .. N - 1), `offset` is
-    added.  inverse turns back; with the same scale that is the gradient.  q_out, k_out may be q and k.  Returns q_out, or
-    (q_out, k_out)."""
+    added.  inverse turns back; with the same scale (0 stands for 1) that is the gradient.  q_out, k_out may be q and k.  Returns
+    q_out, or (q_out, k_out)."""
     if inv_freq is None:
         raise ValueError("inv_freq is needed (see sage_rope_frequencies)")
     dtype, index = _dtype_code(q), _gpu_of("q", q)
@@ -558,6 +558,8 @@ def sage_rope(q, k=None, inv_freq=None, positions=None, offset=0, interleaved=Fa
         if packed:
             s = (0,) + s[:-1]
         st[0], st[1], st[2] = (s[0], s[2], s[1]) if nhd else s[:3]
+        if not any(st):
+            raise ValueError("one row expanded over all others is not supported (strides of zero stand for a contiguous tensor)")
     _call("sage_rope", a, index)
     return outs[0] if k is None else tuple(outs)
 

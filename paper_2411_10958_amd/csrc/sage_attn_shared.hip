@@ -20,6 +20,11 @@
 namespace sage {
 namespace {
 
+template <bool BF16> __device__ __forceinline__ bool not_finite(unsigned x) {
+  constexpr unsigned EXP = BF16 ? 0x7f80 : 0x7c00;
+  return (x & EXP) == EXP;
+}
+
 constexpr int SH_KEYS = 64;      // keys of a tile
 // Wavefronts of a workgroup, 32 query rows each.  Two wavefronts share a SIMD where 128 rows do (one's vector work runs beside
 // the other's products); 256-wide heads, whose two tiles of K and V fill the LDS of a CU, need eight in one workgroup for that.
@@ -124,6 +129,7 @@ __global__ void __launch_bounds__(64 * shared_waves<D>(), shared_occupancy<D>())
   const int coff = max(nk - p.N, 0);
   const int vis = prefix || !p.causal ? nk : min(coff + (int)rn + 1, nk);
   const int vis_all = prefix || !p.causal ? nk : min(coff + 1, nk);       // keys that every query sees
+  const bool part_seen = vis_all < nk;            // ... and others that some do
 
   // ---- copies of a tile: rows behind the last key repeat it, so that masked places hold finite values where the keys do
   const TensorMap& m = prefix ? p.pm : p.om;
@@ -173,6 +179,33 @@ __global__ void __launch_bounds__(64 * shared_waves<D>(), shared_occupancy<D>())
   for (int c = 0; c < CT; ++c)
 #pragma unroll
     for (int v = 0; v < 16; ++v) o[c][v] = 0.0f;
+  // A value that is not finite, of a key that some queries of a tile see and others do not: 0 times it would reach those that do not.  Such
+  // tiles - the last ones of a causal chunk of queries, looked at only there - have these values taken out before the
+  // products; in the end they are added to the outputs of the queries that see them.
+  bool taken_out = false;
+  auto take_out = [&](int stage) {
+    v4i* tv = &s_kv[stage][TILE];
+    int odd = 0;
+#pragma unroll 1
+    for (int x = t; x < TILE; x += 64 * W) {
+      const v4i u = tv[x];
+#pragma unroll
+      for (int y = 0; y < 4; ++y) odd |= not_finite<BF16>((unsigned)u[y] & 0xffff) || not_finite<BF16>((unsigned)u[y] >> 16);
+    }
+    if (__syncthreads_or(odd) == 0) return;
+    taken_out = true;
+#pragma unroll 1
+    for (int x = t; x < TILE; x += 64 * W) {
+      v4i u = tv[x];
+#pragma unroll
+      for (int y = 0; y < 4; ++y) {
+        if (not_finite<BF16>((unsigned)u[y] & 0xffff)) u[y] &= (int)0xffff0000;
+        if (not_finite<BF16>((unsigned)u[y] >> 16)) u[y] &= 0xffff;
+      }
+      tv[x] = u;
+    }
+    __syncthreads();
+  };
   float mx = -INFINITY, l = 0.0f;                 // running maximum (of both halves) and this half's sum
 
   // Where my operands start in a tile.  A row's first byte has its low bits zero and the swizzle of a row repeats every 16 rows, so a
@@ -264,6 +297,7 @@ __global__ void __launch_bounds__(64 * shared_waves<D>(), shared_occupancy<D>())
     __builtin_amdgcn_s_barrier();                 // tile j is there
     asm volatile("" ::: "memory");
     const unsigned at = lds0 + (unsigned)stage * (2 * TILE * 16);
+    if (part_seen && (j + 1) * SH_KEYS > vis_all) take_out(stage);
     if (active) {
       if (D < 256 && WK == 1 && j * SH_KEYS + 32 < nk) tile_keys(std::integral_constant<int, 2>{}, at, j * SH_KEYS, 0);
       else for (int sub = kg; sub < 2 && j * SH_KEYS + 32 * sub < nk; sub += WK) tile_keys(std::integral_constant<int, 1>{}, at, j * SH_KEYS, sub);
@@ -306,6 +340,22 @@ __global__ void __launch_bounds__(64 * shared_waves<D>(), shared_occupancy<D>())
     }
   }
   if (!active || rg * 32 + col >= nr) return;
+  if (taken_out) {
+    const int to = min(vis, j1 * SH_KEYS);
+#pragma unroll 1
+    for (int k = max(vis_all, j0 * SH_KEYS) / SH_KEYS * SH_KEYS; k < to; ++k) {      // (whole tiles were looked at)
+      const char* v = gv + (size_t)k * step + 8 * half;
+#pragma unroll
+      for (int c = 0; c < CT; ++c)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const uint2 u = *reinterpret_cast<const uint2*>(v + 64 * c + 16 * g);
+          const unsigned y[4] = {u.x & 0xffff, u.x >> 16, u.y & 0xffff, u.y >> 16};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[c][4 * g + e] += not_finite<BF16>(y[e]) ? load16<BF16>((unsigned short)y[e]) : 0.0f;
+        }
+    }
+  }
   const size_t pr = part_row(p, sp, (int)hkv, i);
   if (half == 0) {
     p.part_ml[pr * 2] = mx;

@@ -197,13 +197,13 @@ extern "C" int sage_rope(const sage_rope_args* a) {
     const int heads = (i & 1) ? a->H_kv : a->H;
     if ((i & 1) && !keys) { st[i][0] = st[i][1] = st[i][2] = 0; continue; }
     if (!tensor_strides(given[i], a->layout, heads, a->N, a->d, st[i])) return SAGE_ERR_INVALID_ARG;
+    const int extent[3] = {a->B, heads, a->N};
+    for (int x = 0; x < 3; ++x) if (extent[x] == 1) st[i][x] = 0;        // (no step is taken: whatever it is, it does not count)
     if (i >= 2 && !rows_apart(st[i], a->B, heads, a->N, a->d)) return SAGE_ERR_INVALID_ARG;
   }
   for (int i = 0; i < 2; ++i) {          // in place: the same rows, or a thread would overwrite what another has still to read
     const bool same = i == 0 ? a->q == a->q_out : keys && a->k == a->k_out;
-    const int heads = i == 0 ? a->H : a->H_kv;
-    if (same && ((a->B > 1 && st[i][0] != st[i + 2][0]) || (heads > 1 && st[i][1] != st[i + 2][1]) || (a->N > 1 && st[i][2] != st[i + 2][2])))
-      return SAGE_ERR_INVALID_ARG;
+    if (same && (st[i][0] != st[i + 2][0] || st[i][1] != st[i + 2][1] || st[i][2] != st[i + 2][2])) return SAGE_ERR_INVALID_ARG;
   }
   auto tensor = [&](const void* x, void* y, int i, int heads) {
     RopeTensor t;

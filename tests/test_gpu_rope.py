@@ -82,6 +82,24 @@ def test_views_of_a_fused_projection_in_place_and_misaligned_rows():
         assert (cache[:, :, :9] == 7).all() and (cache[:, :, 9 + N:] == 7).all()
 
 
+def test_expanded_inputs_and_strides_that_take_no_step():
+    pa = _pa()
+    g = _gen(8)
+    f = pa.sage_rope_frequencies(64)
+    pos = torch.arange(7, device="cuda")
+    one = torch.randn((1, 3, 1, 64), generator=g, device="cuda").to(torch.bfloat16)
+    x = one.expand(2, 3, 7, 64)                  # the same row at every token
+    ref.check("expanded", pa.sage_rope(x, None, f), *ref.rope(x, f, pos, False, False, 1.0, "HND"))
+    row = torch.randn(64, generator=g, device="cuda").to(torch.bfloat16)
+    with pytest.raises(ValueError):
+        pa.sage_rope(row.expand(2, 3, 7, 64), None, f)
+    with pytest.raises(pa.SageError):            # an output whose rows share memory
+        pa.sage_rope(x.contiguous(), None, f, q_out=x)
+    y = torch.randn(2 * 64 * 7 + 1, generator=g, device="cuda").to(torch.bfloat16)
+    y = torch.as_strided(y, (1, 2, 7, 64), (3, 448, 64, 1), 0)       # a stride of an extent of one
+    ref.check("no step", pa.sage_rope(y, None, f), *ref.rope(y, f, pos, False, False, 1.0, "HND"))
+
+
 def test_packed_batch_and_channels_that_are_not_turned():
     pa = _pa()
     g = _gen(5)

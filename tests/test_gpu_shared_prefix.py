@@ -96,6 +96,31 @@ def test_large_scores_and_values_that_are_not_numbers():
     assert torch.equal(out[~bad], clean[0][~bad]) and torch.equal(lse[~bad], clean[1][~bad])
 
 
+@pytest.mark.parametrize("d,H,N,Nk", [(64, 4, 2, 100), (128, 2, 5, 130), (128, 8, 40, 200), (256, 4, 40, 90), (256, 2, 3, 64)])
+def test_what_a_later_token_holds_does_not_reach_an_earlier_query(d, H, N, Nk):
+    """Keys and values of the chunk's own tokens that are not finite: queries before them have what they had, to the bit."""
+    pa = _pa()
+    q, kp, vp, k, v = _inputs(2, H, 2, N, 70, Nk, d, torch.float16 if d == 64 else torch.bfloat16, "HND", seed=d)
+    lens = torch.tensor([Nk, Nk - 3], dtype=torch.int32, device="cuda")
+    clean = pa.sage_attn_shared_prefix(q, kp, vp, k, v, kv_lens=lens, return_lse=True)
+    r = N // 2                                  # the token of query r of sequence 1: keys from there on are odd
+    t = Nk - 3 - N + r
+    v[1, 1, t, 5], v[1, 1, t + 1 if r + 1 < N else t, d - 1] = math.inf, math.nan
+    out, lse = pa.sage_attn_shared_prefix(q, kp, vp, k, v, kv_lens=lens, return_lse=True)
+    heads = torch.zeros(2, H, dtype=torch.bool, device="cuda")
+    heads[1, H // 2:] = True                    # those of KV head 1
+    assert torch.equal(out[~heads], clean[0][~heads]) and torch.equal(lse, clean[1])
+    assert torch.equal(out[1, H // 2:, :r], clean[0][1, H // 2:, :r])
+    assert (out[1, H // 2:, r:, 5] == math.inf).all() and out[1, H // 2:, -1, d - 1].isnan().all()
+    same = torch.ones(d, dtype=torch.bool, device="cuda")
+    same[5] = same[d - 1] = False
+    assert torch.equal(out[1, H // 2:, r:][..., same], clean[0][1, H // 2:, r:][..., same])
+    k[1, 1, t] = math.nan
+    out, lse = pa.sage_attn_shared_prefix(q, kp, vp, k, v, kv_lens=lens, return_lse=True)
+    assert torch.equal(out[1, H // 2:, :r], clean[0][1, H // 2:, :r]) and torch.equal(lse[1, H // 2:, :r], clean[1][1, H // 2:, :r])
+    assert lse[1, H // 2:, r:].isnan().all() and out[1, H // 2:, r:].isnan().all()
+
+
 def test_lse_merges_with_other_keys():
     """The prefix alone and the own keys alone, merged by their log-sum-exps, are the whole."""
     pa = _pa()
