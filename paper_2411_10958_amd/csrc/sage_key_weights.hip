@@ -428,10 +428,13 @@ int kw_params(const sage_attn_key_weights_args* a, KwParams* p, bool need_io) {
   p->pieces = (most + p->piece - 1) / p->piece;
   // (With two operands, 33 to 64 rows, the registers leave two wavefronts per SIMD: 64 rows on 16 caches of 6000 keys 23.6 us, with tiles 13.6.)
   p->few = (long long)p->G * a->N <= KW_FEW;
-  if (p->few) {                  // tiles of 32 keys per wavefront: until there are 12 wavefronts per CU
+  // tiles of 32 keys per wavefront: until there are 16 wavefronts per CU, a round and a third of those it holds.  (Us, for 8 / 12 / 16 / 32 of them,
+  // caches read from memory: 32 of 32768 keys, 128 channels, 45.4 / 51.3 / 46.3 / 46.9, 128 of 9000, 64, 26.0 / 27.1 / 25.1 / 24.5, 16 of 20000, 256, 32.3 / 34.1 /
+  // 32.5 / 33.8: with 12 a few are left for a round of their own.)
+  if (p->few) {
     const long long tiles = (a->N_kv + 31) / 32;
     p->pieces = 1;
-    p->piece = (int)std::max(1LL, std::min(64LL, heads * tiles / (256 * 12)));
+    p->piece = (int)std::max(1LL, std::min(64LL, heads * tiles / (256 * 16)));
     p->key_tiles = (int)((tiles + 4 * p->piece - 1) / (4 * p->piece));
   }
   if (heads * p->key_tiles * p->pieces > 0x7fffffffLL) return SAGE_ERR_UNSUPPORTED;

@@ -26,6 +26,7 @@ struct RopeParams {
   const int* positions;                  // null: the token's index
   long long pos_sb, offset, total;       // total: units of all tokens
   int N, d, rot, units, turned, hchunk;  // units per token, the first `turned` of which are rotated, the others copied
+  int lanes;                             // heads side by side in a workgroup
   float scale, sign;
 };
 
@@ -83,8 +84,8 @@ template <bool BF16, int VW, bool INTER>
 __global__ void __launch_bounds__(256) k_rope(const RopeParams p) {
   const long long id = (long long)blockIdx.x * 256 + threadIdx.x;
   if (id >= p.total) return;
-  const long long tok = id / p.units;
-  const int unit = (int)(id - tok * p.units);
+  const long long th = id / p.units, tok = th / p.lanes;
+  const int unit = (int)(id - th * p.units), hl = (int)(th - tok * p.lanes);
   const long long b = tok / p.N;
   const int n = (int)(tok - b * p.N);
   const bool turned = unit < p.turned;
@@ -113,19 +114,19 @@ __global__ void __launch_bounds__(256) k_rope(const RopeParams p) {
   auto run = [&](const RopeTensor& t, int ha, int hb) {
     const unsigned short* x = t.x + b * t.xb + (long long)n * t.xn;
     unsigned short* y = t.y + b * t.yb + (long long)n * t.yn;
-    for (int h = ha; h < hb; h += HU) {
+    for (int h = ha + hl; h < hb; h += HU * p.lanes) {
       V v0[HU], v1[HU];
 #pragma unroll
       for (int i = 0; i < HU; ++i) {
-        const unsigned short* r = x + (long long)min(h + i, hb - 1) * t.xh;
+        const unsigned short* r = x + (long long)min(h + i * p.lanes, hb - 1) * t.xh;
         v0[i] = *reinterpret_cast<const V*>(r + c0);
         v1[i] = *reinterpret_cast<const V*>(r + c1);
       }
 #pragma unroll
       for (int i = 0; i < HU; ++i) {
-        if (h + i >= hb) break;
+        if (h + i * p.lanes >= hb) break;
         if (turned) turn<BF16, VW, INTER>(v0[i], v1[i], c, s);
-        unsigned short* r = y + (long long)(h + i) * t.yh;
+        unsigned short* r = y + (long long)(h + i * p.lanes) * t.yh;
         *reinterpret_cast<V*>(r + c0) = v0[i];
         *reinterpret_cast<V*>(r + c1) = v1[i];
       }
@@ -229,13 +230,17 @@ extern "C" int sage_rope(const sage_rope_args* a) {
   // (in place, what is not turned stays where it is)
   const bool in_place = a->q == a->q_out && (!keys || a->k == a->k_out);
   p.units = p.turned + (in_place ? 0 : (a->d - a->rot_dim) / (2 * vw));
-  p.total = (long long)a->B * a->N * p.units;
+  // Token-major rows: neighbouring threads take neighbouring heads of a token, which are one stretch of memory; with a token each they
+  // would read pieces of 256 bytes, a token's row apart (4 x 4096 tokens of 40 heads of 128: 79 us, so 67).
+  p.lanes = 1;
+  if (st[0][1] < st[0][2] && a->N > 1) while (p.lanes * 2 * p.units <= 64 && p.lanes * 2 <= a->H) p.lanes *= 2;
+  p.total = (long long)a->B * a->N * p.units * p.lanes;
   const long long blocks = (p.total + 255) / 256;
   if (blocks > 0x7fffffffLL) return SAGE_ERR_UNSUPPORTED;
-  // Heads are divided over workgroups only until there are eight of these per CU: each pays for the angles again.
+  // Heads are divided over workgroups only until there are sixteen of these per CU: each pays for the angles again.  (Eight: 2 x 17776
+  // tokens of 96 heads of 64 172 us, sixteen 165.)  Heads that lie side by side in one stay together.
   const int heads = p.q.heads + p.k.heads;
-  long long pieces = (2048 + blocks - 1) / blocks;
-  if (pieces > heads) pieces = heads;
+  const long long pieces = std::max(1LL, std::min((4096 + blocks - 1) / blocks, (long long)heads / p.lanes));
   p.hchunk = (int)((heads + pieces - 1) / pieces);
   const dim3 grid((unsigned)blocks, (unsigned)((heads + p.hchunk - 1) / p.hchunk));
   const hipStream_t s = (hipStream_t)a->stream;
