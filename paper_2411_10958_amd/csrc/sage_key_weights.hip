@@ -286,14 +286,15 @@ __global__ void __launch_bounds__(256, kw_occupancy<D>()) k_key_weights(const Kw
   }
 }
 
-// Few queries (a group's rows fit one operand): nothing but the keys is read to speak of, and each of them once.  The queries stay in
+// Few queries (16 RT rows of a group at most): nothing but the keys is read to speak of, and each of them once.  The queries stay in
 // registers, and a wavefront walks over tiles of 32 keys that go from memory to registers, one tile ahead; no LDS, no
-// barrier, and rows that are not there are paid for in products that nobody waits for.
-template <int D, bool BF16>
-__global__ void __launch_bounds__(256, D == 256 ? 2 : 3) k_key_weights_few(const KwParams p) {
-  constexpr int KS = D / 16;
+// barrier, and rows that are not there are paid for in products that nobody waits for.  (Bound by reading: 64 caches of 16000 keys of 128
+// channels 50.5 us, 5.3 TB/s.)
+template <int D, bool BF16, int RT>
+__global__ void __launch_bounds__(256, D == 256 ? 2 : D == 128 && RT == 2 ? 3 : 4) k_key_weights_few(const KwParams p) {
+  constexpr int KS = D / 32;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int col = lane & 31, half = lane >> 5;
+  const int col = lane & 15, quad = lane >> 4;
   unsigned bh = blockIdx.x;
   const int chunk = (int)split_by(bh, p.by_heads);
   unsigned hkv = bh;
@@ -301,26 +302,29 @@ __global__ void __launch_bounds__(256, D == 256 ? 2 : 3) k_key_weights_few(const
   const int len = kw_len(p, b), rows = p.G * p.N, coff = max(len - p.N, 0);
   const int tiles = (len + 31) / 32, j0 = chunk * 4 * p.piece + wave, j1 = min(j0 + 4 * p.piece, tiles);
   if (j0 >= j1) return;
-  const unsigned short* kb = p.k + head_offset_of(p.km, b, (int)hkv) + 8 * half;
+  const unsigned short* kb = p.k + head_offset_of(p.km, b, (int)hkv) + 8 * quad;
   const size_t wb = (size_t)bh * p.Nk;
-  struct Keys { v4i k[KS]; float w; };
+  struct Keys { v4i k[2][KS]; float w; };
   auto load = [&](Keys& x, int j) __attribute__((always_inline)) {
-    const int key = min(32 * j + col, len - 1);
-    const unsigned short* at = kb + (size_t)key * p.km.sn;
 #pragma unroll
-    for (int s = 0; s < KS; ++s) x.k[s] = *reinterpret_cast<const v4i*>(at + 16 * s);
-    x.w = p.w_in ? p.w_in[wb + key] : 0.0f;
+    for (int c = 0; c < 2; ++c) {
+      const unsigned short* at = kb + (size_t)min(32 * j + 16 * c + col, len - 1) * p.km.sn;
+#pragma unroll
+      for (int s = 0; s < KS; ++s) x.k[c][s] = *reinterpret_cast<const v4i*>(at + 32 * s);
+    }
+    x.w = p.w_in && lane < 32 ? p.w_in[wb + min(32 * j + lane, len - 1)] : 0.0f;
   };
   Keys ka, kc;
   load(ka, j0);
-  // ---- the queries: row l % 32 of the operand, and the constants of the rows of my accumulators (8 g + 4 h + r)
-  v4i q[KS];
-  {
-    unsigned n = (unsigned)min(col, rows - 1);
-    const int g = (int)split_by(n, p.by_n);
-    const unsigned short* at = p.q + head_offset_of(p.qm, b, (int)hkv * p.G + g) + (size_t)n * p.qm.sn + 8 * half;
+  // ---- the queries: row l % 16 of RT operands, and the constants of the rows of my accumulators (4 (l / 16) + 0..3)
+  v4i q[RT][KS];
 #pragma unroll
-    for (int s = 0; s < KS; ++s) q[s] = *reinterpret_cast<const v4i*>(at + 16 * s);
+  for (int x = 0; x < RT; ++x) {
+    unsigned n = (unsigned)min(16 * x + col, rows - 1);
+    const int g = (int)split_by(n, p.by_n);
+    const unsigned short* at = p.q + head_offset_of(p.qm, b, (int)hkv * p.G + g) + (size_t)n * p.qm.sn + 8 * quad;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) q[x][s] = *reinterpret_cast<const v4i*>(at + 32 * s);
   }
   float mine = INFINITY;                          // lse of row `lane`
   if (lane < rows) {
@@ -330,34 +334,56 @@ __global__ void __launch_bounds__(256, D == 256 ? 2 : 3) k_key_weights_few(const
   }
   const bool blind = __ballot(mine == -INFINITY) != 0;      // (a row that saw nothing: whatever its scores, it adds nothing)
   const int sees_all = blind ? 0 : p.causal ? min(coff + 1, len) : len;
-  float nl[16];
+  float nl[RT][4];
 #pragma unroll
-  for (int v = 0; v < 16; ++v) nl[v] = -__shfl(mine, 8 * (v >> 2) + 4 * half + (v & 3)) * LOG2E;
+  for (int x = 0; x < RT; ++x)
+#pragma unroll
+    for (int v = 0; v < 4; ++v) nl[x][v] = -__shfl(mine, 16 * x + 4 * quad + v) * LOG2E;
 
   auto tile = [&](const Keys& k, int j) __attribute__((always_inline)) {
-    v16f acc;
+    v4f acc[2][RT];
 #pragma unroll
-    for (int v = 0; v < 16; ++v) acc[v] = 0.0f;
+    for (int c = 0; c < 2; ++c)
 #pragma unroll
-    for (int s = 0; s < KS; ++s) acc = mfma16<BF16>(q[s], k.k[s], acc);
-    const int key = 32 * j + col;
-    float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+      for (int x = 0; x < RT; ++x) acc[c][x] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int s = 0; s < KS; ++s)
+#pragma unroll
+      for (int c = 0; c < 2; ++c)
+#pragma unroll
+        for (int x = 0; x < RT; ++x) acc[c][x] = mfma16_small<BF16>(q[x][s], k.k[c][s], acc[c][x]);
+    float sum[2] = {0.0f, 0.0f};
     if (32 * j + 32 <= sees_all) {
 #pragma unroll
-      for (int v = 0; v < 16; ++v) sum[v & 3] += __builtin_amdgcn_exp2f(__fmaf_rn(acc[v], p.kappa, nl[v]));
+      for (int c = 0; c < 2; ++c)
+#pragma unroll
+        for (int x = 0; x < RT; ++x)
+#pragma unroll
+          for (int v = 0; v < 4; ++v) sum[c] += __builtin_amdgcn_exp2f(__fmaf_rn(acc[c][x][v], p.kappa, nl[x][v]));
     } else {
 #pragma unroll
-      for (int v = 0; v < 16; ++v) {
-        unsigned n = (unsigned)min(8 * (v >> 2) + 4 * half + (v & 3), rows - 1);
-        (void)split_by(n, p.by_n);
-        // (an lse of -inf or a row that is not there has +inf or -inf here)
-        const bool see = fabsf(nl[v]) < INFINITY || nl[v] != nl[v];
-        const float e = __builtin_amdgcn_exp2f(__fmaf_rn(acc[v], p.kappa, nl[v]));
-        sum[v & 3] += see && key < (p.causal ? min(coff + (int)n + 1, len) : len) ? e : 0.0f;
-      }
+      for (int x = 0; x < RT; ++x)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+          unsigned n = (unsigned)min(16 * x + 4 * quad + v, rows - 1);
+          (void)split_by(n, p.by_n);
+          // (an lse of -inf or a row that is not there has +inf or -inf here)
+          const bool see = fabsf(nl[x][v]) < INFINITY || nl[x][v] != nl[x][v];
+          const int vis = !see ? 0 : p.causal ? min(coff + (int)n + 1, len) : len;
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {
+            const float e = __builtin_amdgcn_exp2f(__fmaf_rn(acc[c][x][v], p.kappa, nl[x][v]));
+            sum[c] += 32 * j + 16 * c + col < vis ? e : 0.0f;
+          }
+        }
     }
-    const float y = half_sum((sum[0] + sum[1]) + (sum[2] + sum[3]));
-    if (half == 0 && key < len) p.w[wb + key] = k.w + y;
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      const unsigned u = __float_as_uint(sum[c]);
+      const auto sw = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+      sum[c] = half_sum(__uint_as_float(sw[0]) + __uint_as_float(sw[1]));
+    }
+    if (lane < 32 && 32 * j + lane < len) p.w[wb + 32 * j + lane] = k.w + (quad == 0 ? sum[0] : sum[1]);
   };
   for (int j = j0; j < j1; j += 8) {
     if (j + 4 < j1) load(kc, j + 4);
@@ -428,13 +454,14 @@ int kw_params(const sage_attn_key_weights_args* a, KwParams* p, bool need_io) {
   p->pieces = (most + p->piece - 1) / p->piece;
   // (With two operands, 33 to 64 rows, the registers leave two wavefronts per SIMD: 64 rows on 16 caches of 6000 keys 23.6 us, with tiles 13.6.)
   p->few = (long long)p->G * a->N <= KW_FEW;
-  // tiles of 32 keys per wavefront: until there are 16 wavefronts per CU, a round and a third of those it holds.  (Us, for 8 / 12 / 16 / 32 of them,
-  // caches read from memory: 32 of 32768 keys, 128 channels, 45.4 / 51.3 / 46.3 / 46.9, 128 of 9000, 64, 26.0 / 27.1 / 25.1 / 24.5, 16 of 20000, 256, 32.3 / 34.1 /
-  // 32.5 / 33.8: with 12 a few are left for a round of their own.)
+  // Tiles of 32 keys per wavefront: until there are 32 wavefronts per CU, two rounds of those it holds; lengths differ, and with one
+  // round the chip empties early.  (Us, for 8 / 16 / 32 / 64 of them, caches read from memory: 32 of 32768 keys, 128 channels, 44.3 / 46.2 / 46.0 /
+  // 46.5; 128 of 20000 99.7 / 101.7 / 93.9 / 91.4; 128 of 9000, 64, 26.8 / 25.9 / 22.2 / 22.2; 16 of 20000, 256, 31.1 / 29.8 / 30.5 / 30.7; 64 of 16000 with
+  // 24 rows 47.3 / 45.8 / 42.9 / 51.7.)
   if (p->few) {
     const long long tiles = (a->N_kv + 31) / 32;
     p->pieces = 1;
-    p->piece = (int)std::max(1LL, std::min(64LL, heads * tiles / (256 * 16)));
+    p->piece = (int)std::max(1LL, std::min(64LL, heads * tiles / (256 * 32)));
     p->key_tiles = (int)((tiles + 4 * p->piece - 1) / (4 * p->piece));
   }
   if (heads * p->key_tiles * p->pieces > 0x7fffffffLL) return SAGE_ERR_UNSUPPORTED;
@@ -443,7 +470,8 @@ int kw_params(const sage_attn_key_weights_args* a, KwParams* p, bool need_io) {
 
 template <int D, bool BF16> hipError_t launch_kw(const KwParams& p, unsigned blocks, hipStream_t s) {
   if (!p.few) k_key_weights<D, BF16><<<blocks, 256, 0, s>>>(p);
-  else k_key_weights_few<D, BF16><<<blocks, 256, 0, s>>>(p);
+  else if (p.G * p.N <= 16) k_key_weights_few<D, BF16, 1><<<blocks, 256, 0, s>>>(p);
+  else k_key_weights_few<D, BF16, 2><<<blocks, 256, 0, s>>>(p);
   return hipGetLastError();
 }
 

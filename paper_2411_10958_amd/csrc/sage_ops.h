@@ -54,6 +54,17 @@ __device__ __forceinline__ unsigned split_by(unsigned& n, const FastDiv& f) {
   return q;
 }
 
+// The same, 16 x 16 x 32: row or column l % 16, contraction slots 8 (l / 16) + 0..7; accumulator v is row 4 (l / 16) + v, column l % 16.
+template <bool BF16> __device__ __forceinline__ v4f mfma16_small(v4i a, v4i b, v4f c) {
+  if constexpr (BF16) {
+    typedef __bf16 v8b __attribute__((ext_vector_type(8)));
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8b, a), __builtin_bit_cast(v8b, b), c, 0, 0, 0);
+  } else {
+    typedef _Float16 v8h __attribute__((ext_vector_type(8)));
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, a), __builtin_bit_cast(v8h, b), c, 0, 0, 0);
+  }
+}
+
 // Sum / maximum of a value over the two halves of the wavefront, in both.
 __device__ __forceinline__ float half_sum(float x) {
   const unsigned u = __float_as_uint(x);
