@@ -45,7 +45,7 @@ struct SharedParams {
   int rtp, rto;                  // row tiles of the prefix (of B G N rows) and of the own keys (of G N rows)
   int n_prefix;                  // workgroups of the prefix; those of the own keys follow
   int full;                      // of them, those of whole groups of 8 chunks
-  FastDiv by_group, by_rtp, by_hkv, by_rto, by_b, by_gn, by_n, by_rows;      // 8 rtp, rtp, H_kv, rto, B, G N, N, B G N
+  FastDiv by_group, by_rtp, by_hkv, by_rto, by_b, by_gn, by_n, by_rows, by_sp, by_so;      // 8 rtp, rtp, H_kv, rto, B, G N, N, B G N, Sp, So
 };
 
 // Where partial result `s` of a row is kept: the prefix's chunks first, then the own ones.  Rows are numbered (KV head, batch, head of
@@ -67,9 +67,12 @@ __global__ void __launch_bounds__(64 * shared_waves<D>(), shared_occupancy<D>())
   constexpr int TILE = SH_KEYS * NP;              // pieces of a K (or V) tile
   constexpr int W = shared_waves<D>(), ROWS = 32 * W;
   __shared__ __align__(1024) v4i s_kv[2][2 * TILE];     // [stage][K, V]
-  __shared__ float s_ml[shared_waves<D>() / 2][64];     // maxima and sums of the second key group
+  __shared__ float s_ml[shared_waves<D>()][64];         // maxima and sums of the rows of each wavefront
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
   const int col = lane & 31, half = lane >> 5;
+
+  // The arguments take six cache lines: one wait for all of them, not one for each where its first word is needed
+  asm volatile("" ::"s"(p.vp), "s"(p.lens), "s"(p.om.sn), "s"(p.causal), "s"(p.by_group.m), "s"(p.by_n.m));
 
   // ---- which rows and keys
   unsigned id = blockIdx.x, hkv, b = 0, rt, s;
@@ -97,13 +100,15 @@ __global__ void __launch_bounds__(64 * shared_waves<D>(), shared_occupancy<D>())
   const int GN = p.G * p.N, rows = prefix ? p.B * GN : GN, r0 = (int)rt * ROWS;
   const int nr = min(ROWS, rows - r0);            // rows of this workgroup
   const int nk = prefix ? p.P : own_len(p, (int)b);
-  const int tiles = (nk + SH_KEYS - 1) / SH_KEYS, S = prefix ? p.Sp : p.So;
-  const int per = (tiles + S - 1) / S;
+  const int tiles = (nk + SH_KEYS - 1) / SH_KEYS;
+  const int per = prefix ? (int)div_by((unsigned)(tiles + p.Sp - 1), p.by_sp) : (int)div_by((unsigned)(tiles + p.So - 1), p.by_so);
   const int j0 = min((int)s * per, tiles), j1 = min(j0 + per, tiles);
   const int sp = (int)s + (prefix ? 0 : p.Sp);
   const int i0 = prefix ? r0 : (int)b * GN + r0;  // first row in the numbering of part_row
 
-  // Wavefronts: 32 rows each; where half of them do for the rows, two share rows and take every other 32 keys
+  // Wavefronts: 32 rows each; where half of them do for the rows, two share rows and take every other 32 keys.  In the end they share
+  // the channels too: each gives its upper CT / 2 channel tiles to the other, so the second has its tiles in the other order
+  // (tile c in place c ^ CT / 2).
   const int WK = nr <= ROWS / 2 ? 2 : 1;
   const int kg = WK == 2 ? wave & 1 : 0, rg = WK == 2 ? wave >> 1 : wave;
   const bool active = rg * 32 < nr;
@@ -219,7 +224,7 @@ __global__ void __launch_bounds__(64 * shared_waves<D>(), shared_occupancy<D>())
   typedef __attribute__((address_space(3))) v4s* lds_v4s;
   const int kr = 16 * (col >> 4) + 8 * ((col >> 2) & 1) + 4 * ((col >> 3) & 1) + (col & 3), vr = 8 * half + ((lane & 15) >> 2);
   const int vc = 16 * ((lane >> 4) & 1) + 4 * (lane & 3);                  // first channel that my lane points at
-  const unsigned k_at = (unsigned)row_piece<D>(kr, half) * 16, v_at = (unsigned)row_piece<D>(vr, vc >> 3) * 16 + (vc & 4) * 2;
+  const unsigned k_at = (unsigned)row_piece<D>(kr, half) * 16, v_at = ((unsigned)row_piece<D>(vr, vc >> 3) * 16 + (vc & 4) * 2) ^ (kg * (CT / 2) * 64);
 
   // NS times 32 keys of a tile, from the sub0-th on: scores, weights and their product with V
   auto tile_keys = [&](auto ns, unsigned stage0, int tile0, int sub0) __attribute__((always_inline)) {
@@ -313,33 +318,39 @@ __global__ void __launch_bounds__(64 * shared_waves<D>(), shared_occupancy<D>())
 
   // ---- the two key groups of the same rows into one
   if (WK == 2) {
-    float* x = reinterpret_cast<float*>(&s_kv[0][0]) + rg * 32 * D;
+    v4f* x = reinterpret_cast<v4f*>(&s_kv[0][0]);
     __syncthreads();
-    if (active && kg == 1) {
+    if (active) {
 #pragma unroll
-      for (int c = 0; c < CT; ++c)
+      for (int c = 0; c < CT / 2; ++c)
 #pragma unroll
-        for (int v = 0; v < 16; ++v) x[(16 * c + v) * 64 + lane] = o[c][v];
+        for (int g = 0; g < 4; ++g)
+          x[((wave * (CT / 2) + c) * 4 + g) * 64 + lane] = v4f{o[CT / 2 + c][4 * g], o[CT / 2 + c][4 * g + 1], o[CT / 2 + c][4 * g + 2], o[CT / 2 + c][4 * g + 3]};
       if (half == 0) {
-        s_ml[rg][2 * col] = mx;
-        s_ml[rg][2 * col + 1] = l;
+        s_ml[wave][2 * col] = mx;
+        s_ml[wave][2 * col + 1] = l;
       }
     }
     __syncthreads();
-    if (kg == 1) return;
     if (active) {
-      const float m1 = s_ml[rg][2 * col], l1 = s_ml[rg][2 * col + 1];
+      const int other = wave ^ 1;
+      const float m1 = s_ml[other][2 * col], l1 = s_ml[other][2 * col + 1];
       const float m_new = fmaxf(mx, m1), base = m_new == -INFINITY ? 0.0f : m_new;
       const float a0 = __builtin_amdgcn_exp2f(mx - base), a1 = __builtin_amdgcn_exp2f(m1 - base);
       l = l * a0 + l1 * a1;
       mx = m_new;
 #pragma unroll
-      for (int c = 0; c < CT; ++c)
+      for (int c = 0; c < CT / 2; ++c)
 #pragma unroll
-        for (int v = 0; v < 16; ++v) o[c][v] = o[c][v] * a0 + x[(16 * c + v) * 64 + lane] * a1;
+        for (int g = 0; g < 4; ++g) {
+          const v4f y = x[((other * (CT / 2) + c) * 4 + g) * 64 + lane];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[c][4 * g + e] = o[c][4 * g + e] * a0 + y[e] * a1;
+        }
     }
   }
   if (!active || rg * 32 + col >= nr) return;
+  const int mine = kg * (CT / 2);                 // channel tile of o[c]: c ^ mine; mine to write are CT / 2 of them, or all
   if (taken_out) {
     const int to = min(vis, j1 * SH_KEYS);
 #pragma unroll 1
@@ -349,7 +360,7 @@ __global__ void __launch_bounds__(64 * shared_waves<D>(), shared_occupancy<D>())
       for (int c = 0; c < CT; ++c)
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
-          const uint2 u = *reinterpret_cast<const uint2*>(v + 64 * c + 16 * g);
+          const uint2 u = *reinterpret_cast<const uint2*>(v + 64 * (c ^ mine) + 16 * g);
           const unsigned y[4] = {u.x & 0xffff, u.x >> 16, u.y & 0xffff, u.y >> 16};
 #pragma unroll
           for (int e = 0; e < 4; ++e) o[c][4 * g + e] += not_finite<BF16>(y[e]) ? load16<BF16>((unsigned short)y[e]) : 0.0f;
@@ -357,17 +368,19 @@ __global__ void __launch_bounds__(64 * shared_waves<D>(), shared_occupancy<D>())
     }
   }
   const size_t pr = part_row(p, sp, (int)hkv, i);
-  if (half == 0) {
+  if (half == 0 && kg == 0) {
     p.part_ml[pr * 2] = mx;
     p.part_ml[pr * 2 + 1] = l;
   }
   float* po = p.part_o + pr * D + 4 * half;
 #pragma unroll
   for (int c = 0; c < CT; ++c)
+    if (c < CT / 2 || WK == 1) {
 #pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      const v4f y = {o[c][4 * g], o[c][4 * g + 1], o[c][4 * g + 2], o[c][4 * g + 3]};
-      *reinterpret_cast<v4f*>(po + 32 * c + 8 * g) = y;
+      for (int g = 0; g < 4; ++g) {
+        const v4f y = {o[c][4 * g], o[c][4 * g + 1], o[c][4 * g + 2], o[c][4 * g + 3]};
+        *reinterpret_cast<v4f*>(po + 32 * (c ^ mine) + 8 * g) = y;
+      }
     }
 }
 
@@ -492,6 +505,7 @@ int shared_params(const sage_attn_shared_prefix_args* a, SharedParams* p, bool n
   p->full = p->Sp * a->H_kv / 8 * 8 * p->rtp;
   p->by_group = fast_div(8u * p->rtp); p->by_rtp = fast_div(p->rtp); p->by_hkv = fast_div(a->H_kv); p->by_rto = fast_div(p->rto);
   p->by_b = fast_div(a->B); p->by_gn = fast_div((unsigned)gn); p->by_n = fast_div(a->N); p->by_rows = fast_div((unsigned)rows);
+  p->by_sp = fast_div(std::max(p->Sp, 1)); p->by_so = fast_div(std::max(p->So, 1));
   return SAGE_OK;
 }
 

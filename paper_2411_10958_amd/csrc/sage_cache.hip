@@ -115,13 +115,20 @@ __global__ void __launch_bounds__(SEL_THREADS) k_evict_select(const EvictParams 
   __syncthreads();
   unsigned above = (unsigned)p.sink, ties = 0;
   for (int i = 0; i < wave; ++i) { above += s_gt[i]; ties += s_eq[i]; }
-  const unsigned long long below = (1ull << lane) - 1;
+  // (lanes of a mask before mine, counted from c on)
+  auto place = [](unsigned long long mask, unsigned c) __attribute__((always_inline)) {
+    return __builtin_amdgcn_mbcnt_hi((unsigned)(mask >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)mask, c));
+  };
   each([&](unsigned v, int i) __attribute__((always_inline)) {
     const unsigned long long bg = __ballot(v > prefix), be = __ballot(v == prefix);
-    const unsigned tie = ties + (unsigned)__popcll(be & below);
-    if (v > prefix || (v == prefix && tie < need)) kept[above + (unsigned)__popcll(bg & below) + min(tie, need)] = c0 + i + lane;
+    if (be == 0) {
+      if (v > prefix) kept[place(bg, above + min(ties, need))] = c0 + i + lane;
+    } else {
+      const unsigned tie = place(be, ties);
+      if (v > prefix || (v == prefix && tie < need)) kept[place(bg, above) + min(tie, need)] = c0 + i + lane;
+      ties += (unsigned)__popcll(be);
+    }
     above += (unsigned)__popcll(bg);
-    ties += (unsigned)__popcll(be);
   });
 }
 
