@@ -150,15 +150,28 @@ __global__ void __launch_bounds__(64 * shared_waves<D>(), shared_occupancy<D>())
     const int pc = (x * W + wave) * 64 + lane, r = pc / NP;
     offs[x] = (unsigned)r * step + (unsigned)((pc % NP) ^ swizzle<D>(r)) * 16;
   }
+  // What one workgroup alone reads passes the caches by.  The prefix only where it has few rows: with more, its workgroups leave partial
+  // results of as many bytes, and reads from memory itself make them later (us, kept in the caches / past them: 16 sequences of up to
+  // 3000 own keys over 20000, 128 channels 56.5 / 52.9; 4 over 100000 84.5 / 75.3; 6 of 5 tokens of 256 channels over 5003, 120
+  // rows: 30.4 / 34.2).
+  const bool once = prefix ? rows <= 64 : p.rto == 1;
   auto copy = [&](int j, int stage) __attribute__((always_inline)) {
     const size_t at = (size_t)j * SH_KEYS * m.sn * 2;
     const unsigned to = lds0 + (unsigned)(stage * 2 * TILE + wave * 64) * 16;
     const int last = nk - 1 - j * SH_KEYS;
     if (last >= SH_KEYS - 1) {
+if (once) {
 #pragma unroll
-      for (int x = 0; x < COPIES; ++x) {
-        dma_b128(gk + at, offs[x], to + x * (W * 1024));
-        dma_b128(gv + at, offs[x], to + TILE * 16 + x * (W * 1024));
+        for (int x = 0; x < COPIES; ++x) {
+          dma_b128_once(gk + at, offs[x], to + x * (W * 1024));
+          dma_b128_once(gv + at, offs[x], to + TILE * 16 + x * (W * 1024));
+        }
+      } else {
+#pragma unroll
+        for (int x = 0; x < COPIES; ++x) {
+          dma_b128(gk + at, offs[x], to + x * (W * 1024));
+          dma_b128(gv + at, offs[x], to + TILE * 16 + x * (W * 1024));
+        }
       }
     } else {
 #pragma unroll 1

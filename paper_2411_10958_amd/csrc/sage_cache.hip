@@ -31,8 +31,8 @@ constexpr int DIGIT = 11, BINS = 1 << DIGIT;      // three digits of 11, 11 and 
 // Which tokens stay, one workgroup per sequence and KV head: the m-th largest weight between sink and recent, found digit by digit by
 // counting, then one pass in order that keeps what is larger and the first of what equals it.  A wavefront has a stretch of
 // 64 K weights in registers, in the order of unsigned numbers, so they are read and converted once; K = 0: more than that, read
-// again each time, eight loads in flight.  Bound by the instructions of its five passes on one CU: 32 rows of 32768 25 us of the call's
-// 122 (51 with 8-bit digits and weights read from memory in each pass; counts in four copies changed nothing).  (The first digit is sign, exponent and two bits: with 8-bit digits a wavefront's
+// again each time, eight loads in flight.  Bound by the instructions of its five passes on one CU: 32 rows of 32768 22 us of the call's
+// 111 (51 with 8-bit digits and weights read from memory in each pass; counts in four copies changed nothing).  (The first digit is sign, exponent and two bits: with 8-bit digits a wavefront's
 // counts would fall on a dozen addresses.)  What a stretch has behind the last weight counts as less than any and comes after
 // all, so it is never taken: n > m.
 template <int K>
@@ -133,7 +133,9 @@ __global__ void __launch_bounds__(SEL_THREADS) k_evict_select(const EvictParams 
 }
 
 // The rows of the kept tokens, and their weights: a thread moves 16 bytes of K and of V of GU tokens, the first of a row also its
-// weight.  Grid: (pieces of the kept tokens, heads).
+// weight.  Reads and writes pass the caches by: none of it is needed again in this call, and lines kept for it cost others their write-back
+// (32 heads of 32768 tokens cut to half: the call 123 us without, 120 for the reads alone, 111 for both: 5.4 TB/s).
+// Grid: (pieces of the kept tokens, heads).
 constexpr int GU = 4;
 template <int D> __global__ void __launch_bounds__(256) k_evict_rows(const EvictParams p) {
   constexpr int P = D / 8, TOK = 256 / P;
@@ -155,15 +157,15 @@ template <int D> __global__ void __launch_bounds__(256) k_evict_rows(const Evict
 #pragma unroll
   for (int i = 0; i < GU; ++i) {
     const size_t at = row_offset(p.in, hi, from[i]);
-    a[i] = *reinterpret_cast<const v4i*>(p.k + at);
-    x[i] = *reinterpret_cast<const v4i*>(p.v + at);
+    a[i] = __builtin_nontemporal_load(reinterpret_cast<const v4i*>(p.k + at));
+    x[i] = __builtin_nontemporal_load(reinterpret_cast<const v4i*>(p.v + at));
   }
 #pragma unroll
   for (int i = 0; i < GU; ++i) {
     if (first + i * TOK < there) {
       const size_t at = row_offset(p.out, ho, first + i * TOK);
-      *reinterpret_cast<v4i*>(p.k_out + at) = a[i];
-      *reinterpret_cast<v4i*>(p.v_out + at) = x[i];
+      __builtin_nontemporal_store(a[i], reinterpret_cast<v4i*>(p.k_out + at));
+      __builtin_nontemporal_store(x[i], reinterpret_cast<v4i*>(p.v_out + at));
       if (weigh) p.w_out[(size_t)blockIdx.y * p.keep + first + i * TOK] = wt[i];
     }
   }

@@ -87,4 +87,11 @@ template <int D> __device__ __forceinline__ int swizzle(int r) {
 }
 template <int D> __device__ __forceinline__ int row_piece(int r, int c) { return r * (D / 8) + (c ^ swizzle<D>(r)); }
 
+// dma_b128 of what is read once: it does not stay in the caches.
+__device__ __forceinline__ void dma_b128_once(const void* gbase, unsigned voff, unsigned lds_byte) {
+  unsigned m0_after;
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %3 nt"
+               : "={m0}"(m0_after) : "s"(lds_byte), "v"(voff), "s"(gbase) : "memory");
+}
+
 }  // namespace sage

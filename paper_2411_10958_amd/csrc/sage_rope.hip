@@ -2,8 +2,8 @@
 //
 // Channel pair i of the first `rot` channels is turned by the angle p f_i: (a, b) -> scale (a cos - b sin, b cos + a sin), the
 // pair being channels (i, i + rot/2) or (2i, 2i + 1).  Nothing but bytes moves this: every value is read and written once, 4 bytes.
-// A thread owns 2 VW channels of a token - VW pairs in either style - works their angles out once and then walks over heads, so the
-// FP64 product and the sine and cosine are shared by all of them.  Angles are taken in 64 bits (position 10^6 times the fastest
+// A thread owns one vector of VW channels of a token, or two, a pair's channels in each, works their angles out once and then walks over
+// heads, so the FP64 product and the sine and cosine are shared by all of them.  Angles are taken in 64 bits (position 10^6 times the fastest
 // frequency in FP32 would be off by 0.03 rad), reduced to a fraction of a turn there, and their sine and cosine in FP32.
 #include "sage_attn.h"
 #include "sage_ops.h"
@@ -31,19 +31,18 @@ struct RopeParams {
 };
 
 template <int VW> struct Vec;
-template <> struct Vec<8> { typedef uint4 type; };
-template <> struct Vec<4> { typedef uint2 type; };
+template <> struct Vec<8> { typedef unsigned type __attribute__((ext_vector_type(4))); };
+template <> struct Vec<4> { typedef unsigned type __attribute__((ext_vector_type(2))); };
 template <> struct Vec<1> { typedef unsigned short type; };
 
 template <bool BF16, int VW> __device__ __forceinline__ void unpack(const typename Vec<VW>::type& v, float (&f)[VW]) {
   if constexpr (VW == 1) {
     f[0] = load16<BF16>(v);
   } else {
-    const unsigned* u = reinterpret_cast<const unsigned*>(&v);
 #pragma unroll
     for (int i = 0; i < VW / 2; ++i) {
-      f[2 * i] = load16<BF16>((unsigned short)u[i]);
-      f[2 * i + 1] = load16<BF16>((unsigned short)(u[i] >> 16));
+      f[2 * i] = load16<BF16>((unsigned short)v[i]);
+      f[2 * i + 1] = load16<BF16>((unsigned short)(v[i] >> 16));
     }
   }
 }
@@ -52,36 +51,44 @@ template <bool BF16, int VW> __device__ __forceinline__ typename Vec<VW>::type p
   if constexpr (VW == 1) {
     v = (unsigned short)pack16x2<BF16>(f[0], 0.0f);
   } else {
-    unsigned* u = reinterpret_cast<unsigned*>(&v);
 #pragma unroll
-    for (int i = 0; i < VW / 2; ++i) u[i] = pack16x2<BF16>(f[2 * i], f[2 * i + 1]);
+    for (int i = 0; i < VW / 2; ++i) v[i] = pack16x2<BF16>(f[2 * i], f[2 * i + 1]);
   }
   return v;
 }
 
-// One vector pair (channels c0.., c1..) of one head; INTER: element 2i, 2i + 1 of the two vectors laid end to end are a pair.
-template <bool BF16, int VW, bool INTER>
-__device__ __forceinline__ void turn(typename Vec<VW>::type& v0, typename Vec<VW>::type& v1, const float (&c)[VW], const float (&s)[VW]) {
-  float x[2 * VW], y[2 * VW], lo[VW], hi[VW];
-  unpack<BF16, VW>(v0, lo);
-  unpack<BF16, VW>(v1, hi);
+// Vectors of a thread: neighbours in a pair are in one vector, halves apart in two.  (Neighbours one by one, VW = 1, are two as well.)
+template <int VW, bool INTER> constexpr int vectors() { return INTER && VW > 1 ? 1 : 2; }
+
+// The vectors of one head; INTER: elements 2i, 2i + 1 of them laid end to end are a pair, otherwise i and VW + i.
+template <bool BF16, int VW, bool INTER, int NV>
+__device__ __forceinline__ void turn(typename Vec<VW>::type (&v)[NV], const float (&c)[NV * VW / 2], const float (&s)[NV * VW / 2]) {
+  float x[NV * VW], f[VW];
 #pragma unroll
-  for (int i = 0; i < VW; ++i) { x[i] = lo[i]; x[VW + i] = hi[i]; }
+  for (int k = 0; k < NV; ++k) {
+    unpack<BF16, VW>(v[k], f);
 #pragma unroll
-  for (int i = 0; i < VW; ++i) {
-    const int a = INTER ? 2 * i : i, b = INTER ? 2 * i + 1 : VW + i;
-    y[a] = __fmaf_rn(x[a], c[i], -__fmul_rn(x[b], s[i]));
-    y[b] = __fmaf_rn(x[b], c[i], __fmul_rn(x[a], s[i]));
+    for (int i = 0; i < VW; ++i) x[k * VW + i] = f[i];
   }
 #pragma unroll
-  for (int i = 0; i < VW; ++i) { lo[i] = y[i]; hi[i] = y[VW + i]; }
-  v0 = pack<BF16, VW>(lo);
-  v1 = pack<BF16, VW>(hi);
+  for (int i = 0; i < NV * VW / 2; ++i) {
+    const int at = INTER ? 2 * i : i, to = INTER ? 2 * i + 1 : VW + i;
+    const float a = x[at], b = x[to];
+    x[at] = __fmaf_rn(a, c[i], -__fmul_rn(b, s[i]));
+    x[to] = __fmaf_rn(b, c[i], __fmul_rn(a, s[i]));
+  }
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+#pragma unroll
+    for (int i = 0; i < VW; ++i) f[i] = x[k * VW + i];
+    v[k] = pack<BF16, VW>(f);
+  }
 }
 
-// Grid: (units of all tokens / 256, pieces of the heads).
-template <bool BF16, int VW, bool INTER>
+// Grid: (units of all tokens / 256, pieces of the heads).  PAST: reads and writes pass the caches by (see whole_lines).
+template <bool BF16, int VW, bool INTER, bool PAST>
 __global__ void __launch_bounds__(256) k_rope(const RopeParams p) {
+  constexpr int NV = vectors<VW, INTER>(), NP = NV * VW / 2;       // vectors and pairs of a thread
   const long long id = (long long)blockIdx.x * 256 + threadIdx.x;
   if (id >= p.total) return;
   const long long th = id / p.units, tok = th / p.lanes;
@@ -89,46 +96,50 @@ __global__ void __launch_bounds__(256) k_rope(const RopeParams p) {
   const long long b = tok / p.N;
   const int n = (int)(tok - b * p.N);
   const bool turned = unit < p.turned;
-  float c[VW], s[VW];
-  int c0, c1;
+  float c[NP], s[NP];
+  int at[NV];                        // first channel of each vector; what is not turned is split like what is
+  at[0] = (turned ? 0 : p.rot) + (INTER ? NV : 1) * VW * (turned ? unit : unit - p.turned);
+  if constexpr (NV == 2) at[1] = at[0] + (INTER ? VW : (turned ? p.rot : p.d - p.rot) / 2);
   if (turned) {
-    c0 = INTER ? 2 * VW * unit : VW * unit;
-    c1 = INTER ? c0 + VW : c0 + p.rot / 2;
-    const double at = (double)((p.positions ? (long long)p.positions[b * p.pos_sb + n] : (long long)n) + p.offset);
+    const double pos = (double)((p.positions ? (long long)p.positions[b * p.pos_sb + n] : (long long)n) + p.offset);
 #pragma unroll
-    for (int i = 0; i < VW; ++i) {
-      const double turns = at * p.inv_freq[VW * unit + i] * 0.15915494309189533577;      // 1 / (2 pi)
+    for (int i = 0; i < NP; ++i) {
+      const double turns = pos * p.inv_freq[NP * unit + i] * 0.15915494309189533577;      // 1 / (2 pi)
       const float x = 2.0f * (float)(turns - rint(turns));
       float si, co;
       sincospif(x, &si, &co);
       c[i] = __fmul_rn(co, p.scale);
       s[i] = __fmul_rn(si, p.sign);
     }
-  } else {                           // (what is left of a row is a multiple of two vectors too)
-    c0 = p.rot + (unit - p.turned) * 2 * VW;
-    c1 = c0 + VW;
   }
   const int h0 = blockIdx.y * p.hchunk, h1 = min(h0 + p.hchunk, p.q.heads + p.k.heads);
   typedef typename Vec<VW>::type V;
-  constexpr int HU = 4;              // heads whose loads are in flight together
+  constexpr int HU = 8 / NV;         // heads whose loads are in flight together
   auto run = [&](const RopeTensor& t, int ha, int hb) {
     const unsigned short* x = t.x + b * t.xb + (long long)n * t.xn;
     unsigned short* y = t.y + b * t.yb + (long long)n * t.yn;
     for (int h = ha + hl; h < hb; h += HU * p.lanes) {
-      V v0[HU], v1[HU];
+      V v[HU][NV];
 #pragma unroll
       for (int i = 0; i < HU; ++i) {
         const unsigned short* r = x + (long long)min(h + i * p.lanes, hb - 1) * t.xh;
-        v0[i] = *reinterpret_cast<const V*>(r + c0);
-        v1[i] = *reinterpret_cast<const V*>(r + c1);
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+          const V* from = reinterpret_cast<const V*>(r + at[k]);
+          v[i][k] = PAST ? __builtin_nontemporal_load(from) : *from;
+        }
       }
 #pragma unroll
       for (int i = 0; i < HU; ++i) {
         if (h + i * p.lanes >= hb) break;
-        if (turned) turn<BF16, VW, INTER>(v0[i], v1[i], c, s);
+        if (turned) turn<BF16, VW, INTER, NV>(v[i], c, s);
         unsigned short* r = y + (long long)(h + i * p.lanes) * t.yh;
-        *reinterpret_cast<V*>(r + c0) = v0[i];
-        *reinterpret_cast<V*>(r + c1) = v1[i];
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+          V* to = reinterpret_cast<V*>(r + at[k]);
+          if (PAST) __builtin_nontemporal_store(v[i][k], to);
+          else *to = v[i][k];
+        }
       }
     }
   };
@@ -166,9 +177,13 @@ bool rows_apart(const long long (&st)[3], long long B, long long heads, long lon
 }
 
 template <bool BF16, int VW>
-void launch(const RopeParams& p, bool inter, dim3 grid, hipStream_t s) {
-  if (inter) k_rope<BF16, VW, true><<<grid, 256, 0, s>>>(p);
-  else k_rope<BF16, VW, false><<<grid, 256, 0, s>>>(p);
+void launch(const RopeParams& p, bool inter, bool past, dim3 grid, hipStream_t s) {
+  if constexpr (VW == 8) {
+    if (past && inter) return k_rope<BF16, VW, true, true><<<grid, 256, 0, s>>>(p);
+    if (past) return k_rope<BF16, VW, false, true><<<grid, 256, 0, s>>>(p);
+  }
+  if (inter) k_rope<BF16, VW, true, false><<<grid, 256, 0, s>>>(p);
+  else k_rope<BF16, VW, false, false><<<grid, 256, 0, s>>>(p);
 }
 
 }  // namespace
@@ -222,14 +237,21 @@ extern "C" int sage_rope(const sage_rope_args* a) {
   p.sign = a->inverse ? -p.scale : p.scale;
 
   // Widest access that every row allows: both halves of a pair's vectors start at a multiple of it.
-  unsigned long long bits = (uintptr_t)a->q / 2 | (uintptr_t)a->q_out / 2 | (uintptr_t)a->k / 2 | (uintptr_t)a->k_out / 2;
-  for (auto& s : st) bits |= (unsigned long long)(s[0] | s[1] | s[2]);
-  bits |= (unsigned long long)(a->rot_dim / 2);
+  unsigned long long rows = (uintptr_t)a->q / 2 | (uintptr_t)a->q_out / 2 | (uintptr_t)a->k / 2 | (uintptr_t)a->k_out / 2;
+  for (auto& s : st) rows |= (unsigned long long)(s[0] | s[1] | s[2]);
+  const unsigned long long bits = rows | (unsigned long long)(a->rot_dim / 2);
   const int vw = (bits & 7) == 0 ? 8 : (bits & 3) == 0 ? 4 : 1;
-  p.turned = a->rot_dim / 2 / vw;
+  const bool inter = a->interleaved != 0;
+  const int unit = inter && vw > 1 ? vw : 2 * vw;       // channels of a thread
+  p.turned = a->rot_dim / unit;
   // (in place, what is not turned stays where it is)
   const bool in_place = a->q == a->q_out && (!keys || a->k == a->k_out);
-  p.units = p.turned + (in_place ? 0 : (a->d - a->rot_dim) / (2 * vw));
+  const int rest = in_place ? 0 : a->d - a->rot_dim;
+  p.units = p.turned + rest / unit;
+  // Every access of a wavefront whole lines of 128 bytes: it can pass the caches by, where pieces of lines would be slower that way (us,
+  // kept in the caches / past them: 4 x 4096 tokens of 40 heads of 128 66.8 / 60.1, heads outside 64.5 / 61.0, 64 x 64 tokens
+  // 28.0 / 23.7; 30000 tokens of 64 heads of 64, halves of 64 bytes, 95 / 107; 2 x 9000 of 20 heads of 256, a quarter turned, 73 / 93).
+  const bool whole_lines = vw == 8 && (rows & 63) == 0 && (inter ? (a->rot_dim + rest) % 64 == 0 : a->rot_dim % 128 == 0 && rest % 128 == 0);
   // Token-major rows: neighbouring threads take neighbouring heads of a token, which are one stretch of memory; with a token each they
   // would read pieces of 256 bytes, a token's row apart (4 x 4096 tokens of 40 heads of 128: 79 us, so 67).
   p.lanes = 1;
@@ -244,11 +266,10 @@ extern "C" int sage_rope(const sage_rope_args* a) {
   p.hchunk = (int)((heads + pieces - 1) / pieces);
   const dim3 grid((unsigned)blocks, (unsigned)((heads + p.hchunk - 1) / p.hchunk));
   const hipStream_t s = (hipStream_t)a->stream;
-  const bool inter = a->interleaved != 0;
   if (a->dtype == SAGE_DT_BF16) {
-    if (vw == 8) launch<true, 8>(p, inter, grid, s); else if (vw == 4) launch<true, 4>(p, inter, grid, s); else launch<true, 1>(p, inter, grid, s);
+    if (vw == 8) launch<true, 8>(p, inter, whole_lines, grid, s); else if (vw == 4) launch<true, 4>(p, inter, false, grid, s); else launch<true, 1>(p, inter, false, grid, s);
   } else {
-    if (vw == 8) launch<false, 8>(p, inter, grid, s); else if (vw == 4) launch<false, 4>(p, inter, grid, s); else launch<false, 1>(p, inter, grid, s);
+    if (vw == 8) launch<false, 8>(p, inter, whole_lines, grid, s); else if (vw == 4) launch<false, 4>(p, inter, false, grid, s); else launch<false, 1>(p, inter, false, grid, s);
   }
   return op_status(hipGetLastError());
 }
