@@ -133,11 +133,13 @@ __global__ void __launch_bounds__(SEL_THREADS) k_evict_select(const EvictParams 
 }
 
 // The rows of the kept tokens, and their weights: a thread moves 16 bytes of K and of V of GU tokens, the first of a row also its
-// weight.  Reads and writes pass the caches by: none of it is needed again in this call, and lines kept for it cost others their write-back
-// (32 heads of 32768 tokens cut to half: the call 123 us without, 120 for the reads alone, 111 for both: 5.4 TB/s).
+// weight.  Reads pass the caches by, since the old rows are not needed again; with PAST writes do too, where rows read and written do not fit
+// the 256 MB of the memory-side cache (32 heads of 32768 tokens of 128 cut to half: the call 123 us with both kept, 120 with reads past,
+// 111 with both, 5.4 TB/s; with the decode step that reads the rows after it 174 either way).  Below that the step finds rows there (32
+// heads of 8000 cut to half, and the step: 54.9, 57.4 with writes past).
 // Grid: (pieces of the kept tokens, heads).
 constexpr int GU = 4;
-template <int D> __global__ void __launch_bounds__(256) k_evict_rows(const EvictParams p) {
+template <int D, bool PAST> __global__ void __launch_bounds__(256) k_evict_rows(const EvictParams p) {
   constexpr int P = D / 8, TOK = 256 / P;
   const int b = blockIdx.y / p.Hkv;
   const int len = p.lens ? min(max(p.lens[b], 0), p.N) : p.N, there = min(len, p.keep);
@@ -164,11 +166,22 @@ template <int D> __global__ void __launch_bounds__(256) k_evict_rows(const Evict
   for (int i = 0; i < GU; ++i) {
     if (first + i * TOK < there) {
       const size_t at = row_offset(p.out, ho, first + i * TOK);
-      __builtin_nontemporal_store(a[i], reinterpret_cast<v4i*>(p.k_out + at));
-      __builtin_nontemporal_store(x[i], reinterpret_cast<v4i*>(p.v_out + at));
+      v4i *ka = reinterpret_cast<v4i*>(p.k_out + at), *va = reinterpret_cast<v4i*>(p.v_out + at);
+      if (PAST) {
+        __builtin_nontemporal_store(a[i], ka);
+        __builtin_nontemporal_store(x[i], va);
+      } else {
+        *ka = a[i];
+        *va = x[i];
+      }
       if (weigh) p.w_out[(size_t)blockIdx.y * p.keep + first + i * TOK] = wt[i];
     }
   }
+}
+
+template <int D> void launch_rows(const EvictParams& p, bool past, dim3 grid, hipStream_t s) {
+  if (past) k_evict_rows<D, true><<<grid, 256, 0, s>>>(p);
+  else k_evict_rows<D, false><<<grid, 256, 0, s>>>(p);
 }
 
 struct Span { const void* at; size_t bytes; };
@@ -219,8 +232,9 @@ extern "C" int sage_cache_evict(const sage_cache_evict_args* a) {
   if (st != SAGE_OK) return st;
   const int per = 256 / (a->d / 8) * GU;
   const dim3 grid((unsigned)((std::min(a->N_keep, a->N_kv) + per - 1) / per), (unsigned)heads);
-  if (a->d == 64) k_evict_rows<64><<<grid, 256, 0, s>>>(p);
-  else if (a->d == 128) k_evict_rows<128><<<grid, 256, 0, s>>>(p);
-  else k_evict_rows<256><<<grid, 256, 0, s>>>(p);
+  const bool past = 8LL * (long long)out_rows * a->d > 256LL << 20;
+  if (a->d == 64) launch_rows<64>(p, past, grid, s);
+  else if (a->d == 128) launch_rows<128>(p, past, grid, s);
+  else launch_rows<256>(p, past, grid, s);
   return op_status(hipGetLastError());
 }

@@ -85,7 +85,7 @@ __device__ __forceinline__ void turn(typename Vec<VW>::type (&v)[NV], const floa
   }
 }
 
-// Grid: (units of all tokens / 256, pieces of the heads).  PAST: reads and writes pass the caches by (see whole_lines).
+// Grid: (units of all tokens / 256, pieces of the heads).  PAST: reads and writes pass the caches by.
 template <bool BF16, int VW, bool INTER, bool PAST>
 __global__ void __launch_bounds__(256) k_rope(const RopeParams p) {
   constexpr int NV = vectors<VW, INTER>(), NP = NV * VW / 2;       // vectors and pairs of a thread
@@ -248,10 +248,13 @@ extern "C" int sage_rope(const sage_rope_args* a) {
   const bool in_place = a->q == a->q_out && (!keys || a->k == a->k_out);
   const int rest = in_place ? 0 : a->d - a->rot_dim;
   p.units = p.turned + rest / unit;
-  // Every access of a wavefront whole lines of 128 bytes: it can pass the caches by, where pieces of lines would be slower that way (us,
-  // kept in the caches / past them: 4 x 4096 tokens of 40 heads of 128 66.8 / 60.1, heads outside 64.5 / 61.0, 64 x 64 tokens
-  // 28.0 / 23.7; 30000 tokens of 64 heads of 64, halves of 64 bytes, 95 / 107; 2 x 9000 of 20 heads of 256, a quarter turned, 73 / 93).
+  // Reads and writes pass the caches by where every access of a wavefront is whole lines of 128 bytes - pieces of lines would be slower that way:
+  // 30000 tokens of 64 heads of 64 in halves of 64 bytes 107 us, not 95 - and where what is read and written does not fit the
+  // 256 MB of the memory-side cache.  Below that what comes next, which reads these rows, finds them there: 2 x 1024 tokens of 40 heads of 128 and
+  // their attention 59.2 us, 60.6 past the caches.  From there on 2 x 17776 tokens of 96 heads of 64 165 kept / 155 past, 4 x 4096 of
+  // 40 heads of 128 65 / 60, with the statistics of the keys after it 76.8 / 76.8.
   const bool whole_lines = vw == 8 && (rows & 63) == 0 && (inter ? (a->rot_dim + rest) % 64 == 0 : a->rot_dim % 128 == 0 && rest % 128 == 0);
+  const bool past = whole_lines && 4LL * a->B * a->N * (p.q.heads + p.k.heads) * (a->rot_dim + rest) > 256LL << 20;
   // Token-major rows: neighbouring threads take neighbouring heads of a token, which are one stretch of memory; with a token each they
   // would read pieces of 256 bytes, a token's row apart (4 x 4096 tokens of 40 heads of 128: 79 us, so 67).
   p.lanes = 1;
@@ -267,9 +270,9 @@ extern "C" int sage_rope(const sage_rope_args* a) {
   const dim3 grid((unsigned)blocks, (unsigned)((heads + p.hchunk - 1) / p.hchunk));
   const hipStream_t s = (hipStream_t)a->stream;
   if (a->dtype == SAGE_DT_BF16) {
-    if (vw == 8) launch<true, 8>(p, inter, whole_lines, grid, s); else if (vw == 4) launch<true, 4>(p, inter, false, grid, s); else launch<true, 1>(p, inter, false, grid, s);
+    if (vw == 8) launch<true, 8>(p, inter, past, grid, s); else if (vw == 4) launch<true, 4>(p, inter, false, grid, s); else launch<true, 1>(p, inter, false, grid, s);
   } else {
-    if (vw == 8) launch<false, 8>(p, inter, whole_lines, grid, s); else if (vw == 4) launch<false, 4>(p, inter, false, grid, s); else launch<false, 1>(p, inter, false, grid, s);
+    if (vw == 8) launch<false, 8>(p, inter, past, grid, s); else if (vw == 4) launch<false, 4>(p, inter, false, grid, s); else launch<false, 1>(p, inter, false, grid, s);
   }
   return op_status(hipGetLastError());
 }
