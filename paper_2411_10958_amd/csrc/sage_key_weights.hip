@@ -10,6 +10,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 namespace sage {
 namespace {
@@ -287,12 +288,22 @@ __global__ void __launch_bounds__(256, kw_occupancy<D>()) k_key_weights(const Kw
 }
 
 // Few queries (16 RT rows of a group at most): nothing but the keys is read to speak of, and each of them once.  The queries stay in
-// registers, and a wavefront walks over tiles of 32 keys that go from memory to registers, one tile ahead; no LDS, no
-// barrier, and rows that are not there are paid for in products that nobody waits for.  (Bound by reading: 64 caches of 16000 keys of 128
-// channels 50.5 us, 5.3 TB/s.)
+// registers, and each wavefront walks over tiles of 16 keys that come to LDS of its own, some ahead of the one it multiplies: no
+// barrier, and rows that are not there are paid for in products that nobody waits for.  Bound by reading: the copies take whole rows and pass the
+// caches by (us, operands loaded to registers, which come in pieces of 64 bytes of a row / this: 16 caches of 20000 keys, 8 heads
+// of 128 channels, 90 / 80, 5.5 TB/s; 8 of them token-major 53.5 / 42.8; 16 of 9000 of 64 22.8 / 19.9; copies that stay in the caches 90).
+// Stages: LDS for 16 wavefronts of 64 channels or 8 of 128 or 256 per CU, three tiles in flight each or, of 256 channels, one (with
+// three of these and 4 wavefronts 30.7 for 26.9 us, of 128 with two for 8 / one for 16 42 and 39.5 for 39.3).
+constexpr int KF_KEYS = 16;
+template <int D> constexpr int kf_stages() { return D == 256 ? 2 : 4; }
+template <int D> constexpr int kf_held() { return D == 64 ? 16 : 8; }       // wavefronts of a CU
 template <int D, bool BF16, int RT>
-__global__ void __launch_bounds__(256, D == 256 ? 2 : D == 128 && RT == 2 ? 3 : 4) k_key_weights_few(const KwParams p) {
-  constexpr int KS = D / 32;
+__global__ void __launch_bounds__(256, kf_held<D>() / 4) k_key_weights_few(const KwParams p) {
+  constexpr int KF_STAGES = kf_stages<D>();
+  constexpr int KS = D / 32, NP = D / 8, TILE = KF_KEYS * NP, COPIES = TILE / 64;
+  constexpr unsigned ROW = D * 2;
+  __shared__ __align__(1024) v4i s_k[4][KF_STAGES][TILE];
+  __shared__ float s_w[4][KF_STAGES][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 15, quad = lane >> 4;
   unsigned bh = blockIdx.x;
@@ -300,22 +311,31 @@ __global__ void __launch_bounds__(256, D == 256 ? 2 : D == 128 && RT == 2 ? 3 : 
   unsigned hkv = bh;
   const int b = (int)split_by(hkv, p.by_hkv);
   const int len = kw_len(p, b), rows = p.G * p.N, coff = max(len - p.N, 0);
-  const int tiles = (len + 31) / 32, j0 = chunk * 4 * p.piece + wave, j1 = min(j0 + 4 * p.piece, tiles);
+  const int tiles = (len + KF_KEYS - 1) / KF_KEYS, j0 = chunk * 4 * p.piece + wave, j1 = min(chunk * 4 * p.piece + 4 * p.piece, tiles);
   if (j0 >= j1) return;
-  const unsigned short* kb = p.k + head_offset_of(p.km, b, (int)hkv) + 8 * quad;
   const size_t wb = (size_t)bh * p.Nk;
-  struct Keys { v4i k[2][KS]; float w; };
-  auto load = [&](Keys& x, int j) __attribute__((always_inline)) {
+
+  // ---- copies of a tile: rows behind the last key repeat it
+  const char* gk = uniform_ptr(reinterpret_cast<const char*>(p.k + head_offset_of(p.km, b, (int)hkv)));
+  const char* gw = uniform_ptr(reinterpret_cast<const char*>(p.w_in + wb));
+  const bool add = p.w_in != nullptr;
+  const unsigned step = (unsigned)p.km.sn * 2;    // bytes from token to token
+  const unsigned k0 = (unsigned)(size_t)(__attribute__((address_space(3))) char*)&s_k[wave][0][0];
+  const unsigned w0 = (unsigned)(size_t)(__attribute__((address_space(3))) char*)&s_w[wave][0][0];
+  auto copy = [&](int j, int stage) __attribute__((always_inline)) {
+    const int last = len - 1 - j * KF_KEYS;
+    const char* from = gk + (size_t)j * KF_KEYS * step;
 #pragma unroll
-    for (int c = 0; c < 2; ++c) {
-      const unsigned short* at = kb + (size_t)min(32 * j + 16 * c + col, len - 1) * p.km.sn;
-#pragma unroll
-      for (int s = 0; s < KS; ++s) x.k[c][s] = *reinterpret_cast<const v4i*>(at + 32 * s);
+    for (int x = 0; x < COPIES; ++x) {
+      const int pc = x * 64 + lane, r = pc / NP;
+      dma_b128_once(from, (unsigned)min(r, last) * step + (unsigned)((pc % NP) ^ swizzle<D>(r)) * 16, k0 + (unsigned)(stage * TILE + x * 64) * 16);
     }
-    x.w = p.w_in && lane < 32 ? p.w_in[wb + min(32 * j + lane, len - 1)] : 0.0f;
+    if (add) dma_b32(gw + (size_t)j * (KF_KEYS * 4), (unsigned)min(col, last) * 4, w0 + stage * 256);
   };
-  Keys ka, kc;
-  load(ka, j0);
+#pragma unroll
+  for (int x = 0; x < KF_STAGES - 1; ++x)
+    if (j0 + 4 * x < j1) copy(j0 + 4 * x, x);
+
   // ---- the queries: row l % 16 of RT operands, and the constants of the rows of my accumulators (4 (l / 16) + 0..3)
   v4i q[RT][KS];
 #pragma unroll
@@ -332,6 +352,13 @@ __global__ void __launch_bounds__(256, D == 256 ? 2 : D == 128 && RT == 2 ? 3 : 
     const int g = (int)split_by(n, p.by_n);
     mine = p.lse[((size_t)b * p.H + (int)hkv * p.G + g) * p.N + n];
   }
+  // (waited for here, with the first tiles: in the loop the compiler would wait for every copy)
+#pragma unroll
+  for (int x = 0; x < RT; ++x)
+#pragma unroll
+    for (int s = 0; s < KS; ++s)
+#pragma unroll
+      for (int y = 0; y < 4; ++y) use_now(q[x][s][y]);
   const bool blind = __ballot(mine == -INFINITY) != 0;      // (a row that saw nothing: whatever its scores, it adds nothing)
   const int sees_all = blind ? 0 : p.causal ? min(coff + 1, len) : len;
   float nl[RT][4];
@@ -340,26 +367,38 @@ __global__ void __launch_bounds__(256, D == 256 ? 2 : D == 128 && RT == 2 ? 3 : 
 #pragma unroll
     for (int v = 0; v < 4; ++v) nl[x][v] = -__shfl(mine, 16 * x + 4 * quad + v) * LOG2E;
 
-  auto tile = [&](const Keys& k, int j) __attribute__((always_inline)) {
-    v4f acc[2][RT];
+  typedef __attribute__((address_space(3))) const v4i* lds_v4i;
+  const unsigned k_at = k0 + (unsigned)row_piece<D>(col, quad) * 16;       // (a step of 4 pieces is an exclusive or: see swizzle)
+  int stage = 0;
+  for (int j = j0; j < j1; j += 4) {
+    // copies are counted in order; stores, which are counted too, can only make the wait longer
+    const int later = min((j1 - 1 - j) / 4, KF_STAGES - 2);
+    auto wait = [&](auto per) __attribute__((always_inline)) {
+      constexpr int P = decltype(per)::value;
+      if (later == 0) asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+      else if (later == 1) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(P) : "memory");
+      else asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(2 * P) : "memory");
+    };
+    if (add) wait(std::integral_constant<int, COPIES + 1>{}); else wait(std::integral_constant<int, COPIES>{});
+    // (the stage of the tile before, whose reads are over)
+    if (j + 4 * (KF_STAGES - 1) < j1) copy(j + 4 * (KF_STAGES - 1), (stage + KF_STAGES - 1) % KF_STAGES);
+    v4f acc[RT];
 #pragma unroll
-    for (int c = 0; c < 2; ++c)
+    for (int x = 0; x < RT; ++x) acc[x] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+    const unsigned at = k_at + (unsigned)stage * (TILE * 16);
 #pragma unroll
-      for (int x = 0; x < RT; ++x) acc[c][x] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int s = 0; s < KS; ++s) {
+      const v4i k = *(lds_v4i)(at ^ (64 * s));
 #pragma unroll
-    for (int s = 0; s < KS; ++s)
+      for (int x = 0; x < RT; ++x) acc[x] = mfma16_small<BF16>(q[x][s], k, acc[x]);
+    }
+    const float was = add ? s_w[wave][stage][lane] : 0.0f;
+    float sum = 0.0f;
+    if (KF_KEYS * j + KF_KEYS <= sees_all) {
 #pragma unroll
-      for (int c = 0; c < 2; ++c)
+      for (int x = 0; x < RT; ++x)
 #pragma unroll
-        for (int x = 0; x < RT; ++x) acc[c][x] = mfma16_small<BF16>(q[x][s], k.k[c][s], acc[c][x]);
-    float sum[2] = {0.0f, 0.0f};
-    if (32 * j + 32 <= sees_all) {
-#pragma unroll
-      for (int c = 0; c < 2; ++c)
-#pragma unroll
-        for (int x = 0; x < RT; ++x)
-#pragma unroll
-          for (int v = 0; v < 4; ++v) sum[c] += __builtin_amdgcn_exp2f(__fmaf_rn(acc[c][x][v], p.kappa, nl[x][v]));
+        for (int v = 0; v < 4; ++v) sum += __builtin_amdgcn_exp2f(__fmaf_rn(acc[x][v], p.kappa, nl[x][v]));
     } else {
 #pragma unroll
       for (int x = 0; x < RT; ++x)
@@ -370,28 +409,16 @@ __global__ void __launch_bounds__(256, D == 256 ? 2 : D == 128 && RT == 2 ? 3 : 
           // (an lse of -inf or a row that is not there has +inf or -inf here)
           const bool see = fabsf(nl[x][v]) < INFINITY || nl[x][v] != nl[x][v];
           const int vis = !see ? 0 : p.causal ? min(coff + (int)n + 1, len) : len;
-#pragma unroll
-          for (int c = 0; c < 2; ++c) {
-            const float e = __builtin_amdgcn_exp2f(__fmaf_rn(acc[c][x][v], p.kappa, nl[x][v]));
-            sum[c] += 32 * j + 16 * c + col < vis ? e : 0.0f;
-          }
+          const float e = __builtin_amdgcn_exp2f(__fmaf_rn(acc[x][v], p.kappa, nl[x][v]));
+          sum += KF_KEYS * j + col < vis ? e : 0.0f;
         }
     }
-#pragma unroll
-    for (int c = 0; c < 2; ++c) {
-      const unsigned u = __float_as_uint(sum[c]);
-      const auto sw = __builtin_amdgcn_permlane16_swap(u, u, false, false);
-      sum[c] = half_sum(__uint_as_float(sw[0]) + __uint_as_float(sw[1]));
-    }
-    if (lane < 32 && 32 * j + lane < len) p.w[wb + 32 * j + lane] = k.w + (quad == 0 ? sum[0] : sum[1]);
-  };
-  for (int j = j0; j < j1; j += 8) {
-    if (j + 4 < j1) load(kc, j + 4);
-    tile(ka, j);
-    if (j + 4 < j1) {
-      if (j + 8 < j1) load(ka, j + 8);
-      tile(kc, j + 4);
-    }
+    const unsigned u = __float_as_uint(sum);
+    const auto sw = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    sum = half_sum(__uint_as_float(sw[0]) + __uint_as_float(sw[1]));
+    const int key = KF_KEYS * j + lane;
+    if (lane < KF_KEYS && key < len) p.w[wb + key] = was + sum;
+    stage = (stage + 1) % KF_STAGES;
   }
 }
 
@@ -452,16 +479,14 @@ int kw_params(const sage_attn_key_weights_args* a, KwParams* p, bool need_io) {
   // channels 8 k 73 / 69 / 73; of 64 33 k 134 / 119 / 116 / 120.
   p->piece = (int)std::min<long long>(std::min(most, KW_PIECE), std::max(2LL, (heads * all + 1023) / 1024));
   p->pieces = (most + p->piece - 1) / p->piece;
-  // (With two operands, 33 to 64 rows, the registers leave two wavefronts per SIMD: 64 rows on 16 caches of 6000 keys 23.6 us, with tiles 13.6.)
+  // (Tiles that come through LDS for all of a workgroup suit more rows: 64 on 16 caches of 6000 keys 13.6 us, 23.6 with few rows' kernel.)
   p->few = (long long)p->G * a->N <= KW_FEW;
-  // Tiles of 32 keys per wavefront: until there are 32 wavefronts per CU, two rounds of those it holds; lengths differ, and with one
-  // round the chip empties early.  (Us, for 8 / 16 / 32 / 64 of them, caches read from memory: 32 of 32768 keys, 128 channels, 44.3 / 46.2 / 46.0 /
-  // 46.5; 128 of 20000 99.7 / 101.7 / 93.9 / 91.4; 128 of 9000, 64, 26.8 / 25.9 / 22.2 / 22.2; 16 of 20000, 256, 31.1 / 29.8 / 30.5 / 30.7; 64 of 16000 with
-  // 24 rows 47.3 / 45.8 / 42.9 / 51.7.)
+  // Tiles of a wavefront: as many as make two rounds of the wavefronts that the chip holds; lengths differ, and with one round it empties
+  // early.  (Us, for one and a half / two / three rounds: 32 caches of 32768 keys of 128 channels 47 / 39 / 42, 128 of 20000 91 / 81 / 80.)
   if (p->few) {
-    const long long tiles = (a->N_kv + 31) / 32;
+    const long long tiles = (a->N_kv + KF_KEYS - 1) / KF_KEYS, held = 256 * (a->d == 64 ? kf_held<64>() : a->d == 128 ? kf_held<128>() : kf_held<256>());
     p->pieces = 1;
-    p->piece = (int)std::max(1LL, std::min(64LL, heads * tiles / (256 * 32)));
+    p->piece = (int)std::max(1LL, std::min(128LL, heads * tiles / (2 * held)));
     p->key_tiles = (int)((tiles + 4 * p->piece - 1) / (4 * p->piece));
   }
   if (heads * p->key_tiles * p->pieces > 0x7fffffffLL) return SAGE_ERR_UNSUPPORTED;
