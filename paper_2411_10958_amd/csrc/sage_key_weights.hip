@@ -17,7 +17,7 @@ namespace {
 
 constexpr int KW_KEYS = 256;     // keys of a workgroup: 64 per wavefront
 constexpr int KW_ROWS = 64;      // queries of a tile
-constexpr int KW_FEW = 32;       // rows of a group that are few
+constexpr int KW_FEW = 64;       // rows of a group that are few
 constexpr int KW_PIECE = 16;     // most query tiles of a workgroup: their constants are kept in LDS
 
 struct KwParams {
@@ -479,14 +479,17 @@ int kw_params(const sage_attn_key_weights_args* a, KwParams* p, bool need_io) {
   // channels 8 k 73 / 69 / 73; of 64 33 k 134 / 119 / 116 / 120.
   p->piece = (int)std::min<long long>(std::min(most, KW_PIECE), std::max(2LL, (heads * all + 1023) / 1024));
   p->pieces = (most + p->piece - 1) / p->piece;
-  // (Tiles that come through LDS for all of a workgroup suit more rows: 64 on 16 caches of 6000 keys 13.6 us, 23.6 with few rows' kernel.)
-  p->few = (long long)p->G * a->N <= KW_FEW;
-  // Tiles of a wavefront: as many as make two rounds of the wavefronts that the chip holds; lengths differ, and with one round it empties
-  // early.  (Us, for one and a half / two / three rounds: 32 caches of 32768 keys of 128 channels 47 / 39 / 42, 128 of 20000 91 / 81 / 80.)
+  // Few rows; more than 32 only from 64 k keys on, because every wavefront has all of them to read first (us, tiles of queries / few rows: 48
+  // rows of 128 channels on 128 caches of 16000 keys 87 / 73, on 8 of 9000 11.7 / 10.9, on 8 of 4000 9.2 / 10.6).  Its key tiles: as
+  // many as make two rounds of the wavefronts that the chip holds - lengths differ, and with one round it empties early (one and a half / two / three: 32
+  // caches of 32768 keys of 128 channels 47 / 39 / 42, 128 of 20000 91 / 81 / 80) - but four at least, eight for more than 16 rows (one / two
+  // / four / eight: 24 rows on 32 caches of 4000 keys of 128 channels 16.3 / 12.1 / 9.6 / 9.5, 4 rows 11.8 / 11.7 / 9.1 / -).
+  const long long rows = (long long)p->G * a->N, tiles = (a->N_kv + KF_KEYS - 1) / KF_KEYS;
+  p->few = rows <= 32 || (rows <= KW_FEW && heads * tiles >= 4096);
   if (p->few) {
-    const long long tiles = (a->N_kv + KF_KEYS - 1) / KF_KEYS, held = 256 * (a->d == 64 ? kf_held<64>() : a->d == 128 ? kf_held<128>() : kf_held<256>());
+    const long long held = 256 * (a->d == 64 ? kf_held<64>() : a->d == 128 ? kf_held<128>() : kf_held<256>());
     p->pieces = 1;
-    p->piece = (int)std::max(1LL, std::min(128LL, heads * tiles / (2 * held)));
+    p->piece = (int)std::max(rows > 16 ? 8LL : 4LL, std::min(128LL, heads * tiles / (2 * held)));
     p->key_tiles = (int)((tiles + 4 * p->piece - 1) / (4 * p->piece));
   }
   if (heads * p->key_tiles * p->pieces > 0x7fffffffLL) return SAGE_ERR_UNSUPPORTED;
@@ -496,7 +499,8 @@ int kw_params(const sage_attn_key_weights_args* a, KwParams* p, bool need_io) {
 template <int D, bool BF16> hipError_t launch_kw(const KwParams& p, unsigned blocks, hipStream_t s) {
   if (!p.few) k_key_weights<D, BF16><<<blocks, 256, 0, s>>>(p);
   else if (p.G * p.N <= 16) k_key_weights_few<D, BF16, 1><<<blocks, 256, 0, s>>>(p);
-  else k_key_weights_few<D, BF16, 2><<<blocks, 256, 0, s>>>(p);
+  else if (p.G * p.N <= 32) k_key_weights_few<D, BF16, 2><<<blocks, 256, 0, s>>>(p);
+  else k_key_weights_few<D, BF16, 4><<<blocks, 256, 0, s>>>(p);
   return hipGetLastError();
 }
 

@@ -62,6 +62,17 @@ def test_a_prompt_in_several_pieces():
     assert abs(total.sum().item() / (4 * 3000) - 1) < 1e-5                           # every query gives away a weight of 1
 
 
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("G,N", [(4, 1), (3, 7), (5, 8), (8, 8)])
+def test_steps_on_long_caches(G, N, d):
+    """Few rows on so many keys that a wavefront walks over many tiles, and that more than 32 rows count as few too."""
+    pa = _pa()
+    lens = torch.tensor([33001, 16389, 17, 1], dtype=torch.int32, device="cuda")
+    dt, layout = (torch.bfloat16, "NHD") if N % 2 else (torch.float16, "HND")
+    for causal, added in ((True, True), (False, False)):
+        _check(pa, _inputs(4, G, 1, N, 33001, d, dt, layout, causal, lens), lens=lens, causal=causal, layout=layout, added=added)
+
+
 def test_rows_without_keys_and_lengths_out_of_range():
     pa = _pa()
     lens = torch.tensor([0, -3, 5000, 1], dtype=torch.int32, device="cuda")
