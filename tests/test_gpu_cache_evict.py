@@ -54,6 +54,14 @@ def test_sizes(nk, keep, sink, recent):
     _check(pa, _w((2, 3, nk), nk), keep, sink, recent)
 
 
+@pytest.mark.parametrize("layout", ["HND", "NHD"])
+def test_more_than_the_caches_hold(layout):
+    """A call that moves over 256 MB."""
+    pa = _pa()
+    lens = torch.tensor([40003, 20000], dtype=torch.int32, device="cuda")
+    _check(pa, _w((2, 4, 40003), 3), 33001, 4, 100, lens, d=128, layout=layout)
+
+
 @pytest.mark.parametrize("d,dt,layout", [(64, torch.float16, "NHD"), (128, torch.bfloat16, "NHD"), (128, torch.float16, "HND"), (256, torch.bfloat16, "HND"),
                                          (256, torch.float16, "NHD")])
 def test_widths_types_and_layouts(d, dt, layout):

@@ -42,6 +42,23 @@ def test_styles_and_parts_of_the_head(d, rot, interleaved):
             assert torch.equal(y[..., rot:], x[..., rot:])           # the other channels are copied
 
 
+@pytest.mark.parametrize("d,rot,interleaved,layout,in_place", [(64, 32, True, "HND", False), (64, 64, True, "NHD", True), (128, 128, False, "NHD", False),
+                                                               (256, 128, False, "HND", False), (128, 128, False, "HND", True), (64, 64, False, "HND", False)])
+def test_more_than_the_caches_hold(d, rot, interleaved, layout, in_place):
+    """Calls that read and write over 256 MB."""
+    pa = _pa()
+    B, H, Hkv, N = 2, 5, 3, (2 ** 22 // d) + 465
+    print(f"rope d={d} rot={rot} interleaved={interleaved} {layout} in place={in_place} N={N}", flush=True)
+    g = _gen(d)
+    q, k = _x(g, B, H, N, d, torch.bfloat16, layout), _x(g, B, Hkv, N, d, torch.bfloat16, layout)
+    f = pa.sage_rope_frequencies(rot)
+    pos = torch.arange(N, device="cuda") + 9
+    want = [ref.rope(x, f, pos, interleaved, True, 1.0, layout) for x in (q, k)]
+    outs = dict(q_out=q, k_out=k) if in_place else {}
+    for name, y, (w, bound) in zip("qk", pa.sage_rope(q, k, f, offset=9, interleaved=interleaved, inverse=True, layout=layout, **outs), want):
+        ref.check(name, y, w, bound)
+
+
 def test_positions():
     pa = _pa()
     g = _gen(3)
