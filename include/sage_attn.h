@@ -6,7 +6,7 @@
  * by its per-block mean with the Delta-S bias added back (Sec. 3.1, Eq. 2), Q and K are
  * quantized to INT4 (or INT8) codes with one scale per fine-grained token group (Sec. 3.2),
  * P~ and V are quantized to FP8 E4M3 (Sec. 3.3) and P~V is accumulated in two levels
- * (Sec. 3.4); the whole loop is Algorithm 1.
+ * (Sec. 3.4); the whole loop is Algorithm 1.  Operators that a serving program runs around it are at the end.
  *
  * Conventions for every entry point
  *   - All tensor pointers are DEVICE pointers owned by the caller, 16-byte aligned; the library never
@@ -340,7 +340,8 @@ int sage_rope_frequencies(int rot_dim, double base, int scaling, double factor, 
  * document - followed by each sequence's own:  out = softmax(sm_scale Q [K_prefix; K]^T) [V_prefix; V].  Nothing is quantized: K and V
  * are read as they are, scores, softmax and sums are FP32, P is rounded to the 16-bit type for its product with V.  The prefix
  * is read once for the whole batch.  Meant for decode steps and short chunks of queries.  Every query sees the whole prefix; `causal`
- * masks the own keys (see above).  A query without any key gets zeros and lse = -inf. */
+ * masks the own keys (see above).  A query without any key gets zeros and lse = -inf; a value that is not finite reaches
+ * only queries that see its key. */
 typedef struct sage_attn_shared_prefix_args {
   const void* q;            /* device, [B, H, N, d] or [B, N, H, d] */
   const void* k_prefix;     /* device, [H_kv, N_prefix, d] or [N_prefix, H_kv, d]; not read if N_prefix = 0 */
@@ -392,14 +393,15 @@ typedef struct sage_cache_evict_args {
   const void* v;
   const float* weights;     /* device, [B, H_kv, N_kv] f32, e.g. from sage_attn_key_weights */
   const int* kv_lens;
-  void* k_out;              /* device, [B, H_kv, N_keep, d] or [B, N_keep, H_kv, d] */
+  void* k_out;              /* device, [B, H_kv, N_out, d] or [B, N_out, H_kv, d] */
   void* v_out;
-  float* weights_out;       /* device, [B, H_kv, N_keep] f32, or NULL */
+  float* weights_out;       /* device, [B, H_kv, N_out] f32, or NULL */
   int* kept;                /* device, [B, H_kv, N_keep] int32: which tokens, ascending */
   int* lens_out;            /* device, [B] int32: min(len, N_keep) */
   int B, H_kv, N_kv, N_keep, d;
   int sink, recent;         /* sink + recent <= N_keep */
   int dtype, layout;
+  int N_out;                /* room of the outputs, N_keep or more, so that the cache can go on growing there; 0 means N_keep */
   void* stream;
 } sage_cache_evict_args;
 int sage_cache_evict(const sage_cache_evict_args* args);

@@ -81,7 +81,7 @@ class sage_attn_key_weights_args(ctypes.Structure):
 
 class sage_cache_evict_args(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in ("k", "v", "weights", "kv_lens", "k_out", "v_out", "weights_out", "kept", "lens_out")] + \
-               [(n, ctypes.c_int) for n in ("B", "H_kv", "N_kv", "N_keep", "d", "sink", "recent", "dtype", "layout")] + \
+               [(n, ctypes.c_int) for n in ("B", "H_kv", "N_kv", "N_keep", "d", "sink", "recent", "dtype", "layout", "N_out")] + \
                [("stream", ctypes.c_void_p)]
 
 
@@ -656,11 +656,12 @@ def sage_attn_key_weights(q, k, lse, weights_in=None, weights=None, kv_lens=None
 
 
 def sage_cache_evict(k, v, weights, n_keep, sink=0, recent=0, kv_lens=None, layout="HND", k_out=None, v_out=None, weights_out=None, kept=None,
-                     lens_out=None, stream=None):
+                     lens_out=None, stream=None, room=None):
     """Cuts a cache k, v [B, H_kv, N_kv, d] to n_keep tokens per KV head: the first `sink` and the last `recent` of those in use
     (kv_lens, int32 [B]; None: all) and the ones of largest weight (float32 [B, H_kv, N_kv]) between.  Returns (k_out, v_out,
     weights_out, kept, lens_out): the rows kept, in their order, their weights, which they were (int32 [B, H_kv, n_keep]) and how many
-    (int32 [B]); what stands behind them keeps what it held (zeros where the output is allocated here)."""
+    (int32 [B]); what stands behind them keeps what it held (zeros where the output is allocated here).  k_out, v_out and weights_out
+    have room for `room` tokens (None: n_keep), so that the cache can go on growing there."""
     dtype, dt, index, nhd = _dtype_code(k), k.dtype, _gpu_of("k", k), _LAYOUTS[layout]
     B, Hkv, Nk, d = _sizes("k", k, nhd)
     _need("k", k, index, dt)
@@ -668,21 +669,24 @@ def sage_cache_evict(k, v, weights, n_keep, sink=0, recent=0, kv_lens=None, layo
     n_keep = int(n_keep)
     if n_keep < 1:
         raise ValueError("n_keep must be at least 1")
+    room = n_keep if room is None else int(room)
+    if room < n_keep:
+        raise ValueError(f"room must be n_keep, {n_keep}, or more, got {room}")
     _need("weights", weights, index, torch.float32, (B, Hkv, Nk))
     if kv_lens is not None:
         _need("kv_lens", kv_lens, index, torch.int32, (B,))
-    make = torch.zeros if kv_lens is not None or n_keep > Nk else torch.empty
-    rows, per = (B, n_keep, Hkv, d) if nhd else (B, Hkv, n_keep, d), (B, Hkv, n_keep)
+    make = torch.zeros if kv_lens is not None or room > Nk or room > n_keep else torch.empty
+    rows = (B, room, Hkv, d) if nhd else (B, Hkv, room, d)
     outs = []
-    for name, t, shape, want in (("k_out", k_out, rows, dt), ("v_out", v_out, rows, dt), ("weights_out", weights_out, per, torch.float32),
-                                 ("kept", kept, per, torch.int32), ("lens_out", lens_out, (B,), torch.int32)):
+    for name, t, shape, want in (("k_out", k_out, rows, dt), ("v_out", v_out, rows, dt), ("weights_out", weights_out, (B, Hkv, room), torch.float32),
+                                 ("kept", kept, (B, Hkv, n_keep), torch.int32), ("lens_out", lens_out, (B,), torch.int32)):
         if t is None:
             t = _new(shape, want, index, stream, make)
         else:
             _need(name, t, index, want, shape)
         outs.append(t)
     a = sage_cache_evict_args(k.data_ptr(), v.data_ptr(), weights.data_ptr(), _address(kv_lens), *[t.data_ptr() for t in outs],
-                              B, Hkv, Nk, n_keep, d, int(sink), int(recent), dtype, nhd,
+                              B, Hkv, Nk, n_keep, d, int(sink), int(recent), dtype, nhd, room,
                               stream.cuda_stream if stream is not None else _current_raw_stream(index))
     _call("sage_cache_evict", a, index)
     return tuple(outs)

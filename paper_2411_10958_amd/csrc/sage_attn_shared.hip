@@ -470,8 +470,8 @@ __global__ void __launch_bounds__(256) k_shared_merge(const SharedParams p) {
 // for, so 512 / d tiles at least.  A workgroup of the prefix takes an even share of all tiles - it has up to 128 rows of partial
 // results to leave - and where it has few rows and is bound by reading, so many that there is one to a CU.  The own keys of a
 // sequence have few rows, and lengths that the host does not know: they are cut finer, 12 tiles at most, so that the chip fills up to
-// the end.  Us, an even share for both / this: 64 sequences of up to 4096 tokens over 32768, 128 channels 174 / 162;
-// 1 of 300 over 32768 33.4 / 31.5; 4 of 2000 over 100000 88.8 / 86.1; 32 of 3000 over 200 50.9 / 49.3.
+// the end.  Us, an even share for both / this, caches read from memory: 64 sequences of up to 4096 tokens over 32768, 128 channels 173 /
+// 158; 1 of 300 over 32768 32.4 / 32.1; 4 of 2000 over 100000 84 / 76; 32 of 3000 over 200 55.9 / 54.3.
 void choose_chunks(SharedParams* p, int d, long long rows) {
   const long long tp = (p->P + SH_KEYS - 1) / SH_KEYS, to = (p->Nk + SH_KEYS - 1) / SH_KEYS;
   const long long prefix = (long long)p->Hkv * p->rtp * tp, own = (long long)p->B * p->Hkv * p->rto * to;

@@ -14,7 +14,7 @@ struct EvictParams {
   unsigned short *k_out, *v_out;
   float* w_out;
   int *kept, *lens_out;
-  int Hkv, N, keep, sink, recent;
+  int Hkv, N, keep, room, sink, recent;
   TensorMap in, out;
 };
 
@@ -174,7 +174,7 @@ template <int D, bool PAST> __global__ void __launch_bounds__(256) k_evict_rows(
         *ka = a[i];
         *va = x[i];
       }
-      if (weigh) p.w_out[(size_t)blockIdx.y * p.keep + first + i * TOK] = wt[i];
+      if (weigh) p.w_out[(size_t)blockIdx.y * p.room + first + i * TOK] = wt[i];
     }
   }
 }
@@ -197,18 +197,19 @@ using namespace sage;
 
 extern "C" int sage_cache_evict(const sage_cache_evict_args* a) {
   if (!a || a->B <= 0 || a->H_kv <= 0 || a->N_kv <= 0 || a->N_keep <= 0 || a->sink < 0 || a->recent < 0) return SAGE_ERR_INVALID_ARG;
-  if ((long long)a->sink + a->recent > a->N_keep) return SAGE_ERR_INVALID_ARG;
+  const int room = a->N_out == 0 ? a->N_keep : a->N_out;
+  if ((long long)a->sink + a->recent > a->N_keep || room < a->N_keep) return SAGE_ERR_INVALID_ARG;
   if (!a->k || !a->v || !a->weights || !a->k_out || !a->v_out || !a->kept || !a->lens_out) return SAGE_ERR_INVALID_ARG;
   if (a->d != 64 && a->d != 128 && a->d != 256) return SAGE_ERR_UNSUPPORTED;
   if (a->dtype != SAGE_DT_FP16 && a->dtype != SAGE_DT_BF16) return SAGE_ERR_UNSUPPORTED;
   if (a->layout != SAGE_LAYOUT_HND && a->layout != SAGE_LAYOUT_NHD) return SAGE_ERR_UNSUPPORTED;
-  if (a->N_kv > MAX_TOKENS || a->N_keep > MAX_TOKENS || (long long)a->B * a->H_kv > 65535) return SAGE_ERR_UNSUPPORTED;
+  if (a->N_kv > MAX_TOKENS || room > MAX_TOKENS || (long long)a->B * a->H_kv > 65535) return SAGE_ERR_UNSUPPORTED;
   if ((((uintptr_t)a->k | (uintptr_t)a->v | (uintptr_t)a->k_out | (uintptr_t)a->v_out) & 15u) != 0) return SAGE_ERR_INVALID_ARG;
   if ((((uintptr_t)a->weights | (uintptr_t)a->weights_out | (uintptr_t)a->kept | (uintptr_t)a->lens_out | (uintptr_t)a->kv_lens) & 3u) != 0)
     return SAGE_ERR_INVALID_ARG;
-  const size_t heads = (size_t)a->B * a->H_kv, rows = heads * a->N_kv, out_rows = heads * a->N_keep;
+  const size_t heads = (size_t)a->B * a->H_kv, rows = heads * a->N_kv, out_rows = heads * room;
   const Span in[4] = {{a->k, rows * a->d * 2}, {a->v, rows * a->d * 2}, {a->weights, rows * 4}, {a->kv_lens, (size_t)a->B * 4}};
-  const Span out[5] = {{a->k_out, out_rows * a->d * 2}, {a->v_out, out_rows * a->d * 2}, {a->weights_out, out_rows * 4}, {a->kept, out_rows * 4},
+  const Span out[5] = {{a->k_out, out_rows * a->d * 2}, {a->v_out, out_rows * a->d * 2}, {a->weights_out, out_rows * 4}, {a->kept, heads * a->N_keep * 4},
                        {a->lens_out, (size_t)a->B * 4}};
   for (int i = 0; i < 5; ++i) {
     for (const Span& s : in) if (overlap(out[i], s)) return SAGE_ERR_INVALID_ARG;
@@ -217,10 +218,10 @@ extern "C" int sage_cache_evict(const sage_cache_evict_args* a) {
   EvictParams p;
   p.k = (const unsigned short*)a->k; p.v = (const unsigned short*)a->v; p.w = a->weights; p.lens = a->kv_lens;
   p.k_out = (unsigned short*)a->k_out; p.v_out = (unsigned short*)a->v_out; p.w_out = a->weights_out; p.kept = a->kept; p.lens_out = a->lens_out;
-  p.Hkv = a->H_kv; p.N = a->N_kv; p.keep = a->N_keep; p.sink = a->sink; p.recent = a->recent;
+  p.Hkv = a->H_kv; p.N = a->N_kv; p.keep = a->N_keep; p.room = room; p.sink = a->sink; p.recent = a->recent;
   const int nhd = a->layout == SAGE_LAYOUT_NHD;
   p.in = make_tensor_map(nhd, a->H_kv, a->N_kv, a->d);
-  p.out = make_tensor_map(nhd, a->H_kv, a->N_keep, a->d);
+  p.out = make_tensor_map(nhd, a->H_kv, room, a->d);
   const hipStream_t s = (hipStream_t)a->stream;
   const int most = a->N_kv - a->sink - a->recent;       // weights to choose from
   if (most <= 4 * SEL_THREADS) k_evict_select<4><<<(unsigned)heads, SEL_THREADS, 0, s>>>(p);
@@ -232,7 +233,7 @@ extern "C" int sage_cache_evict(const sage_cache_evict_args* a) {
   if (st != SAGE_OK) return st;
   const int per = 256 / (a->d / 8) * GU;
   const dim3 grid((unsigned)((std::min(a->N_keep, a->N_kv) + per - 1) / per), (unsigned)heads);
-  const bool past = 8LL * (long long)out_rows * a->d > 256LL << 20;
+  const bool past = 8LL * (long long)heads * a->N_keep * a->d > 256LL << 20;
   if (a->d == 64) launch_rows<64>(p, past, grid, s);
   else if (a->d == 128) launch_rows<128>(p, past, grid, s);
   else launch_rows<256>(p, past, grid, s);

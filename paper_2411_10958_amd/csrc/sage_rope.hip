@@ -1,7 +1,8 @@
 // Rotary positions of queries and keys (sage_rope) and their frequencies (sage_rope_frequencies).
 //
 // Channel pair i of the first `rot` channels is turned by the angle p f_i: (a, b) -> scale (a cos - b sin, b cos + a sin), the
-// pair being channels (i, i + rot/2) or (2i, 2i + 1).  Nothing but bytes moves this: every value is read and written once, 4 bytes.
+// pair being channels (i, i + rot/2) or (2i, 2i + 1).  Nothing but bytes moves this: every value is read and written once, 4 bytes
+// (4 x 4096 tokens of 40 heads of 128: 57 to 60 us, 5.6 to 5.9 TB/s; a copy of 2 GB 5.0).
 // A thread owns one vector of VW channels of a token, or two, a pair's channels in each, works their angles out once and then walks over
 // heads, so the FP64 product and the sine and cosine are shared by all of them.  Angles are taken in 64 bits (position 10^6 times the fastest
 // frequency in FP32 would be off by 0.03 rad), reduced to a fraction of a turn there, and their sine and cosine in FP32.
@@ -256,14 +257,14 @@ extern "C" int sage_rope(const sage_rope_args* a) {
   const bool whole_lines = vw == 8 && (rows & 63) == 0 && (inter ? (a->rot_dim + rest) % 64 == 0 : a->rot_dim % 128 == 0 && rest % 128 == 0);
   const bool past = whole_lines && 4LL * a->B * a->N * (p.q.heads + p.k.heads) * (a->rot_dim + rest) > 256LL << 20;
   // Token-major rows: neighbouring threads take neighbouring heads of a token, which are one stretch of memory; with a token each they
-  // would read pieces of 256 bytes, a token's row apart (4 x 4096 tokens of 40 heads of 128: 79 us, so 67).
+  // would read pieces of 256 bytes, a token's row apart (4 x 4096 tokens of 40 heads of 128: 80 us, so 60).
   p.lanes = 1;
   if (st[0][1] < st[0][2] && a->N > 1) while (p.lanes * 2 * p.units <= 64 && p.lanes * 2 <= a->H) p.lanes *= 2;
   p.total = (long long)a->B * a->N * p.units * p.lanes;
   const long long blocks = (p.total + 255) / 256;
   if (blocks > 0x7fffffffLL) return SAGE_ERR_UNSUPPORTED;
   // Heads are divided over workgroups only until there are sixteen of these per CU: each pays for the angles again.  (Eight: 2 x 17776
-  // tokens of 96 heads of 64 172 us, sixteen 165.)  Heads that lie side by side in one stay together.
+  // tokens of 96 heads of 64 163 us, sixteen 155.)  Heads that lie side by side in one stay together.
   const int heads = p.q.heads + p.k.heads;
   const long long pieces = std::max(1LL, std::min((4096 + blocks - 1) / blocks, (long long)heads / p.lanes));
   p.hchunk = (int)((heads + pieces - 1) / pieces);

@@ -132,3 +132,29 @@ def test_long_rows_another_stream_and_replays():
         n = min(n, keep)
         assert torch.equal(kw["lens_out"], again[4])
         assert all(torch.equal(kw[x][:, :, :n], again[i][:, :, :n]) for i, x in enumerate(("k_out", "v_out", "weights_out", "kept")))
+
+
+@pytest.mark.parametrize("layout", ["HND", "NHD"])
+def test_room_for_more_than_is_kept(layout):
+    """A cache cut into one of the same size: places behind what is kept stay as they were."""
+    pa = _pa()
+    B, Hkv, nk, d, keep = 3, 2, 500, 128, 200
+    g = torch.Generator(device="cuda")
+    g.manual_seed(5)
+    k, v = (ref.to_layout(torch.randn((B, Hkv, nk, d), generator=g, device="cuda").half(), layout) for _ in range(2))
+    w, lens = _w((B, Hkv, nk), 6), torch.tensor([500, 150, 333], dtype=torch.int32, device="cuda")
+    want = ref.evict(k, v, w, keep, 4, 50, lens, layout)
+    old = dict(k_out=torch.full_like(k, 5.0), v_out=torch.full_like(v, 6.0), weights_out=torch.full_like(w, 7.0))
+    for room, outs in ((nk, old), (nk, {}), (201, {})):
+        ko, vo, wo, kept, left = pa.sage_cache_evict(k, v, w, keep, sink=4, recent=50, kv_lens=lens, layout=layout, room=room, **outs)
+        kh, vh, ko, vo = (ref.heads_first(x, layout) for x in (k, v, ko, vo))
+        assert ko.shape == (B, Hkv, room, d) and wo.shape == (B, Hkv, room) and kept.shape == (B, Hkv, keep)
+        for b in range(B):
+            n = len(want[b][0])
+            assert left[b].item() == n
+            for h in range(Hkv):
+                at = torch.tensor(want[b][h], device="cuda", dtype=torch.long)
+                assert kept[b, h, :n].tolist() == want[b][h]
+                assert torch.equal(ko[b, h, :n], kh[b, h][at]) and torch.equal(vo[b, h, :n], vh[b, h][at]) and torch.equal(wo[b, h, :n], w[b, h][at])
+                for x, y in ((ko, 5.0), (vo, 6.0), (wo, 7.0)):
+                    assert (x[b, h, n:] == (y if outs else 0.0)).all()

@@ -103,6 +103,13 @@ def test_cache_evict(kw, status):
     assert _status(pa, lib, "sage_cache_evict", EVICT, **kw) == status
 
 
+@pytest.mark.parametrize("kw,status", [(dict(N_out=39), -1), (dict(N_out=-1), -1), (dict(N_out=(1 << 24) + 1), -2),
+                                       (dict(k_out=(1 << 20) - 2 * 300 * 64 * 2 + 16, N_out=300), -1), (dict(kept=(6 << 20) + 2 * 300 * 4 - 4, N_out=300), -1)])
+def test_cache_evict_room(kw, status):
+    pa, lib = _pa()
+    assert _status(pa, lib, "sage_cache_evict", EVICT, **kw) == status
+
+
 def test_null_arguments():
     pa, lib = _pa()
     for name in ("sage_rope", "sage_attn_shared_prefix", "sage_attn_key_weights", "sage_cache_evict"):
