@@ -397,22 +397,24 @@ if (once) {
     }
 }
 
-// The partial results of a row into its output, a wavefront per row: lane s looks at partial results s, s + 64, .. for the
-// maximum and the weights; then D / 4 lanes take four channels each of every GRP-th partial result, MERGE_LOADS of them in flight.  Bound by
+// The partial results of a row into its output, a wavefront per row, or per 64 channels of 256 (7.2 us, so 6.0, for 480 rows of 34 partial
+// results; of 128 channels halves cost 1 to 4 us on large batches): lane s looks at partial results s, s + 64, .. for the
+// maximum and the weights; then a lane takes four channels of every GRP-th partial result, MERGE_LOADS of them in flight.  Bound by
 // the two trips to memory, not by bytes.  Scores that are NaN leave their mark in the sum, whatever the maximum.
+template <int D> constexpr int merge_channels() { return D == 256 ? 64 : D; }
 constexpr int MERGE_LOADS = 8, MERGE_PER_LANE = 4;
 constexpr int MAX_PARTS = 64 * MERGE_PER_LANE;
 template <int D, bool BF16>
 __global__ void __launch_bounds__(256) k_shared_merge(const SharedParams p) {
-  constexpr int LPR = D / 4, GRP = 64 / LPR;
+  constexpr int MC = merge_channels<D>(), LPR = MC / 4, GRP = 64 / LPR, SLICES = D / MC;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  unsigned row = blockIdx.x * 4 + (unsigned)wave;
+  unsigned row = blockIdx.x * (4 / SLICES) + (unsigned)wave / SLICES;
   if (row >= (unsigned)(p.B * p.G * p.N * p.Hkv)) return;
   const int hkv = (int)split_by(row, p.by_rows);
   const long long i = row;
   unsigned n = row;
   const int b = (int)split_by(n, p.by_gn), g = (int)split_by(n, p.by_n);
-  const int S = p.Sp + p.So, c = 4 * (lane % LPR), grp = lane / LPR;
+  const int S = p.Sp + p.So, c = MC * (wave % SLICES) + 4 * (lane % LPR), grp = lane / LPR;
   float ms[MERGE_PER_LANE], w[MERGE_PER_LANE], m = -INFINITY, l = 0.0f;
 #pragma unroll
   for (int x = 0; x < MERGE_PER_LANE; ++x) {
@@ -507,13 +509,13 @@ int shared_params(const sage_attn_shared_prefix_args* a, SharedParams* p, bool n
   p->pm = make_tensor_map(nhd, a->H_kv, a->N_prefix, a->d);
   p->om = make_tensor_map(nhd, a->H_kv, a->N_kv, a->d);
   const long long gn = (long long)p->G * p->N, rows = gn * p->B;
-  if (rows > (1LL << 30)) return SAGE_ERR_UNSUPPORTED;
+  if (rows * p->Hkv > (1LL << 24)) return SAGE_ERR_UNSUPPORTED;
   const int per = shared_rows(a->d);
   p->rtp = (int)((rows + per - 1) / per);
   p->rto = (int)((gn + per - 1) / per);
   choose_chunks(p, a->d, rows);
   const long long np = (long long)p->Sp * p->Hkv * p->rtp, no = (long long)p->So * p->B * p->Hkv * p->rto;
-  if (np + no > 0x7fffffffLL || rows * p->Hkv > 0x7fffffffLL) return SAGE_ERR_UNSUPPORTED;
+  if ((np + no) * (a->d == 256 ? 64 * shared_waves<256>() : 64 * shared_waves<128>()) > MAX_THREADS) return SAGE_ERR_UNSUPPORTED;
   p->n_prefix = (int)np;
   p->full = p->Sp * a->H_kv / 8 * 8 * p->rtp;
   p->by_group = fast_div(8u * p->rtp); p->by_rtp = fast_div(p->rtp); p->by_hkv = fast_div(a->H_kv); p->by_rto = fast_div(p->rto);
@@ -532,7 +534,7 @@ template <int D, bool BF16> hipError_t launch_shared(const SharedParams& p, hipS
     if (e != hipSuccess) return e;
   }
   const long long rows = (long long)p.B * p.G * p.N * p.Hkv;
-  k_shared_merge<D, BF16><<<(unsigned)((rows + 3) / 4), 256, 0, s>>>(p);
+  k_shared_merge<D, BF16><<<(unsigned)((rows * (D / merge_channels<D>()) + 3) / 4), 256, 0, s>>>(p);
   return hipGetLastError();
 }
 

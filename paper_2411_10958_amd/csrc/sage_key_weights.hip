@@ -31,7 +31,7 @@ struct KwParams {
   int causal, flat;              // flat: tiles run over the G N queries of a group, else over the N of each head
   float kappa;
   int key_tiles, pieces, piece;  // most pieces of a key tile, query tiles of a piece
-  FastDiv by_heads, by_hkv, by_kt, by_n;      // B H_kv, H_kv, key_tiles, N
+  FastDiv by_heads, by_hkv, by_n;      // B H_kv, H_kv, N
 };
 
 // Query tiles of the keys t0 .. t0 + 255 of a sequence with `len` keys: per head those from the first query that sees t0 on.
@@ -67,8 +67,10 @@ __global__ void __launch_bounds__(256, kw_occupancy<D>()) k_key_weights(const Kw
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
   const int col = lane & 31, half = lane >> 5;
   // workgroups in order: piece, key tile, head - the first keys' (the longest) first, heads side by side on different XCDs
-  unsigned bh = blockIdx.x, kt = split_by(bh, p.by_heads), hkv = bh;
-  const int piece = (int)split_by(kt, p.by_kt), b = (int)split_by(hkv, p.by_hkv);
+  unsigned bh = blockIdx.x;
+  const unsigned kt = split_by(bh, p.by_heads);
+  unsigned hkv = bh;
+  const int piece = blockIdx.y, b = (int)split_by(hkv, p.by_hkv);
   const int len = kw_len(p, b), t0 = (int)kt * KW_KEYS;
   if (t0 >= len) return;
   const KwItems it = kw_items(p.flat, p.causal, p.G, p.N, len, t0);
@@ -472,7 +474,7 @@ int kw_params(const sage_attn_key_weights_args* a, KwParams* p, bool need_io) {
     most = std::max(most, c);
   }
   p->key_tiles = (int)kts;
-  p->by_heads = fast_div((unsigned)heads); p->by_hkv = fast_div((unsigned)a->H_kv); p->by_kt = fast_div((unsigned)kts); p->by_n = fast_div((unsigned)a->N);
+  p->by_heads = fast_div((unsigned)heads); p->by_hkv = fast_div((unsigned)a->H_kv); p->by_n = fast_div((unsigned)a->N);
   // As many tiles as give 1024 workgroups, 2 to 16: what a workgroup does before its first tile costs as much as three to six, but
   // with fewer of them the last ones run alone.  Us, tiles of a workgroup: 66 k tiles (8192 causal queries, 32 heads of 128) 4 / 8 / 16 / 32
   // 339 / 306 / 296 / 293, 17 k 103 / 94 / 93 / 97, 9 k (not causal) 52 / 49 / 53 / 60, 1.2 k 24 / 28 / 46 / 64, 96 (2 / 4 / 8) 15 / 19 / 24; of 256
@@ -492,11 +494,12 @@ int kw_params(const sage_attn_key_weights_args* a, KwParams* p, bool need_io) {
     p->piece = (int)std::max(rows > 16 ? 8LL : 4LL, std::min(128LL, heads * tiles / (2 * held)));
     p->key_tiles = (int)((tiles + 4 * p->piece - 1) / (4 * p->piece));
   }
-  if (heads * p->key_tiles * p->pieces > 0x7fffffffLL) return SAGE_ERR_UNSUPPORTED;
+  if (heads * p->key_tiles * 256 > MAX_THREADS || p->pieces > 65535) return SAGE_ERR_UNSUPPORTED;
   return SAGE_OK;
 }
 
-template <int D, bool BF16> hipError_t launch_kw(const KwParams& p, unsigned blocks, hipStream_t s) {
+template <int D, bool BF16> hipError_t launch_kw(const KwParams& p, hipStream_t s) {
+  const dim3 blocks((unsigned)((long long)p.B * p.Hkv * p.key_tiles), (unsigned)p.pieces);
   if (!p.few) k_key_weights<D, BF16><<<blocks, 256, 0, s>>>(p);
   else if (p.G * p.N <= 16) k_key_weights_few<D, BF16, 1><<<blocks, 256, 0, s>>>(p);
   else if (p.G * p.N <= 32) k_key_weights_few<D, BF16, 2><<<blocks, 256, 0, s>>>(p);
@@ -523,11 +526,10 @@ extern "C" int sage_attn_key_weights(const sage_attn_key_weights_args* a) {
   const size_t need = kw_bytes(p);
   if (need > 0 && (!a->workspace || a->workspace_bytes < need || ((uintptr_t)a->workspace & 255u) != 0)) return SAGE_ERR_WORKSPACE;
   const hipStream_t s = (hipStream_t)a->stream;
-  const unsigned blocks = (unsigned)((long long)p.B * p.Hkv * p.key_tiles * p.pieces);
   const bool bf16 = a->dtype == SAGE_DT_BF16;
-  const hipError_t e = a->d == 64 ? (bf16 ? launch_kw<64, true>(p, blocks, s) : launch_kw<64, false>(p, blocks, s))
-                     : a->d == 128 ? (bf16 ? launch_kw<128, true>(p, blocks, s) : launch_kw<128, false>(p, blocks, s))
-                                   : (bf16 ? launch_kw<256, true>(p, blocks, s) : launch_kw<256, false>(p, blocks, s));
+  const hipError_t e = a->d == 64 ? (bf16 ? launch_kw<64, true>(p, s) : launch_kw<64, false>(p, s))
+                     : a->d == 128 ? (bf16 ? launch_kw<128, true>(p, s) : launch_kw<128, false>(p, s))
+                                   : (bf16 ? launch_kw<256, true>(p, s) : launch_kw<256, false>(p, s));
   st = op_status(e);
   if (st != SAGE_OK || p.pieces == 1) return st;
   k_key_weights_sum<<<dim3((unsigned)p.key_tiles, (unsigned)(p.B * p.Hkv)), 256, 0, s>>>(p);

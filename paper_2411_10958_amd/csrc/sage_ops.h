@@ -1,4 +1,4 @@
-// Shared by the operators around attention (sage_rope.hip, sage_attn_shared.hip, sage_cache.hip).
+// Shared by the operators around attention (sage_rope.hip, sage_attn_shared.hip, sage_key_weights.hip, sage_cache.hip).
 #pragma once
 #include "sage_attn_core.h"
 
@@ -10,6 +10,9 @@ inline int op_status(hipError_t e) {
   (void)hipGetLastError();
   return -4;      // SAGE_ERR_HIP
 }
+
+// Most threads of a grid in one of its dimensions: the launch packet counts them in 32 bits.
+constexpr long long MAX_THREADS = 0xffffffffLL;
 
 // Element offset of head h of batch b.
 __device__ __forceinline__ size_t head_offset_of(const TensorMap& m, int b, int h) { return (size_t)b * m.sb + (size_t)h * m.sh; }
@@ -24,6 +27,17 @@ template <bool BF16> __device__ __forceinline__ v16f mfma16(v4i a, v4i b, v16f c
   } else {
     typedef _Float16 v8h __attribute__((ext_vector_type(8)));
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(v8h, a), __builtin_bit_cast(v8h, b), c, 0, 0, 0);
+  }
+}
+
+// The same, 16 x 16 x 32: row or column l % 16, contraction slots 8 (l / 16) + 0..7; accumulator v is row 4 (l / 16) + v, column l % 16.
+template <bool BF16> __device__ __forceinline__ v4f mfma16_small(v4i a, v4i b, v4f c) {
+  if constexpr (BF16) {
+    typedef __bf16 v8b __attribute__((ext_vector_type(8)));
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8b, a), __builtin_bit_cast(v8b, b), c, 0, 0, 0);
+  } else {
+    typedef _Float16 v8h __attribute__((ext_vector_type(8)));
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, a), __builtin_bit_cast(v8h, b), c, 0, 0, 0);
   }
 }
 
@@ -52,17 +66,6 @@ __device__ __forceinline__ unsigned split_by(unsigned& n, const FastDiv& f) {
   const unsigned q = div_by(n, f);
   n -= q * f.d;
   return q;
-}
-
-// The same, 16 x 16 x 32: row or column l % 16, contraction slots 8 (l / 16) + 0..7; accumulator v is row 4 (l / 16) + v, column l % 16.
-template <bool BF16> __device__ __forceinline__ v4f mfma16_small(v4i a, v4i b, v4f c) {
-  if constexpr (BF16) {
-    typedef __bf16 v8b __attribute__((ext_vector_type(8)));
-    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8b, a), __builtin_bit_cast(v8b, b), c, 0, 0, 0);
-  } else {
-    typedef _Float16 v8h __attribute__((ext_vector_type(8)));
-    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, a), __builtin_bit_cast(v8h, b), c, 0, 0, 0);
-  }
 }
 
 // Sum / maximum of a value over the two halves of the wavefront, in both.

@@ -86,11 +86,11 @@ __device__ __forceinline__ void turn(typename Vec<VW>::type (&v)[NV], const floa
   }
 }
 
-// Grid: (units of all tokens / 256, pieces of the heads).  PAST: reads and writes pass the caches by.
+// Grid: (units of all tokens / 256, pieces of the heads, what of the first does not fit a dimension).  PAST: reads and writes pass the caches by.
 template <bool BF16, int VW, bool INTER, bool PAST>
 __global__ void __launch_bounds__(256) k_rope(const RopeParams p) {
   constexpr int NV = vectors<VW, INTER>(), NP = NV * VW / 2;       // vectors and pairs of a thread
-  const long long id = (long long)blockIdx.x * 256 + threadIdx.x;
+  const long long id = ((long long)blockIdx.z * gridDim.x + blockIdx.x) * 256 + threadIdx.x;
   if (id >= p.total) return;
   const long long th = id / p.units, tok = th / p.lanes;
   const int unit = (int)(id - th * p.units), hl = (int)(th - tok * p.lanes);
@@ -262,13 +262,14 @@ extern "C" int sage_rope(const sage_rope_args* a) {
   if (st[0][1] < st[0][2] && a->N > 1) while (p.lanes * 2 * p.units <= 64 && p.lanes * 2 <= a->H) p.lanes *= 2;
   p.total = (long long)a->B * a->N * p.units * p.lanes;
   const long long blocks = (p.total + 255) / 256;
-  if (blocks > 0x7fffffffLL) return SAGE_ERR_UNSUPPORTED;
+  const long long wide = std::min(blocks, 1LL << 22), deep = (blocks + wide - 1) / wide;
+  if (deep > 65535) return SAGE_ERR_UNSUPPORTED;
   // Heads are divided over workgroups only until there are sixteen of these per CU: each pays for the angles again.  (Eight: 2 x 17776
   // tokens of 96 heads of 64 163 us, sixteen 155.)  Heads that lie side by side in one stay together.
   const int heads = p.q.heads + p.k.heads;
   const long long pieces = std::max(1LL, std::min((4096 + blocks - 1) / blocks, (long long)heads / p.lanes));
   p.hchunk = (int)((heads + pieces - 1) / pieces);
-  const dim3 grid((unsigned)blocks, (unsigned)((heads + p.hchunk - 1) / p.hchunk));
+  const dim3 grid((unsigned)wide, (unsigned)((heads + p.hchunk - 1) / p.hchunk), (unsigned)deep);
   const hipStream_t s = (hipStream_t)a->stream;
   if (a->dtype == SAGE_DT_BF16) {
     if (vw == 8) launch<true, 8>(p, inter, past, grid, s); else if (vw == 4) launch<true, 4>(p, inter, false, grid, s); else launch<true, 1>(p, inter, false, grid, s);

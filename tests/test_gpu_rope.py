@@ -59,6 +59,21 @@ def test_more_than_the_caches_hold(d, rot, interleaved, layout, in_place):
         ref.check(name, y, w, bound)
 
 
+def test_more_units_than_a_grid_is_wide():
+    """17 million rows at odd addresses: 2^31 threads and more, elements past 2^32."""
+    pa = _pa()
+    B, N, d = 2, (1 << 23) + 3333, 256
+    buf = torch.empty(B * N * (d + 1), dtype=torch.bfloat16, device="cuda")
+    for i in range(0, buf.numel(), 1 << 28):
+        buf[i:i + (1 << 28)].normal_(generator=_gen(i >> 28))
+    q = buf.view(B, 1, N, d + 1)[..., 1:]
+    f = pa.sage_rope_frequencies(d)
+    y = pa.sage_rope(q, None, f, offset=3)
+    for b, n in ((0, 0), (0, N - 500), (1, 0), (1, N // 2), (1, N - 500)):
+        pos = torch.arange(n, n + 500, device="cuda") + 3
+        ref.check(f"rows {b}, {n}", y[b:b + 1, :, n:n + 500], *ref.rope(q[b:b + 1, :, n:n + 500], f, pos, False, False, 1.0, "HND"))
+
+
 def test_positions():
     pa = _pa()
     g = _gen(3)

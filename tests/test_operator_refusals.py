@@ -110,6 +110,15 @@ def test_cache_evict_room(kw, status):
     assert _status(pa, lib, "sage_cache_evict", EVICT, **kw) == status
 
 
+def test_more_than_a_launch_can_hold():
+    pa, lib = _pa()
+    assert _status(pa, lib, "sage_attn_shared_prefix", SHARED, B=1, H=32, H_kv=8, N=(1 << 19) + 1) == -2
+    assert pa.sage_attn_shared_prefix_workspace_bytes(_args(pa, "sage_attn_shared_prefix", **{**SHARED, **dict(B=1, H=32, H_kv=8, N=(1 << 19) + 1)})) == 0
+    assert pa.sage_attn_shared_prefix_workspace_bytes(_args(pa, "sage_attn_shared_prefix", **{**SHARED, **dict(B=1, H=32, H_kv=8, N=1 << 19)})) > 0
+    assert _status(pa, lib, "sage_attn_key_weights", WEIGHTS, B=1, H=8, H_kv=1, N=1 << 24, N_kv=1 << 24) == -2
+    assert _status(pa, lib, "sage_attn_key_weights", WEIGHTS, B=8000, H=8, H_kv=8, N=70, N_kv=1 << 24) == -2
+
+
 def test_null_arguments():
     pa, lib = _pa()
     for name in ("sage_rope", "sage_attn_shared_prefix", "sage_attn_key_weights", "sage_cache_evict"):
