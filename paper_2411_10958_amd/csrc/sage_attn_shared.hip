@@ -4,7 +4,7 @@
 // product over them are the queries of all sequences and of all query heads of a KV head (B G N rows, G = H / H_kv), and the
 // prefix is read once instead of B times.  A sequence's own keys meet only its own G N rows.  The two parts, and chunks
 // of their keys, are independent workgroups of one launch; each leaves (m, l, O) under its own running maximum (Sec. 2.1, Eq. 1)
-// and a second kernel merges them: O = sum_i 2^(m_i - m) O_i / sum_i 2^(m_i - m) l_i.
+// and a second kernel merges them: O = sum_i 2^(m_i - m) O_i / sum_i 2^(m_i - m) l_i.  (Where there are few keys, a workgroup takes them all.)
 //
 // With few rows this reads the cache and nothing else bounds it, so K and V stay in the 16 bits they are kept in: quantizing them
 // on the way would cost vector instructions for nothing.  P is rounded to the type of V for the second product (half a step, 2^-9
@@ -39,7 +39,7 @@ struct SharedParams {
   float *part_o, *part_ml;       // [partial][row][d], [partial][row][2]: see part_row
   TensorMap qm, pm, om;          // of q and out; of the prefix; of the own caches
   int B, H, Hkv, G, N, P, Nk;
-  int causal;
+  int causal, one;               // one: no key chunks and no merge (ONE)
   float kappa;                   // sm_scale log2(e)
   int Sp, So;                    // key chunks of the prefix and of the own keys
   int rtp, rto;                  // row tiles of the prefix (of B G N rows) and of the own keys (of G N rows)
@@ -59,7 +59,8 @@ __device__ __forceinline__ int own_len(const SharedParams& p, int b) { return p.
 
 template <int D> constexpr int shared_occupancy() { return D == 64 ? 3 : 2; }   // wavefronts per SIMD
 
-template <int D, bool BF16>
+// ONE: a workgroup walks over the whole prefix and then its sequence's own keys, and leaves the output itself (see choose_chunks).
+template <int D, bool BF16, bool ONE>
 __global__ void __launch_bounds__(64 * shared_waves<D>(), shared_occupancy<D>()) k_shared(const SharedParams p) {
   constexpr int NP = D / 8;                       // 16-byte pieces of a row
   constexpr int KS = D / 16;                      // contraction steps of the score product
@@ -76,7 +77,7 @@ __global__ void __launch_bounds__(64 * shared_waves<D>(), shared_occupancy<D>())
 
   // ---- which rows and keys
   unsigned id = blockIdx.x, hkv, b = 0, rt, s;
-  const bool prefix = (int)id < p.n_prefix;
+  const bool prefix = !ONE && (int)id < p.n_prefix;
   if (prefix) {
     // The row tiles of a chunk read the same keys: they are 8 apart, since workgroups go to the 8 XCDs in turn and each has a cache
     // of its own.  (The last chunks, fewer than 8, have a chunk's side by side.)
@@ -100,9 +101,13 @@ __global__ void __launch_bounds__(64 * shared_waves<D>(), shared_occupancy<D>())
   const int GN = p.G * p.N, rows = prefix ? p.B * GN : GN, r0 = (int)rt * ROWS;
   const int nr = min(ROWS, rows - r0);            // rows of this workgroup
   const int nk = prefix ? p.P : own_len(p, (int)b);
-  const int tiles = (nk + SH_KEYS - 1) / SH_KEYS;
-  const int per = prefix ? (int)div_by((unsigned)(tiles + p.Sp - 1), p.by_sp) : (int)div_by((unsigned)(tiles + p.So - 1), p.by_so);
-  const int j0 = min((int)s * per, tiles), j1 = min(j0 + per, tiles);
+  const int tp = ONE ? (p.P + SH_KEYS - 1) / SH_KEYS : 0, tiles = tp + (nk + SH_KEYS - 1) / SH_KEYS;     // tiles of the prefix come first
+  int j0 = 0, j1 = tiles;
+  if constexpr (!ONE) {
+    const int per = prefix ? (int)div_by((unsigned)(tiles + p.Sp - 1), p.by_sp) : (int)div_by((unsigned)(tiles + p.So - 1), p.by_so);
+    j0 = min((int)s * per, tiles);
+    j1 = min(j0 + per, tiles);
+  }
   const int sp = (int)s + (prefix ? 0 : p.Sp);
   const int i0 = prefix ? r0 : (int)b * GN + r0;  // first row in the numbering of part_row
 
@@ -113,7 +118,7 @@ __global__ void __launch_bounds__(64 * shared_waves<D>(), shared_occupancy<D>())
   const int kg = WK == 2 ? wave & 1 : 0, rg = WK == 2 ? wave >> 1 : wave;
   const bool active = rg * 32 < nr;
 
-  if (j0 >= j1) {                                 // no keys: a partial result that the merge skips
+  if (!ONE && j0 >= j1) {                         // no keys: a partial result that the merge skips
     for (int i = t; i < nr; i += 64 * W) {
       float* ml = p.part_ml + part_row(p, sp, (int)hkv, i0 + i) * 2;
       ml[0] = -INFINITY;
@@ -137,10 +142,13 @@ __global__ void __launch_bounds__(64 * shared_waves<D>(), shared_occupancy<D>())
   const bool part_seen = vis_all < nk;            // ... and others that some do
 
   // ---- copies of a tile: rows behind the last key repeat it, so that masked places hold finite values where the keys do
-  const TensorMap& m = prefix ? p.pm : p.om;
+  const TensorMap& m = prefix ? p.pm : p.om;      // (a step from token to token is the same in both)
   const size_t head = head_offset_of(m, (int)b, (int)hkv);
   const char* gk = uniform_ptr(reinterpret_cast<const char*>((prefix ? p.kp : p.ko) + head));
   const char* gv = uniform_ptr(reinterpret_cast<const char*>((prefix ? p.vp : p.vo) + head));
+  const size_t first = ONE ? head_offset_of(p.pm, 0, (int)hkv) : 0;
+  const char* gkp = uniform_ptr(reinterpret_cast<const char*>(p.kp + first));       // (ONE: the prefix's)
+  const char* gvp = uniform_ptr(reinterpret_cast<const char*>(p.vp + first));
   const unsigned lds0 = (unsigned)(size_t)(__attribute__((address_space(3))) char*)&s_kv[0][0];
   const unsigned step = (unsigned)m.sn * 2;       // bytes from token to token
   constexpr int COPIES = TILE / (64 * W);         // of a tile of K (or V), by a wavefront
@@ -156,21 +164,24 @@ __global__ void __launch_bounds__(64 * shared_waves<D>(), shared_occupancy<D>())
   // rows: 30.4 / 34.2).
   const bool once = prefix ? rows <= 64 : p.rto == 1;
   auto copy = [&](int j, int stage) __attribute__((always_inline)) {
+    const bool before = ONE && j < tp;
+    if (!before) j -= tp;
     const size_t at = (size_t)j * SH_KEYS * m.sn * 2;
+    const char *fk = before ? gkp : gk, *fv = before ? gvp : gv;
     const unsigned to = lds0 + (unsigned)(stage * 2 * TILE + wave * 64) * 16;
-    const int last = nk - 1 - j * SH_KEYS;
+    const int last = (before ? p.P : nk) - 1 - j * SH_KEYS;
     if (last >= SH_KEYS - 1) {
 if (once) {
 #pragma unroll
         for (int x = 0; x < COPIES; ++x) {
-          dma_b128_once(gk + at, offs[x], to + x * (W * 1024));
-          dma_b128_once(gv + at, offs[x], to + TILE * 16 + x * (W * 1024));
+          dma_b128_once(fk + at, offs[x], to + x * (W * 1024));
+          dma_b128_once(fv + at, offs[x], to + TILE * 16 + x * (W * 1024));
         }
       } else {
 #pragma unroll
         for (int x = 0; x < COPIES; ++x) {
-          dma_b128(gk + at, offs[x], to + x * (W * 1024));
-          dma_b128(gv + at, offs[x], to + TILE * 16 + x * (W * 1024));
+          dma_b128(fk + at, offs[x], to + x * (W * 1024));
+          dma_b128(fv + at, offs[x], to + TILE * 16 + x * (W * 1024));
         }
       }
     } else {
@@ -178,14 +189,14 @@ if (once) {
       for (int x = 0; x < COPIES; ++x) {
         const int pc = (x * W + wave) * 64 + lane, r = pc / NP, c = (pc % NP) ^ swizzle<D>(r);
         const unsigned off = (unsigned)min(r, last) * step + (unsigned)c * 16;
-        dma_b128(gk + at, off, to + x * (W * 1024));
-        dma_b128(gv + at, off, to + TILE * 16 + x * (W * 1024));
+        dma_b128(fk + at, off, to + x * (W * 1024));
+        dma_b128(fv + at, off, to + TILE * 16 + x * (W * 1024));
       }
     }
   };
   // The first tile is on its way while the queries come; the wait for them is one for it too, since loads are counted in order.  From
   // there on two tiles are in flight.
-  copy(j0, 0);
+  if (!ONE || j0 < j1) copy(j0, 0);
 #pragma unroll
   for (int st = 0; st < KS; ++st)
 #pragma unroll
@@ -240,7 +251,7 @@ if (once) {
   const unsigned k_at = (unsigned)row_piece<D>(kr, half) * 16, v_at = ((unsigned)row_piece<D>(vr, vc >> 3) * 16 + (vc & 4) * 2) ^ (kg * (CT / 2) * 64);
 
   // NS times 32 keys of a tile, from the sub0-th on: scores, weights and their product with V
-  auto tile_keys = [&](auto ns, unsigned stage0, int tile0, int sub0) __attribute__((always_inline)) {
+  auto tile_keys = [&](auto ns, unsigned stage0, int tile0, int sub0, int vis, int vis_all) __attribute__((always_inline)) {
     constexpr int NS = decltype(ns)::value;
     const int key0 = tile0 + 32 * sub0;
     // S^T = K Q^T: with the rows as above, half h of the lanes has keys 8h + 0..7 and 16 + 8h + 0..7 of its query, in the order in
@@ -315,10 +326,13 @@ if (once) {
     __builtin_amdgcn_s_barrier();                 // tile j is there
     asm volatile("" ::: "memory");
     const unsigned at = lds0 + (unsigned)stage * (2 * TILE * 16);
-    if (part_seen && (j + 1) * SH_KEYS > vis_all) take_out(stage);
+    const bool before = ONE && j < tp;
+    const int tile0 = (before ? j : j - tp) * SH_KEYS, end = before ? p.P : nk;
+    const int seen = before ? p.P : vis, seen_all = before ? p.P : vis_all;
+    if (!before && part_seen && tile0 + SH_KEYS > vis_all) take_out(stage);
     if (active) {
-      if (D < 256 && WK == 1 && j * SH_KEYS + 32 < nk) tile_keys(std::integral_constant<int, 2>{}, at, j * SH_KEYS, 0);
-      else for (int sub = kg; sub < 2 && j * SH_KEYS + 32 * sub < nk; sub += WK) tile_keys(std::integral_constant<int, 1>{}, at, j * SH_KEYS, sub);
+      if (D < 256 && WK == 1 && tile0 + 32 < end) tile_keys(std::integral_constant<int, 2>{}, at, tile0, 0, seen, seen_all);
+      else for (int sub = kg; sub < 2 && tile0 + 32 * sub < end; sub += WK) tile_keys(std::integral_constant<int, 1>{}, at, tile0, sub, seen, seen_all);
     }
     if (j + 2 < j1) {                             // the next tile but one takes this one's place when all have read it
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -365,9 +379,9 @@ if (once) {
   if (!active || rg * 32 + col >= nr) return;
   const int mine = kg * (CT / 2);                 // channel tile of o[c]: c ^ mine; mine to write are CT / 2 of them, or all
   if (taken_out) {
-    const int to = min(vis, j1 * SH_KEYS);
+    const int to = min(vis, (j1 - tp) * SH_KEYS);
 #pragma unroll 1
-    for (int k = max(vis_all, j0 * SH_KEYS) / SH_KEYS * SH_KEYS; k < to; ++k) {      // (whole tiles were looked at)
+    for (int k = max(vis_all, (j0 - tp) * SH_KEYS) / SH_KEYS * SH_KEYS; k < to; ++k) {      // (whole tiles were looked at)
       const char* v = gv + (size_t)k * step + 8 * half;
 #pragma unroll
       for (int c = 0; c < CT; ++c)
@@ -379,6 +393,22 @@ if (once) {
           for (int e = 0; e < 4; ++e) o[c][4 * g + e] += not_finite<BF16>(y[e]) ? load16<BF16>((unsigned short)y[e]) : 0.0f;
         }
     }
+  }
+  if constexpr (ONE) {
+    const bool none = mx == -INFINITY && l == 0.0f;      // no key at all: zeros
+    const float inv = none ? 0.0f : __fdiv_rn(1.0f, l);
+    if (p.lse && half == 0 && kg == 0)
+      p.lse[((size_t)rb * p.H + hkv * p.G + rh) * p.N + rn] = none ? -INFINITY : LN2 * (mx + __builtin_amdgcn_logf(l));
+    unsigned short* y = p.out + qrow + 4 * half;
+#pragma unroll
+    for (int c = 0; c < CT; ++c)
+      if (c < CT / 2 || WK == 1) {
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+          *reinterpret_cast<uint2*>(y + 32 * (c ^ mine) + 8 * g) = make_uint2(pack16x2<BF16>(o[c][4 * g] * inv, o[c][4 * g + 1] * inv),
+                                                                             pack16x2<BF16>(o[c][4 * g + 2] * inv, o[c][4 * g + 3] * inv));
+      }
+    return;
   }
   const size_t pr = part_row(p, sp, (int)hkv, i);
   if (half == 0 && kg == 0) {
@@ -476,6 +506,14 @@ __global__ void __launch_bounds__(256) k_shared_merge(const SharedParams p) {
 // 158; 1 of 300 over 32768 32.4 / 32.1; 4 of 2000 over 100000 84 / 76; 32 of 3000 over 200 55.9 / 54.3.
 void choose_chunks(SharedParams* p, int d, long long rows) {
   const long long tp = (p->P + SH_KEYS - 1) / SH_KEYS, to = (p->Nk + SH_KEYS - 1) / SH_KEYS;
+  // So few tiles that a workgroup is over them before a second kernel could start: one launch, in which each sequence reads the prefix for
+  // itself.  (Us, chunks / this: 4 heads of 300 + 50 keys of 64 channels 17.7 / 15.1, 128 of 380 + 128 of 128 16.6 / 15.2, of 500 + 250 16.7 /
+  // 19.6; of 256 channels 128 of 180 + 60 18.2 / 14.9, of 300 + 50 18.2 / 18.5; 512 of 60 + 60 29.6 / 19.5.)
+  p->one = tp + to <= 2 + 640 / d;
+  if (p->one) {
+    p->Sp = p->So = 0;
+    return;
+  }
   const long long prefix = (long long)p->Hkv * p->rtp * tp, own = (long long)p->B * p->Hkv * p->rto * to;
   const long long places = 256LL * (d == 64 ? 3 : d == 128 ? 2 : 1), least = 512 / d;
   long long share = (prefix + own + places - 1) / places;
@@ -527,9 +565,13 @@ int shared_params(const sage_attn_shared_prefix_args* a, SharedParams* p, bool n
 size_t part_rows(const SharedParams& p) { return (size_t)(p.Sp + p.So) * p.Hkv * p.B * p.G * p.N; }
 
 template <int D, bool BF16> hipError_t launch_shared(const SharedParams& p, hipStream_t s) {
+  if (p.one) {
+    k_shared<D, BF16, true><<<(unsigned)(p.B * p.Hkv * p.rto), 64 * shared_waves<D>(), 0, s>>>(p);
+    return hipGetLastError();
+  }
   const long long own = (long long)p.So * p.B * p.Hkv * p.rto, blocks = p.n_prefix + own;
   if (blocks > 0) {
-    k_shared<D, BF16><<<(unsigned)blocks, 64 * shared_waves<D>(), 0, s>>>(p);
+    k_shared<D, BF16, false><<<(unsigned)blocks, 64 * shared_waves<D>(), 0, s>>>(p);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }

@@ -26,6 +26,7 @@ __device__ __forceinline__ unsigned order_of(float w) {
 }
 
 constexpr int SEL_THREADS = 1024, SEL_WAVES = SEL_THREADS / 64;
+constexpr int SMALL_K = 4, SMALL_ROWS = 32768;        // of the kernel that copies rows too: 64s of a wavefront, elements of K for a workgroup
 constexpr int DIGIT = 11, BINS = 1 << DIGIT;      // three digits of 11, 11 and 10 bits
 
 // Which tokens stay, one workgroup per sequence and KV head: the m-th largest weight between sink and recent, found digit by digit by
@@ -35,8 +36,7 @@ constexpr int DIGIT = 11, BINS = 1 << DIGIT;      // three digits of 11, 11 and 
 // 111 (51 with 8-bit digits and weights read from memory in each pass; counts in four copies changed nothing).  (The first digit is sign, exponent and two bits: with 8-bit digits a wavefront's
 // counts would fall on a dozen addresses.)  What a stretch has behind the last weight counts as less than any and comes after
 // all, so it is never taken: n > m.
-template <int K>
-__global__ void __launch_bounds__(SEL_THREADS) k_evict_select(const EvictParams p) {
+template <int K> __device__ __forceinline__ int select_tokens(const EvictParams& p) {
   __shared__ unsigned s_hist[BINS];
   __shared__ unsigned s_wave[SEL_WAVES], s_pick[2];
   __shared__ unsigned s_gt[SEL_WAVES], s_eq[SEL_WAVES];
@@ -48,7 +48,7 @@ __global__ void __launch_bounds__(SEL_THREADS) k_evict_select(const EvictParams 
   if (t == 0 && blockIdx.x % p.Hkv == 0) p.lens_out[b] = min(len, p.keep);
   if (len <= p.keep) {
     for (int i = t; i < len; i += SEL_THREADS) kept[i] = i;
-    return;
+    return len;
   }
   const int c0 = p.sink, n = len - p.recent - p.sink, m = p.keep - p.sink - p.recent;     // n > m >= 0 tokens to choose from
   constexpr int STEP = K > 0 ? K : 8;             // 64s that a wavefront has at a time
@@ -65,7 +65,7 @@ __global__ void __launch_bounds__(SEL_THREADS) k_evict_select(const EvictParams 
   if (K > 0) load(i0);
   for (int i = t; i < p.sink; i += SEL_THREADS) kept[i] = i;
   for (int i = t; i < p.recent; i += SEL_THREADS) kept[p.keep - p.recent + i] = len - p.recent + i;
-  if (m == 0) return;
+  if (m == 0) return p.keep;
   // f(weights in order, first token) for the 64s of my stretch
   auto each = [&](auto f) __attribute__((always_inline)) {
     for (int i = i0; i < i1; i += 64 * STEP) {
@@ -130,6 +130,39 @@ __global__ void __launch_bounds__(SEL_THREADS) k_evict_select(const EvictParams 
     }
     above += (unsigned)__popcll(bg);
   });
+  return p.keep;
+}
+
+template <int K> __global__ void __launch_bounds__(SEL_THREADS) k_evict_select(const EvictParams p) { select_tokens<K>(p); }
+
+// The same, and the rows too: one launch, where a row's workgroup has at most 4096 weights and 64 KB of K and as much of V (us, two launches /
+// this: 4 heads cut to 256 tokens of 64 14.7 / 11.5, of 128 14.2 / 11.3; 32 heads cut to 1000 of 64, 128 KB, 15.0 / 19.5).
+template <int D> __global__ void __launch_bounds__(SEL_THREADS) k_evict_small(const EvictParams p) {
+  constexpr int P = D / 8, U = 4;                 // pieces of a row, those in flight
+  const int there = select_tokens<SMALL_K>(p);
+  __syncthreads();                                // (the indices, which this workgroup wrote, are read from memory)
+  const int* kept = p.kept + (size_t)blockIdx.x * p.keep;
+  const size_t hi = head_offset(p.in, blockIdx.x), ho = head_offset(p.out, blockIdx.x);
+  if (p.w_out)
+    for (int i = threadIdx.x; i < there; i += SEL_THREADS) p.w_out[(size_t)blockIdx.x * p.room + i] = p.w[(size_t)blockIdx.x * p.N + kept[i]];
+  for (int i = threadIdx.x; i < there * P; i += SEL_THREADS * U) {
+    v4i a[U], x[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int at = min(i + u * SEL_THREADS, there * P - 1);
+      const size_t from = row_offset(p.in, hi, kept[at / P]) + 8 * (at % P);
+      a[u] = *reinterpret_cast<const v4i*>(p.k + from);
+      x[u] = *reinterpret_cast<const v4i*>(p.v + from);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int at = i + u * SEL_THREADS;
+      if (at >= there * P) break;
+      const size_t to = row_offset(p.out, ho, at / P) + 8 * (at % P);
+      *reinterpret_cast<v4i*>(p.k_out + to) = a[u];
+      *reinterpret_cast<v4i*>(p.v_out + to) = x[u];
+    }
+  }
 }
 
 // The rows of the kept tokens, and their weights: a thread moves 16 bytes of K and of V of GU tokens, the first of a row also its
@@ -224,6 +257,12 @@ extern "C" int sage_cache_evict(const sage_cache_evict_args* a) {
   p.out = make_tensor_map(nhd, a->H_kv, room, a->d);
   const hipStream_t s = (hipStream_t)a->stream;
   const int most = a->N_kv - a->sink - a->recent;       // weights to choose from
+  if (most <= SMALL_K * 64 * SEL_WAVES && (long long)std::min(a->N_keep, a->N_kv) * a->d <= SMALL_ROWS) {
+    if (a->d == 64) k_evict_small<64><<<(unsigned)heads, SEL_THREADS, 0, s>>>(p);
+    else if (a->d == 128) k_evict_small<128><<<(unsigned)heads, SEL_THREADS, 0, s>>>(p);
+    else k_evict_small<256><<<(unsigned)heads, SEL_THREADS, 0, s>>>(p);
+    return op_status(hipGetLastError());
+  }
   if (most <= 4 * SEL_THREADS) k_evict_select<4><<<(unsigned)heads, SEL_THREADS, 0, s>>>(p);
   else if (most <= 16 * SEL_THREADS) k_evict_select<16><<<(unsigned)heads, SEL_THREADS, 0, s>>>(p);
   else if (most <= 32 * SEL_THREADS) k_evict_select<32><<<(unsigned)heads, SEL_THREADS, 0, s>>>(p);

@@ -39,7 +39,8 @@ def _check(pa, x, lens=None, causal=True, sm_scale=0.0, layout="HND", **kw):
 
 @pytest.mark.parametrize("d", [64, 128, 256])
 @pytest.mark.parametrize("B,H,Hkv,N,P,Nk", [(1, 1, 1, 1, 1, 1), (1, 2, 1, 1, 0, 64), (2, 2, 2, 1, 64, 0), (3, 8, 2, 1, 65, 63), (2, 4, 4, 5, 130, 65),
-                                            (5, 8, 1, 3, 1000, 200), (2, 6, 2, 33, 257, 129), (3, 8, 1, 40, 333, 700)])
+                                            (5, 8, 1, 3, 1000, 200), (2, 6, 2, 33, 257, 129), (3, 8, 1, 40, 333, 700), (2, 2, 2, 1, 900, 0), (3, 8, 2, 1, 0, 900),
+                                            (2, 8, 1, 40, 100, 60)])
 def test_sizes(B, H, Hkv, N, P, Nk, d):
     pa = _pa()
     dt, layout = (torch.bfloat16, "HND") if (B + N + d // 64) % 2 else (torch.float16, "NHD")
@@ -60,18 +61,20 @@ def test_rows_of_the_prefix_around_the_tiles(rows):
     _check(pa, _inputs(B, 2 * G, 2, 1, 777, 100, 128, torch.bfloat16, "HND", seed=B))
 
 
-def test_no_keys_at_all_and_lengths_out_of_range():
+@pytest.mark.parametrize("Nk", [70, 990])
+def test_no_keys_at_all_and_lengths_out_of_range(Nk):
     pa = _pa()
-    x = _inputs(4, 4, 2, 3, 0, 70, 64, torch.bfloat16, "HND")
+    x = _inputs(4, 4, 2, 3, 0, Nk, 64, torch.bfloat16, "HND")
     lens = torch.tensor([0, -5, 1000, 2], dtype=torch.int32, device="cuda")
     out, lse = _check(pa, x, lens=lens)
     assert (out[:2] == 0).all() and (lse[:2] == -math.inf).all()
 
 
-def test_what_stands_behind_a_length_is_not_read():
+@pytest.mark.parametrize("P", [50, 1000])
+def test_what_stands_behind_a_length_is_not_read(P):
     pa = _pa()
     for layout in ("HND", "NHD"):
-        q, kp, vp, k, v = _inputs(3, 4, 2, 2, 50, 190, 128, torch.bfloat16, layout)
+        q, kp, vp, k, v = _inputs(3, 4, 2, 2, P, 190, 128, torch.bfloat16, layout)
         lens = torch.tensor([0, 65, 100], dtype=torch.int32, device="cuda")
         want = _check(pa, (q, kp, vp, k, v), lens=lens, layout=layout)
         for b in range(3):
@@ -81,11 +84,12 @@ def test_what_stands_behind_a_length_is_not_read():
         assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
 
 
-def test_large_scores_and_values_that_are_not_numbers():
+@pytest.mark.parametrize("P", [300, 1000])
+def test_large_scores_and_values_that_are_not_numbers(P):
     pa = _pa()
-    x = _inputs(2, 4, 2, 1, 300, 100, 128, torch.bfloat16, "HND", spread=60.0)             # a few keys take it all
+    x = _inputs(2, 4, 2, 1, P, 100, 128, torch.bfloat16, "HND", spread=60.0)             # a few keys take it all
     _check(pa, x)
-    q, kp, vp, k, v = _inputs(2, 4, 2, 1, 300, 100, 128, torch.bfloat16, "HND")
+    q, kp, vp, k, v = _inputs(2, 4, 2, 1, P, 100, 128, torch.bfloat16, "HND")
     clean = pa.sage_attn_shared_prefix(q, kp, vp, k, v, return_lse=True)
     q[0, 1] = math.nan                       # one query: its row and no other
     k[1, 1, 7, 3] = math.nan                 # one key of one sequence: its group's rows
@@ -96,11 +100,12 @@ def test_large_scores_and_values_that_are_not_numbers():
     assert torch.equal(out[~bad], clean[0][~bad]) and torch.equal(lse[~bad], clean[1][~bad])
 
 
+@pytest.mark.parametrize("P", [70, 1000])
 @pytest.mark.parametrize("d,H,N,Nk", [(64, 4, 2, 100), (128, 2, 5, 130), (128, 8, 40, 200), (256, 4, 40, 90), (256, 2, 3, 64)])
-def test_what_a_later_token_holds_does_not_reach_an_earlier_query(d, H, N, Nk):
+def test_what_a_later_token_holds_does_not_reach_an_earlier_query(d, H, N, Nk, P):
     """Keys and values of the chunk's own tokens that are not finite: queries before them have what they had, to the bit."""
     pa = _pa()
-    q, kp, vp, k, v = _inputs(2, H, 2, N, 70, Nk, d, torch.float16 if d == 64 else torch.bfloat16, "HND", seed=d)
+    q, kp, vp, k, v = _inputs(2, H, 2, N, P, Nk, d, torch.float16 if d == 64 else torch.bfloat16, "HND", seed=d)
     lens = torch.tensor([Nk, Nk - 3], dtype=torch.int32, device="cuda")
     clean = pa.sage_attn_shared_prefix(q, kp, vp, k, v, kv_lens=lens, return_lse=True)
     r = N // 2                                  # the token of query r of sequence 1: keys from there on are odd

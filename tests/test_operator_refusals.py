@@ -69,8 +69,9 @@ def test_shared_prefix(kw, status):
 def test_shared_prefix_workspace():
     pa, _ = _pa()
     size = lambda **kw: pa.sage_attn_shared_prefix_workspace_bytes(_args(pa, "sage_attn_shared_prefix", **{**SHARED, **kw}))
-    assert size() % 256 == 0 and size() >= 2 * 2 * 4 * 130 * 4         # a prefix and an own partial result per row at least
-    assert size(N_prefix=0) > 0 and size(N_kv=0) > 0
+    long = dict(N_prefix=5000, N_kv=700)
+    assert size(**long) % 256 == 0 and size(**long) >= 2 * 2 * 4 * 130 * 4         # a prefix and an own partial result per row at least
+    assert size() > 0 and size(N_prefix=0) > 0 and size(N_kv=0) > 0
 
 
 WEIGHTS = dict(q=P, k=P, lse=P, weights=P, B=2, H=4, H_kv=2, N=1, N_kv=500, d=128, dtype=1)
