@@ -355,11 +355,11 @@ typedef struct sage_attn_shared_prefix_args {
   int causal;
   float sm_scale;           /* <= 0 means 1/sqrt(d) */
   int dtype, layout;
-  void* workspace;          /* device, 256-byte aligned */
+  void* workspace;          /* device, 256-byte aligned; may be NULL where the size is 0 */
   size_t workspace_bytes;
   void* stream;
 } sage_attn_shared_prefix_args;
-size_t sage_attn_shared_prefix_workspace_bytes(const sage_attn_shared_prefix_args* args);   /* 0 if the arguments are invalid */
+size_t sage_attn_shared_prefix_workspace_bytes(const sage_attn_shared_prefix_args* args);   /* 0: none is needed (few keys), or the arguments are invalid */
 int sage_attn_shared_prefix(const sage_attn_shared_prefix_args* args);
 
 /* The attention weight that each key has received from N queries of the heads that read it:

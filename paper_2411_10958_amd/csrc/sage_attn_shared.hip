@@ -563,6 +563,9 @@ int shared_params(const sage_attn_shared_prefix_args* a, SharedParams* p, bool n
 }
 
 size_t part_rows(const SharedParams& p) { return (size_t)(p.Sp + p.So) * p.Hkv * p.B * p.G * p.N; }
+size_t shared_bytes(const SharedParams& p, int d) {
+  return align256(part_rows(p) * 2 * sizeof(float)) + align256(part_rows(p) * d * sizeof(float));
+}
 
 template <int D, bool BF16> hipError_t launch_shared(const SharedParams& p, hipStream_t s) {
   if (p.one) {
@@ -588,16 +591,15 @@ using namespace sage;
 extern "C" size_t sage_attn_shared_prefix_workspace_bytes(const sage_attn_shared_prefix_args* a) {
   SharedParams p;
   if (shared_params(a, &p, false) != SAGE_OK) return 0;
-  const size_t rows = part_rows(p);
-  return align256(align256(rows * 2 * sizeof(float)) + rows * a->d * sizeof(float)) + 256;
+  return shared_bytes(p, a->d);
 }
 
 extern "C" int sage_attn_shared_prefix(const sage_attn_shared_prefix_args* a) {
   SharedParams p;
   int st = shared_params(a, &p, true);
   if (st != SAGE_OK) return st;
-  if (!a->workspace || a->workspace_bytes < sage_attn_shared_prefix_workspace_bytes(a) || ((uintptr_t)a->workspace & 255u) != 0)
-    return SAGE_ERR_WORKSPACE;
+  const size_t need = shared_bytes(p, a->d);
+  if (need > 0 && (!a->workspace || a->workspace_bytes < need || ((uintptr_t)a->workspace & 255u) != 0)) return SAGE_ERR_WORKSPACE;
   p.part_ml = (float*)a->workspace;
   p.part_o = (float*)((char*)a->workspace + align256(part_rows(p) * 2 * sizeof(float)));
   const hipStream_t s = (hipStream_t)a->stream;

@@ -57,7 +57,7 @@ SHARED = dict(q=P, k_prefix=P, v_prefix=P, k=P, v=P, out=P, B=2, H=4, H_kv=2, N=
     (dict(kv_lens=P + 2), -1), (dict(lse=P + 1), -1), (dict(B=0), -1), (dict(H=3), -1), (dict(H_kv=0), -1), (dict(N=0), -1), (dict(N_prefix=-1), -1), (dict(N_kv=-1), -1),
     (dict(d=96), -2), (dict(dtype=5), -2), (dict(layout=-1), -2), (dict(N=(1 << 24) + 1), -2), (dict(N_prefix=(1 << 24) + 1), -2), (dict(N_kv=(1 << 24) + 1), -2),
     (dict(B=40000, H=2), -2), (dict(N=1 << 24, B=100), -2),
-    (dict(workspace=0), -3), (dict(workspace_bytes=16), -3), (dict(workspace=P + 16), -3),
+    (dict(workspace=0, N_prefix=5000), -3), (dict(workspace_bytes=16, N_prefix=5000), -3), (dict(workspace=P + 16, N_prefix=5000), -3),
 ])
 def test_shared_prefix(kw, status):
     pa, lib = _pa()
@@ -71,7 +71,7 @@ def test_shared_prefix_workspace():
     size = lambda **kw: pa.sage_attn_shared_prefix_workspace_bytes(_args(pa, "sage_attn_shared_prefix", **{**SHARED, **kw}))
     long = dict(N_prefix=5000, N_kv=700)
     assert size(**long) % 256 == 0 and size(**long) >= 2 * 2 * 4 * 130 * 4         # a prefix and an own partial result per row at least
-    assert size() > 0 and size(N_prefix=0) > 0 and size(N_kv=0) > 0
+    assert size(**{**long, "N_prefix": 0}) > 0 and size(**{**long, "N_kv": 0}) > 0 and size(N_prefix=0) == size() == 0      # (few keys: none)
 
 
 WEIGHTS = dict(q=P, k=P, lse=P, weights=P, B=2, H=4, H_kv=2, N=1, N_kv=500, d=128, dtype=1)
@@ -114,8 +114,8 @@ def test_cache_evict_room(kw, status):
 def test_more_than_a_launch_can_hold():
     pa, lib = _pa()
     assert _status(pa, lib, "sage_attn_shared_prefix", SHARED, B=1, H=32, H_kv=8, N=(1 << 19) + 1) == -2
-    assert pa.sage_attn_shared_prefix_workspace_bytes(_args(pa, "sage_attn_shared_prefix", **{**SHARED, **dict(B=1, H=32, H_kv=8, N=(1 << 19) + 1)})) == 0
-    assert pa.sage_attn_shared_prefix_workspace_bytes(_args(pa, "sage_attn_shared_prefix", **{**SHARED, **dict(B=1, H=32, H_kv=8, N=1 << 19)})) > 0
+    size = lambda n: pa.sage_attn_shared_prefix_workspace_bytes(_args(pa, "sage_attn_shared_prefix", **{**SHARED, **dict(B=1, H=32, H_kv=8, N=n, N_prefix=5000)}))
+    assert size((1 << 19) + 1) == 0 and size(1 << 19) > 0
     assert _status(pa, lib, "sage_attn_key_weights", WEIGHTS, B=1, H=8, H_kv=1, N=1 << 24, N_kv=1 << 24) == -2
     assert _status(pa, lib, "sage_attn_key_weights", WEIGHTS, B=8000, H=8, H_kv=8, N=70, N_kv=1 << 24) == -2
 
