@@ -480,6 +480,9 @@ int kw_params(const sage_attn_key_weights_args* a, KwParams* p, bool need_io) {
   // 339 / 306 / 296 / 293, 17 k 103 / 94 / 93 / 97, 9 k (not causal) 52 / 49 / 53 / 60, 1.2 k 24 / 28 / 46 / 64, 96 (2 / 4 / 8) 15 / 19 / 24; of 256
   // channels 8 k 73 / 69 / 73; of 64 33 k 134 / 119 / 116 / 120.
   p->piece = (int)std::min<long long>(std::min(most, KW_PIECE), std::max(2LL, (heads * all + 1023) / 1024));
+  // A few are not divided, for then nothing has to be added up.  (Us, divided / not: 3 tiles on 4 heads of 64 channels 15.0 / 10.9, of 128
+  // 14.7 / 13.3, of 256 17.5 / 18.5; 4 tiles 14.6 / 12.8, 15.0 / 15.8, 18.1 / 22.4.)
+  if (most * (a->d + 64) <= 576) p->piece = most;
   p->pieces = (most + p->piece - 1) / p->piece;
   // Few rows; more than 32 only from 64 k keys on, because every wavefront has all of them to read first (us, tiles of queries / few rows: 48
   // rows of 128 channels on 128 caches of 16000 keys 87 / 73, on 8 of 9000 11.7 / 10.9, on 8 of 4000 9.2 / 10.6).  Its key tiles: as
