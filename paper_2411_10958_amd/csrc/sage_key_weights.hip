@@ -31,7 +31,7 @@ struct KwParams {
   int causal, flat;              // flat: tiles run over the G N queries of a group, else over the N of each head
   float kappa;
   int key_tiles, pieces, piece;  // most pieces of a key tile, query tiles of a piece
-  FastDiv by_heads, by_hkv, by_n;      // B H_kv, H_kv, N
+  FastDiv by_heads, by_hkv, by_kt, by_n;      // B H_kv, H_kv, key_tiles, N
 };
 
 // Query tiles of the keys t0 .. t0 + 255 of a sequence with `len` keys: per head those from the first query that sees t0 on.
@@ -53,6 +53,8 @@ __host__ __device__ __forceinline__ KwItems kw_items(int flat, int causal, int G
 
 __device__ __forceinline__ int kw_len(const KwParams& p, int b) { return p.lens ? min(max(p.lens[b], 0), p.Nk) : p.Nk; }
 
+constexpr long long WIDE = 1 << 22;       // workgroups in the first dimension of a grid: more are in the second
+
 // Wavefronts per SIMD that registers and LDS are cut for.
 template <int D> constexpr int kw_occupancy() { return D == 256 ? 2 : 3; }
 
@@ -67,12 +69,10 @@ __global__ void __launch_bounds__(256, kw_occupancy<D>()) k_key_weights(const Kw
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
   const int col = lane & 31, half = lane >> 5;
   // workgroups in order: piece, key tile, head - the first keys' (the longest) first, heads side by side on different XCDs
-  unsigned bh = blockIdx.x;
-  const unsigned kt = split_by(bh, p.by_heads);
-  unsigned hkv = bh;
-  const int piece = blockIdx.y, b = (int)split_by(hkv, p.by_hkv);
+  unsigned bh = blockIdx.y * gridDim.x + blockIdx.x, kt = split_by(bh, p.by_heads), hkv = bh;
+  const int piece = (int)split_by(kt, p.by_kt), b = (int)split_by(hkv, p.by_hkv);
   const int len = kw_len(p, b), t0 = (int)kt * KW_KEYS;
-  if (t0 >= len) return;
+  if (piece >= p.pieces || t0 >= len) return;
   const KwItems it = kw_items(p.flat, p.causal, p.G, p.N, len, t0);
   const int used = (it.count + p.piece - 1) / p.piece, each = used > 0 ? (it.count + used - 1) / used : 0;     // pieces of this key tile, all of a length
   const int i0 = min(piece * each, it.count), i1 = min(i0 + each, it.count);
@@ -474,7 +474,7 @@ int kw_params(const sage_attn_key_weights_args* a, KwParams* p, bool need_io) {
     most = std::max(most, c);
   }
   p->key_tiles = (int)kts;
-  p->by_heads = fast_div((unsigned)heads); p->by_hkv = fast_div((unsigned)a->H_kv); p->by_n = fast_div((unsigned)a->N);
+  p->by_heads = fast_div((unsigned)heads); p->by_hkv = fast_div((unsigned)a->H_kv); p->by_kt = fast_div((unsigned)kts); p->by_n = fast_div((unsigned)a->N);
   // As many tiles as give 1024 workgroups, 2 to 16: what a workgroup does before its first tile costs as much as three to six, but
   // with fewer of them the last ones run alone.  Us, tiles of a workgroup: 66 k tiles (8192 causal queries, 32 heads of 128) 4 / 8 / 16 / 32
   // 339 / 306 / 296 / 293, 17 k 103 / 94 / 93 / 97, 9 k (not causal) 52 / 49 / 53 / 60, 1.2 k 24 / 28 / 46 / 64, 96 (2 / 4 / 8) 15 / 19 / 24; of 256
@@ -497,12 +497,13 @@ int kw_params(const sage_attn_key_weights_args* a, KwParams* p, bool need_io) {
     p->piece = (int)std::max(rows > 16 ? 8LL : 4LL, std::min(128LL, heads * tiles / (2 * held)));
     p->key_tiles = (int)((tiles + 4 * p->piece - 1) / (4 * p->piece));
   }
-  if (heads * p->key_tiles * 256 > MAX_THREADS || p->pieces > 65535) return SAGE_ERR_UNSUPPORTED;
+  if (heads * p->key_tiles * p->pieces > 0x7fffffffLL - WIDE || (p->few && heads * p->key_tiles > WIDE)) return SAGE_ERR_UNSUPPORTED;
   return SAGE_OK;
 }
 
 template <int D, bool BF16> hipError_t launch_kw(const KwParams& p, hipStream_t s) {
-  const dim3 blocks((unsigned)((long long)p.B * p.Hkv * p.key_tiles), (unsigned)p.pieces);
+  const long long all = (long long)p.B * p.Hkv * p.key_tiles * p.pieces;
+  const dim3 blocks((unsigned)std::min(all, WIDE), (unsigned)((all + WIDE - 1) / WIDE));
   if (!p.few) k_key_weights<D, BF16><<<blocks, 256, 0, s>>>(p);
   else if (p.G * p.N <= 16) k_key_weights_few<D, BF16, 1><<<blocks, 256, 0, s>>>(p);
   else if (p.G * p.N <= 32) k_key_weights_few<D, BF16, 2><<<blocks, 256, 0, s>>>(p);
