@@ -73,6 +73,22 @@ def test_steps_on_long_caches(G, N, d):
         _check(pa, _inputs(4, G, 1, N, 33001, d, dt, layout, causal, lens), lens=lens, causal=causal, layout=layout, added=added)
 
 
+def test_more_workgroups_than_a_grid_is_wide():
+    """64 heads of 140001 queries: over 4 million workgroups; some of the keys."""
+    pa = _pa()
+    H, N, d = 64, 140001, 64
+    g = torch.Generator(device="cuda")
+    g.manual_seed(1)
+    q, k = (torch.randn((1, H, N, d), generator=g, device="cuda").half() for _ in range(2))
+    lse = torch.rand((1, H, N), generator=g, device="cuda") + 11.0
+    got = pa.sage_attn_key_weights(q, k, lse, causal=False)
+    at = torch.tensor([0, 1, 255, 256, 70000, 139775, 139776, 140000], device="cuda")
+    for h in (0, 31, 63):
+        x = (q[:, h:h + 1], k[:, h:h + 1, at], lse[:, h:h + 1])
+        want, bound = ref.key_weights(*x, None, torch.zeros((1, 1, 8), device="cuda"), None, False, 0.0, "HND")
+        ref.check(f"head {h}", got[:, h:h + 1, at], want, bound)
+
+
 def test_rows_without_keys_and_lengths_out_of_range():
     pa = _pa()
     lens = torch.tensor([0, -3, 5000, 1], dtype=torch.int32, device="cuda")
