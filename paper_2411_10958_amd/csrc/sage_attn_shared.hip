@@ -265,7 +265,7 @@ if (once) {
 #pragma unroll
     for (int st = 0; st < KS; ++st)
 #pragma unroll
-      for (int y = 0; y < NS; ++y) sc[y] = mfma16<BF16>(*(lds_v4i)((ka ^ (32 * st)) + 32 * y * ROW), q[st], sc[y]);
+      for (int y = 0; y < NS; ++y) sc[y] = mfma16<BF16>(*(lds_v4i)(uintptr_t)((ka ^ (32 * st)) + 32 * y * ROW), q[st], sc[y]);
     if (key0 + 32 * NS > vis_all) {
 #pragma unroll
       for (int y = 0; y < NS; ++y)
@@ -310,8 +310,8 @@ if (once) {
 #pragma unroll
         for (int c = 0; c < CT; ++c) {
           const unsigned rows = (32 * y + 16 * ks) * ROW;
-          const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s)((va ^ (64 * c)) + rows));
-          const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s)((va ^ (64 * c + 16)) + rows + 4 * ROW));
+          const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s)(uintptr_t)((va ^ (64 * c)) + rows));
+          const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s)(uintptr_t)((va ^ (64 * c + 16)) + rows + 4 * ROW));
           const v8s a = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
           o[c] = mfma16<BF16>(__builtin_bit_cast(v4i, a), pb[y][ks], o[c]);
         }

@@ -197,10 +197,10 @@ __global__ void __launch_bounds__(256, kw_occupancy<D>()) k_key_weights(const Kw
     v4i a[KS];
     v4f n = constants(row, 0), next;
 #pragma unroll
-    for (int s = 0; s < AHEAD; ++s) a[s] = *(lds_v4i)(at ^ (32 * s));
+    for (int s = 0; s < AHEAD; ++s) a[s] = *(lds_v4i)(uintptr_t)(at ^ (32 * s));
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
-      if (s + AHEAD < KS) a[s + AHEAD] = *(lds_v4i)(at ^ (32 * (s + AHEAD)));
+      if (s + AHEAD < KS) a[s + AHEAD] = *(lds_v4i)(uintptr_t)(at ^ (32 * (s + AHEAD)));
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
         v16f c = acc[x];
@@ -258,7 +258,7 @@ __global__ void __launch_bounds__(256, kw_occupancy<D>()) k_key_weights(const Kw
 #pragma unroll
         for (int s = 0; s < KS; ++s)
 #pragma unroll
-          for (int x = 0; x < 2; ++x) acc_a[x] = mfma16<BF16>(*(lds_v4i)(here ^ (32 * s)), kreg[x][s], acc_a[x]);
+          for (int x = 0; x < 2; ++x) acc_a[x] = mfma16<BF16>(*(lds_v4i)(uintptr_t)(here ^ (32 * s)), kreg[x][s], acc_a[x]);
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
           const v4f n = constants(row + 32 * hr, g);
@@ -390,7 +390,7 @@ __global__ void __launch_bounds__(256, kf_held<D>() / 4) k_key_weights_few(const
     const unsigned at = k_at + (unsigned)stage * (TILE * 16);
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
-      const v4i k = *(lds_v4i)(at ^ (64 * s));
+      const v4i k = *(lds_v4i)(uintptr_t)(at ^ (64 * s));
 #pragma unroll
       for (int x = 0; x < RT; ++x) acc[x] = mfma16_small<BF16>(q[x][s], k, acc[x]);
     }
