@@ -141,7 +141,7 @@ __global__ void __launch_bounds__(64 * shared_waves<D>(), shared_occupancy<D>())
   const int vis_all = prefix || !p.causal ? nk : min(coff + 1, nk);       // keys that every query sees
   const bool part_seen = vis_all < nk;            // ... and others that some do
 
-  // ---- copies of a tile: rows behind the last key repeat it, so that masked places hold finite values where the keys do
+  // ---- copies of a tile: rows behind the last key repeat it
   const TensorMap& m = prefix ? p.pm : p.om;      // (a step from token to token is the same in both)
   const size_t head = head_offset_of(m, (int)b, (int)hkv);
   const char* gk = uniform_ptr(reinterpret_cast<const char*>((prefix ? p.kp : p.ko) + head));
@@ -232,6 +232,16 @@ if (once) {
         if (not_finite<BF16>((unsigned)u[y] >> 16)) u[y] &= 0xffff;
       }
       tv[x] = u;
+    }
+    __syncthreads();
+  };
+  // Values behind the last key (copies of the last, which need not be finite): zeros
+  auto clear = [&](int stage, int from) {
+#pragma unroll 1
+    for (int x = from * NP + t; x < TILE; x += 64 * W) {
+      int zero = 0;
+      asm volatile("" : "+v"(zero));              // (or four registers of zeros would be kept over the loop)
+      s_kv[stage][TILE + x] = v4i{zero, zero, zero, zero};
     }
     __syncthreads();
   };
@@ -329,6 +339,7 @@ if (once) {
     const bool before = ONE && j < tp;
     const int tile0 = (before ? j : j - tp) * SH_KEYS, end = before ? p.P : nk;
     const int seen = before ? p.P : vis, seen_all = before ? p.P : vis_all;
+    if (tile0 + SH_KEYS > end) clear(stage, end - tile0);
     if (!before && part_seen && tile0 + SH_KEYS > vis_all) take_out(stage);
     if (active) {
       if (D < 256 && WK == 1 && tile0 + 32 < end) tile_keys(std::integral_constant<int, 2>{}, at, tile0, 0, seen, seen_all);

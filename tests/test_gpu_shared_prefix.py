@@ -100,6 +100,24 @@ def test_large_scores_and_values_that_are_not_numbers(P):
     assert torch.equal(out[~bad], clean[0][~bad]) and torch.equal(lse[~bad], clean[1][~bad])
 
 
+@pytest.mark.parametrize("d,H,P,Nk", [(64, 4, 70, 100), (128, 8, 70, 33), (256, 2, 65, 10), (64, 4, 1001, 700), (128, 64, 1001, 300), (256, 8, 1001, 130)])
+def test_infinite_values_of_the_last_keys(d, H, P, Nk):
+    """Their channels become infinite, as their sum is, and no other changes."""
+    pa = _pa()
+    for layout in ("HND", "NHD"):
+        q, kp, vp, k, v = _inputs(2, H, 2, 1, P, Nk, d, torch.bfloat16, layout, seed=P)
+        lens = torch.tensor([Nk, Nk - 3], dtype=torch.int32, device="cuda")
+        clean = pa.sage_attn_shared_prefix(q, kp, vp, k, v, kv_lens=lens, layout=layout, return_lse=True)
+        ref.heads_first(v, layout)[1, :, Nk - 4, 5] = math.inf
+        ref.heads_first(vp, layout)[:, P - 1, 9] = -math.inf
+        out, lse = pa.sage_attn_shared_prefix(q, kp, vp, k, v, kv_lens=lens, layout=layout, return_lse=True)
+        out, was = ref.heads_first(out, layout), ref.heads_first(clean[0], layout)
+        assert torch.equal(lse, clean[1]) and (out[1, ..., 5] == math.inf).all() and (out[..., 9] == -math.inf).all()
+        same = torch.ones(d, dtype=torch.bool, device="cuda")
+        same[5] = same[9] = False
+        assert torch.equal(out[..., same], was[..., same]) and torch.equal(out[0, ..., 5], was[0, ..., 5])
+
+
 @pytest.mark.parametrize("P", [70, 1000])
 @pytest.mark.parametrize("d,H,N,Nk", [(64, 4, 2, 100), (128, 2, 5, 130), (128, 8, 40, 200), (256, 4, 40, 90), (256, 2, 3, 64)])
 def test_what_a_later_token_holds_does_not_reach_an_earlier_query(d, H, N, Nk, P):
