@@ -64,7 +64,7 @@ __global__ void __launch_bounds__(256, kw_occupancy<D>()) k_key_weights(const Kw
   constexpr unsigned ROW = D * 2;
   __shared__ __align__(1024) v4i s_q[NST][TILE];
   __shared__ __align__(16) float s_nl[KW_PIECE * KW_ROWS + 32];    // -lse log2(e) of the piece's queries; -inf: adds nothing; 32 of those
-  __shared__ __align__(16) int s_vis[KW_PIECE * KW_ROWS];     // how many keys they see
+  __shared__ __align__(16) int s_vis[KW_PIECE * KW_ROWS];     // how many keys they see; -1: no query
   __shared__ int s_masked[KW_PIECE];                          // whether a query of the tile does not see all of the workgroup's keys
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
   const int col = lane & 31, half = lane >> 5;
@@ -141,13 +141,15 @@ __global__ void __launch_bounds__(256, kw_occupancy<D>()) k_key_weights(const Kw
     for (int y = 0; y < 4; ++y, qi += 4) {
       for (; qi >= it.per_head && gi < p.G; qi -= it.per_head) ++gi;
       const int r = (it.first + qi) * KW_ROWS + lane;
-      lse[y] = INFINITY;                // (rows behind the last repeat it, and add nothing)
-      seen[y] = len;
+      // Rows behind the last repeat it, and add nothing: they see no key, since a row that adds nothing may hold anything.  They do not
+      // make a tile one that needs the mask: where the row that they repeat does not either, its scores count, and theirs are as good.
+      lse[y] = INFINITY;
+      seen[y] = -1;
       if (i + 4 * y < i1 && r < rows_all) {
         unsigned n = (unsigned)r;
         const int gg = p.flat ? (int)split_by(n, p.by_n) : gi;
         lse[y] = p.lse[((size_t)b * p.H + (int)hkv * p.G + gg) * p.N + n];
-        if (p.causal) seen[y] = min(coff + (int)n + 1, len);
+        seen[y] = p.causal ? min(coff + (int)n + 1, len) : len;
       }
     }
 #pragma unroll
@@ -155,7 +157,7 @@ __global__ void __launch_bounds__(256, kw_occupancy<D>()) k_key_weights(const Kw
       const int at = i - i0 + 4 * y;
       if (at < i1 - i0) {
         const int vis = lse[y] == -INFINITY ? 0 : seen[y];
-        const int masked = __ballot(vis < min(t0 + KW_KEYS, len)) != 0;
+        const int masked = __ballot(vis >= 0 && vis < min(t0 + KW_KEYS, len)) != 0;
         s_nl[at * KW_ROWS + lane] = -lse[y] * LOG2E;
         s_vis[at * KW_ROWS + lane] = vis;
         if (lane == 0) s_masked[at] = masked;
