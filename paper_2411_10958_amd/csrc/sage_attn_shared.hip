@@ -449,7 +449,7 @@ template <int D, bool BF16>
 __global__ void __launch_bounds__(256) k_shared_merge(const SharedParams p) {
   constexpr int MC = merge_channels<D>(), LPR = MC / 4, GRP = 64 / LPR, SLICES = D / MC;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  unsigned row = blockIdx.x * (4 / SLICES) + (unsigned)wave / SLICES;
+  unsigned row = (blockIdx.y * gridDim.x + blockIdx.x) * (4 / SLICES) + (unsigned)wave / SLICES;
   if (row >= (unsigned)(p.B * p.G * p.N * p.Hkv)) return;
   const int hkv = (int)split_by(row, p.by_rows);
   const long long i = row;
@@ -589,8 +589,9 @@ template <int D, bool BF16> hipError_t launch_shared(const SharedParams& p, hipS
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  const long long rows = (long long)p.B * p.G * p.N * p.Hkv;
-  k_shared_merge<D, BF16><<<(unsigned)((rows * (D / merge_channels<D>()) + 3) / 4), 256, 0, s>>>(p);
+  // (2^24 rows of 256 channels are 2^32 threads: more than a million workgroups are in the second dimension too)
+  const long long merges = ((long long)p.B * p.G * p.N * p.Hkv * (D / merge_channels<D>()) + 3) / 4, wide = std::min(merges, 1LL << 20);
+  k_shared_merge<D, BF16><<<dim3((unsigned)wide, (unsigned)((merges + wide - 1) / wide)), 256, 0, s>>>(p);
   return hipGetLastError();
 }
 
