@@ -9,7 +9,9 @@
 // With few rows this reads the cache and nothing else bounds it, so K and V stay in the 16 bits they are kept in: quantizing them
 // on the way would cost vector instructions for nothing.  P is rounded to the type of V for the second product (half a step, 2^-9
 // of a weight with bf16, which averages out over the keys; the output is rounded to the same type); scores, the running
-// maximum, the sum and O are FP32.
+// maximum, the sum and O are FP32.  fp16 has no numbers for weights below 2^-25 of the largest, which are in the sum all the same: there m
+// is kept 14 below the maximum, so that weights are up to 2^14 and vanish from 2^-39 of the largest on, too small for 2^25 keys (the most)
+// to add up to half a step of the output (2^-11).
 #include "sage_attn.h"
 #include "sage_ops.h"
 
@@ -245,7 +247,7 @@ if (once) {
     }
     __syncthreads();
   };
-  float mx = -INFINITY, l = 0.0f;                 // running maximum (of both halves) and this half's sum
+  float mx = -INFINITY, l = 0.0f;                 // running maximum (of both halves; fp16: less 14) and this half's sum
 
   // Where my operands start in a tile.  A row's first byte has its low bits zero and the swizzle of a row repeats every 16 rows, so a
   // step to another piece of a row is one exclusive or and a step of 16 or 32 rows an offset: no address is kept over the loop.
@@ -288,6 +290,8 @@ if (once) {
 #pragma unroll
       for (int y = 0; y < NS; ++y) top = fmaxf(top, sc[y][v]);
     top = half_max(top) * p.kappa;
+    // (m is a whole step or less off for scores below 2^24, so weights stay below 2^15; beyond, where a step of 14 may be lost, none is taken)
+    if (!BF16) top = fabsf(top) < 16777216.0f ? top - 14.0f : top;
     const float m_new = fmaxf(mx, top);
     const float base = m_new == -INFINITY ? 0.0f : m_new;       // (no key seen yet: every weight 2^-inf)
     if (__ballot(m_new > mx) != 0) {

@@ -34,3 +34,48 @@ def test_the_most_rows():
     assert torch.equal(lse, lse[:1].expand_as(lse))
     for i in range(0, len(out), 256):
         assert torch.equal(out[i:i + 256], out[:1].expand(256, -1, -1)), i
+
+
+@pytest.mark.parametrize("dt", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("d,H,N,P,Nk", [(64, 2, 1, 500, 200), (128, 2, 1, 300, 100), (256, 2, 1, 100, 100), (64, 8, 1, 20000, 3000), (128, 8, 40, 9000, 700), (256, 4, 5, 9000, 700)])
+def test_weights_far_below_the_largest(d, H, N, P, Nk, dt):
+    """Every 64th key gets e^18.5 times the weight of the others, and has values of zero: the output is what the others add up to,
+    each 2^-26.7 of the largest.  All of them are positive, so the output is off by half a step for P and half a step for itself; scores of 18.5
+    are exact, and with the constant log2 e and the exponent's two roundings at 26.7 a weight is off by less than 2^-18."""
+    pa = _pa()
+    g = torch.Generator(device="cuda")
+    g.manual_seed(P)
+    print(f"small weights d={d} H={H} N={N} P={P} Nk={Nk} {dt}", flush=True)
+    q = torch.zeros((2, H, N, d), device="cuda", dtype=dt)
+    q[..., 3] = 1.0
+    def cache(*shape):
+        k = torch.zeros((*shape, d), device="cuda", dtype=dt)
+        v = (torch.rand((*shape, d), generator=g, device="cuda") * 1000 + 500).to(dt)
+        k[..., ::64, 3], v[..., ::64, :] = 18.5, 0.0
+        return k, v
+    kp, vp = cache(2, P)
+    k, v = cache(2, 2, Nk)
+    lens = torch.tensor([Nk, Nk - 7], dtype=torch.int32, device="cuda")
+    out, lse = pa.sage_attn_shared_prefix(q, kp, vp, k, v, kv_lens=lens, sm_scale=1.0, return_lse=True)
+    want, wl, _, lb = ref.shared_prefix(q, kp, vp, k, v, lens, True, 1.0, "HND")
+    ref.check("lse", lse, wl, lb)
+    assert want.min() > 1e-4
+    ref.check("out", out, want, ref.TINY[dt] + (2.01 * ref.HALF[dt] + 2.0 ** -18) * want.abs())
+
+
+def test_scores_beyond_all_reason():
+    """Of a size at which FP32 has no halves any more (fp16): the largest takes all, as in the formula.  (P and the output are off by half a
+    step each; the log-sum-exp by four FP32 roundings of its size.)"""
+    pa = _pa()
+    d = 128
+    for size in (2.0 ** 10, 2.0 ** 12, 2.0 ** 13):                       # scores of sign times size^2 = 2^20, 2^24, 2^26, in units of log 2 1.44 times that
+        q = torch.zeros((1, 2, 1, d), device="cuda", dtype=torch.float16)
+        q[0, 0, 0, 0], q[0, 1, 0, 0] = size, -size
+        kp = torch.zeros((2, 1000, d), device="cuda", dtype=torch.float16)
+        kp[:, :, 0] = size / 2
+        kp[:, 5, 0], kp[:, 900, 0] = size, -size
+        vp = torch.rand((2, 1000, d), generator=torch.Generator(device="cuda").manual_seed(1), device="cuda").half()
+        out, lse = pa.sage_attn_shared_prefix(q, kp, vp, sm_scale=1.0, return_lse=True)
+        want = torch.stack([vp[0, 5], vp[1, 900]])[None, :, None].double()
+        ref.check(f"out of {size}", out, want, ref.TINY[torch.float16] + (2 * ref.HALF[torch.float16] + 2.0 ** -20) * want)
+        assert (lse - size * size).abs().max() <= 2.0 ** -22 * size * size
