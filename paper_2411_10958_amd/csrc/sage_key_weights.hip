@@ -29,7 +29,8 @@ struct KwParams {
   int B, H, Hkv, G, N, Nk;
   int few;                       // k_key_weights_few takes it: `piece` is then key tiles of a wavefront, `key_tiles` workgroups per head
   int causal, flat;              // flat: tiles run over the G N queries of a group, else over the N of each head
-  float kappa;
+  float kappa;                   // sm_scale log2(e), rounded ..
+  float lse_hi, lse_lo;          // .. and what that makes of log2(e): kappa / sm_scale, in two parts (see nl_of)
   int key_tiles, pieces, piece;  // most pieces of a key tile, query tiles of a piece
   FastDiv by_heads, by_hkv, by_kt, by_n;      // B H_kv, H_kv, key_tiles, N
 };
@@ -49,6 +50,13 @@ __host__ __device__ __forceinline__ KwItems kw_items(int flat, int causal, int G
   x.per_head = all - x.first;
   x.count = x.per_head * G;
   return x;
+}
+
+// The constant of a query's exponents, -lse log2(e).  Of two numbers that nearly cancel, so the same log2(e) as in kappa, in more bits than one
+// FP32 number has: each rounded for itself, the difference would be a share of lse that is the same for all keys and does not average out
+// (weights 4e-6 too large at lse 80).
+__device__ __forceinline__ float nl_of(const KwParams& p, float lse) {
+  return fabsf(lse) < INFINITY ? __fmaf_rn(-lse, p.lse_hi, -(lse * p.lse_lo)) : -lse;
 }
 
 __device__ __forceinline__ int kw_len(const KwParams& p, int b) { return p.lens ? min(max(p.lens[b], 0), p.Nk) : p.Nk; }
@@ -158,7 +166,7 @@ __global__ void __launch_bounds__(256, kw_occupancy<D>()) k_key_weights(const Kw
       if (at < i1 - i0) {
         const int vis = lse[y] == -INFINITY ? 0 : seen[y];
         const int masked = __ballot(vis >= 0 && vis < min(t0 + KW_KEYS, len)) != 0;
-        s_nl[at * KW_ROWS + lane] = -lse[y] * LOG2E;
+        s_nl[at * KW_ROWS + lane] = nl_of(p, lse[y]);
         s_vis[at * KW_ROWS + lane] = vis;
         if (lane == 0) s_masked[at] = masked;
       }
@@ -365,11 +373,12 @@ __global__ void __launch_bounds__(256, kf_held<D>() / 4) k_key_weights_few(const
       for (int y = 0; y < 4; ++y) use_now(q[x][s][y]);
   const bool blind = __ballot(mine == -INFINITY) != 0;      // (a row that saw nothing: whatever its scores, it adds nothing)
   const int sees_all = blind ? 0 : p.causal ? min(coff + 1, len) : len;
+  const float my_nl = nl_of(p, mine);
   float nl[RT][4];
 #pragma unroll
   for (int x = 0; x < RT; ++x)
 #pragma unroll
-    for (int v = 0; v < 4; ++v) nl[x][v] = -__shfl(mine, 16 * x + 4 * quad + v) * LOG2E;
+    for (int v = 0; v < 4; ++v) nl[x][v] = __shfl(my_nl, 16 * x + 4 * quad + v);
 
   typedef __attribute__((address_space(3))) const v4i* lds_v4i;
   const unsigned k_at = k0 + (unsigned)row_piece<D>(col, quad) * 16;       // (a step of 4 pieces is an exclusive or: see swizzle)
@@ -460,7 +469,10 @@ int kw_params(const sage_attn_key_weights_args* a, KwParams* p, bool need_io) {
   p->lse = a->lse; p->w_in = a->weights_in; p->w = a->weights; p->lens = a->kv_lens; p->part = (float*)a->workspace;
   p->B = a->B; p->H = a->H; p->Hkv = a->H_kv; p->G = a->H / a->H_kv; p->N = a->N; p->Nk = a->N_kv;
   p->causal = a->causal != 0;
-  p->kappa = (a->sm_scale > 0.0f ? a->sm_scale : (float)(1.0 / std::sqrt((double)a->d))) * LOG2E;
+  const double scale = a->sm_scale > 0.0f ? (double)a->sm_scale : 1.0 / std::sqrt((double)a->d);
+  p->kappa = (float)(scale * 1.4426950408889634);
+  p->lse_hi = (float)(p->kappa / scale);
+  p->lse_lo = (float)(p->kappa / scale - p->lse_hi);
   const int nhd = a->layout == SAGE_LAYOUT_NHD;
   p->qm = make_tensor_map(nhd, a->H, a->N, a->d);
   p->km = make_tensor_map(nhd, a->H_kv, a->N_kv, a->d);
