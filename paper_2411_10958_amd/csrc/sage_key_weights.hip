@@ -58,6 +58,8 @@ __host__ __device__ __forceinline__ KwItems kw_items(int flat, int causal, int G
 __device__ __forceinline__ float nl_of(const KwParams& p, float lse) {
   return fabsf(lse) < INFINITY ? __fmaf_rn(-lse, p.lse_hi, -(lse * p.lse_lo)) : -lse;
 }
+// That of a row that is not there, a copy of the last one: finite, so that it adds zero to finite scores and no NaN to an infinite weight.
+constexpr float NL_NO_ROW = -3.40282347e38f;
 
 __device__ __forceinline__ int kw_len(const KwParams& p, int b) { return p.lens ? min(max(p.lens[b], 0), p.Nk) : p.Nk; }
 
@@ -151,7 +153,7 @@ __global__ void __launch_bounds__(256, kw_occupancy<D>()) k_key_weights(const Kw
       const int r = (it.first + qi) * KW_ROWS + lane;
       // Rows behind the last repeat it, and add nothing: they see no key, since a row that adds nothing may hold anything.  They do not
       // make a tile one that needs the mask: where the row that they repeat does not either, its scores count, and theirs are as good.
-      lse[y] = INFINITY;
+      lse[y] = 0.0f;
       seen[y] = -1;
       if (i + 4 * y < i1 && r < rows_all) {
         unsigned n = (unsigned)r;
@@ -166,7 +168,7 @@ __global__ void __launch_bounds__(256, kw_occupancy<D>()) k_key_weights(const Kw
       if (at < i1 - i0) {
         const int vis = lse[y] == -INFINITY ? 0 : seen[y];
         const int masked = __ballot(vis >= 0 && vis < min(t0 + KW_KEYS, len)) != 0;
-        s_nl[at * KW_ROWS + lane] = nl_of(p, lse[y]);
+        s_nl[at * KW_ROWS + lane] = seen[y] < 0 ? NL_NO_ROW : nl_of(p, lse[y]);
         s_vis[at * KW_ROWS + lane] = vis;
         if (lane == 0) s_masked[at] = masked;
       }
@@ -358,7 +360,7 @@ __global__ void __launch_bounds__(256, kf_held<D>() / 4) k_key_weights_few(const
 #pragma unroll
     for (int s = 0; s < KS; ++s) q[x][s] = *reinterpret_cast<const v4i*>(at + 32 * s);
   }
-  float mine = INFINITY;                          // lse of row `lane`
+  float mine = 0.0f;                              // lse of row `lane`
   if (lane < rows) {
     unsigned n = (unsigned)lane;
     const int g = (int)split_by(n, p.by_n);
@@ -373,7 +375,7 @@ __global__ void __launch_bounds__(256, kf_held<D>() / 4) k_key_weights_few(const
       for (int y = 0; y < 4; ++y) use_now(q[x][s][y]);
   const bool blind = __ballot(mine == -INFINITY) != 0;      // (a row that saw nothing: whatever its scores, it adds nothing)
   const int sees_all = blind ? 0 : p.causal ? min(coff + 1, len) : len;
-  const float my_nl = nl_of(p, mine);
+  const float my_nl = lane < rows ? nl_of(p, mine) : NL_NO_ROW;
   float nl[RT][4];
 #pragma unroll
   for (int x = 0; x < RT; ++x)
@@ -417,10 +419,10 @@ __global__ void __launch_bounds__(256, kf_held<D>() / 4) k_key_weights_few(const
       for (int x = 0; x < RT; ++x)
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
-          unsigned n = (unsigned)min(16 * x + 4 * quad + v, rows - 1);
+          const int r = 16 * x + 4 * quad + v;
+          unsigned n = (unsigned)min(r, rows - 1);
           (void)split_by(n, p.by_n);
-          // (an lse of -inf or a row that is not there has +inf or -inf here)
-          const bool see = fabsf(nl[x][v]) < INFINITY || nl[x][v] != nl[x][v];
+          const bool see = r < rows && nl[x][v] != INFINITY;      // (+inf: an lse of -inf)
           const int vis = !see ? 0 : p.causal ? min(coff + (int)n + 1, len) : len;
           const float e = __builtin_amdgcn_exp2f(__fmaf_rn(acc[x][v], p.kappa, nl[x][v]));
           sum += KF_KEYS * j + col < vis ? e : 0.0f;
