@@ -403,6 +403,7 @@ typedef struct sage_cache_evict_args {
   int dtype, layout;
   int N_out;                /* room of the outputs, N_keep or more, so that the cache can go on growing there; 0 means N_keep */
   void* stream;
+  int clear;                /* 0: places behind the kept tokens stay as they were; 1: they are set to zeros, in all outputs */
 } sage_cache_evict_args;
 int sage_cache_evict(const sage_cache_evict_args* args);
 

@@ -82,7 +82,7 @@ class sage_attn_key_weights_args(ctypes.Structure):
 class sage_cache_evict_args(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in ("k", "v", "weights", "kv_lens", "k_out", "v_out", "weights_out", "kept", "lens_out")] + \
                [(n, ctypes.c_int) for n in ("B", "H_kv", "N_kv", "N_keep", "d", "sink", "recent", "dtype", "layout", "N_out")] + \
-               [("stream", ctypes.c_void_p)]
+               [("stream", ctypes.c_void_p), ("clear", ctypes.c_int)]
 
 
 def lib_path():
@@ -675,18 +675,21 @@ def sage_cache_evict(k, v, weights, n_keep, sink=0, recent=0, kv_lens=None, layo
     _need("weights", weights, index, torch.float32, (B, Hkv, Nk))
     if kv_lens is not None:
         _need("kv_lens", kv_lens, index, torch.int32, (B,))
-    make = torch.zeros if kv_lens is not None or room > Nk or room > n_keep else torch.empty
+    # Places behind what is kept: where all outputs are made here, the call itself writes zeros there, and nothing is filled before
+    behind = kv_lens is not None or room > Nk or room > n_keep
+    clear = behind and k_out is None and v_out is None and weights_out is None and kept is None
+    make = torch.zeros if behind and not clear else torch.empty
     rows = (B, room, Hkv, d) if nhd else (B, Hkv, room, d)
     outs = []
     for name, t, shape, want in (("k_out", k_out, rows, dt), ("v_out", v_out, rows, dt), ("weights_out", weights_out, (B, Hkv, room), torch.float32),
                                  ("kept", kept, (B, Hkv, n_keep), torch.int32), ("lens_out", lens_out, (B,), torch.int32)):
         if t is None:
-            t = _new(shape, want, index, stream, make)
+            t = _new(shape, want, index, stream, make if name != "lens_out" else torch.empty)
         else:
             _need(name, t, index, want, shape)
         outs.append(t)
     a = sage_cache_evict_args(k.data_ptr(), v.data_ptr(), weights.data_ptr(), _address(kv_lens), *[t.data_ptr() for t in outs],
                               B, Hkv, Nk, n_keep, d, int(sink), int(recent), dtype, nhd, room,
-                              stream.cuda_stream if stream is not None else _current_raw_stream(index))
+                              stream.cuda_stream if stream is not None else _current_raw_stream(index), int(clear))
     _call("sage_cache_evict", a, index)
     return tuple(outs)

@@ -14,7 +14,8 @@ struct EvictParams {
   unsigned short *k_out, *v_out;
   float* w_out;
   int *kept, *lens_out;
-  int Hkv, N, keep, room, sink, recent;
+  int Hkv, N, keep, room, sink, recent, clear;
+  int heads, d;                  // B H_kv
   TensorMap in, out;
 };
 
@@ -133,7 +134,38 @@ template <int K> __device__ __forceinline__ int select_tokens(const EvictParams&
   return p.keep;
 }
 
-template <int K> __global__ void __launch_bounds__(SEL_THREADS) k_evict_select(const EvictParams p) { select_tokens<K>(p); }
+// Place `at` behind what head bh keeps: its weight, and which token it would be.
+__device__ __forceinline__ void clear_place(const EvictParams& p, unsigned bh, int at) {
+  if (p.w_out) p.w_out[(size_t)bh * p.room + at] = 0.0f;
+  if (at < p.keep) p.kept[(size_t)bh * p.keep + at] = 0;
+}
+
+// Zeros in the places of the outputs behind what is kept, by workgroup z of n: stretches of CLEAR values of K and as many of V.
+constexpr int CLEAR = 32768;
+__device__ __forceinline__ void clear_places(const EvictParams& p, unsigned z, unsigned n) {
+  const int per = CLEAR / p.d, row = 31 - __builtin_clz((unsigned)p.d / 8);      // places of a stretch, log2(pieces of a row)
+  const unsigned stretches = (unsigned)((p.room + per - 1) / per);
+  for (unsigned long long s = z; s < (unsigned long long)stretches * p.heads; s += n) {
+    const unsigned bh = (unsigned)(s / stretches);
+    const int b = (int)bh / p.Hkv, len = p.lens ? min(max(p.lens[b], 0), p.N) : p.N, at = (int)(s - (unsigned long long)bh * stretches) * per;
+    const int from = max(at, min(len, p.keep)), to = min(at + per, p.room);
+    const size_t ho = head_offset(p.out, bh);
+    for (int i = from + (int)threadIdx.x; i < to; i += SEL_THREADS) clear_place(p, bh, i);
+    for (int i = (int)threadIdx.x; i < (to - from) << row; i += SEL_THREADS) {
+      const size_t x = row_offset(p.out, ho, from + (i >> row)) + 8 * (i & ((1 << row) - 1));
+      *reinterpret_cast<v4i*>(p.k_out + x) = v4i{0, 0, 0, 0};
+      *reinterpret_cast<v4i*>(p.v_out + x) = v4i{0, 0, 0, 0};
+    }
+  }
+}
+
+// Workgroups: one to a row; where `clear` is set, more that write the zeros, while the rows' have the memory to themselves.  (Us, outputs of the
+// caches' size filled before the call / this / zeros by the kernel that moves the rows: 32 heads of 32768 tokens of 128 cut to half 198 / 128 / 138, of
+// 8192 62 / 40 / 44, 16 of 100000 cut to a fifth 270 / 227 / 291.)
+template <int K> __global__ void __launch_bounds__(SEL_THREADS) k_evict_select(const EvictParams p) {
+  if (blockIdx.x < (unsigned)p.heads) select_tokens<K>(p);
+  else clear_places(p, blockIdx.x - (unsigned)p.heads, gridDim.x - (unsigned)p.heads);
+}
 
 // The same, and the rows too: one launch, where a row's workgroup has at most 4096 weights and 64 KB of K and as much of V (us, two launches /
 // this: 4 heads cut to 256 tokens of 64 14.7 / 11.5, of 128 14.2 / 11.3; 32 heads cut to 1000 of 64, 128 KB, 15.0 / 19.5).
@@ -162,6 +194,14 @@ template <int D> __global__ void __launch_bounds__(SEL_THREADS) k_evict_small(co
       *reinterpret_cast<v4i*>(p.k_out + to) = a[u];
       *reinterpret_cast<v4i*>(p.v_out + to) = x[u];
     }
+  }
+  if (!p.clear) return;
+  for (int i = threadIdx.x; i < (p.room - there) * P; i += SEL_THREADS) {
+    const int at = there + i / P;
+    const size_t to = row_offset(p.out, ho, at) + 8 * (i % P);
+    *reinterpret_cast<v4i*>(p.k_out + to) = v4i{0, 0, 0, 0};
+    *reinterpret_cast<v4i*>(p.v_out + to) = v4i{0, 0, 0, 0};
+    if (i % P == 0) clear_place(p, blockIdx.x, at);
   }
 }
 
@@ -230,6 +270,7 @@ using namespace sage;
 
 extern "C" int sage_cache_evict(const sage_cache_evict_args* a) {
   if (!a || a->B <= 0 || a->H_kv <= 0 || a->N_kv <= 0 || a->N_keep <= 0 || a->sink < 0 || a->recent < 0) return SAGE_ERR_INVALID_ARG;
+  if ((a->clear & ~1) != 0) return SAGE_ERR_UNSUPPORTED;
   const int room = a->N_out == 0 ? a->N_keep : a->N_out;
   if ((long long)a->sink + a->recent > a->N_keep || room < a->N_keep) return SAGE_ERR_INVALID_ARG;
   if (!a->k || !a->v || !a->weights || !a->k_out || !a->v_out || !a->kept || !a->lens_out) return SAGE_ERR_INVALID_ARG;
@@ -251,27 +292,31 @@ extern "C" int sage_cache_evict(const sage_cache_evict_args* a) {
   EvictParams p;
   p.k = (const unsigned short*)a->k; p.v = (const unsigned short*)a->v; p.w = a->weights; p.lens = a->kv_lens;
   p.k_out = (unsigned short*)a->k_out; p.v_out = (unsigned short*)a->v_out; p.w_out = a->weights_out; p.kept = a->kept; p.lens_out = a->lens_out;
-  p.Hkv = a->H_kv; p.N = a->N_kv; p.keep = a->N_keep; p.room = room; p.sink = a->sink; p.recent = a->recent;
+  p.Hkv = a->H_kv; p.N = a->N_kv; p.keep = a->N_keep; p.room = room; p.sink = a->sink; p.recent = a->recent; p.clear = a->clear;
+  p.heads = (int)heads; p.d = a->d;
   const int nhd = a->layout == SAGE_LAYOUT_NHD;
   p.in = make_tensor_map(nhd, a->H_kv, a->N_kv, a->d);
   p.out = make_tensor_map(nhd, a->H_kv, room, a->d);
   const hipStream_t s = (hipStream_t)a->stream;
   const int most = a->N_kv - a->sink - a->recent;       // weights to choose from
-  if (most <= SMALL_K * 64 * SEL_WAVES && (long long)std::min(a->N_keep, a->N_kv) * a->d <= SMALL_ROWS) {
+  const long long moved = std::min(a->N_keep, a->N_kv), places = a->clear ? room : moved;       // tokens of a head, at most; those written
+  if (most <= SMALL_K * 64 * SEL_WAVES && places * a->d <= SMALL_ROWS) {
     if (a->d == 64) k_evict_small<64><<<(unsigned)heads, SEL_THREADS, 0, s>>>(p);
     else if (a->d == 128) k_evict_small<128><<<(unsigned)heads, SEL_THREADS, 0, s>>>(p);
     else k_evict_small<256><<<(unsigned)heads, SEL_THREADS, 0, s>>>(p);
     return op_status(hipGetLastError());
   }
-  if (most <= 4 * SEL_THREADS) k_evict_select<4><<<(unsigned)heads, SEL_THREADS, 0, s>>>(p);
-  else if (most <= 16 * SEL_THREADS) k_evict_select<16><<<(unsigned)heads, SEL_THREADS, 0, s>>>(p);
-  else if (most <= 32 * SEL_THREADS) k_evict_select<32><<<(unsigned)heads, SEL_THREADS, 0, s>>>(p);
-  else if (most <= 64 * SEL_THREADS) k_evict_select<64><<<(unsigned)heads, SEL_THREADS, 0, s>>>(p);
-  else k_evict_select<0><<<(unsigned)heads, SEL_THREADS, 0, s>>>(p);
+  const long long stretches = p.clear ? (long long)heads * ((room + CLEAR / a->d - 1) / (CLEAR / a->d)) : 0;
+  const unsigned groups = (unsigned)(heads + std::min(stretches, 2048LL));
+  if (most <= 4 * SEL_THREADS) k_evict_select<4><<<groups, SEL_THREADS, 0, s>>>(p);
+  else if (most <= 16 * SEL_THREADS) k_evict_select<16><<<groups, SEL_THREADS, 0, s>>>(p);
+  else if (most <= 32 * SEL_THREADS) k_evict_select<32><<<groups, SEL_THREADS, 0, s>>>(p);
+  else if (most <= 64 * SEL_THREADS) k_evict_select<64><<<groups, SEL_THREADS, 0, s>>>(p);
+  else k_evict_select<0><<<groups, SEL_THREADS, 0, s>>>(p);
   int st = op_status(hipGetLastError());
   if (st != SAGE_OK) return st;
   const int per = 256 / (a->d / 8) * GU;
-  const dim3 grid((unsigned)((std::min(a->N_keep, a->N_kv) + per - 1) / per), (unsigned)heads);
+  const dim3 grid((unsigned)((moved + per - 1) / per), (unsigned)heads);
   const bool past = 8LL * (long long)heads * a->N_keep * a->d > 256LL << 20;
   if (a->d == 64) launch_rows<64>(p, past, grid, s);
   else if (a->d == 128) launch_rows<128>(p, past, grid, s);
