@@ -317,7 +317,7 @@ extern "C" int sage_cache_evict(const sage_cache_evict_args* a) {
   if (st != SAGE_OK) return st;
   const int per = 256 / (a->d / 8) * GU;
   const dim3 grid((unsigned)((moved + per - 1) / per), (unsigned)heads);
-  const bool past = 8LL * (long long)heads * a->N_keep * a->d > 256LL << 20;
+  const bool past = 8LL * (long long)heads * moved * a->d > 256LL << 20;
   if (a->d == 64) launch_rows<64>(p, past, grid, s);
   else if (a->d == 128) launch_rows<128>(p, past, grid, s);
   else launch_rows<256>(p, past, grid, s);

@@ -91,3 +91,12 @@ def test_replays():
         again = pa.sage_cache_evict(k, v, w, 500, sink=3, recent=9, kv_lens=lens, room=3000)
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(outs, again)), n
+
+
+def test_a_bound_above_what_there_is():
+    """Up to 4000 tokens of 32 heads under a bound of 16384: all stay, in their order, and zeros behind them."""
+    pa = _pa()
+    k, v, w = _caches(4, 8, 4000, 128, "HND", 3)
+    lens = torch.tensor([4000, 0, 1, 3999], dtype=torch.int32, device="cuda")
+    outs = pa.sage_cache_evict(k, v, w, 16384, sink=4, recent=64, kv_lens=lens)
+    _expect(k, v, w, 16384, 4, 64, lens, "HND", outs)
