@@ -304,7 +304,8 @@ int sage_attn_debug_mfma_fp8(const uint8_t* a_codes, const uint8_t* b_codes, con
 /* Rotary positions.  Channel pair i of the first rot_dim channels of every row is turned by the angle
  * (position + offset) * inv_freq[i] and multiplied by scale:  (x, y) -> scale (x cos - y sin, x sin + y cos);  the others are copied.
  * Angles are computed in 64 bits.  inverse: by the negative angle - with the same scale, the gradient of the forward rotation.
- * In place is allowed (q_out = q and / or k_out = k, then with the same strides); other overlaps are not. */
+ * In place is allowed (q_out = q and / or k_out = k, then with the same strides); other outputs whose rows share a value with those of
+ * another tensor are refused. */
 enum { SAGE_ROPE_PLAIN = 0, SAGE_ROPE_LINEAR = 1, SAGE_ROPE_BASE = 2, SAGE_ROPE_PARTS = 3 };
 typedef struct sage_rope_args {
   const void* q;            /* device, [B, H, N, d] or [B, N, H, d]; rows are aligned to 2 bytes at least (16 is fastest) */

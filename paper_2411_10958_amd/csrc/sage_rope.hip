@@ -177,6 +177,47 @@ bool rows_apart(const long long (&st)[3], long long B, long long heads, long lon
   return true;
 }
 
+// Whether a row of x and a row of y share a value: whether some  delta + sum of stride times index  lies within d of zero, the indices of y
+// counted up and those of x down.  Strides are taken from the largest on; an index is tried where what the smaller ones can add may still
+// reach zero - one or two values each for tensors in the usual orders.  (After 65536 tries the answer is no.)
+struct Terms {
+  int n;
+  long long stride[6], lo[6], hi[6], low[7], high[7];      // low, high: the least and the most that terms i .. n - 1 add
+  long long d;
+  int tries;
+};
+bool reaches(Terms& t, int i, long long at) {
+  if (i == t.n) return at > -t.d && at < t.d;
+  const long long s = t.stride[i], least = -t.d + 1 - at - t.high[i + 1], most = t.d - 1 - at - t.low[i + 1];
+  const long long from = std::max(t.lo[i], least >= 0 ? (least + s - 1) / s : -(-least / s)), to = std::min(t.hi[i], most >= 0 ? most / s : -((-most + s - 1) / s));
+  for (long long v = from; v <= to; ++v)
+    if (t.tries-- <= 0 || reaches(t, i + 1, at + v * s)) return t.tries > 0;
+  return false;
+}
+bool rows_meet(const void* x, const long long (&sx)[3], int hx, const void* y, const long long (&sy)[3], int hy, long long B, long long N, long long d) {
+  const long long ex[3] = {B, hx, N}, ey[3] = {B, hy, N};
+  long long span_x = d, span_y = d;                // values from the first to the last
+  for (int i = 0; i < 3; ++i) { span_x += sx[i] * (ex[i] - 1); span_y += sy[i] * (ey[i] - 1); }
+  const long long delta = ((long long)(uintptr_t)y - (long long)(uintptr_t)x) / 2;
+  if (delta >= span_x || -delta >= span_y) return false;
+  Terms t;
+  t.n = 0; t.d = d; t.tries = 65536;
+  auto add = [&](long long s, long long lo, long long hi) {
+    if (s == 0) return;
+    int i = 0;
+    while (i < t.n && t.stride[i] > s) ++i;
+    if (i == t.n || t.stride[i] != s) {
+      for (int j = t.n++; j > i; --j) { t.stride[j] = t.stride[j - 1]; t.lo[j] = t.lo[j - 1]; t.hi[j] = t.hi[j - 1]; }
+      t.stride[i] = s; t.lo[i] = t.hi[i] = 0;
+    }
+    t.lo[i] += lo; t.hi[i] += hi;
+  };
+  for (int i = 0; i < 3; ++i) { add(sx[i], 1 - ex[i], 0); add(sy[i], 0, ey[i] - 1); }
+  t.low[t.n] = t.high[t.n] = 0;
+  for (int i = t.n - 1; i >= 0; --i) { t.low[i] = t.low[i + 1] + t.stride[i] * t.lo[i]; t.high[i] = t.high[i + 1] + t.stride[i] * t.hi[i]; }
+  return reaches(t, 0, delta);
+}
+
 template <bool BF16, int VW>
 void launch(const RopeParams& p, bool inter, bool past, dim3 grid, hipStream_t s) {
   if constexpr (VW == 8) {
@@ -215,13 +256,24 @@ extern "C" int sage_rope(const sage_rope_args* a) {
     if ((i & 1) && !keys) { st[i][0] = st[i][1] = st[i][2] = 0; continue; }
     if (!tensor_strides(given[i], a->layout, heads, a->N, a->d, st[i])) return SAGE_ERR_INVALID_ARG;
     const int extent[3] = {a->B, heads, a->N};
-    for (int x = 0; x < 3; ++x) if (extent[x] == 1) st[i][x] = 0;        // (no step is taken: whatever it is, it does not count)
+    for (int x = 0; x < 3; ++x) {
+      if (extent[x] == 1) st[i][x] = 0;        // (no step is taken: whatever it is, it does not count)
+      else if (st[i][x] > (1LL << 50) / (extent[x] - 1)) return SAGE_ERR_INVALID_ARG;        // (past any memory, and sums stay within 64 bits)
+    }
     if (i >= 2 && !rows_apart(st[i], a->B, heads, a->N, a->d)) return SAGE_ERR_INVALID_ARG;
   }
-  for (int i = 0; i < 2; ++i) {          // in place: the same rows, or a thread would overwrite what another has still to read
-    const bool same = i == 0 ? a->q == a->q_out : keys && a->k == a->k_out;
-    if (same && (st[i][0] != st[i + 2][0] || st[i][1] != st[i + 2][1] || st[i][2] != st[i + 2][2])) return SAGE_ERR_INVALID_ARG;
-  }
+  // Each output against all that is there before it: in place the same rows, or a thread would overwrite what another has still to read.
+  const void* at[4] = {a->q, a->k, a->q_out, a->k_out};
+  const int heads_of[4] = {a->H, a->H_kv, a->H, a->H_kv};
+  for (int y = 2; y < (keys ? 4 : 3); ++y)
+    for (int x = 0; x < y; ++x) {
+      if (x == 1 && !keys) continue;
+      if (x == y - 2 && at[x] == at[y]) {
+        if (st[x][0] != st[y][0] || st[x][1] != st[y][1] || st[x][2] != st[y][2]) return SAGE_ERR_INVALID_ARG;
+      } else if (rows_meet(at[x], st[x], heads_of[x], at[y], st[y], heads_of[y], a->B, a->N, a->d)) {
+        return SAGE_ERR_INVALID_ARG;
+      }
+    }
   auto tensor = [&](const void* x, void* y, int i, int heads) {
     RopeTensor t;
     t.x = (const unsigned short*)x; t.y = (unsigned short*)y;

@@ -9,3 +9,60 @@ from test_operator_refusals import EVICT, _pa, _status
 def test_cache_evict_clear(clear):
     pa, lib = _pa()
     assert _status(pa, lib, "sage_cache_evict", EVICT, clear=clear) == -2
+
+
+D = 64
+BIG = 1 << 40            # (addresses nothing is at)
+
+
+def _meet(x, sx, ex, y, sy, ey):
+    """Whether two sets of rows of D values share one, value by value."""
+    rows = lambda at, s, e: {at // 2 + s[0] * b + s[1] * h + s[2] * n for b in range(e[0]) for h in range(e[1]) for n in range(e[2])}
+    return any(abs(i - j) < D for i in rows(x, sx, ex) for j in rows(y, sy, ey))
+
+
+def _rope_overlap(q, qs, k, ks, qo, qos, ko, kos, B, H, Hkv, N):
+    """What the call should say of these tensors: True if it has to refuse them."""
+    tensors = [(q, qs, (B, H, N)), (k, ks, (B, Hkv, N)), (qo, qos, (B, H, N)), (ko, kos, (B, Hkv, N))]
+    for y in (2, 3):
+        for x in range(y):
+            if not (x == y - 2 and tensors[x][0] == tensors[y][0]) and _meet(*tensors[x], *tensors[y]):
+                return True
+    return False
+
+
+def test_rope_refuses_outputs_that_overlap_another_tensor():
+    """Outputs that would be written while they are read, or twice; what is right (the last of the cases) is not called here."""
+    pa, lib = _pa()
+    B, H, Hkv, N = 2, 4, 2, 3
+    row = (H + 2 * Hkv) * D
+    fused = (N * row, D, row)                                            # slices of a fused projection, token-major
+    heads = lambda h: (h * N * D, N * D, D)
+    base = dict(B=B, H=H, H_kv=Hkv, N=N, d=D, rot_dim=D, dtype=1, inv_freq=1 << 20, layout=1)
+    far = BIG + (1 << 30)
+    cases = [
+        (BIG + 2 * row, fused),                                          # q_out: q a token later
+        (BIG + 2 * D, fused),                                            # .. a head later
+        (BIG + 2 * H * D, fused),                                        # .. where k is
+        (BIG + 2 * (H * D - 1), fused),                                  # .. one value before k
+        (BIG + 2, heads(H)),                                             # head-major over token-major
+        (BIG + 2 * (B * N * row - D), heads(H)),                         # .. its first row over the last of the projection, which is neither q nor k
+    ]
+    seen = []
+    for qo, qos in cases:
+        x = (BIG, fused, BIG + 2 * H * D, fused, qo, qos, far, heads(Hkv), B, H, Hkv, N)
+        seen.append(_rope_overlap(*x))
+        if seen[-1]:
+            assert _status(pa, lib, "sage_rope", base, q=BIG, q_strides=fused, k=BIG + 2 * H * D, k_strides=fused, q_out=qo, q_out_strides=qos, k_out=far,
+                           k_out_strides=heads(Hkv)) == -1, (qo, qos)
+    assert seen == [True, True, True, True, True, False]
+    # outputs over each other, and each over the other's input
+    for kw in (dict(q_out=far, k_out=far + 2 * 5 * D), dict(q_out=far, k_out=BIG), dict(q_out=BIG + 2 * H * D, k_out=far)):
+        assert _status(pa, lib, "sage_rope", base, q=BIG, q_strides=fused, k=BIG + 2 * H * D, k_strides=fused, q_out_strides=heads(H), k_out_strides=heads(Hkv), **kw) == -1
+
+
+def test_rope_refuses_strides_past_any_memory():
+    pa, lib = _pa()
+    base = dict(q=BIG, q_out=BIG << 1, H=2, N=3, B=2, d=D, rot_dim=D, dtype=1, inv_freq=1 << 20)
+    for kw in (dict(q_strides=((1 << 62), D, 2 * D)), dict(q_out_strides=((1 << 62), D, 2 * D)), dict(q_strides=(1 << 10, D, 1 << 50))):
+        assert _status(pa, lib, "sage_rope", base, **kw) == -1
