@@ -366,7 +366,8 @@ int sage_attn_shared_prefix(const sage_attn_shared_prefix_args* args);
 /* The attention weight that each key has received from N queries of the heads that read it:
  *   weights[b, j, t] = weights_in[b, j, t] + sum over heads h of KV head j, queries r that see t of exp(sm_scale <q_r, k_t> - lse[b, h, r])
  * with the log-sum-exp that an attention call returned (over these keys and any others).  Sums are FP32, in a fixed order.  Added up
- * over the steps of a generation it is what sage_cache_evict goes by. */
+ * over the steps of a generation it is what sage_cache_evict goes by.  weights may be weights_in; other overlaps of weights or the workspace are
+ * refused. */
 typedef struct sage_attn_key_weights_args {
   const void* q;            /* device, [B, H, N, d] or [B, N, H, d] */
   const void* k;            /* device, [B, H_kv, N_kv, d] or [B, N_kv, H_kv, d] */

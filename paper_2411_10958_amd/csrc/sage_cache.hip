@@ -257,12 +257,6 @@ template <int D> void launch_rows(const EvictParams& p, bool past, dim3 grid, hi
   else k_evict_rows<D, false><<<grid, 256, 0, s>>>(p);
 }
 
-struct Span { const void* at; size_t bytes; };
-bool overlap(const Span& a, const Span& b) {
-  const uintptr_t x = (uintptr_t)a.at, y = (uintptr_t)b.at;
-  return a.at && b.at && x < y + b.bytes && y < x + a.bytes;
-}
-
 }  // namespace
 }  // namespace sage
 

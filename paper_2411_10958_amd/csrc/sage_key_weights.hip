@@ -545,6 +545,12 @@ extern "C" int sage_attn_key_weights(const sage_attn_key_weights_args* a) {
   if (st != SAGE_OK) return st;
   const size_t need = kw_bytes(p);
   if (need > 0 && (!a->workspace || a->workspace_bytes < need || ((uintptr_t)a->workspace & 255u) != 0)) return SAGE_ERR_WORKSPACE;
+  // (workgroups add to keys in any order: weights_in is the same tensor, or another one)
+  const size_t rows = (size_t)a->B * a->H * a->N, keys = (size_t)a->B * a->H_kv * a->N_kv;
+  const Span w = {a->weights, keys * 4}, ws = {need > 0 ? a->workspace : nullptr, need}, in[5] = {{a->q, rows * a->d * 2}, {a->k, keys * a->d * 2}, {a->lse, rows * 4},
+                       {a->kv_lens, (size_t)a->B * 4}, {a->weights_in == a->weights ? nullptr : a->weights_in, keys * 4}};
+  for (const Span& x : in) if (overlap(w, x) || overlap(ws, x)) return SAGE_ERR_INVALID_ARG;
+  if (overlap(w, ws)) return SAGE_ERR_INVALID_ARG;
   const hipStream_t s = (hipStream_t)a->stream;
   const bool bf16 = a->dtype == SAGE_DT_BF16;
   const hipError_t e = a->d == 64 ? (bf16 ? launch_kw<64, true>(p, s) : launch_kw<64, false>(p, s))

@@ -11,6 +11,13 @@ inline int op_status(hipError_t e) {
   return -4;      // SAGE_ERR_HIP
 }
 
+// A contiguous tensor, and whether two share a byte (none does with what is not there).
+struct Span { const void* at; size_t bytes; };
+inline bool overlap(const Span& a, const Span& b) {
+  const uintptr_t x = (uintptr_t)a.at, y = (uintptr_t)b.at;
+  return a.at && b.at && x < y + b.bytes && y < x + a.bytes;
+}
+
 // Most threads of a grid in one of its dimensions: the launch packet counts them in 32 bits.
 constexpr long long MAX_THREADS = 0xffffffffLL;
 

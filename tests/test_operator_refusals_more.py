@@ -66,3 +66,20 @@ def test_rope_refuses_strides_past_any_memory():
     base = dict(q=BIG, q_out=BIG << 1, H=2, N=3, B=2, d=D, rot_dim=D, dtype=1, inv_freq=1 << 20)
     for kw in (dict(q_strides=((1 << 62), D, 2 * D)), dict(q_out_strides=((1 << 62), D, 2 * D)), dict(q_strides=(1 << 10, D, 1 << 50))):
         assert _status(pa, lib, "sage_rope", base, **kw) == -1
+
+
+KW = dict(q=1 << 20, k=2 << 20, lse=3 << 20, weights_in=4 << 20, weights=5 << 20, kv_lens=6 << 20, B=2, H=4, H_kv=2, N=1, N_kv=500, d=128, dtype=1)
+
+
+@pytest.mark.parametrize("kw", [dict(weights=(4 << 20) + 4), dict(weights=(4 << 20) - 4), dict(weights=(4 << 20) + 2 * 2 * 500 * 4 - 4), dict(weights=1 << 20), dict(weights=(2 << 20) + 16),
+                                dict(weights=3 << 20), dict(weights=(6 << 20) + 4), dict(weights=(6 << 20) - 2 * 2 * 500 * 4 + 4)])
+def test_key_weights_overlaps(kw):
+    pa, lib = _pa()
+    assert _status(pa, lib, "sage_attn_key_weights", KW, **kw) == -1
+
+
+@pytest.mark.parametrize("at", [1 << 20, 2 << 20, 3 << 20, 4 << 20, 5 << 20])
+def test_key_weights_workspace_over_a_tensor(at):
+    pa, lib = _pa()
+    far = dict(q=1 << 30, k=2 << 30, lse=3 << 30, weights_in=4 << 30, weights=5 << 30, kv_lens=6 << 30)
+    assert _status(pa, lib, "sage_attn_key_weights", {**KW, **far}, N=9000, N_kv=9000, workspace=at << 10, workspace_bytes=1 << 40) == -1
