@@ -342,7 +342,7 @@ int sage_rope_frequencies(int rot_dim, double base, int scaling, double factor, 
  * are read as they are, scores, softmax and sums are FP32, P is rounded to the 16-bit type for its product with V.  The prefix
  * is read once for the whole batch.  Meant for decode steps and short chunks of queries.  Every query sees the whole prefix; `causal`
  * masks the own keys (see above).  A query without any key gets zeros and lse = -inf; a value that is not finite reaches
- * only queries that see its key.  B H N is 2^24 at most. */
+ * only queries that see its key.  B H N is 2^24 at most.  out may be q; other overlaps of out, lse or the workspace are refused. */
 typedef struct sage_attn_shared_prefix_args {
   const void* q;            /* device, [B, H, N, d] or [B, N, H, d] */
   const void* k_prefix;     /* device, [H_kv, N_prefix, d] or [N_prefix, H_kv, d]; not read if N_prefix = 0 */

@@ -616,6 +616,15 @@ extern "C" int sage_attn_shared_prefix(const sage_attn_shared_prefix_args* a) {
   if (st != SAGE_OK) return st;
   const size_t need = shared_bytes(p, a->d);
   if (need > 0 && (!a->workspace || a->workspace_bytes < need || ((uintptr_t)a->workspace & 255u) != 0)) return SAGE_ERR_WORKSPACE;
+  // (a row's query is read before its output is written, by the same workgroup or a kernel before: out may be q)
+  const size_t rows = (size_t)a->B * a->H * a->N, bytes = (size_t)a->d * 2, prefix = (size_t)a->H_kv * a->N_prefix, own = (size_t)a->B * a->H_kv * a->N_kv;
+  const Span in[6] = {{a->out == a->q ? nullptr : a->q, rows * bytes}, {prefix > 0 ? a->k_prefix : nullptr, prefix * bytes}, {prefix > 0 ? a->v_prefix : nullptr, prefix * bytes},
+                      {own > 0 ? a->k : nullptr, own * bytes}, {own > 0 ? a->v : nullptr, own * bytes}, {a->kv_lens, (size_t)a->B * 4}};
+  const Span out[3] = {{a->out, rows * bytes}, {a->lse, rows * 4}, {need > 0 ? a->workspace : nullptr, need}};
+  for (int i = 0; i < 3; ++i) {
+    for (const Span& x : in) if (overlap(out[i], x)) return SAGE_ERR_INVALID_ARG;
+    for (int j = 0; j < i; ++j) if (overlap(out[i], out[j])) return SAGE_ERR_INVALID_ARG;
+  }
   p.part_ml = (float*)a->workspace;
   p.part_o = (float*)((char*)a->workspace + align256(part_rows(p) * 2 * sizeof(float)));
   const hipStream_t s = (hipStream_t)a->stream;

@@ -79,3 +79,17 @@ def test_scores_beyond_all_reason():
         want = torch.stack([vp[0, 5], vp[1, 900]])[None, :, None].double()
         ref.check(f"out of {size}", out, want, ref.TINY[torch.float16] + (2 * ref.HALF[torch.float16] + 2.0 ** -20) * want)
         assert (lse - size * size).abs().max() <= 2.0 ** -22 * size * size
+
+
+@pytest.mark.parametrize("B,H,N,P,Nk,d", [(2, 4, 1, 70, 60, 128), (2, 8, 40, 100, 60, 64), (3, 8, 5, 1000, 300, 128), (2, 8, 70, 500, 300, 256)])
+@pytest.mark.parametrize("layout", ["HND", "NHD"])
+def test_the_output_in_place_of_the_queries(B, H, N, P, Nk, d, layout):
+    pa = _pa()
+    g = torch.Generator(device="cuda")
+    g.manual_seed(P)
+    r = lambda *s: torch.randn(s, generator=g, device="cuda").bfloat16()
+    q, k, v = (ref.to_layout(r(B, h, n, d), layout) for h, n in ((H, N), (2, Nk), (2, Nk)))
+    kp, vp = (ref.heads_first(r(2, P, d), layout).contiguous() for _ in range(2))
+    want, lse = pa.sage_attn_shared_prefix(q, kp, vp, k, v, layout=layout, return_lse=True)
+    got, lse2 = pa.sage_attn_shared_prefix(q, kp, vp, k, v, layout=layout, return_lse=True, out=q)
+    assert got is q and torch.equal(got, want) and torch.equal(lse2, lse)

@@ -83,3 +83,15 @@ def test_key_weights_workspace_over_a_tensor(at):
     pa, lib = _pa()
     far = dict(q=1 << 30, k=2 << 30, lse=3 << 30, weights_in=4 << 30, weights=5 << 30, kv_lens=6 << 30)
     assert _status(pa, lib, "sage_attn_key_weights", {**KW, **far}, N=9000, N_kv=9000, workspace=at << 10, workspace_bytes=1 << 40) == -1
+
+
+SP = dict(q=1 << 30, k_prefix=2 << 30, v_prefix=3 << 30, k=4 << 30, v=5 << 30, out=6 << 30, lse=7 << 30, kv_lens=8 << 30, B=2, H=4, H_kv=2, N=1, N_prefix=5000, N_kv=700, d=128, dtype=1,
+          workspace=9 << 30, workspace_bytes=1 << 29)
+
+
+@pytest.mark.parametrize("kw", [dict(out=(1 << 30) + 256), dict(out=2 << 30), dict(out=(3 << 30) + 2 * 5000 * 256 - 16), dict(out=4 << 30), dict(out=(5 << 30) - 16), dict(out=(7 << 30) + 16),
+                                dict(out=8 << 30), dict(lse=1 << 30), dict(lse=(2 << 30) + 4), dict(lse=8 << 30), dict(lse=(9 << 30) + 256), dict(workspace=1 << 30), dict(workspace=4 << 30),
+                                dict(workspace=6 << 30), dict(workspace=(5 << 30) + 256)])
+def test_shared_prefix_overlaps(kw):
+    pa, lib = _pa()
+    assert _status(pa, lib, "sage_attn_shared_prefix", SP, **kw) == -1
