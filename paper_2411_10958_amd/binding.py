@@ -451,6 +451,15 @@ def _new(shape, dtype, index, stream, make=torch.empty):
     return t
 
 
+def _stream_on(index, stream):
+    """The raw stream of a call on GPU `index`.  A kernel started on another GPU's stream would run there, on these addresses."""
+    if stream is None:
+        return _current_raw_stream(index)
+    if stream.device_index != index:
+        raise ValueError(f"stream must be one of GPU {index} like the tensors, is of GPU {stream.device_index}")
+    return stream.cuda_stream
+
+
 def _address(t):
     return 0 if t is None else t.data_ptr()
 
@@ -511,6 +520,7 @@ def sage_rope(q, k=None, inv_freq=None, positions=None, offset=0, interleaved=Fa
     if inv_freq is None:
         raise ValueError("inv_freq is needed (see sage_rope_frequencies)")
     dtype, index = _dtype_code(q), _gpu_of("q", q)
+    raw_stream = _stream_on(index, stream)
     packed = q.dim() == 3
     if not packed and q.dim() != 4:
         raise ValueError(f"q must have 4 dimensions, or 3 if packed, got {q.dim()}")
@@ -548,7 +558,7 @@ def sage_rope(q, k=None, inv_freq=None, positions=None, offset=0, interleaved=Fa
     a = sage_rope_args(q.data_ptr(), _address(k), outs[0].data_ptr(), _address(outs[1]), B, H, Hkv, N, d, 2 * inv_freq.numel(), dtype, nhd,
                        int(bool(interleaved)), int(bool(inverse)), float(scale), inv_freq.data_ptr(), _address(positions),
                        N if positions is not None and positions.dim() == 2 else 0, int(offset))
-    a.stream = stream.cuda_stream if stream is not None else _current_raw_stream(index)
+    a.stream = raw_stream
     for t, st in ((q, a.q_strides), (k, a.k_strides), (outs[0], a.q_out_strides), (outs[1], a.k_out_strides)):
         if t is None or t.is_contiguous():
             continue                            # (all zero: contiguous)
@@ -566,6 +576,7 @@ def sage_rope(q, k=None, inv_freq=None, positions=None, offset=0, interleaved=Fa
 
 def _shared_prefix_args(q, k_prefix, v_prefix, k, v, kv_lens, out, causal, sm_scale, layout, stream):
     dtype, dt, index, nhd = _dtype_code(q), q.dtype, _gpu_of("q", q), _LAYOUTS[layout]
+    raw_stream = _stream_on(index, stream)
     B, H, N, d = _sizes("q", q, nhd)
     _need("q", q, index, dt)
     if (k_prefix is None) != (v_prefix is None) or (k is None) != (v is None) or (k is None and k_prefix is None):
@@ -593,7 +604,7 @@ def _shared_prefix_args(q, k_prefix, v_prefix, k, v, kv_lens, out, causal, sm_sc
         _need("out", out, index, dt, q.shape)
     return sage_attn_shared_prefix_args(q.data_ptr(), _address(k_prefix), _address(v_prefix), _address(k), _address(v), _address(out), _address(kv_lens), 0,
                                         B, H, Hkv, N, P, Nk, d, int(bool(causal)), float(sm_scale), dtype, nhd, 0, 0,
-                                        stream.cuda_stream if stream is not None else _current_raw_stream(index))
+                                        raw_stream)
 
 
 def sage_attn_shared_prefix_workspace_bytes(args):
@@ -630,6 +641,7 @@ def sage_attn_key_weights(q, k, lse, weights_in=None, weights=None, kv_lens=None
     attention calls return it), summed over the queries of its KV head and added to weights_in.  Returns weights, float32
     [B, H_kv, N_kv]; may be weights_in.  Entries behind kv_lens keep what they hold (zeros if the result is allocated here)."""
     dtype, index, nhd = _dtype_code(q), _gpu_of("q", q), _LAYOUTS[layout]
+    raw_stream = _stream_on(index, stream)
     B, H, N, d = _sizes("q", q, nhd)
     Bk, Hkv, Nk, dk = _sizes("k", k, nhd)
     _need("q", q, index, q.dtype)
@@ -648,7 +660,7 @@ def sage_attn_key_weights(q, k, lse, weights_in=None, weights=None, kv_lens=None
         _need("weights", weights, index, torch.float32, shape)
     a = sage_attn_key_weights_args(q.data_ptr(), k.data_ptr(), lse.data_ptr(), _address(weights_in), weights.data_ptr(), _address(kv_lens),
                                    B, H, Hkv, N, Nk, d, int(bool(causal)), float(sm_scale), dtype, nhd, 0, 0,
-                                   stream.cuda_stream if stream is not None else _current_raw_stream(index))
+                                   raw_stream)
     keep = _own_workspace("sage_attn_key_weights", a, index, workspace, stream)
     _call("sage_attn_key_weights", a, index)
     del keep
@@ -663,6 +675,7 @@ def sage_cache_evict(k, v, weights, n_keep, sink=0, recent=0, kv_lens=None, layo
     (int32 [B]); what stands behind them keeps what it held (zeros where the output is allocated here).  k_out, v_out and weights_out
     have room for `room` tokens (None: n_keep), so that the cache can go on growing there."""
     dtype, dt, index, nhd = _dtype_code(k), k.dtype, _gpu_of("k", k), _LAYOUTS[layout]
+    raw_stream = _stream_on(index, stream)
     B, Hkv, Nk, d = _sizes("k", k, nhd)
     _need("k", k, index, dt)
     _need("v", v, index, dt, k.shape)
@@ -690,6 +703,6 @@ def sage_cache_evict(k, v, weights, n_keep, sink=0, recent=0, kv_lens=None, layo
         outs.append(t)
     a = sage_cache_evict_args(k.data_ptr(), v.data_ptr(), weights.data_ptr(), _address(kv_lens), *[t.data_ptr() for t in outs],
                               B, Hkv, Nk, n_keep, d, int(sink), int(recent), dtype, nhd, room,
-                              stream.cuda_stream if stream is not None else _current_raw_stream(index), int(clear))
+                              raw_stream, int(clear))
     _call("sage_cache_evict", a, index)
     return tuple(outs)
