@@ -608,6 +608,8 @@ def _shared_prefix_args(q, k_prefix, v_prefix, k, v, kv_lens, out, causal, sm_sc
 
 
 def sage_attn_shared_prefix_workspace_bytes(args):
+    """The size of the workspace to hand to sage_attn_shared_prefix, 0 if it needs none.  args: a sage_attn_shared_prefix_args, of which the sizes, dtype
+    (SAGE_DT_*), layout (0 HND, 1 NHD) and causal are looked at."""
     return int(load_library().sage_attn_shared_prefix_workspace_bytes(ctypes.byref(args)))
 
 
@@ -632,6 +634,8 @@ def sage_attn_shared_prefix(q, k_prefix, v_prefix, k=None, v=None, kv_lens=None,
 
 
 def sage_attn_key_weights_workspace_bytes(args):
+    """The size of the workspace to hand to sage_attn_key_weights, 0 if it needs none.  args: a sage_attn_key_weights_args, of which the sizes, dtype
+    (SAGE_DT_*), layout (0 HND, 1 NHD) and causal are looked at."""
     return int(load_library().sage_attn_key_weights_workspace_bytes(ctypes.byref(args)))
 
 

@@ -95,3 +95,12 @@ SP = dict(q=1 << 30, k_prefix=2 << 30, v_prefix=3 << 30, k=4 << 30, v=5 << 30, o
 def test_shared_prefix_overlaps(kw):
     pa, lib = _pa()
     assert _status(pa, lib, "sage_attn_shared_prefix", SP, **kw) == -1
+
+
+def test_workspaces_are_sized_with_public_names():
+    pa, _ = _pa()
+    a = pa.sage_attn_shared_prefix_args(B=2, H=4, H_kv=2, N=1, N_prefix=5000, N_kv=700, d=128, causal=1, dtype=pa.SAGE_DT_BF16)
+    assert pa.sage_attn_shared_prefix_workspace_bytes(a) > 0
+    a = pa.sage_attn_key_weights_args(B=1, H=4, H_kv=1, N=3001, N_kv=3001, d=64, causal=1, dtype=pa.SAGE_DT_FP16, layout=1)
+    assert pa.sage_attn_key_weights_workspace_bytes(a) > 0
+    assert {"sage_attn_shared_prefix_args", "sage_attn_key_weights_args"} <= set(pa.__all__)
