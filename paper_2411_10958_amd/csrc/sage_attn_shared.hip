@@ -534,8 +534,13 @@ void choose_chunks(SharedParams* p, int d, long long rows) {
   long long share = (prefix + own + places - 1) / places;
   if (rows <= 64) share = std::max(share, (prefix + 255) / 256);
   const long long pp = std::max(least, share), po = std::max(least, std::min(12LL, (own + places - 1) / places));
-  p->Sp = (int)std::min((long long)MAX_PARTS / 2, (tp + pp - 1) / pp);
-  p->So = (int)std::min((long long)MAX_PARTS / 2, (to + po - 1) / po);
+  // The merge takes MAX_PARTS in all: half for each part, and what the other leaves where half would leave places of the chip empty, with one KV head
+  // or two.  (Us, half / this: 1 sequence of 1000000 own keys, one KV head of 128 channels 160 / 97; 1 of 512 over 131072 35.8 / 33.5; 4
+  // over 200000 of 256 channels 73 / 50; 8 of 200000 own keys, where half does, 143, with all 153.)
+  const long long wp = (tp + pp - 1) / pp, wo = (to + po - 1) / po, half = MAX_PARTS / 2;
+  const long long fp = places / ((long long)p->Hkv * p->rtp), fo = places / ((long long)p->B * p->Hkv * p->rto);
+  p->Sp = (int)std::min(wp, std::max(half, std::min(MAX_PARTS - wo, fp)));
+  p->So = (int)std::min(wo, std::max(half, std::min(MAX_PARTS - wp, fo)));
 }
 
 int shared_params(const sage_attn_shared_prefix_args* a, SharedParams* p, bool need_io) {

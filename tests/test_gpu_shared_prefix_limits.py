@@ -93,3 +93,21 @@ def test_the_output_in_place_of_the_queries(B, H, N, P, Nk, d, layout):
     want, lse = pa.sage_attn_shared_prefix(q, kp, vp, k, v, layout=layout, return_lse=True)
     got, lse2 = pa.sage_attn_shared_prefix(q, kp, vp, k, v, layout=layout, return_lse=True, out=q)
     assert got is q and torch.equal(got, want) and torch.equal(lse2, lse)
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("B,H,N,P,Nk", [(1, 8, 1, 131072, 512), (1, 4, 3, 0, 140001), (2, 2, 1, 140001, 0), (1, 2, 5, 90000, 60001)])
+def test_one_head_of_many_keys(B, H, N, P, Nk, d):
+    """As many partial results to merge as there can be."""
+    pa = _pa()
+    g = torch.Generator(device="cuda")
+    g.manual_seed(d)
+    print(f"one head B={B} H={H} N={N} P={P} Nk={Nk} d={d}", flush=True)
+    r = lambda *s: torch.randn(s, generator=g, device="cuda").bfloat16()
+    q = r(B, H, N, d)
+    kp, vp = (r(1, P, d) if P else None for _ in range(2))
+    k, v = (r(B, 1, Nk, d) if Nk else None for _ in range(2))
+    out, lse = pa.sage_attn_shared_prefix(q, kp, vp, k, v, return_lse=True)
+    want, wl, ob, lb = ref.shared_prefix(q, kp, vp, k, v, None, True, 0.0, "HND")
+    ref.check("lse", lse, wl, lb)
+    ref.check("out", out, want, ob)

@@ -104,3 +104,11 @@ def test_workspaces_are_sized_with_public_names():
     a = pa.sage_attn_key_weights_args(B=1, H=4, H_kv=1, N=3001, N_kv=3001, d=64, causal=1, dtype=pa.SAGE_DT_FP16, layout=1)
     assert pa.sage_attn_key_weights_workspace_bytes(a) > 0
     assert {"sage_attn_shared_prefix_args", "sage_attn_key_weights_args"} <= set(pa.__all__)
+
+
+@pytest.mark.parametrize("kw", [dict(N_prefix=131072, N_kv=512), dict(N_prefix=0, N_kv=131072), dict(N_prefix=131072, N_kv=0)])
+def test_long_keys_of_one_head_are_cut_for_the_whole_chip(kw):
+    """A call bound by reading, with one KV head: as many partial results as a row may have, 256, which the workspace has room for."""
+    pa, _ = _pa()
+    a = pa.sage_attn_shared_prefix_args(B=1, H=8, H_kv=1, N=1, d=128, causal=1, dtype=pa.SAGE_DT_BF16, **kw)
+    assert pa.sage_attn_shared_prefix_workspace_bytes(a) == 256 * 8 * (128 + 2) * 4
