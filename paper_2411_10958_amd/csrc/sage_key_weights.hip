@@ -188,13 +188,12 @@ __global__ void __launch_bounds__(256, kw_occupancy<D>()) k_key_weights(const Kw
   typedef __attribute__((address_space(3))) const v4i* lds_v4i;
   const unsigned q_at = (unsigned)row_piece<D>(col, half) * 16;
   float sum[2][2] = {{0.0f, 0.0f}, {0.0f, 0.0f}};
-  float kappa = p.kappa;
   auto constants = [&](int row, int g) __attribute__((always_inline)) {        // rows 8 g + 4 h + 0..3
     return *reinterpret_cast<const v4f*>(&s_nl[row + 8 * g + 4 * half]);
   };
   auto weight = [&](int e, const v16f (&sc)[2], const v4f& n) __attribute__((always_inline)) {
     const int x = e & 1, v = e >> 1;
-    sum[x][v & 1] += __builtin_amdgcn_exp2f(__fmaf_rn(sc[x][v], kappa, n[v & 3]));
+    sum[x][v & 1] += __builtin_amdgcn_exp2f(__fmaf_rn(sc[x][v], p.kappa, n[v & 3]));
   };
   auto weights = [&](const v16f (&sc)[2], int row) __attribute__((always_inline)) {
 #pragma unroll
@@ -258,7 +257,7 @@ __global__ void __launch_bounds__(256, kw_occupancy<D>()) k_key_weights(const Kw
       scores(at + 32 * ROW, acc_b, acc_a, row);
       row_b = row + 32;
     } else {
-      asm volatile("" : "+s"(kappa));             // (or the weights of acc_b, common to both ways, would be taken before them)
+      asm volatile("" : "+s"(row_b));             // (or the weights of acc_b, common to both ways, would be taken before them)
       weights(acc_b, row_b);
 #pragma unroll 1
       for (int hr = 0; hr < 2; ++hr) {
