@@ -33,8 +33,8 @@ constexpr int DIGIT = 11, BINS = 1 << DIGIT;      // three digits of 11, 11 and 
 // Which tokens stay, one workgroup per sequence and KV head: the m-th largest weight between sink and recent, found digit by digit by
 // counting, then one pass in order that keeps what is larger and the first of what equals it.  A wavefront has a stretch of
 // 64 K weights in registers, in the order of unsigned numbers, so they are read and converted once; K = 0: more than that, read
-// again each time, eight loads in flight.  Bound by the instructions of its five passes on one CU: 32 rows of 32768 22 us of the call's
-// 111 (51 with 8-bit digits and weights read from memory in each pass; counts in four copies changed nothing).  (The first digit is sign, exponent and two bits: with 8-bit digits a wavefront's
+// again each time, eight loads in flight.  Bound by the instructions of its five passes on one CU: 32 rows of 32768 20 us of the call's
+// 107 (51 with 8-bit digits and weights read from memory in each pass; counts in four copies changed nothing).  (The first digit is sign, exponent and two bits: with 8-bit digits a wavefront's
 // counts would fall on a dozen addresses.)  What a stretch has behind the last weight counts as less than any and comes after
 // all, so it is never taken: n > m.
 template <int K> __device__ __forceinline__ int select_tokens(const EvictParams& p) {
@@ -57,11 +57,16 @@ template <int K> __device__ __forceinline__ int select_tokens(const EvictParams&
   const int i0 = min(wave * seg, n), i1 = min(i0 + seg, n);
   unsigned u[STEP];
   auto load = [&](int from) __attribute__((always_inline)) {
-    float x[STEP];
+    constexpr int PART = STEP < 32 ? STEP : 32;   // loads in flight (64 at once would leave no registers for the weights)
 #pragma unroll
-    for (int j = 0; j < STEP; ++j) x[j] = from + 64 * j < i1 ? w[c0 + min(from + 64 * j + lane, i1 - 1)] : 0.0f;
+    for (int j0 = 0; j0 < STEP; j0 += PART) {
+      float x[PART];
 #pragma unroll
-    for (int j = 0; j < STEP; ++j) u[j] = from + 64 * j + lane < i1 ? order_of(x[j]) : 0u;
+      for (int j = 0; j < PART; ++j) x[j] = from + 64 * (j0 + j) < i1 ? w[c0 + min(from + 64 * (j0 + j) + lane, i1 - 1)] : 0.0f;
+#pragma unroll
+      for (int j = 0; j < PART; ++j) u[j0 + j] = from + 64 * (j0 + j) + lane < i1 ? order_of(x[j]) : 0u;
+      __builtin_amdgcn_sched_barrier(0);
+    }
   };
   if (K > 0) load(i0);
   for (int i = t; i < p.sink; i += SEL_THREADS) kept[i] = i;
@@ -73,7 +78,13 @@ template <int K> __device__ __forceinline__ int select_tokens(const EvictParams&
       if (K == 0) load(i);
 #pragma unroll
       for (int j = 0; j < STEP; ++j)
-        if (i + 64 * j < i1) f(u[j], i + 64 * j);
+        if (i + 64 * j < i1) {
+          unsigned v = u[j];
+          // (What the compiler knows of a weight it would keep from one pass to the next, masks of 64 lanes for each and more than there are
+          // registers for.  Us, with that kept / this: 32 rows of 30000 25.6 / 23.2, of 50000 44.6 / 32.9.)
+          if (K > 16) asm volatile("" : "+v"(v));
+          f(v, i + 64 * j);
+        }
     }
   };
   unsigned prefix = 0, need = (unsigned)m;
