@@ -163,8 +163,9 @@ __global__ void __launch_bounds__(64 * shared_waves<D>(), shared_occupancy<D>())
   // What one workgroup alone reads passes the caches by.  The prefix only where it has few rows: with more, its workgroups leave partial
   // results of as many bytes, and reads from memory itself make them later (us, kept in the caches / past them: 16 sequences of up to
   // 3000 own keys over 20000, 128 channels 56.5 / 52.9; 4 over 100000 84.5 / 75.3; 6 of 5 tokens of 256 channels over 5003, 120
-  // rows: 30.4 / 34.2).  In one launch every sequence reads the prefix (512 of 380 + 60 of 128 channels, past the caches / kept 108.2 / 105.9).
-  const bool once = prefix ? rows <= 64 : p.rto == 1, first_once = once && p.B == 1;
+  // rows: 30.4 / 34.2).  In one launch every sequence reads the prefix: with more than one to an XCD it is kept (sequences of 380 + 60 keys of
+  // 128 channels, kept / past the caches: 512 106.4 / 108.4, 128 29.4 / 30.3, 32 13.4 / 13.6; 4 of 300 + 50 of 64 the kernel 9.6 / 9.4).
+  const bool once = prefix ? rows <= 64 : p.rto == 1 && (!ONE || p.B <= 8);
   auto copy = [&](int j, int stage) __attribute__((always_inline)) {
     const bool before = ONE && j < tp;
     if (!before) j -= tp;
@@ -173,7 +174,7 @@ __global__ void __launch_bounds__(64 * shared_waves<D>(), shared_occupancy<D>())
     const unsigned to = lds0 + (unsigned)(stage * 2 * TILE + wave * 64) * 16;
     const int last = (before ? p.P : nk) - 1 - j * SH_KEYS;
     if (last >= SH_KEYS - 1) {
-      if (ONE && before ? first_once : once) {
+      if (once) {
 #pragma unroll
         for (int x = 0; x < COPIES; ++x) {
           dma_b128_once(fk + at, offs[x], to + x * (W * 1024));
