@@ -160,6 +160,7 @@ __device__ __forceinline__ void clear_places(const EvictParams& p, unsigned z, u
     const unsigned bh = (unsigned)(s / stretches);
     const int b = (int)bh / p.Hkv, len = p.lens ? min(max(p.lens[b], 0), p.N) : p.N, at = (int)(s - (unsigned long long)bh * stretches) * per;
     const int from = max(at, min(len, p.keep)), to = min(at + per, p.room);
+    if (from >= to) continue;
     const size_t ho = head_offset(p.out, bh);
     for (int i = from + (int)threadIdx.x; i < to; i += SEL_THREADS) clear_place(p, bh, i);
     for (int i = (int)threadIdx.x; i < (to - from) << row; i += SEL_THREADS) {
