@@ -340,6 +340,7 @@ extern "C" int sage_rope_frequencies(int rot_dim, double base, int scaling, doub
     return SAGE_ERR_INVALID_ARG;
   if (scaling == SAGE_ROPE_BASE && rot_dim == 2) return SAGE_ERR_UNSUPPORTED;      // (one frequency, which no base moves)
   if (scaling == SAGE_ROPE_BASE) base *= std::pow(factor, (double)rot_dim / (rot_dim - 2));
+  if (!std::isfinite(base)) return SAGE_ERR_INVALID_ARG;                            // (the raised one)
   for (int i = 0; i < rot_dim / 2; ++i) {
     double f = std::pow(base, -2.0 * i / rot_dim);
     if (scaling == SAGE_ROPE_LINEAR) f /= factor;

@@ -112,3 +112,11 @@ def test_long_keys_of_one_head_are_cut_for_the_whole_chip(kw):
     pa, _ = _pa()
     a = pa.sage_attn_shared_prefix_args(B=1, H=8, H_kv=1, N=1, d=128, causal=1, dtype=pa.SAGE_DT_BF16, **kw)
     assert pa.sage_attn_shared_prefix_workspace_bytes(a) == 256 * 8 * (128 + 2) * 4
+
+
+def test_frequencies_of_a_base_raised_past_64_bits():
+    pa, _ = _pa()
+    for rot, base, factor in ((64, 1e300, 1e10), (4, 10000.0, 1e200)):
+        with pytest.raises(pa.SageError):
+            pa.sage_rope_frequencies(rot, base=base, scaling="base", factor=factor, device="cpu")
+    assert pa.sage_rope_frequencies(64, base=1e300, scaling="base", factor=2.0, device="cpu")[-1] > 0
