@@ -321,7 +321,7 @@ typedef struct sage_rope_args {
   const double* inv_freq;   /* device, [rot_dim / 2]: radians per position, e.g. from sage_rope_frequencies */
   const int* positions;     /* device, or NULL: token n stands at n.  positions[b * positions_stride + n] */
   long long positions_stride;  /* 0: the same for every sequence */
-  long long offset;         /* added to every position */
+  long long offset;         /* added to every position; 2^52 at most, either way */
   /* Strides of batch, head and token in elements, for views - slices of a fused projection, rows of a cache; all 0: contiguous in
      `layout`.  The channels of a row are contiguous, and no two rows of an output overlap. */
   long long q_strides[3], k_strides[3], q_out_strides[3], k_out_strides[3];

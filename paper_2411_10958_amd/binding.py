@@ -460,6 +460,12 @@ def _stream_on(index, stream):
     return stream.cuda_stream
 
 
+def _whole(x, bits):
+    """A whole number for a C field of so many bits: one that does not fit becomes the field's end, which the call refuses, instead of another number."""
+    x = int(x)
+    return max(-(1 << bits - 1), min(x, (1 << bits - 1) - 1))
+
+
 def _address(t):
     return 0 if t is None else t.data_ptr()
 
@@ -557,7 +563,7 @@ def sage_rope(q, k=None, inv_freq=None, positions=None, offset=0, interleaved=Fa
         outs.append(y)
     a = sage_rope_args(q.data_ptr(), _address(k), outs[0].data_ptr(), _address(outs[1]), B, H, Hkv, N, d, 2 * inv_freq.numel(), dtype, nhd,
                        int(bool(interleaved)), int(bool(inverse)), float(scale), inv_freq.data_ptr(), _address(positions),
-                       N if positions is not None and positions.dim() == 2 else 0, int(offset))
+                       N if positions is not None and positions.dim() == 2 else 0, _whole(offset, 64))
     a.stream = raw_stream
     for t, st in ((q, a.q_strides), (k, a.k_strides), (outs[0], a.q_out_strides), (outs[1], a.k_out_strides)):
         if t is None or t.is_contiguous():
@@ -706,7 +712,7 @@ def sage_cache_evict(k, v, weights, n_keep, sink=0, recent=0, kv_lens=None, layo
             _need(name, t, index, want, shape)
         outs.append(t)
     a = sage_cache_evict_args(k.data_ptr(), v.data_ptr(), weights.data_ptr(), _address(kv_lens), *[t.data_ptr() for t in outs],
-                              B, Hkv, Nk, n_keep, d, int(sink), int(recent), dtype, nhd, room,
+                              B, Hkv, Nk, n_keep, d, _whole(sink, 32), _whole(recent, 32), dtype, nhd, room,
                               raw_stream, int(clear))
     _call("sage_cache_evict", a, index)
     return tuple(outs)

@@ -246,7 +246,7 @@ extern "C" int sage_rope(const sage_rope_args* a) {
   if ((a->interleaved & ~1) != 0 || (a->inverse & ~1) != 0) return SAGE_ERR_UNSUPPORTED;
   if ((((uintptr_t)a->q | (uintptr_t)a->k | (uintptr_t)a->q_out | (uintptr_t)a->k_out) & 1u) != 0) return SAGE_ERR_INVALID_ARG;
   if (((uintptr_t)a->inv_freq & 7u) != 0 || ((uintptr_t)a->positions & 3u) != 0 || a->positions_stride < 0) return SAGE_ERR_INVALID_ARG;
-  if (!std::isfinite(a->scale)) return SAGE_ERR_INVALID_ARG;
+  if (!std::isfinite(a->scale) || a->offset > 1LL << 52 || a->offset < -(1LL << 52)) return SAGE_ERR_INVALID_ARG;        // (positions stay whole numbers in FP64)
 
   RopeParams p;
   long long st[4][3];

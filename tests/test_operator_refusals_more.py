@@ -120,3 +120,9 @@ def test_frequencies_of_a_base_raised_past_64_bits():
         with pytest.raises(pa.SageError):
             pa.sage_rope_frequencies(rot, base=base, scaling="base", factor=factor, device="cpu")
     assert pa.sage_rope_frequencies(64, base=1e300, scaling="base", factor=2.0, device="cpu")[-1] > 0
+
+
+@pytest.mark.parametrize("offset", [(1 << 52) + 1, -(1 << 52) - 1, (1 << 63) - 1, -(1 << 63)])
+def test_rope_offsets_that_are_no_whole_numbers_in_64_bits(offset):
+    pa, lib = _pa()
+    assert _status(pa, lib, "sage_rope", dict(q=BIG, q_out=BIG << 1, H=2, N=3, B=2, d=D, rot_dim=D, dtype=1, inv_freq=1 << 20), offset=offset) == -1
