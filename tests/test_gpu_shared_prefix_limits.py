@@ -111,3 +111,42 @@ def test_one_head_of_many_keys(B, H, N, P, Nk, d):
     want, wl, ob, lb = ref.shared_prefix(q, kp, vp, k, v, None, True, 0.0, "HND")
     ref.check("lse", lse, wl, lb)
     ref.check("out", out, want, ob)
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_caches_without_any_place(d):
+    """No prefix and no own keys: zeros and -inf; and each of them empty beside the other."""
+    pa = _pa()
+    g = torch.Generator(device="cuda")
+    g.manual_seed(d)
+    r = lambda *s: torch.randn(s, generator=g, device="cuda").bfloat16()
+    for H, N in ((4, 1), (2, 300)):
+        q, none, own = r(3, H, N, d), r(2, 0, d), r(3, 2, 0, d)
+        lens = torch.tensor([0, 5, -1], dtype=torch.int32, device="cuda")
+        for args in ((none, none, own, own), (none, none), (None, None, own, own)):
+            out, lse = pa.sage_attn_shared_prefix(q, *args, kv_lens=lens if len(args) > 2 else None, out=torch.full_like(q, 3.0), return_lse=True)
+            assert (out == 0).all() and (lse == -math.inf).all()
+        kp, vp, k, v = r(2, 700, d), r(2, 700, d), r(3, 2, 400, d), r(3, 2, 400, d)
+        for a, b in (((kp, vp, own, own), (kp, vp)), ((none, none, k, v), (None, None, k, v))):
+            x, y = (pa.sage_attn_shared_prefix(q, *args, return_lse=True) for args in (a, b))
+            assert torch.equal(x[0], y[0]) and torch.equal(x[1], y[1])
+
+
+@pytest.mark.parametrize("B,H,N,P,Nk", [(1, 4, 513, 700, 600), (2, 2, 1000, 300, 1300), (3, 4, 130, 200, 60), (1, 8, 257, 0, 300)])
+@pytest.mark.parametrize("d,dt,layout", [(64, torch.float16, "NHD"), (128, torch.bfloat16, "HND"), (256, torch.bfloat16, "NHD")])
+def test_chunks_of_a_prompt(B, H, N, P, Nk, d, dt, layout):
+    """Many queries over a prefix and their own keys, also with fewer keys than queries."""
+    pa = _pa()
+    g = torch.Generator(device="cuda")
+    g.manual_seed(N)
+    print(f"chunk B={B} H={H} N={N} P={P} Nk={Nk} d={d} {dt} {layout}", flush=True)
+    r = lambda *s: torch.randn(s, generator=g, device="cuda").to(dt)
+    q, k, v = ref.to_layout(r(B, H, N, d), layout), ref.to_layout(r(B, 2, Nk, d), layout), ref.to_layout(r(B, 2, Nk, d), layout)
+    kp, vp = (ref.heads_first(r(2, P, d), layout).contiguous() if P else None for _ in range(2))
+    lens = torch.randint(0, Nk + 1, (B,), generator=torch.Generator().manual_seed(N)).to(torch.int32)
+    lens[0] = Nk
+    for causal, x in ((True, None), (True, lens.cuda()), (False, lens.cuda())):
+        out, lse = pa.sage_attn_shared_prefix(q, kp, vp, k, v, kv_lens=x, causal=causal, layout=layout, return_lse=True)
+        want, wl, ob, lb = ref.shared_prefix(q, kp, vp, k, v, x, causal, 0.0, layout)
+        ref.check("lse", lse, wl, lb)
+        ref.check("out", out, want, ob)
