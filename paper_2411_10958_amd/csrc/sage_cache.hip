@@ -219,7 +219,7 @@ template <int D> __global__ void __launch_bounds__(SEL_THREADS) k_evict_small(co
 
 // The rows of the kept tokens, and their weights: a thread moves 16 bytes of K and of V of GU tokens, the first of a row also its
 // weight.  Reads pass the caches by, since the old rows are not needed again; with PAST writes do too, where rows read and written do not fit
-// the 256 MB of the memory-side cache (32 heads of 32768 tokens of 128 cut to half: the call 123 us with both kept, 120 with reads past,
+// the 256 MB of the memory-side cache (32 heads of 32768 tokens of 128 cut to half: the call, with 22 us of selection, 123 us with both kept, 120 with reads past,
 // 111 with both, 5.4 TB/s; with the decode step that reads the rows after it 174 either way).  Below that the step finds rows there (32
 // heads of 8000 cut to half, and the step: 54.9, 57.4 with writes past).
 // Grid: (pieces of the kept tokens, heads).
