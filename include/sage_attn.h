@@ -292,7 +292,8 @@ int sage_attn_debug_mfma_fp8(const uint8_t* a_codes, const uint8_t* b_codes, con
 
 /* ------------------------------------------------------------------------------------------------------------------
  * Operators around the attention calls of a serving program: rotary positions of Q and K, 16-bit attention of a batch that
- * shares a prefix, the attention weight that each key of a cache has received, and the eviction of the others.  The conventions at
+ * shares a prefix, the attention weight that each key of a cache has received, and the eviction of the others; norms of Q and K with
+ * their rotation, and a cache in 8 bits and pages with its appends and its attention.  The conventions at
  * the head of this file hold for them too; d is 64, 128 or 256 and tensors are fp16 or bf16 throughout.  None of them allocates,
  * synchronises or keeps anything between calls, so all can be captured into a graph; results do not depend on the order in
  * which workgroups run.
@@ -408,6 +409,123 @@ typedef struct sage_cache_evict_args {
   int clear;                /* 0: places behind the kept tokens stay as they were; 1: they are set to zeros, in all outputs */
 } sage_cache_evict_args;
 int sage_cache_evict(const sage_cache_evict_args* args);
+
+/* Norm of every head's queries and keys, and their rotation, in one pass - what models with normalised queries and keys do in front of
+ * attention.  Every row x of d channels becomes  R(x / sqrt(mean(x^2) + eps) * weight)  with R the rotation of sage_rope (its positions,
+ * frequencies and pairs); rounded once, at the end.  Sums are FP32.  Rows whose squares do not fit it, beyond 1.8e19, become zeros, as the division by
+ * infinity says; a value that is not finite reaches its own row only.  In place and views: as sage_rope. */
+enum { SAGE_WEIGHT_FP32 = 0, SAGE_WEIGHT_SAME = 1 };
+typedef struct sage_qk_norm_rope_args {
+  const void* q;            /* device, [B, H, N, d] or [B, N, H, d]; rows are aligned to 2 bytes at least (16 is fastest) */
+  const void* k;            /* device, [B, H_kv, N, d] or [B, N, H_kv, d]; NULL: q only */
+  void* q_out;
+  void* k_out;              /* NULL iff k is */
+  const void* q_weight;     /* device, [d], or NULL: ones */
+  const void* k_weight;     /* (must be NULL without k) */
+  int B, H, H_kv, N, d;
+  int rot_dim;              /* even, 0 .. d; 0: no rotation */
+  int dtype, layout;        /* SAGE_DT_*, SAGE_LAYOUT_* */
+  int weight_type;          /* SAGE_WEIGHT_FP32, or SAGE_WEIGHT_SAME: of the tensors' type */
+  int interleaved;          /* as sage_rope_args */
+  float eps;                /* finite, >= 0 */
+  float scale;              /* of the rotated channels, as sage_rope_args; 0 means 1 */
+  const double* inv_freq;   /* device, [rot_dim / 2]; not read if rot_dim = 0 */
+  const int* positions;     /* device, or NULL: token n stands at n.  positions[b * positions_stride + n] */
+  long long positions_stride;  /* 0: the same for every sequence */
+  long long offset;         /* added to every position; 2^52 at most, either way */
+  long long q_strides[3], k_strides[3], q_out_strides[3], k_out_strides[3];   /* batch, head, token, in elements; all 0: contiguous in `layout` */
+  void* stream;
+} sage_qk_norm_rope_args;
+int sage_qk_norm_rope(const sage_qk_norm_rope_args* args);
+
+/* Its gradient: from that of q_out and k_out, and q and k as they went in, that of q, k and the weights.  With g the gradient turned back,
+ * r = 1 / sqrt(mean(x^2) + eps):  dweight = sum over rows of g x r;  dx = r (g weight - x r^2 mean(g weight x)).  The sums over rows are taken in a
+ * fixed order, FP32 within a workgroup and FP64 over them.  dq may be dq_out and dk dk_out (then with the same strides). */
+typedef struct sage_qk_norm_rope_bwd_args {
+  const void* dq_out;       /* device, shaped like q */
+  const void* dk_out;       /* NULL iff k is */
+  const void* q;
+  const void* k;
+  void* dq;
+  void* dk;                 /* NULL iff k is */
+  const void* q_weight;
+  const void* k_weight;
+  float* dq_weight;         /* device, [d] f32, or NULL: not wanted */
+  float* dk_weight;
+  int B, H, H_kv, N, d, rot_dim, dtype, layout, weight_type, interleaved;
+  float eps, scale;
+  const double* inv_freq;
+  const int* positions;
+  long long positions_stride, offset;
+  long long dq_out_strides[3], dk_out_strides[3], q_strides[3], k_strides[3], dq_strides[3], dk_strides[3];
+  void* workspace;          /* device, 256-byte aligned; may be NULL where the size is 0 */
+  size_t workspace_bytes;
+  void* stream;
+} sage_qk_norm_rope_bwd_args;
+size_t sage_qk_norm_rope_bwd_workspace_bytes(const sage_qk_norm_rope_bwd_args* args);   /* 0: none is needed (no weight's gradient is wanted), or the arguments are invalid */
+int sage_qk_norm_rope_bwd(const sage_qk_norm_rope_bwd_args* args);
+
+/* A cache in 8 bits and in pages.  It is four arrays over a pool of n_pages pages of `page` tokens (a multiple of 32):
+ *   k_cache, v_cache  [n_pages, H_kv, page, d]        E4M3 codes
+ *   k_scale, v_scale  [n_pages, H_kv, page / 32]      one byte for each block of 32 tokens and head: the scale 2^(byte - 127); 255: NaN
+ * and page_table [B, max_pages] int32: token t of sequence b stands in page page_table[b, t / page], place t % page; a value is its code times
+ * its block's scale.  E4M3's step is relative, so powers of two lose nothing to finer scales, and dividing by them is exact: a code is its value
+ * correctly rounded.  kv_lens counts the tokens of each sequence, up to max_pages * page.  A number that is no page of the pool (-1, say: a page that was
+ * given back) stands for no page: its tokens are not there - never written, and seen by no query.  Sequences may share pages.
+ *
+ * The append of a call's new tokens: of the N rows of sequence b in k and v the first new_lens[b] (NULL: N) are new; they are the
+ * last of the kv_lens[b] tokens that the sequence has WITH them (kv_lens as the attention call after it takes it; more new than that: the first ones are left out).
+ * The scale of a block without earlier tokens is the smallest power of two of which 448 times is its largest new magnitude or more,
+ * 2^-64 at least and at most 2^119 for bf16, 2^7 for fp16 tokens (whose largest values are kept as 448 times that).  A block that holds earlier tokens
+ * keeps its scale, or, where the new ones need a larger one, gets that, and the earlier codes are rounded once more: to the same value but for
+ * those below 2^-6 of the new scale.  A value that is not finite becomes NaN and does not count for the scale.  Codes behind the last token stay as they were.
+ * No page that new tokens go to may belong to another sequence's new tokens too. */
+typedef struct sage_cache_append_args {
+  const void* k;            /* device, [B, H_kv, N, d] or [B, N, H_kv, d]; fp16 or bf16; rows are aligned to 2 bytes at least (16 is fastest) */
+  const void* v;
+  void* k_cache;            /* 16-byte aligned */
+  void* v_cache;
+  void* k_scale;
+  void* v_scale;
+  const int* page_table;    /* device, [B, max_pages] */
+  const int* kv_lens;       /* device, [B], or NULL: max_pages * page for all */
+  const int* new_lens;      /* device, [B], or NULL: N for all; cut to 0 .. N */
+  int B, H_kv, N, d;
+  int n_pages, page, max_pages;
+  int dtype, layout;
+  long long k_strides[3], v_strides[3];   /* batch, head, token, in elements; all 0: contiguous in `layout` */
+  void* stream;
+} sage_cache_append_args;
+int sage_cache_append(const sage_cache_append_args* args);
+
+/* Attention of N queries per sequence over such a cache:  out = softmax(sm_scale Q K^T) V.  Scores, softmax and sums are FP32, the products
+ * 16-bit (codes are exact in them; P is rounded to the 16-bit type).  The first q_lens[b] queries of sequence b are there (NULL: all N);
+ * those behind are not read and their places in out and lse stay as they were.  Query r stands at p = max(len - q_len, 0) + r.  causal: it
+ * sees the tokens t <= p; with window > 0, of these, t > p - window and, whatever the window, the first `sink` of the sequence.  Without causal it sees all
+ * len (and window must be 0).  What no query sees is not read: a sequence's pages behind its window can be given back.  A query that sees no token gets zeros
+ * and lse = -inf; a NaN reaches only queries that see its token.  With fp16 queries values of V beyond 65504 count as infinite.  out may be q. */
+typedef struct sage_attn_paged_args {
+  const void* q;            /* device, [B, H, N, d] or [B, N, H, d] */
+  const void* k_cache;      /* as above */
+  const void* v_cache;
+  const void* k_scale;
+  const void* v_scale;
+  void* out;                /* device, like q */
+  const int* page_table;
+  const int* kv_lens;       /* device, [B], or NULL: max_pages * page for all */
+  const int* q_lens;        /* device, [B], or NULL: N for all; cut to 0 .. N */
+  float* lse;               /* device, [B, H, N] f32, or NULL */
+  int B, H, H_kv, N, d;
+  int n_pages, page, max_pages;
+  int causal, window, sink; /* window 0: none; sink counts only with a window */
+  float sm_scale;           /* <= 0 means 1/sqrt(d) */
+  int dtype, layout;
+  void* workspace;          /* device, 256-byte aligned; may be NULL where the size is 0 */
+  size_t workspace_bytes;
+  void* stream;
+} sage_attn_paged_args;
+size_t sage_attn_paged_workspace_bytes(const sage_attn_paged_args* args);   /* 0: none is needed, or the arguments are invalid */
+int sage_attn_paged(const sage_attn_paged_args* args);
 
 const char* sage_status_string(int status);
 

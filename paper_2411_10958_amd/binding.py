@@ -85,6 +85,36 @@ class sage_cache_evict_args(ctypes.Structure):
                [("stream", ctypes.c_void_p), ("clear", ctypes.c_int)]
 
 
+class sage_qk_norm_rope_args(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("q", "k", "q_out", "k_out", "q_weight", "k_weight")] + \
+               [(n, ctypes.c_int) for n in ("B", "H", "H_kv", "N", "d", "rot_dim", "dtype", "layout", "weight_type", "interleaved")] + \
+               [("eps", ctypes.c_float), ("scale", ctypes.c_float), ("inv_freq", ctypes.c_void_p), ("positions", ctypes.c_void_p),
+                ("positions_stride", ctypes.c_longlong), ("offset", ctypes.c_longlong)] + \
+               [(n, ctypes.c_longlong * 3) for n in ("q_strides", "k_strides", "q_out_strides", "k_out_strides")] + [("stream", ctypes.c_void_p)]
+
+
+class sage_qk_norm_rope_bwd_args(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("dq_out", "dk_out", "q", "k", "dq", "dk", "q_weight", "k_weight", "dq_weight", "dk_weight")] + \
+               [(n, ctypes.c_int) for n in ("B", "H", "H_kv", "N", "d", "rot_dim", "dtype", "layout", "weight_type", "interleaved")] + \
+               [("eps", ctypes.c_float), ("scale", ctypes.c_float), ("inv_freq", ctypes.c_void_p), ("positions", ctypes.c_void_p),
+                ("positions_stride", ctypes.c_longlong), ("offset", ctypes.c_longlong)] + \
+               [(n, ctypes.c_longlong * 3) for n in ("dq_out_strides", "dk_out_strides", "q_strides", "k_strides", "dq_strides", "dk_strides")] + \
+               [("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t), ("stream", ctypes.c_void_p)]
+
+
+class sage_cache_append_args(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("k", "v", "k_cache", "v_cache", "k_scale", "v_scale", "page_table", "kv_lens", "new_lens")] + \
+               [(n, ctypes.c_int) for n in ("B", "H_kv", "N", "d", "n_pages", "page", "max_pages", "dtype", "layout")] + \
+               [(n, ctypes.c_longlong * 3) for n in ("k_strides", "v_strides")] + [("stream", ctypes.c_void_p)]
+
+
+class sage_attn_paged_args(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("q", "k_cache", "v_cache", "k_scale", "v_scale", "out", "page_table", "kv_lens", "q_lens", "lse")] + \
+               [(n, ctypes.c_int) for n in ("B", "H", "H_kv", "N", "d", "n_pages", "page", "max_pages", "causal", "window", "sink")] + \
+               [("sm_scale", ctypes.c_float), ("dtype", ctypes.c_int), ("layout", ctypes.c_int), ("workspace", ctypes.c_void_p),
+                ("workspace_bytes", ctypes.c_size_t), ("stream", ctypes.c_void_p)]
+
+
 def lib_path():
     """The in-tree library; SAGEATTN_LIB may name another build of the same sources."""
     return os.environ.get("SAGEATTN_LIB") or os.path.join(_PKG, "libsageattn.so")
@@ -121,10 +151,11 @@ def load_library():
         lib.sage_attn_debug_qk.argtypes = [P(sage_attn_args)] + [ctypes.c_int] * 4 + [ctypes.c_void_p]
         lib.sage_attn_debug_mfma_fp8.restype = ctypes.c_int
         lib.sage_attn_debug_mfma_fp8.argtypes = [ctypes.c_void_p] * 5
-        for name in ("sage_rope", "sage_attn_shared_prefix", "sage_attn_key_weights", "sage_cache_evict"):
+        for name in ("sage_rope", "sage_attn_shared_prefix", "sage_attn_key_weights", "sage_cache_evict", "sage_qk_norm_rope", "sage_qk_norm_rope_bwd",
+                     "sage_cache_append", "sage_attn_paged"):
             getattr(lib, name).restype = ctypes.c_int
             getattr(lib, name).argtypes = [P(globals()[name + "_args"])]
-        for name in ("sage_attn_shared_prefix", "sage_attn_key_weights"):
+        for name in ("sage_attn_shared_prefix", "sage_attn_key_weights", "sage_qk_norm_rope_bwd", "sage_attn_paged"):
             getattr(lib, name + "_workspace_bytes").restype = ctypes.c_size_t
             getattr(lib, name + "_workspace_bytes").argtypes = [P(globals()[name + "_args"])]
         lib.sage_rope_frequencies.restype = ctypes.c_int
@@ -413,6 +444,7 @@ def sage_attn_debug_mfma_fp8(a_codes, b_codes, c_in):
 # ---- operators around the attention calls: rotary positions, a shared prefix, key weights, eviction ----
 
 SAGE_ROPE_PLAIN, SAGE_ROPE_LINEAR, SAGE_ROPE_BASE, SAGE_ROPE_PARTS = 0, 1, 2, 3
+SAGE_WEIGHT_FP32, SAGE_WEIGHT_SAME = 0, 1
 _ROPE_SCALINGS = {"plain": 0, "linear": 1, "base": 2, "parts": 3, 0: 0, 1: 1, 2: 2, 3: 3}
 
 
@@ -716,3 +748,200 @@ def sage_cache_evict(k, v, weights, n_keep, sink=0, recent=0, kv_lens=None, layo
                               raw_stream, int(clear))
     _call("sage_cache_evict", a, index)
     return tuple(outs)
+
+
+def _set_strides(field, t, packed, nhd):
+    """Batch, head and token strides of t into a field of an argument structure; left at zeros for a contiguous tensor."""
+    if t is None or t.is_contiguous():
+        return
+    s = t.stride()
+    if s[-1] != 1:
+        raise ValueError("the channels of a row must be contiguous")
+    if packed:
+        s = (0,) + s[:-1]
+    field[0], field[1], field[2] = (s[0], s[2], s[1]) if nhd else s[:3]
+    if not any(field):
+        raise ValueError("one row expanded over all others is not supported (strides of zero stand for a contiguous tensor)")
+
+
+def _norm_rope_fields(q, k, inv_freq, q_weight, k_weight, eps, positions, offset, interleaved, scale, layout):
+    """What the two calls have in common, checked: (fields of the argument structures, index, packed, nhd)."""
+    dtype, index = _dtype_code(q), _gpu_of("q", q)
+    packed = q.dim() == 3
+    if not packed and q.dim() != 4:
+        raise ValueError(f"q must have 4 dimensions, or 3 if packed, got {q.dim()}")
+    nhd = 1 if packed else _LAYOUTS[layout]
+    B, H, N, d = (1, q.shape[1], q.shape[0], q.shape[2]) if packed else _sizes("q", q, nhd)
+    Hkv = 0
+    if k is not None:
+        if k.get_device() != index or k.dtype != q.dtype or k.dim() != q.dim():
+            raise ValueError("k must have the type, device and number of dimensions of q")
+        Bk, Hkv, Nk, dk = (1, k.shape[1], k.shape[0], k.shape[2]) if packed else _sizes("k", k, nhd)
+        if (Bk, Nk, dk) != (B, N, d):
+            raise ValueError("k shape does not match q")
+    elif k_weight is not None:
+        raise ValueError("k_weight without k")
+    if q.numel() == 0 or (k is not None and Hkv == 0):
+        raise ValueError("q or k is empty")
+    rot = 0
+    if inv_freq is not None:
+        _need("inv_freq", inv_freq, index, torch.float64)
+        if inv_freq.dim() != 1 or inv_freq.numel() == 0:
+            raise ValueError("inv_freq must have one dimension and a frequency at least")
+        rot = 2 * inv_freq.numel()
+    if positions is not None:
+        _need("positions", positions, index, torch.int32)
+        if positions.shape != (N,) and positions.shape != (B, N):
+            raise ValueError(f"positions must have shape ({N},) or ({B}, {N}), got {tuple(positions.shape)}")
+    elif packed and rot:
+        raise ValueError("a packed batch needs positions")
+    weights = [w for w in (q_weight, k_weight) if w is not None]
+    for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
+        if w is not None:
+            if w.dtype not in (torch.float32, q.dtype) or w.dtype != weights[0].dtype:
+                raise TypeError(f"the weights must both be float32 or both {q.dtype}, got {name} of {w.dtype}")
+            _need(name, w, index, w.dtype, (d,))
+    return dict(q=q.data_ptr(), k=_address(k), q_weight=_address(q_weight), k_weight=_address(k_weight), B=B, H=H, H_kv=Hkv, N=N, d=d, rot_dim=rot, dtype=dtype,
+                layout=nhd, weight_type=SAGE_WEIGHT_SAME if weights and weights[0].dtype != torch.float32 else SAGE_WEIGHT_FP32, interleaved=int(bool(interleaved)),
+                eps=float(eps), scale=float(scale), inv_freq=_address(inv_freq), positions=_address(positions),
+                positions_stride=N if positions is not None and positions.dim() == 2 else 0, offset=_whole(offset, 64)), index, packed, nhd
+
+
+def _output_like(name, x, y, index, stream):
+    if x is None:
+        return None
+    if y is None:
+        return _new(x.shape, x.dtype, index, stream)
+    if y.get_device() != index or y.dtype != x.dtype or y.shape != x.shape:
+        raise ValueError(f"{name} must have the type, shape and device of its input")
+    return y
+
+
+def sage_qk_norm_rope(q, k=None, inv_freq=None, q_weight=None, k_weight=None, eps=1e-6, positions=None, offset=0, interleaved=False, scale=1.0, layout="HND",
+                      q_out=None, k_out=None, stream=None):
+    """Every row of q and k divided by the root of its mean square (plus eps), times the weight of its channels (float32 or the tensors' type, [d]; None:
+    ones), and its first 2 * len(inv_freq) channels turned as sage_rope does (inv_freq None: none), in one pass.  q [B, H, N, d], k [B, H_kv, N, d] or None
+    (layout "HND"; tokens outside heads with "NHD"), or packed [tokens, heads, d]; any strides will do while the channels are contiguous.  q_out, k_out may be q and
+    k.  Returns q_out, or (q_out, k_out)."""
+    f, index, packed, nhd = _norm_rope_fields(q, k, inv_freq, q_weight, k_weight, eps, positions, offset, interleaved, scale, layout)
+    raw_stream = _stream_on(index, stream)
+    if k is None and k_out is not None:
+        raise ValueError("k_out without k")
+    q_out, k_out = _output_like("q_out", q, q_out, index, stream), _output_like("k_out", k, k_out, index, stream)
+    a = sage_qk_norm_rope_args(q_out=q_out.data_ptr(), k_out=_address(k_out), stream=raw_stream, **f)
+    for t, st in ((q, a.q_strides), (k, a.k_strides), (q_out, a.q_out_strides), (k_out, a.k_out_strides)):
+        _set_strides(st, t, packed, nhd)
+    _call("sage_qk_norm_rope", a, index)
+    return q_out if k is None else (q_out, k_out)
+
+
+def sage_qk_norm_rope_bwd_workspace_bytes(args):
+    """The size of the workspace to hand to sage_qk_norm_rope_bwd, 0 if it needs none.  args: a sage_qk_norm_rope_bwd_args, of which the sizes, dtype, layout, k and
+    whether the weights' gradients are wanted are looked at."""
+    return int(load_library().sage_qk_norm_rope_bwd_workspace_bytes(ctypes.byref(args)))
+
+
+def sage_qk_norm_rope_bwd(dq_out, q, dk_out=None, k=None, inv_freq=None, q_weight=None, k_weight=None, eps=1e-6, positions=None, offset=0, interleaved=False,
+                          scale=1.0, layout="HND", dq=None, dk=None, dq_weight=None, dk_weight=None, workspace=None, stream=None):
+    """The gradient of sage_qk_norm_rope: from that of its outputs, dq_out and dk_out, and its inputs, (dq, dk, dq_weight, dk_weight); dk is None
+    without k.  The weights' are float32 [d], and None for a weight that is None.  dq may be dq_out, and dk dk_out."""
+    f, index, packed, nhd = _norm_rope_fields(q, k, inv_freq, q_weight, k_weight, eps, positions, offset, interleaved, scale, layout)
+    raw_stream = _stream_on(index, stream)
+    if (k is None) != (dk_out is None) or (k is None and dk is not None):
+        raise ValueError("k, its gradient and that of its output go together")
+    for name, x, g in (("dq_out", q, dq_out), ("dk_out", k, dk_out)):
+        if x is not None and (g.get_device() != index or g.dtype != x.dtype or g.shape != x.shape):
+            raise ValueError(f"{name} must have the type, shape and device of its input")
+    dq, dk = _output_like("dq", q, dq, index, stream), _output_like("dk", k, dk, index, stream)
+    grads = []
+    for name, w, g in (("dq_weight", q_weight, dq_weight), ("dk_weight", k_weight, dk_weight)):
+        if w is None:
+            if g is not None:
+                raise ValueError(f"{name} without its weight")
+        elif g is None:
+            g = _new((f["d"],), torch.float32, index, stream)
+        else:
+            _need(name, g, index, torch.float32, (f["d"],))
+        grads.append(g)
+    a = sage_qk_norm_rope_bwd_args(dq_out=dq_out.data_ptr(), dk_out=_address(dk_out), dq=dq.data_ptr(), dk=_address(dk), dq_weight=_address(grads[0]),
+                                   dk_weight=_address(grads[1]), stream=raw_stream, **f)
+    for t, st in ((dq_out, a.dq_out_strides), (dk_out, a.dk_out_strides), (q, a.q_strides), (k, a.k_strides), (dq, a.dq_strides), (dk, a.dk_strides)):
+        _set_strides(st, t, packed, nhd)
+    keep = _own_workspace("sage_qk_norm_rope_bwd", a, index, workspace, stream)
+    _call("sage_qk_norm_rope_bwd", a, index)
+    del keep
+    return dq, dk, grads[0], grads[1]
+
+
+def _paged_cache(k_cache, v_cache, k_scale, v_scale, page_table, index, B, Hkv, d):
+    """The arrays of a cache in pages, checked: (pages, tokens of a page, pages of a sequence)."""
+    if k_cache.dim() != 4 or page_table.dim() != 2:
+        raise ValueError("k_cache must have 4 dimensions and page_table 2")
+    pages, heads, page, dc = k_cache.shape
+    if heads != Hkv or dc != d:
+        raise ValueError(f"k_cache must have shape [pages, {Hkv}, page, {d}], got {tuple(k_cache.shape)}")
+    if page % 32 != 0 or page == 0:
+        raise ValueError(f"a page must hold a multiple of 32 tokens, got {page}")
+    _need("k_cache", k_cache, index, torch.float8_e4m3fn)
+    _need("v_cache", v_cache, index, torch.float8_e4m3fn, k_cache.shape)
+    _need("k_scale", k_scale, index, torch.float8_e8m0fnu, (pages, Hkv, page // 32))
+    _need("v_scale", v_scale, index, torch.float8_e8m0fnu, (pages, Hkv, page // 32))
+    _need("page_table", page_table, index, torch.int32, (B, page_table.shape[1]))
+    return pages, page, page_table.shape[1]
+
+
+def sage_cache_append(k, v, k_cache, v_cache, k_scale, v_scale, page_table, kv_lens=None, new_lens=None, layout="HND", stream=None):
+    """Writes new tokens k, v [B, H_kv, N, d] (layout "NHD": tokens outside heads; any strides will do while the channels are contiguous) into a cache in 8
+    bits and pages: k_cache, v_cache float8_e4m3fn [pages, H_kv, page, d], k_scale, v_scale float8_e8m0fnu [pages, H_kv, page / 32], one power of two for
+    each block of 32 tokens; page_table int32 [B, pages of a sequence], a number that is no page stands for none.  kv_lens (int32 [B]; None: the
+    table's capacity): tokens of each sequence with the new ones, of which the first new_lens (int32 [B]; None: N) rows are the last."""
+    dtype, index, nhd = _dtype_code(k), _gpu_of("k", k), _LAYOUTS[layout]
+    raw_stream = _stream_on(index, stream)
+    B, Hkv, N, d = _sizes("k", k, nhd)
+    if v.get_device() != index or v.dtype != k.dtype or v.shape != k.shape:
+        raise ValueError("v must have the type, shape and device of k")
+    pages, page, max_pages = _paged_cache(k_cache, v_cache, k_scale, v_scale, page_table, index, B, Hkv, d)
+    for name, t in (("kv_lens", kv_lens), ("new_lens", new_lens)):
+        if t is not None:
+            _need(name, t, index, torch.int32, (B,))
+    a = sage_cache_append_args(k.data_ptr(), v.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), page_table.data_ptr(),
+                               _address(kv_lens), _address(new_lens), B, Hkv, N, d, pages, page, max_pages, dtype, nhd)
+    a.stream = raw_stream
+    _set_strides(a.k_strides, k, False, nhd)
+    _set_strides(a.v_strides, v, False, nhd)
+    _call("sage_cache_append", a, index)
+
+
+def sage_attn_paged_workspace_bytes(args):
+    """The size of the workspace to hand to sage_attn_paged, 0 if it needs none.  args: a sage_attn_paged_args, of which the sizes, dtype, layout, causal, window and
+    sink are looked at."""
+    return int(load_library().sage_attn_paged_workspace_bytes(ctypes.byref(args)))
+
+
+def sage_attn_paged(q, k_cache, v_cache, k_scale, v_scale, page_table, kv_lens=None, q_lens=None, out=None, causal=True, window=0, sink=0, sm_scale=0.0,
+                    layout="HND", return_lse=False, workspace=None, stream=None):
+    """Attention of q [B, H, N, d] over a cache in 8 bits and pages (see sage_cache_append), of which the first kv_lens tokens (int32 [B]; None: the table's
+    capacity) of each sequence are in use.  The first q_lens queries (int32 [B]; None: N) of a sequence are there, the last of them aligned with its last
+    token if causal; the others' rows keep what they held (zeros where the output is allocated here).  window > 0: a query sees the last `window` tokens up
+    to its own and the first `sink`.  Returns out, or (out, lse) with lse float32 [B, H, N]."""
+    dtype, index, nhd = _dtype_code(q), _gpu_of("q", q), _LAYOUTS[layout]
+    raw_stream = _stream_on(index, stream)
+    B, H, N, d = _sizes("q", q, nhd)
+    _need("q", q, index, q.dtype)
+    pages, page, max_pages = _paged_cache(k_cache, v_cache, k_scale, v_scale, page_table, index, B, k_cache.shape[1] if k_cache.dim() == 4 else 0, d)
+    for name, t in (("kv_lens", kv_lens), ("q_lens", q_lens)):
+        if t is not None:
+            _need(name, t, index, torch.int32, (B,))
+    make = torch.empty if q_lens is None else torch.zeros
+    if out is None:
+        out = _new(q.shape, q.dtype, index, stream, make)
+    else:
+        _need("out", out, index, q.dtype, q.shape)
+    lse = _new((B, H, N), torch.float32, index, stream, make) if return_lse else None
+    a = sage_attn_paged_args(q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), out.data_ptr(), page_table.data_ptr(),
+                             _address(kv_lens), _address(q_lens), _address(lse), B, H, k_cache.shape[1], N, d, pages, page, max_pages, int(bool(causal)),
+                             _whole(window, 32), _whole(sink, 32), float(sm_scale), dtype, nhd, 0, 0, raw_stream)
+    keep = _own_workspace("sage_attn_paged", a, index, workspace, stream)
+    _call("sage_attn_paged", a, index)
+    del keep
+    return (out, lse) if return_lse else out

@@ -6,7 +6,8 @@ import sys
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 SOURCES = ["sage_api.hip", "sage_prologue.hip", "sage_attn_kernel.hip", "sage_attn_raw.hip", "sage_rope.hip",
-           "sage_attn_shared.hip", "sage_key_weights.hip", "sage_cache.hip"]
+           "sage_attn_shared.hip", "sage_key_weights.hip", "sage_cache.hip",
+           "sage_norm_rope.hip", "sage_cache_append.hip", "sage_attn_paged.hip"]
 LIB = os.path.join(PKG, "libsageattn.so")
 
 HIPCC_FLAGS = [
