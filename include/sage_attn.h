@@ -503,7 +503,8 @@ int sage_cache_append(const sage_cache_append_args* args);
  * those behind are not read and their places in out and lse stay as they were.  Query r stands at p = max(len - q_len, 0) + r.  causal: it
  * sees the tokens t <= p; with window > 0, of these, t > p - window and, whatever the window, the first `sink` of the sequence.  Without causal it sees all
  * len (and window must be 0).  What no query sees is not read: a sequence's pages behind its window can be given back.  A query that sees no token gets zeros
- * and lse = -inf; a NaN reaches only queries that see its token.  With fp16 queries values of V beyond 65504 count as infinite.  out may be q. */
+ * and lse = -inf; a NaN reaches only queries that see its token.
+ * out may be q; other overlaps of out, lse or the workspace are refused. */
 typedef struct sage_attn_paged_args {
   const void* q;            /* device, [B, H, N, d] or [B, N, H, d] */
   const void* k_cache;      /* as above */

@@ -1,13 +1,23 @@
 // Attention over a cache of 8 bits and pages (sage_attn_paged).
 //
-// O = softmax(kappa Q K^T) V with K = codes 2^ek, V = codes 2^ev, one exponent for each block of 32 tokens.  One wavefront per query: a block's 32
-// scores at a time, half of the channels in each half of the lanes, then its 32 weights times V, a few channels in each lane.
+// O = softmax(kappa Q K^T) V with K = codes 2^ek, V = codes 2^ev, one exponent for each block of 32 tokens.  E4M3 codes are exact in both 16-bit types, so
+// Q stays as it is and the products are 16-bit ones with FP32 sums.  A block is one 32 x 32 tile of scores: 2^ek is a scalar beside kappa, 2^ev goes into the instruction
+// that converts the codes of V.  Softmax in one pass with the running maximum m and sum l (Sec. 2.1, Eq. 1); chunks of the keys are independent workgroups that leave
+// (m, l, O), and a second kernel merges them: O = sum_i 2^(m_i - m) O_i / sum_i 2^(m_i - m) l_i.
+// P is rounded to the 16-bit type for its product with V (half a step, which averages out over the keys).  fp16 has no numbers for weights below 2^-25 of the largest, which
+// are in the sum all the same: there m is kept 14 below the maximum, so that weights are up to 2^14 and vanish from 2^-39 of the largest on.
+//
+// With few queries it reads the cache and nothing else should bound it.  A block's K (or V) is 32 d contiguous bytes whatever the size of a page; each wavefront copies its own blocks
+// into LDS, two tiles ahead.  Where all queries of a KV head are 32 rows at most, it also attends to just those blocks, with no barrier; more rows are divided over the wavefronts.
 #include "sage_paged.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace sage {
 namespace {
+
+constexpr int PT_BLOCKS = 4;         // blocks of a tile: one for each wavefront to copy
 
 struct PagedParams {
   PagedCache c;
@@ -15,75 +25,476 @@ struct PagedParams {
   unsigned short* out;
   float* lse;
   const int *lens, *qlens;
+  float *part_o, *part_ml;           // [chunk][B H_kv][G N][d], [chunk][B H_kv][G N][2]
   TensorMap qm;
   int B, H, N, G, cap;               // cap: max_pages * page
   int causal, window, sink;
   float kappa;                       // sm_scale log2(e)
+  int S, rt, units;                  // key chunks, row tiles, workgroups of one row tile: B H_kv S
+  FastDiv by_rt8, by_s, by_hkv, by_g, by_gn;      // 8 rt, S, H_kv, G, G N
 };
 
-// The tokens that query r sees: t < sink and from <= t < to.
+__device__ __forceinline__ int len_of(const PagedParams& p, int b) { return p.lens ? min(max(p.lens[b], 0), p.cap) : p.cap; }
+__device__ __forceinline__ int count_of(const PagedParams& p, int b) { return p.qlens ? min(max(p.qlens[b], 0), p.N) : p.N; }
+
+// The tokens that the query at `pos` sees: t < to, and t >= from or t < sink.
 struct Seen { int sink, from, to; };
-__device__ __forceinline__ Seen seen_by(const PagedParams& p, int len, int count, int r) {
-  const int pos = max(len - count, 0) + r;
+__device__ __forceinline__ Seen seen_from(const PagedParams& p, int len, int pos) {
   Seen s;
   s.to = p.causal ? min(len, pos + 1) : len;
   s.from = p.window > 0 ? max(pos + 1 - p.window, 0) : 0;
   s.sink = p.window > 0 ? min(p.sink, s.to) : 0;
   return s;
 }
+__device__ __forceinline__ bool sees(const Seen& s, int t) { return t < s.to && (t >= s.from || t < s.sink); }
 
-template <int D, bool BF16>
-__global__ void __launch_bounds__(64) k_paged(const PagedParams p) {
-  constexpr int C = D / 64;
-  __shared__ float s_q[D];
-  const int lane = threadIdx.x, col = lane & 31, half = lane >> 5;
-  const int r = blockIdx.x, h = blockIdx.y % p.H, b = blockIdx.y / p.H, hkv = h / p.G;
-  const int len = p.lens ? min(max(p.lens[b], 0), p.cap) : p.cap, count = p.qlens ? min(max(p.qlens[b], 0), p.N) : p.N;
-  if (r >= count) return;
-  const Seen s = seen_by(p, len, count, r);
-  const size_t row = row_offset(p.qm, head_offset_of(p.qm, b, h), r);
-  for (int c = lane; c < D; c += 64) s_q[c] = load16<BF16>(p.q[row + c]);
-  __syncthreads();
-  float m = -INFINITY, l = 0.0f, o[C] = {};
-  for (int i = 0; i * BLOCK < s.to; ++i) {
-    const int t0 = i * BLOCK;
-    if (t0 >= s.sink && t0 + BLOCK <= s.from) continue;
-    const long long at = pool_block(p.c, b, hkv, i);
-    if (at < 0) continue;
-    const unsigned* kr = reinterpret_cast<const unsigned*>(p.c.k + ((size_t)at * BLOCK + col) * D + half * (D / 2));
-    float x = 0.0f;
-    for (int c = 0; c < D / 8; ++c) {
-      const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)kr[c], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)kr[c], true);
-      const float* q = s_q + half * (D / 2) + 4 * c;
-      x += lo[0] * q[0] + lo[1] * q[1] + hi[0] * q[2] + hi[1] * q[3];
+// A block in LDS: 32 rows of D bytes, D / 16 pieces of 16; piece c of row r stands at piece c ^ turn(r), so that the pieces which a matrix operand takes together -
+// the same one of rows 0..3 and 8..11, or of rows 0..7 - fall on different banks.
+template <int D> __device__ __forceinline__ int turn(int r) {
+  const int x = ((r >> 2) ^ (r >> 3)) & 1;
+  if constexpr (D == 64) return ((r >> 1) & 1) | x << 1;
+  return (r & 3) | x << 2;
+}
+
+// Eight codes (two dwords) as 16-bit numbers times a power of two: exact but below fp16's normal numbers.
+template <bool BF16> __device__ __forceinline__ v4i widen(int u, int w, float scale) {
+  v4i a;
+  if constexpr (BF16) {
+    a[0] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((unsigned)u, scale, false));
+    a[1] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((unsigned)u, scale, true));
+    a[2] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((unsigned)w, scale, false));
+    a[3] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((unsigned)w, scale, true));
+  } else {
+    a[0] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((unsigned)u, scale, false));
+    a[1] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((unsigned)u, scale, true));
+    a[2] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((unsigned)w, scale, false));
+    a[3] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((unsigned)w, scale, true));
+  }
+  return a;
+}
+
+template <int D> constexpr int paged_occupancy() { return D == 64 ? 3 : D == 128 ? 2 : 1; }      // wavefronts per SIMD
+
+// RG: groups of 32 rows of a workgroup.  Its four wavefronts are RG row groups times 4 / RG key groups: wavefront w has row group w / KG and the blocks kg, kg + KG, .. of a
+// tile.  ONE: a workgroup takes all keys and leaves the output itself.
+template <int D, bool BF16, int RG, bool ONE>
+__global__ void __launch_bounds__(256, paged_occupancy<D>()) k_paged(const PagedParams p) {
+  constexpr int KS = D / 16, CT = D / 32, KG = 4 / RG, ROWS = 32 * RG;
+  constexpr unsigned BYTES = BLOCK * D;           // of a block of K or V
+  constexpr int COPIES = D / 32;                  // copies of 64 pieces of a block of K (or V)
+  __shared__ __align__(1024) v4i s_kv[2 * PT_BLOCKS * 2 * BYTES / 16];      // [stage][block][K, V]
+  __shared__ float s_ml[4][64];
+  const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
+  const int col = lane & 31, half = lane >> 5, kg = wave % KG, rg = wave / KG;
+
+  // ---- which rows and keys.  The row tiles of the same keys are 8 apart: workgroups go to the 8 XCDs in turn and each has a cache of its own.
+  unsigned rt = blockIdx.x;
+  unsigned unit = split_by(rt, p.by_rt8) * 8 + rt % 8;
+  rt /= 8;
+  if ((int)unit >= p.units) return;
+  unsigned s = unit;
+  const unsigned bh = split_by(s, p.by_s);
+  unsigned hkv = bh;
+  const unsigned b = split_by(hkv, p.by_hkv);
+  const int len = len_of(p, (int)b), count = count_of(p, (int)b);
+  const int rows = count * p.G, r0 = (int)rt * ROWS, nr = min(ROWS, rows - r0);      // rows: (query, head of the group)
+  if (nr <= 0) return;
+  const int coff = max(len - count, 0);
+  const Seen first = seen_from(p, len, coff + (int)div_by((unsigned)r0, p.by_g)), last = seen_from(p, len, coff + (int)div_by((unsigned)(r0 + nr - 1), p.by_g));
+  // Blocks that some row sees: those of the sinks, then from the first row's window to the last row's end
+  const int ns = (last.sink + BLOCK - 1) / BLOCK, w0 = max(ns, first.from / BLOCK), nb = ns + max((last.to + BLOCK - 1) / BLOCK - w0, 0);
+  const int tiles = (nb + PT_BLOCKS - 1) / PT_BLOCKS;
+  int j0 = 0, j1 = tiles;
+  if constexpr (!ONE) {
+    const int per = (int)div_by((unsigned)(tiles + p.S - 1), p.by_s);
+    j0 = min((int)s * per, tiles);
+    j1 = min(j0 + per, tiles);
+  }
+  const bool active = rg * 32 < nr;
+  const size_t part0 = ((size_t)s * (p.B * p.c.Hkv) + bh) * ((size_t)p.G * p.N) + r0;      // of the partial results' rows
+  if (!ONE && j0 >= j1) {                         // no keys: a partial result that the merge skips
+    for (int i = t; i < nr; i += 256) {
+      p.part_ml[(part0 + i) * 2] = -INFINITY;
+      p.part_ml[(part0 + i) * 2 + 1] = 0.0f;
     }
-    x = half_sum(x) * (p.kappa * scale_of(p.c.ks[at]));
-    const int t = t0 + col;
-    const bool see = t < s.to && (t >= s.from || t < s.sink);
-    x = see ? x : -INFINITY;
-    float top = x;
+    return;
+  }
+
+  // ---- the pool's block and the two scales of the next 16 tiles' blocks, one block a lane; 8 tiles are fetched at a time
+  int at_lo = -1, at_hi = -1, scales = 0;
+  auto fetch = [&](int j) {
+    const int slot = (j - j0) & 15, i = 4 * (j - slot) + lane;
+    if ((lane >> 2 & 8) != slot) return;
+    long long at = -1;
+    if (i < nb) at = pool_block(p.c, (int)b, (int)hkv, i < ns ? i : i - ns + w0);
+    at_lo = (int)at; at_hi = (int)(at >> 32);
+    scales = at >= 0 ? p.c.ks[at] | p.c.vs[at] << 8 : 0;
+  };
+  fetch(j0);
+
+  // ---- my row's query as the B operand: channels 32 u + 16 half + 0..15 are two steps
+  const int i0 = r0 + min(rg * 32 + col, nr - 1);
+  unsigned rh = (unsigned)i0;
+  const unsigned rn = split_by(rh, p.by_g);
+  const size_t qrow = row_offset(p.qm, head_offset_of(p.qm, (int)b, (int)(hkv * p.G + rh)), (int)rn);
+  v4i q[KS];
 #pragma unroll
-    for (int y = 16; y > 0; y >>= 1) top = fmaxf(top, __shfl_xor(top, y));
-    const float m_new = fmaxf(m, top), base = m_new == -INFINITY ? 0.0f : m_new, alpha = exp2f(m - base);
-    const float e = see ? exp2f(x - base) : 0.0f;
-    float sum = e;
+  for (int st = 0; st < KS; ++st) q[st] = *reinterpret_cast<const v4i*>(p.q + qrow + 32 * (st >> 1) + 16 * half + 8 * (st & 1));
+  const Seen mine = seen_from(p, len, coff + (int)rn);
+
+  // ---- copies
+  const unsigned lds0 = (unsigned)(size_t)(__attribute__((address_space(3))) char*)&s_kv[0];
+  unsigned offs[COPIES];
 #pragma unroll
-    for (int y = 16; y > 0; y >>= 1) sum += __shfl_xor(sum, y);
-    l = l * alpha + sum;
-    m = m_new;
-    const float vs = scale_of(p.c.vs[at]);
-    for (int c = 0; c < C; ++c) o[c] *= alpha;
-    for (int k = 0; k < BLOCK; ++k) {
-      if (!__shfl((int)see, k)) continue;
-      const float w = __shfl(e, k) * vs;
-      const unsigned char* v = p.c.v + ((size_t)at * BLOCK + k) * D + lane * C;
-      for (int c = 0; c < C; ++c) o[c] += w * __builtin_amdgcn_cvt_f32_fp8((int)v[c], 0);
+  for (int x = 0; x < COPIES; ++x) {
+    const int pc = x * 64 + lane, r = pc / (D / 16);
+    offs[x] = (unsigned)(r * D + ((pc % (D / 16)) ^ turn<D>(r)) * 16);
+  }
+  auto copy = [&](int j, int stage) __attribute__((always_inline)) -> bool {      // my block of tile j; whether there is one
+    const int at_lane = ((j - j0) & 15) * 4 + wave;
+    const int hi = __builtin_amdgcn_readlane(at_hi, at_lane);
+    if (hi < 0) return false;
+    const size_t at = (size_t)((unsigned long long)(unsigned)hi << 32 | (unsigned)__builtin_amdgcn_readlane(at_lo, at_lane)) * BYTES;
+    const unsigned char *gk = p.c.k + at, *gv = p.c.v + at;
+    const unsigned to = lds0 + (unsigned)(stage * PT_BLOCKS + wave) * (2 * BYTES);
+#pragma unroll
+    for (int x = 0; x < COPIES; ++x) {
+      dma_b128(gk, offs[x], to + x * 1024);
+      dma_b128(gv, offs[x], to + BYTES + x * 1024);
+    }
+    return true;
+  };
+  copy(j0, 0);
+#pragma unroll
+  for (int st = 0; st < KS; ++st)
+#pragma unroll
+    for (int x = 0; x < 4; ++x) use_now(q[st][x]);
+  bool next = j0 + 1 < j1 && copy(j0 + 1, 1);     // whether tile j + 1 is on its way
+
+  v16f o[CT];
+#pragma unroll
+  for (int c = 0; c < CT; ++c)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) o[c][v] = 0.0f;
+  float mx = -INFINITY, l = 0.0f;                 // running maximum (of both halves; fp16: less 14) and this half's sum
+
+  // Where my operands start in a block.  K: row of token 16 (g / 2) + 8h + 4 (g % 2) + r for operand row 8g + 4h + r, so that half h of the lanes gets scores of
+  // tokens 8h + 0..7 and 16 + 8h + 0..7, as the second product wants its weights; two pieces' steps are an exclusive or.  V: the transposed read gives lane l channel
+  // l % 16 of the eight tokens whose rows its group of 16 lanes point at, two lanes a row.
+  typedef __attribute__((address_space(3))) const v4i* lds_v4i;
+  typedef __attribute__((address_space(3))) v2i* lds_v2i;
+  const int kr = 16 * (col >> 4) + 8 * ((col >> 2) & 1) + 4 * ((col >> 3) & 1) + (col & 3), vr = 8 * half + ((lane & 15) >> 1);
+  const unsigned k_at = (unsigned)(kr * D + (half ^ turn<D>(kr)) * 16);
+  const unsigned v_at = BYTES + (unsigned)(vr * D + (((lane >> 4) & 1) ^ turn<D>(vr)) * 16 + 8 * (lane & 1));
+
+  // One block: scores, weights and their product with V.  PART: some row does not see some token of it.
+  constexpr int FITS = BF16 ? 246 : 134;           // 448 2^119 and 448 2^7 are numbers of the type
+  auto attend = [&](auto part, unsigned base, int t0, float kk, int ev) __attribute__((always_inline)) {
+    constexpr bool PART = decltype(part)::value;
+    const float vs = scale_of((unsigned)(PART ? min(ev, FITS) : ev));
+    v16f sc;
+#pragma unroll
+    for (int v = 0; v < 16; ++v) sc[v] = 0.0f;
+#pragma unroll
+    for (int u = 0; u < KS / 2; ++u) {
+      const v4i x = *(lds_v4i)(uintptr_t)(base + (k_at ^ (32 * u)));
+      sc = mfma16<BF16>(widen<BF16>(x[0], x[1], 1.0f), q[2 * u], sc);
+      sc = mfma16<BF16>(widen<BF16>(x[2], x[3], 1.0f), q[2 * u + 1], sc);
+    }
+    unsigned seen = 0xffff;                       // bit v: my row sees score v's token
+    if constexpr (PART) {
+      seen = 0;
+#pragma unroll
+      for (int v = 0; v < 16; ++v) {
+        const bool see = sees(mine, t0 + 16 * (v >> 3) + 8 * half + (v & 7));
+        seen |= (unsigned)see << v;
+        sc[v] = see ? sc[v] : -INFINITY;
+      }
+    }
+    float top = -INFINITY;
+#pragma unroll
+    for (int v = 0; v < 16; ++v) top = fmaxf(top, sc[v]);
+    top = half_max(top) * kk;
+    // (m is a whole step or less off for scores below 2^24, so weights stay below 2^15; beyond, where a step of 14 may be lost, none is taken)
+    if (!BF16) top = fabsf(top) < 16777216.0f ? top - 14.0f : top;
+    const float m_new = fmaxf(mx, top);
+    const float m = m_new == -INFINITY ? 0.0f : m_new;          // (no token seen yet: every weight 2^-inf)
+    if (__ballot(m_new > mx) != 0) {
+      const float alpha = __builtin_amdgcn_exp2f(mx - m);
+      l *= alpha;
+#pragma unroll
+      for (int c = 0; c < CT; ++c)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) o[c][v] *= alpha;
+      mx = m_new;
+    }
+    float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    v4i pb[2];
+#pragma unroll
+    for (int v = 0; v < 16; v += 2) {
+      float e0 = __builtin_amdgcn_exp2f(__fmaf_rn(sc[v], kk, -m)), e1 = __builtin_amdgcn_exp2f(__fmaf_rn(sc[v + 1], kk, -m));
+      if constexpr (PART) {                       // (where kk is NaN, or m infinite, a hidden token's weight would not be zero)
+        e0 = seen >> v & 1 ? e0 : 0.0f;
+        e1 = seen >> (v + 1) & 1 ? e1 : 0.0f;
+      }
+      sum[v & 2] += e0;
+      sum[(v & 2) + 1] += e1;
+      pb[v >> 3][(v & 7) >> 1] = (int)pack16x2<BF16>(e0, e1);
+    }
+    l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+    if constexpr (!PART) {
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+        for (int c = 0; c < CT; ++c) {
+          const v2i x = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_v2i)(uintptr_t)(base + (v_at ^ (32 * c)) + ks * 16 * D));
+          o[c] = mfma16<BF16>(widen<BF16>(x[0], x[1], vs), pb[ks], o[c]);
+        }
+    } else {
+      // A NaN among V times a weight of zero would reach rows that do not see it: NaN is taken out before the product.  How many of a channel's a row sees is a product
+      // too, of ones; where that is not zero, the output is NaN.  What no row sees counts as zeros.
+      constexpr unsigned UNIT = BF16 ? 0x3f80 : 0x3c00;
+      const float more = ev <= FITS ? 1.0f : scale_of((unsigned)(127 + ev - FITS));      // what vs leaves out
+      v4i sb[2];
+      unsigned keep[2][2];                        // bytes of tokens that some row sees
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+          keep[ks][y] = 0;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int tok = t0 + 16 * ks + 8 * half + 4 * y + e;
+            keep[ks][y] |= tok < last.to && (tok >= first.from || tok < last.sink) ? 0xffu << (8 * e) : 0u;
+          }
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const unsigned two = seen >> (8 * ks + 4 * y + 2 * e);
+            sb[ks][2 * y + e] = (int)((two & 1 ? UNIT : 0u) | (two & 2 ? UNIT << 16 : 0u));
+          }
+        }
+#pragma unroll
+      for (int c = 0; c < CT; ++c) {
+        unsigned nan[2][2];
+        v16f y16;
+#pragma unroll
+        for (int v = 0; v < 16; ++v) y16[v] = 0.0f;
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks) {
+          v2i x = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_v2i)(uintptr_t)(base + (v_at ^ (32 * c)) + ks * 16 * D));
+#pragma unroll
+          for (int y = 0; y < 2; ++y) {
+            const unsigned u = (unsigned)x[y] & keep[ks][y];
+            nan[ks][y] = ((u & 0x7f7f7f7fu) + 0x01010101u) >> 7 & 0x01010101u;      // 0x7f and 0xff
+            x[y] = (int)(u & ~(nan[ks][y] * 0xffu));
+          }
+          y16 = mfma16<BF16>(widen<BF16>(x[0], x[1], vs), pb[ks], y16);
+        }
+#pragma unroll
+        for (int v = 0; v < 16; ++v) o[c][v] = __fmaf_rn(y16[v], more, o[c][v]);
+        if (__ballot((nan[0][0] | nan[0][1] | nan[1][0] | nan[1][1]) != 0) != 0) {
+          v16f hits;
+#pragma unroll
+          for (int v = 0; v < 16; ++v) hits[v] = 0.0f;
+#pragma unroll
+          for (int ks = 0; ks < 2; ++ks) {
+            v4i a;
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+              const unsigned n = nan[ks][y];
+              a[2 * y] = (int)((n & 1 ? UNIT : 0u) | (n >> 8 & 1 ? UNIT << 16 : 0u));
+              a[2 * y + 1] = (int)((n >> 16 & 1 ? UNIT : 0u) | (n >> 24 & 1 ? UNIT << 16 : 0u));
+            }
+            hits = mfma16<BF16>(a, sb[ks], hits);
+          }
+#pragma unroll
+          for (int v = 0; v < 16; ++v) o[c][v] = hits[v] > 0.0f ? NAN : o[c][v];
+        }
+      }
+    }
+  };
+
+  constexpr int PER_TILE = 2 * COPIES;            // copies that a wavefront starts for a tile
+  for (int j = j0; j < j1; ++j) {
+    const int stage = (j - j0) & 1;
+    if (next) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(PER_TILE) : "memory");
+    else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    if constexpr (RG > 1) __builtin_amdgcn_s_barrier();      // tile j is there
+    asm volatile("" ::: "memory");
+    if (active) {
+#pragma unroll 1
+      for (int x = kg; x < PT_BLOCKS; x += KG) {
+        const int at_lane = ((j - j0) & 15) * 4 + x, i = 4 * j + x;
+        if (__builtin_amdgcn_readlane(at_hi, at_lane) < 0) continue;      // no tokens: past the last, or no page
+        const int two = __builtin_amdgcn_readlane(scales, at_lane), t0 = BLOCK * (i < ns ? i : i - ns + w0);
+        // A NaN among the scales makes the rows NaN that see the block, through kk.  Values that may not fit the 16-bit type go the way of partly seen blocks, which scales their
+        // product.
+        const int ev = two >> 8 == 255 ? 127 : two >> 8;
+        const float kk = two >> 8 == 255 ? NAN : p.kappa * scale_of((unsigned)two & 255);
+        const unsigned base = lds0 + (unsigned)(stage * PT_BLOCKS + x) * (2 * BYTES);
+        if (ev <= FITS && t0 + BLOCK <= first.to && (t0 >= last.from || t0 + BLOCK <= first.sink)) attend(std::false_type{}, base, t0, kk, ev);
+        else attend(std::true_type{}, base, t0, kk, ev);
+      }
+    }
+    next = false;
+    if (j + 2 < j1) {                             // the next tile but one takes this one's place when all have read it
+      if (((j + 2 - j0) & 7) == 0) fetch(j + 2);
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      if constexpr (RG > 1) __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+      next = copy(j + 2, stage);
+    } else {
+      next = false;
     }
   }
-  const bool none = m == -INFINITY && l == 0.0f;
-  const float inv = none ? 0.0f : 1.0f / l;
-  for (int c = 0; c < C; ++c) p.out[row + lane * C + c] = (unsigned short)pack16x2<BF16>(o[c] * inv, 0.0f);
-  if (p.lse && lane == 0) p.lse[((size_t)b * p.H + h) * p.N + r] = none ? -INFINITY : LN2 * (m + log2f(l));
+  l = half_sum(l);
+
+  // ---- the key groups of the same rows into one, each wavefront's share of the channels: units of four of them a lane, unit 4 c + g is channels 32 c + 8 g + 4 half + 0..3
+  constexpr int UN = 4 * CT / KG;
+  v4f res[UN];
+  if constexpr (KG == 1) {
+#pragma unroll
+    for (int u = 0; u < UN; ++u) res[u] = v4f{o[u / 4][4 * (u % 4)], o[u / 4][4 * (u % 4) + 1], o[u / 4][4 * (u % 4) + 2], o[u / 4][4 * (u % 4) + 3]};
+  } else {
+    v4f* x = reinterpret_cast<v4f*>(&s_kv[0]);
+    __syncthreads();
+    if (active) {
+#pragma unroll
+      for (int u = 0; u < 4 * CT; ++u)
+        x[(wave * 4 * CT + u) * 64 + lane] = v4f{o[u / 4][4 * (u % 4)], o[u / 4][4 * (u % 4) + 1], o[u / 4][4 * (u % 4) + 2], o[u / 4][4 * (u % 4) + 3]};
+      if (half == 0) {
+        s_ml[wave][2 * col] = mx;
+        s_ml[wave][2 * col + 1] = l;
+      }
+    }
+    __syncthreads();
+    if (active) {
+      float a[KG], m = -INFINITY;
+#pragma unroll
+      for (int k = 0; k < KG; ++k) m = fmaxf(m, s_ml[rg * KG + k][2 * col]);
+      l = 0.0f;
+#pragma unroll
+      for (int k = 0; k < KG; ++k) {
+        a[k] = __builtin_amdgcn_exp2f(s_ml[rg * KG + k][2 * col] - (m == -INFINITY ? 0.0f : m));
+        l = __fmaf_rn(a[k], s_ml[rg * KG + k][2 * col + 1], l);
+      }
+      mx = m;
+#pragma unroll
+      for (int u = 0; u < UN; ++u) {
+        res[u] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int k = 0; k < KG; ++k) {
+          const v4f y = x[((rg * KG + k) * 4 * CT + kg * UN + u) * 64 + lane];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) res[u][e] = __fmaf_rn(a[k], y[e], res[u][e]);
+        }
+      }
+    }
+  }
+  if (!active || rg * 32 + col >= nr) return;
+  if constexpr (ONE) {
+    const bool none = mx == -INFINITY && l == 0.0f;      // no token at all: zeros
+    const float inv = none ? 0.0f : __fdiv_rn(1.0f, l);
+    if (p.lse && half == 0 && kg == 0) p.lse[((size_t)b * p.H + hkv * p.G + rh) * p.N + rn] = none ? -INFINITY : LN2 * (mx + __builtin_amdgcn_logf(l));
+    unsigned short* y = p.out + qrow + 4 * half;
+#pragma unroll
+    for (int u = 0; u < UN; ++u)
+      *reinterpret_cast<uint2*>(y + 8 * (kg * UN + u)) = make_uint2(pack16x2<BF16>(res[u][0] * inv, res[u][1] * inv), pack16x2<BF16>(res[u][2] * inv, res[u][3] * inv));
+  } else {
+    const size_t pr = part0 + rg * 32 + col;
+    if (half == 0 && kg == 0) {
+      p.part_ml[pr * 2] = mx;
+      p.part_ml[pr * 2 + 1] = l;
+    }
+    float* po = p.part_o + pr * D + 4 * half;
+#pragma unroll
+    for (int u = 0; u < UN; ++u) *reinterpret_cast<v4f*>(po + 8 * (kg * UN + u)) = res[u];
+  }
+}
+
+// The partial results of a row into its output, a wavefront per row, or per 64 channels of 256: lane s looks at partial results s, s + 64, .. for the maximum and the weights;
+// then a lane takes four channels of every GRP-th partial result, MERGE_LOADS of them in flight.  Bound by the two trips to memory, not by bytes.
+template <int D> constexpr int merge_channels() { return D == 256 ? 64 : D; }
+constexpr int MERGE_LOADS = 8, MERGE_PER_LANE = 2, MAX_PARTS = 64 * MERGE_PER_LANE;
+template <int D, bool BF16>
+__global__ void __launch_bounds__(256) k_paged_merge(const PagedParams p) {
+  constexpr int MC = merge_channels<D>(), LPR = MC / 4, GRP = 64 / LPR, SLICES = D / MC;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const unsigned rows = (unsigned)p.B * p.H * p.N;
+  const unsigned row = blockIdx.x * (4 / SLICES) + (unsigned)wave / SLICES;
+  if (row >= rows) return;
+  unsigned g = row;                               // row: (batch and KV head, query, head of the group)
+  unsigned hkv = split_by(g, p.by_gn);
+  const unsigned b = split_by(hkv, p.by_hkv), n = split_by(g, p.by_g);
+  if ((int)n >= count_of(p, (int)b)) return;
+  const int S = p.S, c = MC * (wave % SLICES) + 4 * (lane % LPR), grp = lane / LPR;
+  float ms[MERGE_PER_LANE], w[MERGE_PER_LANE], m = -INFINITY, l = 0.0f;
+#pragma unroll
+  for (int x = 0; x < MERGE_PER_LANE; ++x) {
+    ms[x] = -INFINITY; w[x] = 0.0f;
+    if (64 * x + lane < S) {
+      const float2 ml = *reinterpret_cast<const float2*>(p.part_ml + ((size_t)(64 * x + lane) * rows + row) * 2);
+      ms[x] = ml.x; w[x] = ml.y;
+    }
+    m = fmaxf(m, ms[x]);
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
+#pragma unroll
+  for (int x = 0; x < MERGE_PER_LANE; ++x) {
+    const float ls = w[x];
+    w[x] = ms[x] == -INFINITY && ls == 0.0f ? -1.0f : __builtin_amdgcn_exp2f(ms[x] - m);    // (-1: no token is seen: O may not even be there)
+    if (w[x] != -1.0f) l = __fmaf_rn(w[x], ls, l);
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) l += __shfl_xor(l, o);
+  v4f acc = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+  for (int x = 0; x < MERGE_PER_LANE; ++x) {
+    const int end = min(S - 64 * x, 64);
+    for (int s0 = 0; s0 < end; s0 += GRP * MERGE_LOADS) {
+      v4f o4[MERGE_LOADS];
+      float ws[MERGE_LOADS];
+#pragma unroll
+      for (int k = 0; k < MERGE_LOADS; ++k) {
+        const int s = s0 + k * GRP + grp;
+        ws[k] = __shfl(w[x], s & 63);
+        ws[k] = s < end ? ws[k] : -1.0f;
+        o4[k] = *reinterpret_cast<const v4f*>(p.part_o + ((size_t)(64 * x + min(s, end - 1)) * rows + row) * D + c);
+      }
+#pragma unroll
+      for (int k = 0; k < MERGE_LOADS; ++k)
+#pragma unroll
+        for (int y = 0; y < 4; ++y) acc[y] = ws[k] == -1.0f ? acc[y] : __fmaf_rn(ws[k], o4[k][y], acc[y]);
+    }
+  }
+#pragma unroll
+  for (int o = LPR; o < 64; o <<= 1)
+#pragma unroll
+    for (int y = 0; y < 4; ++y) acc[y] += __shfl_xor(acc[y], o);
+  if (grp != 0) return;
+  const unsigned h = hkv * p.G + g;
+  const bool none = m == -INFINITY && l == 0.0f;  // no token at all: zeros
+  const float inv = none ? 0.0f : __fdiv_rn(1.0f, l);
+  if (p.lse && c == 0) p.lse[((size_t)b * p.H + h) * p.N + n] = none ? -INFINITY : LN2 * (m + __builtin_amdgcn_logf(l));
+  unsigned short* y = p.out + row_offset(p.qm, head_offset_of(p.qm, (int)b, (int)h), (int)n) + c;
+  *reinterpret_cast<uint2*>(y) = make_uint2(pack16x2<BF16>(acc[0] * inv, acc[1] * inv), pack16x2<BF16>(acc[2] * inv, acc[3] * inv));
+}
+
+int row_groups(const PagedParams& p) { return p.G * p.N <= 32 ? 1 : p.G * p.N <= 64 ? 2 : 4; }
+
+// Key chunks of a row tile.  The chip has room for `places` workgroups; lengths that the host does not know are cut fine, so that it fills up to the end.
+void choose_chunks(PagedParams* p, int d) {
+  const int rg = row_groups(*p);
+  const long long gn = (long long)p->G * p->N;
+  p->rt = (int)((gn + 32 * rg - 1) / (32 * rg));
+  long long keys = p->cap;
+  if (p->window > 0) keys = std::min(keys, (long long)p->sink + p->window + std::min((long long)p->N, (32LL * rg + p->G - 1) / p->G + 1) + 2 * BLOCK);
+  const long long tiles = (keys + BLOCK * PT_BLOCKS - 1) / (BLOCK * PT_BLOCKS);
+  const long long heads = (long long)p->B * p->c.Hkv * p->rt, places = 256LL * (d == 64 ? 3 : d == 128 ? 2 : 1);
+  const long long share = std::max(2LL, std::min(12LL, (heads * tiles + places - 1) / places));
+  p->S = heads >= 2 * places || tiles <= 4 ? 1 : (int)std::min((tiles + share - 1) / share, (long long)MAX_PARTS);
+  p->units = p->B * p->c.Hkv * p->S;
 }
 
 int paged_params(const sage_attn_paged_args* a, PagedParams* p, bool need_io) {
@@ -105,13 +516,33 @@ int paged_params(const sage_attn_paged_args* a, PagedParams* p, bool need_io) {
   p->B = a->B; p->H = a->H; p->N = a->N; p->G = a->H / a->H_kv; p->cap = a->max_pages * a->page;
   p->causal = a->causal; p->window = std::min(a->window, MAX_TOKENS * 2); p->sink = std::min(a->sink, MAX_TOKENS);
   p->kappa = (a->sm_scale > 0.0f ? a->sm_scale : (float)(1.0 / std::sqrt((double)a->d))) * LOG2E;
+  choose_chunks(p, a->d);
+  if (((long long)p->units + 7) / 8 * 8 * p->rt * 256 > MAX_THREADS) return SAGE_ERR_UNSUPPORTED;
+  p->by_rt8 = fast_div(8u * p->rt); p->by_s = fast_div(p->S); p->by_hkv = fast_div(a->H_kv); p->by_g = fast_div(p->G);
+  p->by_gn = fast_div((unsigned)p->G * a->N);
   return SAGE_OK;
 }
 
-template <int D> void launch(const PagedParams& p, bool bf16, hipStream_t s) {
-  const dim3 grid((unsigned)p.N, (unsigned)(p.B * p.H));
-  if (bf16) k_paged<D, true><<<grid, 64, 0, s>>>(p);
-  else k_paged<D, false><<<grid, 64, 0, s>>>(p);
+size_t part_rows(const PagedParams& p) { return p.S > 1 ? (size_t)p.S * p.B * p.H * p.N : 0; }
+size_t paged_bytes(const PagedParams& p, int d) { return align256(part_rows(p) * 2 * sizeof(float)) + align256(part_rows(p) * d * sizeof(float)); }
+
+template <int D, bool BF16> hipError_t launch(const PagedParams& p, hipStream_t s) {
+  const unsigned grid = (unsigned)((p.units + 7) / 8 * 8) * p.rt;
+  const int rg = row_groups(p);
+  if (p.S == 1) {
+    if (rg == 1) k_paged<D, BF16, 1, true><<<grid, 256, 0, s>>>(p);
+    else if (rg == 2) k_paged<D, BF16, 2, true><<<grid, 256, 0, s>>>(p);
+    else k_paged<D, BF16, 4, true><<<grid, 256, 0, s>>>(p);
+    return hipGetLastError();
+  }
+  if (rg == 1) k_paged<D, BF16, 1, false><<<grid, 256, 0, s>>>(p);
+  else if (rg == 2) k_paged<D, BF16, 2, false><<<grid, 256, 0, s>>>(p);
+  else k_paged<D, BF16, 4, false><<<grid, 256, 0, s>>>(p);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  const unsigned per = 4 * merge_channels<D>() / D;
+  k_paged_merge<D, BF16><<<((unsigned)(p.B * p.H) * p.N + per - 1) / per, 256, 0, s>>>(p);
+  return hipGetLastError();
 }
 
 }  // namespace
@@ -122,14 +553,14 @@ using namespace sage;
 extern "C" size_t sage_attn_paged_workspace_bytes(const sage_attn_paged_args* a) {
   PagedParams p;
   if (paged_params(a, &p, false) != SAGE_OK) return 0;
-  return 0;
+  return paged_bytes(p, a->d);
 }
 
 extern "C" int sage_attn_paged(const sage_attn_paged_args* a) {
   PagedParams p;
   const int st = paged_params(a, &p, true);
   if (st != SAGE_OK) return st;
-  const size_t rows = (size_t)a->B * a->H * a->N, blocks = cache_blocks(p.c), bytes = blocks * BLOCK * a->d, need = 0;
+  const size_t rows = (size_t)a->B * a->H * a->N, blocks = cache_blocks(p.c), bytes = blocks * BLOCK * a->d, need = paged_bytes(p, a->d);
   if (need > 0 && (!a->workspace || a->workspace_bytes < need || ((uintptr_t)a->workspace & 255u) != 0)) return SAGE_ERR_WORKSPACE;
   // (a row's query is read before its output is written, by the same workgroup or a kernel before: out may be q)
   const Span in[8] = {{a->out == a->q ? nullptr : a->q, rows * a->d * 2}, {a->k_cache, bytes}, {a->v_cache, bytes}, {a->k_scale, blocks}, {a->v_scale, blocks},
@@ -139,10 +570,13 @@ extern "C" int sage_attn_paged(const sage_attn_paged_args* a) {
     for (const Span& x : in) if (overlap(out[i], x)) return SAGE_ERR_INVALID_ARG;
     for (int j = 0; j < i; ++j) if (overlap(out[i], out[j])) return SAGE_ERR_INVALID_ARG;
   }
+  p.part_ml = (float*)a->workspace;
+  p.part_o = (float*)((char*)a->workspace + align256(part_rows(p) * 2 * sizeof(float)));
   const hipStream_t s = (hipStream_t)a->stream;
   const bool bf16 = a->dtype == SAGE_DT_BF16;
-  if (a->d == 64) launch<64>(p, bf16, s);
-  else if (a->d == 128) launch<128>(p, bf16, s);
-  else launch<256>(p, bf16, s);
-  return op_status(hipGetLastError());
+  hipError_t e;
+  if (a->d == 64) e = bf16 ? launch<64, true>(p, s) : launch<64, false>(p, s);
+  else if (a->d == 128) e = bf16 ? launch<128, true>(p, s) : launch<128, false>(p, s);
+  else e = bf16 ? launch<256, true>(p, s) : launch<256, false>(p, s);
+  return op_status(e);
 }

@@ -221,3 +221,14 @@ def test_the_same_twice_and_on_a_stream():
     again = pa.sage_attn_paged(q, **c, kv_lens=lens, return_lse=True)
     for a, b, d in zip(want, got, again):
         assert torch.equal(a, b) and torch.equal(a, d)
+
+
+def test_a_larger_workspace_and_a_small_one():
+    pa = _pa()
+    c = pref.filled(2, 2, 8192, 64, 128, torch.bfloat16)
+    q = _q(2, 8, 1, 128, torch.bfloat16, "HND")
+    want = pa.sage_attn_paged(q, **c)
+    room = torch.full((1 << 26,), 0xff, dtype=torch.uint8, device="cuda")
+    assert torch.equal(pa.sage_attn_paged(q, **c, workspace=room), want)
+    with pytest.raises(pa.SageError):
+        pa.sage_attn_paged(q, **c, workspace=room[:256])
