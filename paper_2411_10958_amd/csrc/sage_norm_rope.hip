@@ -3,14 +3,15 @@
 // y = R(x r w), r = 1 / sqrt(mean(x^2) + eps), R the rotation of sage_rope.hip.  With g = R^T dy:  dw = sum over rows of g x r  and, since
 // x r has a norm of its own that no step along x changes,  dx = r (g w - x r^2 mean(g w x)).  Both sums of a row, x^2 and g w x, are taken
 // in one go, so every value is read once.
-// A row is d / 16 neighbouring threads, each with 8 pairs of channels in registers; a thread works the angles and weights of its channels out once and then walks over
-// the heads of its token.  Only bytes bound it: 4 a value forward, 6 backward.
+// A row is d / 16 neighbouring threads, each with 8 pairs of channels in registers.  A workgroup takes the heads of a few tokens: it works their angles out
+// once, an angle a thread, and leaves them and the weights in LDS.  Only bytes bound it: 4 a value forward, 6 backward.
 #include "sage_attn.h"
 #include "sage_quant.h"
 #include "sage_rows.h"
 
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 namespace sage {
 namespace {
@@ -27,10 +28,13 @@ struct NormParams {
   NormTensor q, k;                       // k.heads = 0 without keys
   const double* inv_freq;
   const int* positions;                  // null: the token's index
-  long long pos_sb, offset, total;       // total: threads of all tokens
-  int N, d, rot, units, hchunk, lanes;   // threads of a row; heads of a workgroup, and those side by side in it
+  long long pos_sb, offset;
+  unsigned tokens;                       // B N
+  int d, rot, units, hchunk;             // threads of a row; heads of a workgroup
+  int lanes, at_once, heads_first;       // of a workgroup: heads side by side, tokens; which of them neighbouring threads are
   int weight_same;
   float eps, scale;
+  FastDiv by_n, by_pairs, by_lanes, by_at_once;      // N, rot / 2
 };
 
 // Sum over the `units` neighbouring threads of a row, in all of them.
@@ -42,28 +46,24 @@ __device__ __forceinline__ float row_sum(float x, int units) {
   return x;
 }
 
-// The 16 channels of a thread of a row, in vectors of VW: pairs 8 u .. 8 u + 7, of which the first rot / 2 of the row are turned.  Neighbours (INTER) are
-// channels 16 u .. 16 u + 15 in order; otherwise the first VW * NV / 2 are the pairs' first channels and the others their second ones, and what
-// is not turned is split like what is.
+// The 16 channels of a thread of a row, in vectors of VW, eight here and eight there so that a row's threads read stretches of d bytes.  Channels i and rot / 2 + i are a pair: pairs
+// 8 u .. 8 u + 7, first channels first; what is not turned is split like what is.  Neighbours (INTER): channels 8 u .. 8 u + 7 and as many d / 2 on.
+template <bool INTER> __device__ __forceinline__ int channel_of(int i, int u, int rot, int d) {      // of the thread's value i
+  if (INTER) return 8 * u + (i & 7) + (i < 8 ? 0 : d / 2);
+  const int pair = 8 * u + (i & 7);
+  return pair + (pair < rot / 2 ? (i < 8 ? 0 : rot / 2) : (i < 8 ? rot / 2 : d / 2));
+}
 template <int VW, bool INTER> struct Channels {
-  static constexpr int NV = 16 / VW;
-  int at[NV];
+  int at[16 / VW];                       // of each vector's first
   __device__ __forceinline__ Channels(int u, int rot, int d) {
 #pragma unroll
-    for (int s = 0; s < NV; ++s) {
-      if (INTER) {
-        at[s] = 16 * u + VW * s;
-      } else {
-        const int pair = 8 * u + VW * (s % (NV / 2));
-        const bool turned = pair < rot / 2, second = s >= NV / 2;
-        at[s] = pair + (second ? (turned ? rot / 2 : d / 2) : (turned ? 0 : rot / 2));
-      }
-    }
+    for (int s = 0; s < 16 / VW; ++s) at[s] = channel_of<INTER>(VW * s, u, rot, d);
   }
 };
-// Where pair i of a thread is among its 16 channels.
+// Where pair i of a thread is among its 16 channels, and which pair of the row it is.
 template <bool INTER> __device__ __forceinline__ constexpr int first_of(int i) { return INTER ? 2 * i : i; }
 template <bool INTER> __device__ __forceinline__ constexpr int second_of(int i) { return INTER ? 2 * i + 1 : 8 + i; }
+template <bool INTER> __device__ __forceinline__ int pair_of(int i, int u, int d) { return INTER ? 4 * u + (i & 3) + (i < 4 ? 0 : d / 4) : 8 * u + i; }
 
 template <bool BF16, int VW> __device__ __forceinline__ void unpack16(const typename Vec<VW>::type (&v)[16 / VW], float (&x)[16]) {
 #pragma unroll
@@ -95,118 +95,195 @@ template <bool BF16, int VW, bool PAST> __device__ __forceinline__ void store_ro
     else *to = v;
   }
 }
-template <bool BF16, int VW> __device__ __forceinline__ void load_weight(float (&w)[16], const void* from, int same, const int (&at)[16 / VW]) {
-#pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    const int c = at[i / VW] + i % VW;
-    w[i] = !from ? 1.0f : same ? load16<BF16>(reinterpret_cast<const unsigned short*>(from)[c]) : reinterpret_cast<const float*>(from)[c];
+// What a workgroup shares: the weights, [q, k][d], and cosines and sines of its tokens' angles, [token][rot / 2], taken as in sage_rope.hip.
+constexpr int MAX_AT_ONCE = 64;          // tokens of a workgroup: 256 threads, 4 a row at least
+constexpr int CS_ENTRIES = 2048;         // (64 tokens of 64 channels, 32 of 128, 16 of 256)
+struct NormShared {
+  float w[512];
+  float2 cs[CS_ENTRIES];
+};
+template <bool BF16> __device__ __forceinline__ void share_weights(const NormParams& p, NormShared& sh) {
+  for (int i = threadIdx.x; i < 2 * p.d; i += 256) {
+    const void* w = i < p.d ? p.q.w : p.k.w;
+    const int c = i < p.d ? i : i - p.d;
+    sh.w[i] = !w ? 1.0f : p.weight_same ? load16<BF16>(reinterpret_cast<const unsigned short*>(w)[c]) : reinterpret_cast<const float*>(w)[c];
   }
 }
-
-// Which token, head and channels a thread has, and the angles of its pairs; angles are taken as in sage_rope.hip.
-struct Place { long long b; int n, unit, hl; };
-__device__ __forceinline__ Place place_of(const NormParams& p, long long id) {
-  Place a;
-  const long long th = id / p.units, tok = th / p.lanes;
-  a.unit = (int)(id - th * p.units);
-  a.hl = (int)(th - tok * p.lanes);
-  a.b = tok / p.N;
-  a.n = (int)(tok - a.b * p.N);
-  return a;
-}
-__device__ __forceinline__ void angles(const NormParams& p, const Place& a, float (&c)[8], float (&s)[8]) {
-  if (16 * a.unit >= p.rot) return;
-  const double pos = (double)((p.positions ? (long long)p.positions[a.b * p.pos_sb + a.n] : (long long)a.n) + p.offset);
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const double turns = 8 * a.unit + i < p.rot / 2 ? pos * p.inv_freq[8 * a.unit + i] * 0.15915494309189533577 : 0.0;      // 1 / (2 pi)
+__device__ __forceinline__ void share_angles(const NormParams& p, NormShared& sh, unsigned tok0) {
+  const int pairs = p.rot / 2;
+  for (int i = threadIdx.x; i < p.at_once * pairs; i += 256) {
+    unsigned pair = (unsigned)i;
+    const unsigned tok = tok0 + split_by(pair, p.by_pairs);
+    if (tok >= p.tokens) break;
+    unsigned n = tok;
+    const unsigned b = split_by(n, p.by_n);
+    const double pos = (double)((p.positions ? (long long)p.positions[(long long)b * p.pos_sb + n] : (long long)n) + p.offset);
+    const double turns = pos * p.inv_freq[pair] * 0.15915494309189533577;      // 1 / (2 pi)
     float si, co;
     sincospif(2.0f * (float)(turns - rint(turns)), &si, &co);
-    c[i] = __fmul_rn(co, p.scale);
-    s[i] = __fmul_rn(si, p.scale);
+    sh.cs[i] = make_float2(__fmul_rn(co, p.scale), __fmul_rn(si, p.scale));
   }
 }
 
-// Grid: (threads of all tokens / 256, pieces of the heads, what of the first does not fit a dimension).  PAST: reads and writes pass the caches by.
+// Which row of a workgroup a thread has, and its channels.
+struct Place { int unit, token, lane; };
+__device__ __forceinline__ Place place_of(const NormParams& p) {
+  Place a;
+  a.unit = (int)(threadIdx.x & (unsigned)(p.units - 1));
+  unsigned row = threadIdx.x / (unsigned)p.units;
+  if (p.heads_first) {
+    a.token = (int)split_by(row, p.by_lanes);
+    a.lane = (int)row;
+  } else {
+    a.lane = (int)split_by(row, p.by_at_once);
+    a.token = (int)row;
+  }
+  return a;
+}
+template <int VW> __device__ __forceinline__ void weights_of(float (&w)[16], const float* from, const int (&at)[16 / VW]) {
+#pragma unroll
+  for (int s = 0; s < 16 / VW; ++s) {
+    if constexpr (VW >= 4) {
+#pragma unroll
+      for (int i = 0; i < VW / 4; ++i) {
+        const v4f y = *reinterpret_cast<const v4f*>(from + at[s] + 4 * i);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[VW * s + 4 * i + e] = y[e];
+      }
+    } else {
+      w[s] = from[at[s]];
+    }
+  }
+}
+// Cosines and sines of a thread's pairs: 1 and 0 for what is not turned.  Whether any is.
+template <bool INTER> __device__ __forceinline__ bool angles_of(const NormParams& p, const NormShared& sh, const Place& a, float (&c)[8], float (&s)[8]) {
+  const int pairs = p.rot / 2;
+  bool any = false;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int pair = pair_of<INTER>(i, a.unit, p.d);
+    c[i] = 1.0f;
+    s[i] = 0.0f;
+    if (pair < pairs) {
+      const float2 y = sh.cs[a.token * pairs + pair];
+      c[i] = y.x;
+      s[i] = y.y;
+      any = true;
+    }
+  }
+  return any;
+}
+// A thread's pairs turned, or turned back.  (A value that is not finite makes its neighbour NaN where nothing is turned: the row has a NaN or zeros in all other
+// places anyway.)
+template <bool INTER, bool BACK> __device__ __forceinline__ void turn(float (&x)[16], const float (&c)[8], const float (&s)[8]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float f = x[first_of<INTER>(i)], g = x[second_of<INTER>(i)], t = BACK ? -s[i] : s[i];
+    x[first_of<INTER>(i)] = __fmaf_rn(f, c[i], -__fmul_rn(g, t));
+    x[second_of<INTER>(i)] = __fmaf_rn(g, c[i], __fmul_rn(f, t));
+  }
+}
+
+// Grid: (groups of tokens, pieces of the heads).  PAST: reads and writes pass the caches by.
 template <bool BF16, int VW, bool INTER, bool PAST>
 __global__ void __launch_bounds__(256) k_norm_rope(const NormParams p) {
-  const long long id = ((long long)blockIdx.z * gridDim.x + blockIdx.x) * 256 + threadIdx.x;
-  if (id >= p.total) return;             // (whole rows)
-  const Place a = place_of(p, id);
+  __shared__ __align__(16) NormShared sh;
+  typedef typename Vec<VW>::type V;
+  constexpr int HU = VW == 8 ? 4 : 1;    // heads whose loads are in flight together
+  const Place a = place_of(p);
   const Channels<VW, INTER> ch(a.unit, p.rot, p.d);
-  const int pairs = p.rot / 2 - 8 * a.unit;       // pairs of mine that are turned: the first
+  const unsigned tok0 = blockIdx.x * (unsigned)p.at_once, tok = tok0 + a.token;
+  const int heads = p.q.heads + p.k.heads, h0 = blockIdx.y * p.hchunk, h1 = min(h0 + p.hchunk, heads);
+  const bool there = tok < p.tokens;
+  unsigned n = there ? tok : p.tokens - 1;
+  const unsigned b = split_by(n, p.by_n);
+  const unsigned short *xq = p.q.x + b * p.q.xs[0] + n * p.q.xs[2], *xk = p.k.x + b * p.k.xs[0] + n * p.k.xs[2];
+  auto row_of = [&](int h) { return h < p.q.heads ? xq + h * p.q.xs[1] : xk + (h - p.q.heads) * p.k.xs[1]; };
+  V v[HU][16 / VW];
+#pragma unroll
+  for (int i = 0; i < HU; ++i) load_row<VW, PAST>(v[i], row_of(min(h0 + a.lane + i * p.lanes, h1 - 1)), ch.at);
+  share_weights<BF16>(p, sh);
+  share_angles(p, sh, tok0);
+  __syncthreads();
+  if (!there) return;                    // (whole rows)
   float c[8], s[8];
-  angles(p, a, c, s);
+  const bool turned = angles_of<INTER>(p, sh, a, c, s);
   const float inv_d = 1.0f / (float)p.d;
-  auto run = [&](const NormTensor& t, int ha, int hb) {
-    float w[16];
-    load_weight<BF16, VW>(w, t.w, p.weight_same, ch.at);
-    const unsigned short* x0 = t.x + a.b * t.xs[0] + (long long)a.n * t.xs[2];
-    unsigned short* y0 = t.y + a.b * t.ys[0] + (long long)a.n * t.ys[2];
-    for (int h = ha + a.hl; h < hb; h += p.lanes) {
-      typename Vec<VW>::type v[16 / VW];
-      load_row<VW, PAST>(v, x0 + (long long)h * t.xs[1], ch.at);
-      float x[16];
-      unpack16<BF16, VW>(v, x);
+  for (int hh = h0 + a.lane; hh < h1; hh += HU * p.lanes) {
+#pragma unroll
+    for (int k = 0; k < HU; ++k) {
+      const int h = hh + k * p.lanes;
+      if (h >= h1) break;
+      float x[16], w[16];
+      unpack16<BF16, VW>(v[k], x);
+      weights_of<VW>(w, sh.w + (h < p.q.heads ? 0 : p.d), ch.at);
       float sum = 0.0f;
 #pragma unroll
       for (int i = 0; i < 16; ++i) sum = __fmaf_rn(x[i], x[i], sum);
       const float r = rsqrtf(__fmaf_rn(row_sum(sum, p.units), inv_d, p.eps));
 #pragma unroll
       for (int i = 0; i < 16; ++i) x[i] = x[i] * r * w[i];
-      if (pairs > 0) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const float f = x[first_of<INTER>(i)], g = x[second_of<INTER>(i)];
-          x[first_of<INTER>(i)] = i < pairs ? __fmaf_rn(f, c[i], -__fmul_rn(g, s[i])) : f;
-          x[second_of<INTER>(i)] = i < pairs ? __fmaf_rn(g, c[i], __fmul_rn(f, s[i])) : g;
-        }
-      }
-      store_row<BF16, VW, PAST>(x, y0 + (long long)h * t.ys[1], ch.at);
+      if (turned) turn<INTER, false>(x, c, s);
+      unsigned short* y = h < p.q.heads ? p.q.y + b * p.q.ys[0] + n * p.q.ys[2] + h * p.q.ys[1] : p.k.y + b * p.k.ys[0] + n * p.k.ys[2] + (h - p.q.heads) * p.k.ys[1];
+      store_row<BF16, VW, PAST>(x, y, ch.at);
     }
-  };
-  const int h0 = blockIdx.y * p.hchunk, h1 = min(h0 + p.hchunk, p.q.heads + p.k.heads);
-  if (h0 < p.q.heads) run(p.q, h0, min(h1, p.q.heads));
-  if (h1 > p.q.heads) run(p.k, max(h0 - p.q.heads, 0), h1 - p.q.heads);
+    if (hh + HU * p.lanes < h1) {
+#pragma unroll
+      for (int i = 0; i < HU; ++i) load_row<VW, PAST>(v[i], row_of(min(hh + (HU + i) * p.lanes, h1 - 1)), ch.at);
+    }
+  }
 }
 
-// A workgroup walks over every gridDim.x-th 256 threads of all tokens, and leaves its sums for the weights' gradients.
+// A workgroup walks over every gridDim.x-th group of tokens, and leaves its sums for the weights' gradients.
 constexpr int BWD_GROUPS = 1024;         // workgroups at most
 template <bool BF16, int VW, bool INTER, bool PAST>
 __global__ void __launch_bounds__(256) k_norm_rope_bwd(const NormParams p) {
+  __shared__ __align__(16) NormShared sh;
   __shared__ float s_dw[4][512];         // [wavefront][q, k][channel]
-  float dw[2][16];
+  typedef typename Vec<VW>::type V;
+  constexpr int HU = VW == 8 ? 2 : 1;    // heads whose loads are in flight together
+  float dw[32];                          // of q, of k
 #pragma unroll
-  for (int i = 0; i < 16; ++i) dw[0][i] = dw[1][i] = 0.0f;
+  for (int i = 0; i < 32; ++i) dw[i] = 0.0f;
+  const Place a = place_of(p);
+  const Channels<VW, INTER> ch(a.unit, p.rot, p.d);
   const float inv_d = 1.0f / (float)p.d;
   const int h0 = blockIdx.y * p.hchunk, h1 = min(h0 + p.hchunk, p.q.heads + p.k.heads);
-  const Channels<VW, INTER> ch((int)(threadIdx.x % p.units), p.rot, p.d);      // (256 is a multiple of the units: the same for all tokens)
-  for (long long id = (long long)blockIdx.x * 256 + threadIdx.x; id < p.total; id += (long long)gridDim.x * 256) {
-    const Place a = place_of(p, id);
-    const int pairs = p.rot / 2 - 8 * a.unit;
-    float c[8], s[8];
-    angles(p, a, c, s);
-    auto run = [&](const NormTensor& t, int ha, int hb, float (&acc)[16]) {
-      float w[16];
-      load_weight<BF16, VW>(w, t.w, p.weight_same, ch.at);
-      const unsigned short* x0 = t.x + a.b * t.xs[0] + (long long)a.n * t.xs[2];
-      const unsigned short* g0 = t.dy + a.b * t.gs[0] + (long long)a.n * t.gs[2];
-      unsigned short* y0 = t.y + a.b * t.ys[0] + (long long)a.n * t.ys[2];
-      for (int h = ha + a.hl; h < hb; h += p.lanes) {
-        typename Vec<VW>::type v[16 / VW], u[16 / VW];
-        load_row<VW, PAST>(v, x0 + (long long)h * t.xs[1], ch.at);
-        load_row<VW, PAST>(u, g0 + (long long)h * t.gs[1], ch.at);
-        float x[16], g[16];
-        unpack16<BF16, VW>(v, x);
-        unpack16<BF16, VW>(u, g);
-        if (pairs > 0) {
+  share_weights<BF16>(p, sh);
+  for (unsigned tok0 = blockIdx.x * (unsigned)p.at_once; tok0 < p.tokens; tok0 += gridDim.x * (unsigned)p.at_once) {
+    const unsigned tok = tok0 + a.token;
+    const bool there = tok < p.tokens;
+    unsigned n = there ? tok : p.tokens - 1;
+    const unsigned b = split_by(n, p.by_n);
+    V v[HU][16 / VW], u[HU][16 / VW];
+    auto load = [&](int hh) {
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const float f = g[first_of<INTER>(i)], e = g[second_of<INTER>(i)];
-            g[first_of<INTER>(i)] = i < pairs ? __fmaf_rn(f, c[i], __fmul_rn(e, s[i])) : f;
-            g[second_of<INTER>(i)] = i < pairs ? __fmaf_rn(e, c[i], -__fmul_rn(f, s[i])) : e;
-          }
-        }
+      for (int k = 0; k < HU; ++k) {
+        int h = min(hh + k * p.lanes, h1 - 1);
+        const NormTensor& t = h < p.q.heads ? p.q : p.k;
+        h -= h < p.q.heads ? 0 : p.q.heads;
+        load_row<VW, PAST>(v[k], t.x + b * t.xs[0] + n * t.xs[2] + h * t.xs[1], ch.at);
+        load_row<VW, PAST>(u[k], t.dy + b * t.gs[0] + n * t.gs[2] + h * t.gs[1], ch.at);
+      }
+    };
+    load(h0 + a.lane);
+    __syncthreads();                     // (the angles of the group before have been read)
+    share_angles(p, sh, tok0);
+    __syncthreads();
+    if (!there) continue;
+    float c[8], s[8];
+    const bool turned = angles_of<INTER>(p, sh, a, c, s);
+    for (int hh = h0 + a.lane; hh < h1; hh += HU * p.lanes) {
+#pragma unroll
+      for (int k = 0; k < HU; ++k) {
+        const int h = hh + k * p.lanes;
+        if (h >= h1) break;
+        const bool key = h >= p.q.heads;
+        float x[16], g[16], w[16];
+        unpack16<BF16, VW>(v[k], x);
+        unpack16<BF16, VW>(u[k], g);
+        weights_of<VW>(w, sh.w + (key ? p.d : 0), ch.at);
+        if (turned) turn<INTER, true>(g, c, s);
         float squares = 0.0f, dot = 0.0f;
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
@@ -215,32 +292,49 @@ __global__ void __launch_bounds__(256) k_norm_rope_bwd(const NormParams p) {
         }
         const float r = rsqrtf(__fmaf_rn(row_sum(squares, p.units), inv_d, p.eps));
         const float m = row_sum(dot, p.units) * inv_d * r * r;
+        if (!key) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          acc[i] = __fmaf_rn(g[i], x[i] * r, acc[i]);
-          x[i] = r * __fmaf_rn(-x[i], m, g[i] * w[i]);
+          for (int i = 0; i < 16; ++i) dw[i] = __fmaf_rn(g[i], x[i] * r, dw[i]);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) dw[16 + i] = __fmaf_rn(g[i], x[i] * r, dw[16 + i]);
         }
-        store_row<BF16, VW, PAST>(x, y0 + (long long)h * t.ys[1], ch.at);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[i] = r * __fmaf_rn(-x[i], m, g[i] * w[i]);
+        const NormTensor& t = key ? p.k : p.q;
+        store_row<BF16, VW, PAST>(x, t.y + b * t.ys[0] + n * t.ys[2] + (h - (key ? p.q.heads : 0)) * t.ys[1], ch.at);
       }
-    };
-    if (h0 < p.q.heads) run(p.q, h0, min(h1, p.q.heads), dw[0]);
-    if (h1 > p.q.heads) run(p.k, max(h0 - p.q.heads, 0), h1 - p.q.heads, dw[1]);
+      if (hh + HU * p.lanes < h1) load(hh + HU * p.lanes);
+    }
   }
-  if (!p.q.part && !p.k.part) return;
-  // Threads of the same channels: those of a wavefront by shuffles, then the four wavefronts'
+  if (!p.q.part) return;
+  // Threads of the same channels, 64 / units of a wavefront: each step leaves half of the values in either half of them (30 exchanges, not 32 a step)
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int first = 0;
+  auto halve = [&](auto left, int o) {
+    constexpr int H = decltype(left)::value / 2;
+    if (o < p.units) return;
+    const bool up = (lane & o) != 0;
 #pragma unroll
-  for (int k = 0; k < 2; ++k)
+    for (int i = 0; i < H; ++i) {
+      const float mine = up ? dw[H + i] : dw[i], other = up ? dw[i] : dw[H + i];
+      dw[i] = mine + __shfl_xor(other, o);
+    }
+    first += up ? H : 0;
+  };
+  halve(std::integral_constant<int, 32>{}, 32);
+  halve(std::integral_constant<int, 16>{}, 16);
+  halve(std::integral_constant<int, 8>{}, 8);
+  halve(std::integral_constant<int, 4>{}, 4);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      float x = dw[k][i];
-      for (int o = p.units; o < 64; o <<= 1) x += __shfl_xor(x, o);
-      if (lane < p.units) s_dw[wave][k * p.d + ch.at[i / VW] + i % VW] = x;
+  for (int i = 0; i < 8; ++i)
+    if (i < p.units / 2) {
+      const int at = first + i;
+      s_dw[wave][(at >> 4) * p.d + channel_of<INTER>(at & 15, a.unit, p.rot, p.d)] = dw[i];
     }
   __syncthreads();
-  float* part = p.q.part ? p.q.part : p.k.part;
   const size_t group = (size_t)blockIdx.y * gridDim.x + blockIdx.x;
-  for (int i = threadIdx.x; i < 2 * p.d; i += 256) part[group * 2 * p.d + i] = (s_dw[0][i] + s_dw[1][i]) + (s_dw[2][i] + s_dw[3][i]);
+  for (int i = threadIdx.x; i < 2 * p.d; i += 256) p.q.part[group * 2 * p.d + i] = (s_dw[0][i] + s_dw[1][i]) + (s_dw[2][i] + s_dw[3][i]);
 }
 
 // The weights' gradients from the workgroups' sums: 32 channels a workgroup, every 32nd workgroup's sum a thread.
@@ -248,7 +342,7 @@ __global__ void __launch_bounds__(1024) k_weight_grad(const float* part, int gro
   __shared__ double s_sum[32][33];
   const int c = threadIdx.x & 31, g = threadIdx.x >> 5, at = blockIdx.x * 32 + c;
   double sum = 0.0;
-#pragma unroll 8
+#pragma unroll 16
   for (int i = g; i < groups; i += 32) sum += (double)part[(size_t)i * 2 * d + at];
   s_sum[g][c] = sum;
   __syncthreads();
@@ -280,7 +374,7 @@ int check_shape(const NormShape& a) {
   if (a.dtype != SAGE_DT_FP16 && a.dtype != SAGE_DT_BF16) return SAGE_ERR_UNSUPPORTED;
   if (a.layout != SAGE_LAYOUT_HND && a.layout != SAGE_LAYOUT_NHD) return SAGE_ERR_UNSUPPORTED;
   if (a.weight_type != SAGE_WEIGHT_FP32 && a.weight_type != SAGE_WEIGHT_SAME) return SAGE_ERR_UNSUPPORTED;
-  if (a.N > MAX_TOKENS || a.B > 65535 || a.H > 65535 || (a.keys && a.Hkv > 65535)) return SAGE_ERR_UNSUPPORTED;
+  if (a.N > MAX_TOKENS || a.B > 65535 || a.H > 65535 || (a.keys && a.Hkv > 65535) || (long long)a.B * a.N > 1LL << 26) return SAGE_ERR_UNSUPPORTED;
   if ((a.interleaved & ~1) != 0) return SAGE_ERR_UNSUPPORTED;
   return SAGE_OK;
 }
@@ -324,31 +418,35 @@ int check_views(NormView* v, int count, const NormShape& a, const Span* read, in
   return SAGE_OK;
 }
 
-// What the kernels take, but for the tensors' pointers; the widest access that every row allows, and the grid.
+// What the kernels take, but for the tensors' pointers; the widest access that every row allows, and the grid (of at most `most` workgroups, if that is not 0).
+constexpr long long PAST_BYTES = 192LL << 20;
 struct NormLaunch { dim3 grid; int vw; bool inter, past; };
-void plan(NormParams* p, NormLaunch* l, const NormShape& a, const NormView* v, int count, int most, int bytes) {
+void plan(NormParams* p, NormLaunch* l, const NormShape& a, const NormView* v, int count, int most) {
   unsigned long long rows = 0;
   for (int i = 0; i < count; ++i) if (v[i].at) rows |= (uintptr_t)v[i].at / 2 | (unsigned long long)(v[i].st[0] | v[i].st[1] | v[i].st[2]);
   l->inter = a.interleaved != 0;
   const unsigned long long bits = rows | (l->inter ? 0ull : (unsigned long long)(a.rot / 2));
   l->vw = (bits & 7) == 0 ? 8 : (bits & 3) == 0 ? 4 : 1;
-  l->past = false;
-  (void)bytes;
   p->inv_freq = a.inv_freq; p->positions = a.positions; p->pos_sb = a.pos_sb; p->offset = a.offset;
-  p->N = a.N; p->d = a.d; p->rot = a.rot; p->units = a.d / 16;
+  p->tokens = (unsigned)(a.B * (long long)a.N); p->d = a.d; p->rot = a.rot; p->units = a.d / 16;
   p->weight_same = a.weight_type == SAGE_WEIGHT_SAME;
   p->eps = a.eps; p->scale = a.scale == 0.0f ? 1.0f : a.scale;
-  // Token-major rows: neighbouring threads take neighbouring heads of a token, which are one stretch of memory.
+  // A workgroup's 256 threads are 4 tokens, or more where there are few heads.
+  const int heads = a.H + (a.keys ? a.Hkv : 0), rows_of = 256 / p->units;
   p->lanes = 1;
-  if (v[0].st[1] < v[0].st[2] && a.N > 1) while (p->lanes * 2 * p->units <= 64 && p->lanes * 2 <= a.H) p->lanes *= 2;
-  p->total = (long long)a.B * a.N * p->units * p->lanes;
-  const long long blocks = (p->total + 255) / 256;
-  const int heads = a.H + (a.keys ? a.Hkv : 0);
-  const long long wide = std::min(blocks, most > 0 ? (long long)most : 1LL << 22), deep = most > 0 ? 1 : (blocks + wide - 1) / wide;
-  const long long want = most > 0 ? most / wide : (4096 + blocks - 1) / blocks;
-  const long long pieces = std::max(1LL, std::min(want, (long long)heads / p->lanes));
+  while (p->lanes * 2 <= rows_of / 4 && p->lanes * 2 <= heads) p->lanes *= 2;
+  p->at_once = rows_of / p->lanes;
+  // Reads and writes pass the caches by where every access is whole lines of 128 bytes and what is read and written does not fit the 256 MB of the memory-side cache
+  // (as sage_rope).
+  const bool whole_lines = l->vw == 8 && (rows & 63) == 0 && (l->inter ? a.d % 128 == 0 : a.rot % 128 == 0 && a.d % 128 == 0);
+  l->past = whole_lines && (most > 0 ? 6LL : 4LL) * p->tokens * heads * a.d > PAST_BYTES;
+  p->heads_first = v[0].st[1] < v[0].st[2];       // (token-major: a token's heads are one stretch of memory)
+  const long long groups = ((long long)p->tokens + p->at_once - 1) / p->at_once;
+  const long long wide = most > 0 ? std::min(groups, (long long)most) : groups;
+  const long long pieces = std::max(1LL, std::min((most > 0 ? most : 1024) / wide, (long long)heads / p->lanes));
   p->hchunk = (int)((heads + pieces - 1) / pieces);
-  l->grid = dim3((unsigned)wide, (unsigned)((heads + p->hchunk - 1) / p->hchunk), (unsigned)deep);
+  l->grid = dim3((unsigned)wide, (unsigned)((heads + p->hchunk - 1) / p->hchunk));
+  p->by_n = fast_div(a.N); p->by_pairs = fast_div(a.rot > 0 ? a.rot / 2 : 1); p->by_lanes = fast_div(p->lanes); p->by_at_once = fast_div(p->at_once);
 }
 
 template <bool BF16, int VW> void launch(const NormParams& p, const NormLaunch& l, hipStream_t s) {
@@ -404,8 +502,7 @@ extern "C" int sage_qk_norm_rope(const sage_qk_norm_rope_args* a) {
   if (st != SAGE_OK) return st;
   NormParams p = {};
   NormLaunch l;
-  plan(&p, &l, sh, v, 4, 0, 4);
-  if (l.grid.z > 65535) return SAGE_ERR_UNSUPPORTED;
+  plan(&p, &l, sh, v, 4, 0);
   p.q = tensor(&v[0], nullptr, v[2], a->q_weight);
   p.k = tensor(&v[1], nullptr, v[3], a->k_weight);
   const hipStream_t s = (hipStream_t)a->stream;
@@ -452,7 +549,7 @@ extern "C" int sage_qk_norm_rope_bwd(const sage_qk_norm_rope_bwd_args* a) {
   }
   NormParams p = {};
   NormLaunch l;
-  plan(&p, &l, sh, v, 6, BWD_GROUPS, 6);
+  plan(&p, &l, sh, v, 6, BWD_GROUPS);
   p.q = tensor(&v[0], &v[2], v[4], a->q_weight);
   p.k = tensor(&v[1], &v[3], v[5], a->k_weight);
   if (need > 0) p.q.part = (float*)a->workspace;
