@@ -73,19 +73,32 @@ template <bool BF16> __device__ __forceinline__ v4i widen(int u, int w, float sc
   return a;
 }
 
-template <int D> constexpr int paged_occupancy() { return D == 64 ? 3 : D == 128 ? 2 : 1; }      // wavefronts per SIMD
+// A byte of each active lane's own address into LDS, a dword a lane.
+__device__ __forceinline__ void dma_u8(const void* from, unsigned lds_byte) {
+  unsigned m0_after;
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_ubyte %2, off" : "={m0}"(m0_after) : "s"(lds_byte), "v"(from) : "memory");
+}
 
-// RG: groups of 32 rows of a workgroup.  Its four wavefronts are RG row groups times 4 / RG key groups: wavefront w has row group w / KG and the blocks kg, kg + KG, .. of a
-// tile.  ONE: a workgroup takes all keys and leaves the output itself.
+template <int D> constexpr int paged_occupancy() { return D == 64 ? 3 : 2; }      // wavefronts per SIMD
+// Wavefronts that share their rows' channels: of 256, whose outputs and queries would take all registers of a SIMD, two form the same scores and have half of the outputs each.
+// (One on a SIMD with 512 registers: 6 caches of 5120, 5 queries of 4 heads, window 3001: 30 us.)
+template <int D> constexpr int channel_groups() { return D == 256 ? 2 : 1; }
+template <int D> constexpr int paged_threads() { return 256 * channel_groups<D>(); }
+
+// RG: groups of 32 rows of a workgroup.  Its wavefronts are RG row groups times KG = 4 / RG key groups (which take the blocks kg, kg + KG, .. of a tile) times CG channel groups.
+// ONE: a workgroup takes all keys and leaves the output itself.
 template <int D, bool BF16, int RG, bool ONE>
-__global__ void __launch_bounds__(256, paged_occupancy<D>()) k_paged(const PagedParams p) {
-  constexpr int KS = D / 16, CT = D / 32, KG = 4 / RG, ROWS = 32 * RG;
+__global__ void __launch_bounds__(paged_threads<D>(), paged_occupancy<D>()) k_paged(const PagedParams p) {
+  constexpr int CG = channel_groups<D>(), THREADS = paged_threads<D>();
+  constexpr int KS = D / 16, CT = D / 32 / CG, KG = 4 / RG, ROWS = 32 * RG;      // CT: channel tiles of a wavefront
+  constexpr bool SHARED = RG > 1 || CG > 1;       // wavefronts read blocks that others copied
   constexpr unsigned BYTES = BLOCK * D;           // of a block of K or V
   constexpr int COPIES = D / 32;                  // copies of 64 pieces of a block of K (or V)
   __shared__ __align__(1024) v4i s_kv[2 * PT_BLOCKS * 2 * BYTES / 16];      // [stage][block][K, V]
-  __shared__ float s_ml[4][64];
+  __shared__ float s_ml[4 * CG][64];
+  __shared__ unsigned s_scale[4 * CG][2][64];     // of the blocks in at_lo, at_hi: K's, V's
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
-  const int col = lane & 31, half = lane >> 5, kg = wave % KG, rg = wave / KG;
+  const int col = lane & 31, half = lane >> 5, cg = wave % CG, own = wave / CG, kg = own % KG, rg = own / KG;      // own: the block of a tile that this one copies
 
   // ---- which rows and keys.  The row tiles of the same keys are 8 apart: workgroups go to the 8 XCDs in turn and each has a cache of its own.
   unsigned rt = blockIdx.x;
@@ -113,24 +126,12 @@ __global__ void __launch_bounds__(256, paged_occupancy<D>()) k_paged(const Paged
   const bool active = rg * 32 < nr;
   const size_t part0 = ((size_t)s * (p.B * p.c.Hkv) + bh) * ((size_t)p.G * p.N) + r0;      // of the partial results' rows
   if (!ONE && j0 >= j1) {                         // no keys: a partial result that the merge skips
-    for (int i = t; i < nr; i += 256) {
+    for (int i = t; i < nr; i += THREADS) {
       p.part_ml[(part0 + i) * 2] = -INFINITY;
       p.part_ml[(part0 + i) * 2 + 1] = 0.0f;
     }
     return;
   }
-
-  // ---- the pool's block and the two scales of the next 16 tiles' blocks, one block a lane; 8 tiles are fetched at a time
-  int at_lo = -1, at_hi = -1, scales = 0;
-  auto fetch = [&](int j) {
-    const int slot = (j - j0) & 15, i = 4 * (j - slot) + lane;
-    if ((lane >> 2 & 8) != slot) return;
-    long long at = -1;
-    if (i < nb) at = pool_block(p.c, (int)b, (int)hkv, i < ns ? i : i - ns + w0);
-    at_lo = (int)at; at_hi = (int)(at >> 32);
-    scales = at >= 0 ? p.c.ks[at] | p.c.vs[at] << 8 : 0;
-  };
-  fetch(j0);
 
   // ---- my row's query as the B operand: channels 32 u + 16 half + 0..15 are two steps
   const int i0 = r0 + min(rg * 32 + col, nr - 1);
@@ -141,6 +142,26 @@ __global__ void __launch_bounds__(256, paged_occupancy<D>()) k_paged(const Paged
 #pragma unroll
   for (int st = 0; st < KS; ++st) q[st] = *reinterpret_cast<const v4i*>(p.q + qrow + 32 * (st >> 1) + 16 * half + 8 * (st & 1));
   const Seen mine = seen_from(p, len, coff + (int)rn);
+  // ---- where the next 16 tiles' blocks are in the pool, one block a lane, and their scales, which go to LDS like the blocks do, so that no wait for them is one for what
+  // is copied after them.  Half of the lanes are refilled every 8 tiles.
+  int at_lo = -1, at_hi = -1;
+  unsigned scales = 0;
+  auto fetch = [&](int j, int from, int to) __attribute__((always_inline)) {      // lanes from .. to - 1, the first of them tile j's first block
+    const int i = 4 * j + lane - from;
+    if (lane < from || lane >= to) return;
+    long long at = -1;
+    if (i < nb) at = pool_block(p.c, (int)b, (int)hkv, i < ns ? i : i - ns + w0);
+    at_lo = (int)at; at_hi = (int)(at >> 32);
+    if (at < 0) return;
+    const unsigned dst = (unsigned)(size_t)(__attribute__((address_space(3))) char*)&s_scale[wave][0][0];
+    dma_u8(p.c.ks + at, dst);
+    dma_u8(p.c.vs + at, dst + 256);
+  };
+  fetch(j0, 0, 64);
+#pragma unroll
+  for (int st = 0; st < KS; ++st)                 // (the queries are there with the page numbers: no wait for them is one for a copy)
+#pragma unroll
+    for (int x = 0; x < 4; ++x) use_now(q[st][x]);
 
   // ---- copies
   const unsigned lds0 = (unsigned)(size_t)(__attribute__((address_space(3))) char*)&s_kv[0];
@@ -150,25 +171,41 @@ __global__ void __launch_bounds__(256, paged_occupancy<D>()) k_paged(const Paged
     const int pc = x * 64 + lane, r = pc / (D / 16);
     offs[x] = (unsigned)(r * D + ((pc % (D / 16)) ^ turn<D>(r)) * 16);
   }
+  const bool once = p.rt == 1;                    // what one workgroup alone reads passes the caches by
   auto copy = [&](int j, int stage) __attribute__((always_inline)) -> bool {      // my block of tile j; whether there is one
-    const int at_lane = ((j - j0) & 15) * 4 + wave;
+    const int at_lane = ((j - j0) & 15) * 4 + own;
     const int hi = __builtin_amdgcn_readlane(at_hi, at_lane);
     if (hi < 0) return false;
     const size_t at = (size_t)((unsigned long long)(unsigned)hi << 32 | (unsigned)__builtin_amdgcn_readlane(at_lo, at_lane)) * BYTES;
-    const unsigned char *gk = p.c.k + at, *gv = p.c.v + at;
-    const unsigned to = lds0 + (unsigned)(stage * PT_BLOCKS + wave) * (2 * BYTES);
+    const unsigned to = lds0 + (unsigned)(stage * PT_BLOCKS + own) * (2 * BYTES);
+    if constexpr (CG == 1) {
+      const unsigned char *gk = p.c.k + at, *gv = p.c.v + at;
+      if (once) {
 #pragma unroll
-    for (int x = 0; x < COPIES; ++x) {
-      dma_b128(gk, offs[x], to + x * 1024);
-      dma_b128(gv, offs[x], to + BYTES + x * 1024);
+        for (int x = 0; x < COPIES; ++x) {
+          dma_b128_once(gk, offs[x], to + x * 1024);
+          dma_b128_once(gv, offs[x], to + BYTES + x * 1024);
+        }
+      } else {
+#pragma unroll
+        for (int x = 0; x < COPIES; ++x) {
+          dma_b128(gk, offs[x], to + x * 1024);
+          dma_b128(gv, offs[x], to + BYTES + x * 1024);
+        }
+      }
+    } else {                                      // (one the keys, the other the values)
+      const unsigned char* g = (cg ? p.c.v : p.c.k) + at;
+      if (once) {
+#pragma unroll
+        for (int x = 0; x < COPIES; ++x) dma_b128_once(g, offs[x], to + cg * BYTES + x * 1024);
+      } else {
+#pragma unroll
+        for (int x = 0; x < COPIES; ++x) dma_b128(g, offs[x], to + cg * BYTES + x * 1024);
+      }
     }
     return true;
   };
   copy(j0, 0);
-#pragma unroll
-  for (int st = 0; st < KS; ++st)
-#pragma unroll
-    for (int x = 0; x < 4; ++x) use_now(q[st][x]);
   bool next = j0 + 1 < j1 && copy(j0 + 1, 1);     // whether tile j + 1 is on its way
 
   v16f o[CT];
@@ -185,19 +222,20 @@ __global__ void __launch_bounds__(256, paged_occupancy<D>()) k_paged(const Paged
   typedef __attribute__((address_space(3))) v2i* lds_v2i;
   const int kr = 16 * (col >> 4) + 8 * ((col >> 2) & 1) + 4 * ((col >> 3) & 1) + (col & 3), vr = 8 * half + ((lane & 15) >> 1);
   const unsigned k_at = (unsigned)(kr * D + (half ^ turn<D>(kr)) * 16);
-  const unsigned v_at = BYTES + (unsigned)(vr * D + (((lane >> 4) & 1) ^ turn<D>(vr)) * 16 + 8 * (lane & 1));
+  const unsigned v_at = BYTES + ((unsigned)(vr * D + (((lane >> 4) & 1) ^ turn<D>(vr)) * 16 + 8 * (lane & 1)) ^ (unsigned)(32 * CT * cg));
 
   // One block: scores, weights and their product with V.  PART: some row does not see some token of it.
   constexpr int FITS = BF16 ? 246 : 134;           // 448 2^119 and 448 2^7 are numbers of the type
   auto attend = [&](auto part, unsigned base, int t0, float kk, int ev) __attribute__((always_inline)) {
     constexpr bool PART = decltype(part)::value;
     const float vs = scale_of((unsigned)(PART ? min(ev, FITS) : ev));
+    const unsigned ka = base + k_at, va = base + v_at;      // (a block's first byte has its low bits zero: steps to other pieces need no address kept over the loop)
     v16f sc;
 #pragma unroll
     for (int v = 0; v < 16; ++v) sc[v] = 0.0f;
 #pragma unroll
     for (int u = 0; u < KS / 2; ++u) {
-      const v4i x = *(lds_v4i)(uintptr_t)(base + (k_at ^ (32 * u)));
+      const v4i x = *(lds_v4i)(uintptr_t)(ka ^ (32 * u));
       sc = mfma16<BF16>(widen<BF16>(x[0], x[1], 1.0f), q[2 * u], sc);
       sc = mfma16<BF16>(widen<BF16>(x[2], x[3], 1.0f), q[2 * u + 1], sc);
     }
@@ -247,7 +285,7 @@ __global__ void __launch_bounds__(256, paged_occupancy<D>()) k_paged(const Paged
       for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
         for (int c = 0; c < CT; ++c) {
-          const v2i x = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_v2i)(uintptr_t)(base + (v_at ^ (32 * c)) + ks * 16 * D));
+          const v2i x = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_v2i)(uintptr_t)((va ^ (32 * c)) + ks * 16 * D));
           o[c] = mfma16<BF16>(widen<BF16>(x[0], x[1], vs), pb[ks], o[c]);
         }
     } else {
@@ -281,7 +319,7 @@ __global__ void __launch_bounds__(256, paged_occupancy<D>()) k_paged(const Paged
         for (int v = 0; v < 16; ++v) y16[v] = 0.0f;
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks) {
-          v2i x = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_v2i)(uintptr_t)(base + (v_at ^ (32 * c)) + ks * 16 * D));
+          v2i x = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_v2i)(uintptr_t)((va ^ (32 * c)) + ks * 16 * D));
 #pragma unroll
           for (int y = 0; y < 2; ++y) {
             const unsigned u = (unsigned)x[y] & keep[ks][y];
@@ -310,23 +348,25 @@ __global__ void __launch_bounds__(256, paged_occupancy<D>()) k_paged(const Paged
 #pragma unroll
           for (int v = 0; v < 16; ++v) o[c][v] = hits[v] > 0.0f ? NAN : o[c][v];
         }
+        __builtin_amdgcn_sched_barrier(0);        // (channel tiles one after the other: side by side they take more registers than there are)
       }
     }
   };
 
-  constexpr int PER_TILE = 2 * COPIES;            // copies that a wavefront starts for a tile
+  constexpr int PER_TILE = 2 * COPIES / CG;       // copies that a wavefront starts for a tile
   for (int j = j0; j < j1; ++j) {
     const int stage = (j - j0) & 1;
     if (next) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(PER_TILE) : "memory");
     else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-    if constexpr (RG > 1) __builtin_amdgcn_s_barrier();      // tile j is there
+    if constexpr (SHARED) __builtin_amdgcn_s_barrier();      // tile j is there
     asm volatile("" ::: "memory");
+    if (((j - j0) & 7) == 0) scales = s_scale[wave][0][lane] | s_scale[wave][1][lane] << 8;
     if (active) {
 #pragma unroll 1
       for (int x = kg; x < PT_BLOCKS; x += KG) {
         const int at_lane = ((j - j0) & 15) * 4 + x, i = 4 * j + x;
         if (__builtin_amdgcn_readlane(at_hi, at_lane) < 0) continue;      // no tokens: past the last, or no page
-        const int two = __builtin_amdgcn_readlane(scales, at_lane), t0 = BLOCK * (i < ns ? i : i - ns + w0);
+        const int two = __builtin_amdgcn_readlane((int)scales, at_lane), t0 = BLOCK * (i < ns ? i : i - ns + w0);
         // A NaN among the scales makes the rows NaN that see the block, through kk.  Values that may not fit the 16-bit type go the way of partly seen blocks, which scales their
         // product.
         const int ev = two >> 8 == 255 ? 127 : two >> 8;
@@ -338,9 +378,9 @@ __global__ void __launch_bounds__(256, paged_occupancy<D>()) k_paged(const Paged
     }
     next = false;
     if (j + 2 < j1) {                             // the next tile but one takes this one's place when all have read it
-      if (((j + 2 - j0) & 7) == 0) fetch(j + 2);
+      if (j + 2 - j0 >= 16 && ((j + 2 - j0) & 7) == 0) fetch(j + 2, 4 * ((j + 2 - j0) & 8), 4 * ((j + 2 - j0) & 8) + 32);
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-      if constexpr (RG > 1) __builtin_amdgcn_s_barrier();
+      if constexpr (SHARED) __builtin_amdgcn_s_barrier();
       asm volatile("" ::: "memory");
       next = copy(j + 2, stage);
     } else {
@@ -351,6 +391,7 @@ __global__ void __launch_bounds__(256, paged_occupancy<D>()) k_paged(const Paged
 
   // ---- the key groups of the same rows into one, each wavefront's share of the channels: units of four of them a lane, unit 4 c + g is channels 32 c + 8 g + 4 half + 0..3
   constexpr int UN = 4 * CT / KG;
+  const int unit0 = 4 * CT * cg + kg * UN;        // the first that I write
   v4f res[UN];
   if constexpr (KG == 1) {
 #pragma unroll
@@ -371,12 +412,12 @@ __global__ void __launch_bounds__(256, paged_occupancy<D>()) k_paged(const Paged
     if (active) {
       float a[KG], m = -INFINITY;
 #pragma unroll
-      for (int k = 0; k < KG; ++k) m = fmaxf(m, s_ml[rg * KG + k][2 * col]);
+      for (int k = 0; k < KG; ++k) m = fmaxf(m, s_ml[(rg * KG + k) * CG + cg][2 * col]);
       l = 0.0f;
 #pragma unroll
       for (int k = 0; k < KG; ++k) {
-        a[k] = __builtin_amdgcn_exp2f(s_ml[rg * KG + k][2 * col] - (m == -INFINITY ? 0.0f : m));
-        l = __fmaf_rn(a[k], s_ml[rg * KG + k][2 * col + 1], l);
+        a[k] = __builtin_amdgcn_exp2f(s_ml[(rg * KG + k) * CG + cg][2 * col] - (m == -INFINITY ? 0.0f : m));
+        l = __fmaf_rn(a[k], s_ml[(rg * KG + k) * CG + cg][2 * col + 1], l);
       }
       mx = m;
 #pragma unroll
@@ -384,7 +425,7 @@ __global__ void __launch_bounds__(256, paged_occupancy<D>()) k_paged(const Paged
         res[u] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int k = 0; k < KG; ++k) {
-          const v4f y = x[((rg * KG + k) * 4 * CT + kg * UN + u) * 64 + lane];
+          const v4f y = x[(((rg * KG + k) * CG + cg) * 4 * CT + kg * UN + u) * 64 + lane];
 #pragma unroll
           for (int e = 0; e < 4; ++e) res[u][e] = __fmaf_rn(a[k], y[e], res[u][e]);
         }
@@ -395,20 +436,20 @@ __global__ void __launch_bounds__(256, paged_occupancy<D>()) k_paged(const Paged
   if constexpr (ONE) {
     const bool none = mx == -INFINITY && l == 0.0f;      // no token at all: zeros
     const float inv = none ? 0.0f : __fdiv_rn(1.0f, l);
-    if (p.lse && half == 0 && kg == 0) p.lse[((size_t)b * p.H + hkv * p.G + rh) * p.N + rn] = none ? -INFINITY : LN2 * (mx + __builtin_amdgcn_logf(l));
+    if (p.lse && half == 0 && kg == 0 && cg == 0) p.lse[((size_t)b * p.H + hkv * p.G + rh) * p.N + rn] = none ? -INFINITY : LN2 * (mx + __builtin_amdgcn_logf(l));
     unsigned short* y = p.out + qrow + 4 * half;
 #pragma unroll
     for (int u = 0; u < UN; ++u)
-      *reinterpret_cast<uint2*>(y + 8 * (kg * UN + u)) = make_uint2(pack16x2<BF16>(res[u][0] * inv, res[u][1] * inv), pack16x2<BF16>(res[u][2] * inv, res[u][3] * inv));
+      *reinterpret_cast<uint2*>(y + 8 * (unit0 + u)) = make_uint2(pack16x2<BF16>(res[u][0] * inv, res[u][1] * inv), pack16x2<BF16>(res[u][2] * inv, res[u][3] * inv));
   } else {
     const size_t pr = part0 + rg * 32 + col;
-    if (half == 0 && kg == 0) {
+    if (half == 0 && kg == 0 && cg == 0) {
       p.part_ml[pr * 2] = mx;
       p.part_ml[pr * 2 + 1] = l;
     }
     float* po = p.part_o + pr * D + 4 * half;
 #pragma unroll
-    for (int u = 0; u < UN; ++u) *reinterpret_cast<v4f*>(po + 8 * (kg * UN + u)) = res[u];
+    for (int u = 0; u < UN; ++u) *reinterpret_cast<v4f*>(po + 8 * (unit0 + u)) = res[u];
   }
 }
 
@@ -483,17 +524,30 @@ __global__ void __launch_bounds__(256) k_paged_merge(const PagedParams p) {
 
 int row_groups(const PagedParams& p) { return p.G * p.N <= 32 ? 1 : p.G * p.N <= 64 ? 2 : 4; }
 
-// Key chunks of a row tile.  The chip has room for `places` workgroups; lengths that the host does not know are cut fine, so that it fills up to the end.
+// Key chunks of a row tile, S.  Workgroups beyond one on each CU (two of 64 channels, and where rows are many and products count, but of 256 channels, which fill the LDS) share
+// what the chip reads, so what counts is rounds of them times the tiles of each, two tiles' worth of a start, and, with a merge, some 9 us of a second launch.  Us, sequences x
+// tokens of 8 KV heads of 128 channels, 32 heads, chunks in parentheses: 32 in a window of 4096 50 (1) 54 (2) 57 (4); 1 x 32768 21 (32) 23 (64) 28 (16); 8 x 4096, 40 queries 62 (4)
+// 69 (3) 64 (6); 1 x 4096, 600 queries 86 (3) 95 (4) 113 (2); 16 heads of 256 over 4 in 4 x 8192 25 (16) 34 (8) 31 (24); 8 heads over 2 in 4 x 1024 15 (1) 19 (8).
+// Lengths that the host does not know are cut finer, 8 tiles or 2048 workgroups, so that the chip stays full up to the end: 8 x 8192 27 (8) 29 (4); 16 x 32768 128 (16) 133 (8) 141 (32).
 void choose_chunks(PagedParams* p, int d) {
   const int rg = row_groups(*p);
   const long long gn = (long long)p->G * p->N;
   p->rt = (int)((gn + 32 * rg - 1) / (32 * rg));
-  long long keys = p->cap;
-  if (p->window > 0) keys = std::min(keys, (long long)p->sink + p->window + std::min((long long)p->N, (32LL * rg + p->G - 1) / p->G + 1) + 2 * BLOCK);
-  const long long tiles = (keys + BLOCK * PT_BLOCKS - 1) / (BLOCK * PT_BLOCKS);
-  const long long heads = (long long)p->B * p->c.Hkv * p->rt, places = 256LL * (d == 64 ? 3 : d == 128 ? 2 : 1);
-  const long long share = std::max(2LL, std::min(12LL, (heads * tiles + places - 1) / places));
-  p->S = heads >= 2 * places || tiles <= 4 ? 1 : (int)std::min((tiles + share - 1) / share, (long long)MAX_PARTS);
+  long long keys = p->cap, seen = keys;
+  if (p->window > 0) seen = (long long)p->sink + p->window + std::min((long long)p->N, (32LL * rg + p->G - 1) / p->G + 1) + 2 * BLOCK;
+  const bool even = p->B == 1 || 3 * seen < 2 * keys;      // all sequences about as long, as far as is known here
+  const long long tiles = (std::min(keys, seen) + BLOCK * PT_BLOCKS - 1) / (BLOCK * PT_BLOCKS);
+  const long long heads = (long long)p->B * p->c.Hkv * p->rt, places = d == 64 || (rg > 1 && d == 128) ? 512 : 256, merge = d == 64 ? 15 : d == 128 ? 8 : 4;
+  long long best = 0, chosen = 1;
+  for (int S : {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 40, 48, 64, 96, 128}) {
+    if (S > tiles) break;
+    const long long per = (tiles + S - 1) / S, cost = (heads * ((tiles + per - 1) / per) + places - 1) / places * (per + 2) + (S > 1 ? merge : 0);
+    if (S == 1 || cost < best) { best = cost; chosen = S; }
+  }
+  if (chosen > 1 && rg == 1 && !even) chosen = std::max(chosen, tiles / std::max(8LL, heads * tiles / 2048));
+  chosen = std::min(chosen, (long long)MAX_PARTS);
+  const long long per = (tiles + chosen - 1) / chosen;
+  p->S = (int)((tiles + per - 1) / per);
   p->units = p->B * p->c.Hkv * p->S;
 }
 
@@ -517,7 +571,7 @@ int paged_params(const sage_attn_paged_args* a, PagedParams* p, bool need_io) {
   p->causal = a->causal; p->window = std::min(a->window, MAX_TOKENS * 2); p->sink = std::min(a->sink, MAX_TOKENS);
   p->kappa = (a->sm_scale > 0.0f ? a->sm_scale : (float)(1.0 / std::sqrt((double)a->d))) * LOG2E;
   choose_chunks(p, a->d);
-  if (((long long)p->units + 7) / 8 * 8 * p->rt * 256 > MAX_THREADS) return SAGE_ERR_UNSUPPORTED;
+  if (((long long)p->units + 7) / 8 * 8 * p->rt * 512 > MAX_THREADS) return SAGE_ERR_UNSUPPORTED;
   p->by_rt8 = fast_div(8u * p->rt); p->by_s = fast_div(p->S); p->by_hkv = fast_div(a->H_kv); p->by_g = fast_div(p->G);
   p->by_gn = fast_div((unsigned)p->G * a->N);
   return SAGE_OK;
@@ -530,14 +584,14 @@ template <int D, bool BF16> hipError_t launch(const PagedParams& p, hipStream_t 
   const unsigned grid = (unsigned)((p.units + 7) / 8 * 8) * p.rt;
   const int rg = row_groups(p);
   if (p.S == 1) {
-    if (rg == 1) k_paged<D, BF16, 1, true><<<grid, 256, 0, s>>>(p);
-    else if (rg == 2) k_paged<D, BF16, 2, true><<<grid, 256, 0, s>>>(p);
-    else k_paged<D, BF16, 4, true><<<grid, 256, 0, s>>>(p);
+    if (rg == 1) k_paged<D, BF16, 1, true><<<grid, paged_threads<D>(), 0, s>>>(p);
+    else if (rg == 2) k_paged<D, BF16, 2, true><<<grid, paged_threads<D>(), 0, s>>>(p);
+    else k_paged<D, BF16, 4, true><<<grid, paged_threads<D>(), 0, s>>>(p);
     return hipGetLastError();
   }
-  if (rg == 1) k_paged<D, BF16, 1, false><<<grid, 256, 0, s>>>(p);
-  else if (rg == 2) k_paged<D, BF16, 2, false><<<grid, 256, 0, s>>>(p);
-  else k_paged<D, BF16, 4, false><<<grid, 256, 0, s>>>(p);
+  if (rg == 1) k_paged<D, BF16, 1, false><<<grid, paged_threads<D>(), 0, s>>>(p);
+  else if (rg == 2) k_paged<D, BF16, 2, false><<<grid, paged_threads<D>(), 0, s>>>(p);
+  else k_paged<D, BF16, 4, false><<<grid, paged_threads<D>(), 0, s>>>(p);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const unsigned per = 4 * merge_channels<D>() / D;
