@@ -233,11 +233,27 @@ __global__ void __launch_bounds__(paged_threads<D>(), paged_occupancy<D>()) k_pa
     v16f sc;
 #pragma unroll
     for (int v = 0; v < 16; ++v) sc[v] = 0.0f;
+    constexpr int AHEAD = PART ? 1 : KS / 2 < 4 ? KS / 2 : 4;      // reads of K in flight
 #pragma unroll
-    for (int u = 0; u < KS / 2; ++u) {
-      const v4i x = *(lds_v4i)(uintptr_t)(ka ^ (32 * u));
-      sc = mfma16<BF16>(widen<BF16>(x[0], x[1], 1.0f), q[2 * u], sc);
-      sc = mfma16<BF16>(widen<BF16>(x[2], x[3], 1.0f), q[2 * u + 1], sc);
+    for (int u0 = 0; u0 < KS / 2; u0 += AHEAD) {
+      v4i x[AHEAD];
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u) x[u] = *(lds_v4i)(uintptr_t)(ka ^ (32 * (u0 + u)));
+      if constexpr (!PART) __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u) {
+        sc = mfma16<BF16>(widen<BF16>(x[u][0], x[u][1], 1.0f), q[2 * (u0 + u)], sc);
+        sc = mfma16<BF16>(widen<BF16>(x[u][2], x[u][3], 1.0f), q[2 * (u0 + u) + 1], sc);
+      }
+    }
+    // The values are read while the weights are worked out
+    v2i xv[PART ? 1 : 2][CT];
+    if constexpr (!PART) {
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+        for (int c = 0; c < CT; ++c) xv[ks][c] = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_v2i)(uintptr_t)((va ^ (32 * c)) + ks * 16 * D));
+      __builtin_amdgcn_sched_barrier(0);
     }
     unsigned seen = 0xffff;                       // bit v: my row sees score v's token
     if constexpr (PART) {
@@ -284,10 +300,7 @@ __global__ void __launch_bounds__(paged_threads<D>(), paged_occupancy<D>()) k_pa
 #pragma unroll
       for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
-        for (int c = 0; c < CT; ++c) {
-          const v2i x = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_v2i)(uintptr_t)((va ^ (32 * c)) + ks * 16 * D));
-          o[c] = mfma16<BF16>(widen<BF16>(x[0], x[1], vs), pb[ks], o[c]);
-        }
+        for (int c = 0; c < CT; ++c) o[c] = mfma16<BF16>(widen<BF16>(xv[ks][c][0], xv[ks][c][1], vs), pb[ks], o[c]);
     } else {
       // A NaN among V times a weight of zero would reach rows that do not see it: NaN is taken out before the product.  How many of a channel's a row sees is a product
       // too, of ones; where that is not zero, the output is NaN.  What no row sees counts as zeros.
@@ -362,19 +375,29 @@ __global__ void __launch_bounds__(paged_threads<D>(), paged_occupancy<D>()) k_pa
     asm volatile("" ::: "memory");
     if (((j - j0) & 7) == 0) scales = s_scale[wave][0][lane] | s_scale[wave][1][lane] << 8;
     if (active) {
-#pragma unroll 1
+      // Blocks that all rows see whole first, then the others.  (In one loop, or with a way round the products, the outputs are copied from register to register for each block.)
+      // Values that may not fit the 16-bit type go the way of partly seen blocks, which scales their product.
+      unsigned whole = 0, others = 0;
+#pragma unroll
       for (int x = kg; x < PT_BLOCKS; x += KG) {
-        const int at_lane = ((j - j0) & 15) * 4 + x, i = 4 * j + x;
-        if (__builtin_amdgcn_readlane(at_hi, at_lane) < 0) continue;      // no tokens: past the last, or no page
-        const int two = __builtin_amdgcn_readlane((int)scales, at_lane), t0 = BLOCK * (i < ns ? i : i - ns + w0);
-        // A NaN among the scales makes the rows NaN that see the block, through kk.  Values that may not fit the 16-bit type go the way of partly seen blocks, which scales their
-        // product.
-        const int ev = two >> 8 == 255 ? 127 : two >> 8;
-        const float kk = two >> 8 == 255 ? NAN : p.kappa * scale_of((unsigned)two & 255);
-        const unsigned base = lds0 + (unsigned)(stage * PT_BLOCKS + x) * (2 * BYTES);
-        if (ev <= FITS && t0 + BLOCK <= first.to && (t0 >= last.from || t0 + BLOCK <= first.sink)) attend(std::false_type{}, base, t0, kk, ev);
-        else attend(std::true_type{}, base, t0, kk, ev);
+        const int at_lane = ((j - j0) & 15) * 4 + x, i = 4 * j + x, t0 = BLOCK * (i < ns ? i : i - ns + w0);
+        const bool there = __builtin_amdgcn_readlane(at_hi, at_lane) >= 0;      // (no tokens: past the last, or no page)
+        const unsigned ev = (unsigned)__builtin_amdgcn_readlane((int)scales, at_lane) >> 8;
+        const bool all = (ev <= FITS || ev == 255) && t0 + BLOCK <= first.to && (t0 >= last.from || t0 + BLOCK <= first.sink);
+        whole |= (unsigned)(there && all) << x;
+        others |= (unsigned)(there && !all) << x;
       }
+      auto block = [&](auto part, int x) __attribute__((always_inline)) {
+        const int i = 4 * j + x;
+        const unsigned two = (unsigned)__builtin_amdgcn_readlane((int)scales, ((j - j0) & 15) * 4 + x);
+        const bool nan = two >> 8 == 255;         // a NaN among the scales makes the rows NaN that see the block, through kk
+        attend(part, lds0 + (unsigned)(stage * PT_BLOCKS + x) * (2 * BYTES), BLOCK * (i < ns ? i : i - ns + w0), nan ? NAN : p.kappa * scale_of(two & 255),
+               nan ? 127 : (int)(two >> 8));
+      };
+#pragma unroll 1
+      for (; whole != 0; whole &= whole - 1) block(std::false_type{}, __builtin_ctz(whole));
+#pragma unroll 1
+      for (; others != 0; others &= others - 1) block(std::true_type{}, __builtin_ctz(others));
     }
     next = false;
     if (j + 2 < j1) {                             // the next tile but one takes this one's place when all have read it
