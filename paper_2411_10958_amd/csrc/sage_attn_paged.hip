@@ -545,6 +545,47 @@ __global__ void __launch_bounds__(256) k_paged_merge(const PagedParams p) {
   *reinterpret_cast<uint2*>(y) = make_uint2(pack16x2<BF16>(acc[0] * inv, acc[1] * inv), pack16x2<BF16>(acc[2] * inv, acc[3] * inv));
 }
 
+// The same of up to FEW partial results: a thread has four channels of a row and all of their loads in flight.
+constexpr int FEW = 8;
+template <int D, bool BF16>
+__global__ void __launch_bounds__(256) k_paged_merge_few(const PagedParams p) {
+  const unsigned rows = (unsigned)p.B * p.H * p.N, row = blockIdx.x * (1024 / D) + threadIdx.x / (D / 4);
+  if (row >= rows) return;
+  const int c = 4 * (int)(threadIdx.x % (D / 4));
+  float2 ml[FEW];
+  v4f o4[FEW];
+#pragma unroll
+  for (int s = 0; s < FEW; ++s) {
+    ml[s] = make_float2(-INFINITY, 0.0f);
+    if (s < p.S) {
+      ml[s] = *reinterpret_cast<const float2*>(p.part_ml + ((size_t)s * rows + row) * 2);
+      o4[s] = *reinterpret_cast<const v4f*>(p.part_o + ((size_t)s * rows + row) * D + c);
+    }
+  }
+  unsigned g = row;                               // row: (batch and KV head, query, head of the group)
+  unsigned hkv = split_by(g, p.by_gn);
+  const unsigned b = split_by(hkv, p.by_hkv), n = split_by(g, p.by_g);
+  if ((int)n >= count_of(p, (int)b)) return;
+  float m = -INFINITY, l = 0.0f;
+#pragma unroll
+  for (int s = 0; s < FEW; ++s) m = fmaxf(m, ml[s].x);
+  v4f acc = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+  for (int s = 0; s < FEW; ++s) {
+    if (ml[s].x == -INFINITY && ml[s].y == 0.0f) continue;      // (no token is seen: O may not even be there)
+    const float w = __builtin_amdgcn_exp2f(ml[s].x - m);
+    l = __fmaf_rn(w, ml[s].y, l);
+#pragma unroll
+    for (int y = 0; y < 4; ++y) acc[y] = __fmaf_rn(w, o4[s][y], acc[y]);
+  }
+  const unsigned h = hkv * p.G + g;
+  const bool none = m == -INFINITY && l == 0.0f;  // no token at all: zeros
+  const float inv = none ? 0.0f : __fdiv_rn(1.0f, l);
+  if (p.lse && c == 0) p.lse[((size_t)b * p.H + h) * p.N + n] = none ? -INFINITY : LN2 * (m + __builtin_amdgcn_logf(l));
+  unsigned short* y = p.out + row_offset(p.qm, head_offset_of(p.qm, (int)b, (int)h), (int)n) + c;
+  *reinterpret_cast<uint2*>(y) = make_uint2(pack16x2<BF16>(acc[0] * inv, acc[1] * inv), pack16x2<BF16>(acc[2] * inv, acc[3] * inv));
+}
+
 int row_groups(const PagedParams& p) { return p.G * p.N <= 32 ? 1 : p.G * p.N <= 64 ? 2 : 4; }
 
 // Key chunks of a row tile, S.  Workgroups beyond one on each CU (two of 64 channels, and where rows are many and products count, but of 256 channels, which fill the LDS) share
@@ -617,6 +658,10 @@ template <int D, bool BF16> hipError_t launch(const PagedParams& p, hipStream_t 
   else k_paged<D, BF16, 4, false><<<grid, paged_threads<D>(), 0, s>>>(p);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
+  if (p.S <= FEW) {
+    k_paged_merge_few<D, BF16><<<((unsigned)(p.B * p.H) * p.N + 1024 / D - 1) / (1024 / D), 256, 0, s>>>(p);
+    return hipGetLastError();
+  }
   const unsigned per = 4 * merge_channels<D>() / D;
   k_paged_merge<D, BF16><<<((unsigned)(p.B * p.H) * p.N + per - 1) / per, 256, 0, s>>>(p);
   return hipGetLastError();
