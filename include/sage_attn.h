@@ -505,6 +505,7 @@ int sage_cache_append(const sage_cache_append_args* args);
  * len (and window must be 0).  What no query sees is not read: a sequence's pages behind its window can be given back.  A query that sees no token gets zeros
  * and lse = -inf; a NaN reaches only queries that see its token.
  * out may be q; other overlaps of out, lse or the workspace are refused. */
+enum { SAGE_CLEAR_OUT = 1, SAGE_CLEAR_LSE = 2 };
 typedef struct sage_attn_paged_args {
   const void* q;            /* device, [B, H, N, d] or [B, N, H, d] */
   const void* k_cache;      /* as above */
@@ -521,6 +522,7 @@ typedef struct sage_attn_paged_args {
   int causal, window, sink; /* window 0: none; sink counts only with a window */
   float sm_scale;           /* <= 0 means 1/sqrt(d) */
   int dtype, layout;
+  int clear;                /* SAGE_CLEAR_OUT, SAGE_CLEAR_LSE: places behind q_lens are set to zeros there instead of staying as they were */
   void* workspace;          /* device, 256-byte aligned; may be NULL where the size is 0 */
   size_t workspace_bytes;
   void* stream;

@@ -11,7 +11,7 @@ from .binding import (make_varlen_args, SAGE_MODE_INT4_FP8, SAGE_MODE_INT8_FP8, 
                       make_args, SAGE_ROPE_PLAIN, SAGE_ROPE_LINEAR, SAGE_ROPE_BASE, SAGE_ROPE_PARTS, sage_rope,
                       sage_rope_frequencies, sage_attn_shared_prefix, sage_attn_shared_prefix_args, sage_attn_shared_prefix_workspace_bytes,
                       sage_attn_key_weights, sage_attn_key_weights_args, sage_attn_key_weights_workspace_bytes, sage_cache_evict,
-                      SAGE_WEIGHT_FP32, SAGE_WEIGHT_SAME, sage_qk_norm_rope, sage_qk_norm_rope_bwd, sage_qk_norm_rope_bwd_args,
+                      SAGE_WEIGHT_FP32, SAGE_WEIGHT_SAME, SAGE_CLEAR_OUT, SAGE_CLEAR_LSE, sage_qk_norm_rope, sage_qk_norm_rope_bwd, sage_qk_norm_rope_bwd_args,
                       sage_qk_norm_rope_bwd_workspace_bytes, sage_cache_append, sage_attn_paged, sage_attn_paged_args, sage_attn_paged_workspace_bytes)
 
 __all__ = [n for n in dir() if n.startswith(("sage_", "SAGE_", "Sage"))] + ["lib_path", "load_library", "make_args", "make_varlen_args"]

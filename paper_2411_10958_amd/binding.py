@@ -111,7 +111,7 @@ class sage_cache_append_args(ctypes.Structure):
 class sage_attn_paged_args(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in ("q", "k_cache", "v_cache", "k_scale", "v_scale", "out", "page_table", "kv_lens", "q_lens", "lse")] + \
                [(n, ctypes.c_int) for n in ("B", "H", "H_kv", "N", "d", "n_pages", "page", "max_pages", "causal", "window", "sink")] + \
-               [("sm_scale", ctypes.c_float), ("dtype", ctypes.c_int), ("layout", ctypes.c_int), ("workspace", ctypes.c_void_p),
+               [("sm_scale", ctypes.c_float), ("dtype", ctypes.c_int), ("layout", ctypes.c_int), ("clear", ctypes.c_int), ("workspace", ctypes.c_void_p),
                 ("workspace_bytes", ctypes.c_size_t), ("stream", ctypes.c_void_p)]
 
 
@@ -445,6 +445,7 @@ def sage_attn_debug_mfma_fp8(a_codes, b_codes, c_in):
 
 SAGE_ROPE_PLAIN, SAGE_ROPE_LINEAR, SAGE_ROPE_BASE, SAGE_ROPE_PARTS = 0, 1, 2, 3
 SAGE_WEIGHT_FP32, SAGE_WEIGHT_SAME = 0, 1
+SAGE_CLEAR_OUT, SAGE_CLEAR_LSE = 1, 2
 _ROPE_SCALINGS = {"plain": 0, "linear": 1, "base": 2, "parts": 3, 0: 0, 1: 1, 2: 2, 3: 3}
 
 
@@ -752,10 +753,8 @@ def sage_cache_evict(k, v, weights, n_keep, sink=0, recent=0, kv_lens=None, layo
 
 def _set_strides(field, t, packed, nhd):
     """Batch, head and token strides of t into a field of an argument structure; left at zeros for a contiguous tensor."""
-    if t is None or t.is_contiguous():
-        return
     s = t.stride()
-    if s[-1] != 1:
+    if s[-1] != 1 and t.shape[-1] != 1:
         raise ValueError("the channels of a row must be contiguous")
     if packed:
         s = (0,) + s[:-1]
@@ -764,15 +763,11 @@ def _set_strides(field, t, packed, nhd):
         raise ValueError("one row expanded over all others is not supported (strides of zero stand for a contiguous tensor)")
 
 
-def _norm_rope_fields(q, k, inv_freq, q_weight, k_weight, eps, positions, offset, interleaved, scale, layout):
-    """What the two calls have in common, checked: (fields of the argument structures, index, packed, nhd)."""
-    dtype, index = _dtype_code(q), _gpu_of("q", q)
-    packed = q.dim() == 3
+def _check_norm_rope(q, k, inv_freq, q_weight, k_weight, positions, index, packed, nhd, sizes):
+    """Raises for what a call of sage_qk_norm_rope or its gradient got that does not go together."""
+    B, H, N, d = sizes
     if not packed and q.dim() != 4:
         raise ValueError(f"q must have 4 dimensions, or 3 if packed, got {q.dim()}")
-    nhd = 1 if packed else _LAYOUTS[layout]
-    B, H, N, d = (1, q.shape[1], q.shape[0], q.shape[2]) if packed else _sizes("q", q, nhd)
-    Hkv = 0
     if k is not None:
         if k.get_device() != index or k.dtype != q.dtype or k.dim() != q.dim():
             raise ValueError("k must have the type, device and number of dimensions of q")
@@ -781,30 +776,36 @@ def _norm_rope_fields(q, k, inv_freq, q_weight, k_weight, eps, positions, offset
             raise ValueError("k shape does not match q")
     elif k_weight is not None:
         raise ValueError("k_weight without k")
-    if q.numel() == 0 or (k is not None and Hkv == 0):
+    if q.numel() == 0 or (k is not None and k.numel() == 0):
         raise ValueError("q or k is empty")
-    rot = 0
     if inv_freq is not None:
         _need("inv_freq", inv_freq, index, torch.float64)
         if inv_freq.dim() != 1 or inv_freq.numel() == 0:
             raise ValueError("inv_freq must have one dimension and a frequency at least")
-        rot = 2 * inv_freq.numel()
     if positions is not None:
         _need("positions", positions, index, torch.int32)
         if positions.shape != (N,) and positions.shape != (B, N):
             raise ValueError(f"positions must have shape ({N},) or ({B}, {N}), got {tuple(positions.shape)}")
-    elif packed and rot:
+    elif packed and inv_freq is not None:
         raise ValueError("a packed batch needs positions")
-    weights = [w for w in (q_weight, k_weight) if w is not None]
+    first = None
     for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
         if w is not None:
-            if w.dtype not in (torch.float32, q.dtype) or w.dtype != weights[0].dtype:
+            first = w if first is None else first
+            if w.dtype not in (torch.float32, q.dtype) or w.dtype != first.dtype:
                 raise TypeError(f"the weights must both be float32 or both {q.dtype}, got {name} of {w.dtype}")
             _need(name, w, index, w.dtype, (d,))
-    return dict(q=q.data_ptr(), k=_address(k), q_weight=_address(q_weight), k_weight=_address(k_weight), B=B, H=H, H_kv=Hkv, N=N, d=d, rot_dim=rot, dtype=dtype,
-                layout=nhd, weight_type=SAGE_WEIGHT_SAME if weights and weights[0].dtype != torch.float32 else SAGE_WEIGHT_FP32, interleaved=int(bool(interleaved)),
-                eps=float(eps), scale=float(scale), inv_freq=_address(inv_freq), positions=_address(positions),
-                positions_stride=N if positions is not None and positions.dim() == 2 else 0, offset=_whole(offset, 64)), index, packed, nhd
+
+
+def _norm_rope_sizes(q, layout):
+    """packed, token-major, (B, H, N, d)."""
+    shape = q.shape
+    if len(shape) == 3:
+        return True, 1, (1, shape[1], shape[0], shape[2])
+    nhd = _LAYOUTS[layout]
+    if len(shape) != 4:
+        raise ValueError(f"q must have 4 dimensions, or 3 if packed, got {len(shape)}")
+    return False, nhd, (shape[0], shape[2], shape[1], shape[3]) if nhd else tuple(shape)
 
 
 def _output_like(name, x, y, index, stream):
@@ -817,20 +818,33 @@ def _output_like(name, x, y, index, stream):
     return y
 
 
+def _norm_rope_common(q, k, inv_freq, q_weight, k_weight, eps, positions, offset, interleaved, scale, packed, sizes, nhd, dtype):
+    """The fields from B on that the two argument structures share."""
+    weight = q_weight if q_weight is not None else k_weight
+    return (*sizes[:2], 0 if k is None else k.shape[1] if packed or not nhd else k.shape[2], *sizes[2:], 0 if inv_freq is None else 2 * inv_freq.numel(), dtype, nhd,
+            0 if weight is None or weight.dtype == torch.float32 else 1, 1 if interleaved else 0, eps, scale, _address(inv_freq), _address(positions),
+            sizes[2] if positions is not None and positions.dim() == 2 else 0, _whole(offset, 64))
+
+
 def sage_qk_norm_rope(q, k=None, inv_freq=None, q_weight=None, k_weight=None, eps=1e-6, positions=None, offset=0, interleaved=False, scale=1.0, layout="HND",
                       q_out=None, k_out=None, stream=None):
     """Every row of q and k divided by the root of its mean square (plus eps), times the weight of its channels (float32 or the tensors' type, [d]; None:
     ones), and its first 2 * len(inv_freq) channels turned as sage_rope does (inv_freq None: none), in one pass.  q [B, H, N, d], k [B, H_kv, N, d] or None
     (layout "HND"; tokens outside heads with "NHD"), or packed [tokens, heads, d]; any strides will do while the channels are contiguous.  q_out, k_out may be q and
     k.  Returns q_out, or (q_out, k_out)."""
-    f, index, packed, nhd = _norm_rope_fields(q, k, inv_freq, q_weight, k_weight, eps, positions, offset, interleaved, scale, layout)
+    dtype, index = _dtype_code(q), _gpu_of("q", q)
+    packed, nhd, sizes = _norm_rope_sizes(q, layout)
     raw_stream = _stream_on(index, stream)
+    _check_norm_rope(q, k, inv_freq, q_weight, k_weight, positions, index, packed, nhd, sizes)
     if k is None and k_out is not None:
         raise ValueError("k_out without k")
     q_out, k_out = _output_like("q_out", q, q_out, index, stream), _output_like("k_out", k, k_out, index, stream)
-    a = sage_qk_norm_rope_args(q_out=q_out.data_ptr(), k_out=_address(k_out), stream=raw_stream, **f)
-    for t, st in ((q, a.q_strides), (k, a.k_strides), (q_out, a.q_out_strides), (k_out, a.k_out_strides)):
-        _set_strides(st, t, packed, nhd)
+    a = sage_qk_norm_rope_args(q.data_ptr(), _address(k), q_out.data_ptr(), _address(k_out), _address(q_weight), _address(k_weight),
+                               *_norm_rope_common(q, k, inv_freq, q_weight, k_weight, eps, positions, offset, interleaved, scale, packed, sizes, nhd, dtype))
+    a.stream = raw_stream
+    for t, field in ((q, "q_strides"), (k, "k_strides"), (q_out, "q_out_strides"), (k_out, "k_out_strides")):
+        if t is not None and not t.is_contiguous():
+            _set_strides(getattr(a, field), t, packed, nhd)
     _call("sage_qk_norm_rope", a, index)
     return q_out if k is None else (q_out, k_out)
 
@@ -845,8 +859,10 @@ def sage_qk_norm_rope_bwd(dq_out, q, dk_out=None, k=None, inv_freq=None, q_weigh
                           scale=1.0, layout="HND", dq=None, dk=None, dq_weight=None, dk_weight=None, workspace=None, stream=None):
     """The gradient of sage_qk_norm_rope: from that of its outputs, dq_out and dk_out, and its inputs, (dq, dk, dq_weight, dk_weight); dk is None
     without k.  The weights' are float32 [d], and None for a weight that is None.  dq may be dq_out, and dk dk_out."""
-    f, index, packed, nhd = _norm_rope_fields(q, k, inv_freq, q_weight, k_weight, eps, positions, offset, interleaved, scale, layout)
+    dtype, index = _dtype_code(q), _gpu_of("q", q)
+    packed, nhd, sizes = _norm_rope_sizes(q, layout)
     raw_stream = _stream_on(index, stream)
+    _check_norm_rope(q, k, inv_freq, q_weight, k_weight, positions, index, packed, nhd, sizes)
     if (k is None) != (dk_out is None) or (k is None and dk is not None):
         raise ValueError("k, its gradient and that of its output go together")
     for name, x, g in (("dq_out", q, dq_out), ("dk_out", k, dk_out)):
@@ -859,35 +875,44 @@ def sage_qk_norm_rope_bwd(dq_out, q, dk_out=None, k=None, inv_freq=None, q_weigh
             if g is not None:
                 raise ValueError(f"{name} without its weight")
         elif g is None:
-            g = _new((f["d"],), torch.float32, index, stream)
+            g = _new(sizes[3:], torch.float32, index, stream)
         else:
-            _need(name, g, index, torch.float32, (f["d"],))
+            _need(name, g, index, torch.float32, sizes[3:])
         grads.append(g)
-    a = sage_qk_norm_rope_bwd_args(dq_out=dq_out.data_ptr(), dk_out=_address(dk_out), dq=dq.data_ptr(), dk=_address(dk), dq_weight=_address(grads[0]),
-                                   dk_weight=_address(grads[1]), stream=raw_stream, **f)
-    for t, st in ((dq_out, a.dq_out_strides), (dk_out, a.dk_out_strides), (q, a.q_strides), (k, a.k_strides), (dq, a.dq_strides), (dk, a.dk_strides)):
-        _set_strides(st, t, packed, nhd)
+    a = sage_qk_norm_rope_bwd_args(dq_out.data_ptr(), _address(dk_out), q.data_ptr(), _address(k), dq.data_ptr(), _address(dk), _address(q_weight), _address(k_weight),
+                                   _address(grads[0]), _address(grads[1]),
+                                   *_norm_rope_common(q, k, inv_freq, q_weight, k_weight, eps, positions, offset, interleaved, scale, packed, sizes, nhd, dtype))
+    a.stream = raw_stream
+    for t, field in ((dq_out, "dq_out_strides"), (dk_out, "dk_out_strides"), (q, "q_strides"), (k, "k_strides"), (dq, "dq_strides"), (dk, "dk_strides")):
+        if t is not None and not t.is_contiguous():
+            _set_strides(getattr(a, field), t, packed, nhd)
     keep = _own_workspace("sage_qk_norm_rope_bwd", a, index, workspace, stream)
     _call("sage_qk_norm_rope_bwd", a, index)
     del keep
     return dq, dk, grads[0], grads[1]
 
 
+_E4M3, _E8M0 = torch.float8_e4m3fn, torch.float8_e8m0fnu
+
+
 def _paged_cache(k_cache, v_cache, k_scale, v_scale, page_table, index, B, Hkv, d):
     """The arrays of a cache in pages, checked: (pages, tokens of a page, pages of a sequence)."""
     if k_cache.dim() != 4 or page_table.dim() != 2:
         raise ValueError("k_cache must have 4 dimensions and page_table 2")
-    pages, heads, page, dc = k_cache.shape
+    shape = k_cache.shape
+    pages, heads, page, dc = shape
     if heads != Hkv or dc != d:
-        raise ValueError(f"k_cache must have shape [pages, {Hkv}, page, {d}], got {tuple(k_cache.shape)}")
+        raise ValueError(f"k_cache must have shape [pages, {Hkv}, page, {d}], got {tuple(shape)}")
     if page % 32 != 0 or page == 0:
         raise ValueError(f"a page must hold a multiple of 32 tokens, got {page}")
-    _need("k_cache", k_cache, index, torch.float8_e4m3fn)
-    _need("v_cache", v_cache, index, torch.float8_e4m3fn, k_cache.shape)
-    _need("k_scale", k_scale, index, torch.float8_e8m0fnu, (pages, Hkv, page // 32))
-    _need("v_scale", v_scale, index, torch.float8_e8m0fnu, (pages, Hkv, page // 32))
-    _need("page_table", page_table, index, torch.int32, (B, page_table.shape[1]))
-    return pages, page, page_table.shape[1]
+    blocks = (pages, heads, page // 32)
+    _need("k_cache", k_cache, index, _E4M3)
+    _need("v_cache", v_cache, index, _E4M3, shape)
+    _need("k_scale", k_scale, index, _E8M0, blocks)
+    _need("v_scale", v_scale, index, _E8M0, blocks)
+    of_one = page_table.shape[1]
+    _need("page_table", page_table, index, torch.int32, (B, of_one))
+    return pages, page, of_one
 
 
 def sage_cache_append(k, v, k_cache, v_cache, k_scale, v_scale, page_table, kv_lens=None, new_lens=None, layout="HND", stream=None):
@@ -901,14 +926,17 @@ def sage_cache_append(k, v, k_cache, v_cache, k_scale, v_scale, page_table, kv_l
     if v.get_device() != index or v.dtype != k.dtype or v.shape != k.shape:
         raise ValueError("v must have the type, shape and device of k")
     pages, page, max_pages = _paged_cache(k_cache, v_cache, k_scale, v_scale, page_table, index, B, Hkv, d)
-    for name, t in (("kv_lens", kv_lens), ("new_lens", new_lens)):
-        if t is not None:
-            _need(name, t, index, torch.int32, (B,))
+    if kv_lens is not None:
+        _need("kv_lens", kv_lens, index, torch.int32, (B,))
+    if new_lens is not None:
+        _need("new_lens", new_lens, index, torch.int32, (B,))
     a = sage_cache_append_args(k.data_ptr(), v.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), page_table.data_ptr(),
                                _address(kv_lens), _address(new_lens), B, Hkv, N, d, pages, page, max_pages, dtype, nhd)
     a.stream = raw_stream
-    _set_strides(a.k_strides, k, False, nhd)
-    _set_strides(a.v_strides, v, False, nhd)
+    if not k.is_contiguous():
+        _set_strides(a.k_strides, k, False, nhd)
+    if not v.is_contiguous():
+        _set_strides(a.v_strides, v, False, nhd)
     _call("sage_cache_append", a, index)
 
 
@@ -928,19 +956,22 @@ def sage_attn_paged(q, k_cache, v_cache, k_scale, v_scale, page_table, kv_lens=N
     raw_stream = _stream_on(index, stream)
     B, H, N, d = _sizes("q", q, nhd)
     _need("q", q, index, q.dtype)
-    pages, page, max_pages = _paged_cache(k_cache, v_cache, k_scale, v_scale, page_table, index, B, k_cache.shape[1] if k_cache.dim() == 4 else 0, d)
-    for name, t in (("kv_lens", kv_lens), ("q_lens", q_lens)):
-        if t is not None:
-            _need(name, t, index, torch.int32, (B,))
-    make = torch.empty if q_lens is None else torch.zeros
+    Hkv = k_cache.shape[1] if k_cache.dim() == 4 else 0
+    pages, page, max_pages = _paged_cache(k_cache, v_cache, k_scale, v_scale, page_table, index, B, Hkv, d)
+    clear = 0                                   # rows behind q_lens: what is made here the call fills with zeros there
+    if kv_lens is not None:
+        _need("kv_lens", kv_lens, index, torch.int32, (B,))
+    if q_lens is not None:
+        _need("q_lens", q_lens, index, torch.int32, (B,))
+        clear = (SAGE_CLEAR_OUT if out is None else 0) | SAGE_CLEAR_LSE
     if out is None:
-        out = _new(q.shape, q.dtype, index, stream, make)
+        out = _new(q.shape, q.dtype, index, stream)
     else:
         _need("out", out, index, q.dtype, q.shape)
-    lse = _new((B, H, N), torch.float32, index, stream, make) if return_lse else None
+    lse = _new((B, H, N), torch.float32, index, stream) if return_lse else None
     a = sage_attn_paged_args(q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), out.data_ptr(), page_table.data_ptr(),
-                             _address(kv_lens), _address(q_lens), _address(lse), B, H, k_cache.shape[1], N, d, pages, page, max_pages, int(bool(causal)),
-                             _whole(window, 32), _whole(sink, 32), float(sm_scale), dtype, nhd, 0, 0, raw_stream)
+                             _address(kv_lens), _address(q_lens), _address(lse), B, H, Hkv, N, d, pages, page, max_pages, 1 if causal else 0,
+                             _whole(window, 32), _whole(sink, 32), sm_scale, dtype, nhd, clear, 0, 0, raw_stream)
     keep = _own_workspace("sage_attn_paged", a, index, workspace, stream)
     _call("sage_attn_paged", a, index)
     del keep

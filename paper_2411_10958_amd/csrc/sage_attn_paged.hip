@@ -28,7 +28,7 @@ struct PagedParams {
   float *part_o, *part_ml;           // [chunk][B H_kv][G N][d], [chunk][B H_kv][G N][2]
   TensorMap qm;
   int B, H, N, G, cap;               // cap: max_pages * page
-  int causal, window, sink;
+  int causal, window, sink, clear;
   float kappa;                       // sm_scale log2(e)
   int S, rt, units;                  // key chunks, row tiles, workgroups of one row tile: B H_kv S
   FastDiv by_rt8, by_s, by_hkv, by_g, by_gn;      // 8 rt, S, H_kv, G, G N
@@ -111,6 +111,14 @@ __global__ void __launch_bounds__(paged_threads<D>(), paged_occupancy<D>()) k_pa
   const unsigned b = split_by(hkv, p.by_hkv);
   const int len = len_of(p, (int)b), count = count_of(p, (int)b);
   const int rows = count * p.G, r0 = (int)rt * ROWS, nr = min(ROWS, rows - r0);      // rows: (query, head of the group)
+  if (p.clear != 0 && s == 0) {                   // rows behind the last query
+    for (int i = max(r0, rows) + t / (D / 8); i < min(r0 + ROWS, p.N * p.G); i += THREADS / (D / 8)) {
+      unsigned g = (unsigned)i;
+      const unsigned n = split_by(g, p.by_g), h = hkv * p.G + g;
+      if (p.clear & SAGE_CLEAR_OUT) *reinterpret_cast<uint4*>(p.out + row_offset(p.qm, head_offset_of(p.qm, (int)b, (int)h), (int)n) + 8 * (t % (D / 8))) = make_uint4(0, 0, 0, 0);
+      if ((p.clear & SAGE_CLEAR_LSE) && p.lse && t % (D / 8) == 0) p.lse[((size_t)b * p.H + h) * p.N + n] = 0.0f;
+    }
+  }
   if (nr <= 0) return;
   const int coff = max(len - count, 0);
   const Seen first = seen_from(p, len, coff + (int)div_by((unsigned)r0, p.by_g)), last = seen_from(p, len, coff + (int)div_by((unsigned)(r0 + nr - 1), p.by_g));
@@ -619,7 +627,7 @@ int paged_params(const sage_attn_paged_args* a, PagedParams* p, bool need_io) {
   if (!a || a->H <= 0 || a->N <= 0) return SAGE_ERR_INVALID_ARG;
   const int st = cache_shape(&p->c, a->B, a->H_kv, a->d, a->n_pages, a->page, a->max_pages);
   if (st != SAGE_OK) return st;
-  if (a->H % a->H_kv != 0 || a->window < 0 || a->sink < 0 || (a->causal & ~1) != 0 || (a->window > 0 && !a->causal)) return SAGE_ERR_INVALID_ARG;
+  if (a->H % a->H_kv != 0 || a->window < 0 || a->sink < 0 || (a->causal & ~1) != 0 || (a->clear & ~3) != 0 || (a->window > 0 && !a->causal)) return SAGE_ERR_INVALID_ARG;
   if (a->dtype != SAGE_DT_FP16 && a->dtype != SAGE_DT_BF16) return SAGE_ERR_UNSUPPORTED;
   if (a->layout != SAGE_LAYOUT_HND && a->layout != SAGE_LAYOUT_NHD) return SAGE_ERR_UNSUPPORTED;
   if (a->N > MAX_TOKENS || (long long)a->B * a->H > 65535 || (long long)a->B * a->H * a->N > 1LL << 24) return SAGE_ERR_UNSUPPORTED;
@@ -632,6 +640,7 @@ int paged_params(const sage_attn_paged_args* a, PagedParams* p, bool need_io) {
   p->q = (const unsigned short*)a->q; p->out = (unsigned short*)a->out; p->lse = a->lse; p->lens = a->kv_lens; p->qlens = a->q_lens;
   p->qm = make_tensor_map(a->layout == SAGE_LAYOUT_NHD, a->H, a->N, a->d);
   p->B = a->B; p->H = a->H; p->N = a->N; p->G = a->H / a->H_kv; p->cap = a->max_pages * a->page;
+  p->clear = a->q_lens ? a->clear : 0;
   p->causal = a->causal; p->window = std::min(a->window, MAX_TOKENS * 2); p->sink = std::min(a->sink, MAX_TOKENS);
   p->kappa = (a->sm_scale > 0.0f ? a->sm_scale : (float)(1.0 / std::sqrt((double)a->d))) * LOG2E;
   choose_chunks(p, a->d);

@@ -198,6 +198,23 @@ def test_rows_behind_the_last_query_stay():
         assert (ref.heads_first(out, layout)[1, :, 4:] == 3.0).all() and (ref.heads_first(out, layout)[0] == 3.0).all()
 
 
+@pytest.mark.parametrize("N,cap", [(1, 64), (6, 256), (6, 4096), (50, 256), (50, 4096)])
+def test_rows_behind_the_last_query_are_zeros_where_the_call_makes_the_output(N, cap):
+    pa = _pa()
+    for d, layout in ((64, "HND"), (256, "NHD")):
+        c = pref.filled(4, 2, cap, 64, d, torch.bfloat16)
+        q = _q(4, 6, N, d, torch.bfloat16, layout)
+        lens, counts = _int([cap - 3, 64, 0, 7]), _int([N, 0, N, N // 2])
+        junk = [torch.full_like(q, 9.0) for _ in range(3)] + [torch.full((4, 6, N), 9.0, device="cuda") for _ in range(3)]
+        torch.cuda.synchronize()
+        del junk                                            # (what the allocator hands out next holds numbers)
+        _check(pa, q, c, lens=lens, q_lens=counts, layout=layout)
+        out = torch.full_like(q, 3.0)
+        _, lse = pa.sage_attn_paged(q, **c, kv_lens=lens, q_lens=counts, out=out, layout=layout, return_lse=True)
+        there = (torch.arange(N, device="cuda") < counts[:, None])[:, None]
+        assert (ref.heads_first(out, layout)[~there.expand(4, 6, N)] == 3.0).all() and (lse[~there.expand(4, 6, N)] == 0).all()
+
+
 def test_in_place_of_the_queries():
     pa = _pa()
     for N, cap in ((1, 64), (3, 4096)):
