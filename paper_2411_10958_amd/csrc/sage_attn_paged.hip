@@ -627,7 +627,8 @@ int paged_params(const sage_attn_paged_args* a, PagedParams* p, bool need_io) {
   if (!a || a->H <= 0 || a->N <= 0) return SAGE_ERR_INVALID_ARG;
   const int st = cache_shape(&p->c, a->B, a->H_kv, a->d, a->n_pages, a->page, a->max_pages);
   if (st != SAGE_OK) return st;
-  if (a->H % a->H_kv != 0 || a->window < 0 || a->sink < 0 || (a->causal & ~1) != 0 || (a->clear & ~3) != 0 || (a->window > 0 && !a->causal)) return SAGE_ERR_INVALID_ARG;
+  if (a->H % a->H_kv != 0 || a->window < 0 || a->sink < 0 || (a->causal & ~1) != 0 || (a->clear & ~3) != 0 || (a->window > 0 && !a->causal) || !std::isfinite(a->sm_scale))
+    return SAGE_ERR_INVALID_ARG;
   if (a->dtype != SAGE_DT_FP16 && a->dtype != SAGE_DT_BF16) return SAGE_ERR_UNSUPPORTED;
   if (a->layout != SAGE_LAYOUT_HND && a->layout != SAGE_LAYOUT_NHD) return SAGE_ERR_UNSUPPORTED;
   if (a->N > MAX_TOKENS || (long long)a->B * a->H > 65535 || (long long)a->B * a->H * a->N > 1LL << 24) return SAGE_ERR_UNSUPPORTED;

@@ -96,7 +96,7 @@ PAGED = dict(q=P, k_cache=3 * P, v_cache=4 * P, k_scale=5 * P, v_scale=6 * P, ou
 
 @pytest.mark.parametrize("kw,status", CACHE + [
     (dict(q=0), -1), (dict(out=0), -1), (dict(q=P + 8), -1), (dict(out=2 * P + 2), -1), (dict(lse=10 * P + 2), -1), (dict(q_lens=9 * P + 1), -1), (dict(H=3), -1), (dict(H=0), -1),
-    (dict(causal=2), -1), (dict(clear=4), -1), (dict(window=-1), -1), (dict(sink=-1), -1), (dict(causal=0, window=5), -1), (dict(B=40000, H=2, H_kv=1), -2), (dict(N=1 << 23), -2),
+    (dict(causal=2), -1), (dict(clear=4), -1), (dict(sm_scale=math.inf), -1), (dict(sm_scale=math.nan), -1), (dict(window=-1), -1), (dict(sink=-1), -1), (dict(causal=0, window=5), -1), (dict(B=40000, H=2, H_kv=1), -2), (dict(N=1 << 23), -2),
     (dict(out=3 * P), -1), (dict(lse=2 * P), -1), (dict(lse=P), -1), (dict(out=6 * P), -1), (dict(out=P + 16), -1), (dict(lse=9 * P), -1),
     (dict(max_pages=4096, workspace=0), -3), (dict(max_pages=4096, workspace_bytes=64), -3), (dict(max_pages=4096, workspace=11 * P + 16), -3),
 ])
