@@ -27,7 +27,27 @@ struct AppendParams {
   FastDiv by_hkv, by_blocks;
 };
 
-// 16-bit magnitudes: larger of two packed pairs, values that are not finite as nothing.
+// Larger of two pairs of 16-bit magnitudes, as numbers of the same order.
+__device__ __forceinline__ unsigned larger_pair(unsigned a, unsigned b) {
+  typedef unsigned short v2u __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(unsigned, __builtin_elementwise_max(__builtin_bit_cast(v2u, a), __builtin_bit_cast(v2u, b)));
+}
+// Four values (two dwords) as codes: divided by the scale, rounded to the nearest, all in one instruction for two.
+template <bool BF16> __device__ __forceinline__ unsigned codes_of(unsigned a, unsigned b, float scale) {
+  typedef short v2s __attribute__((ext_vector_type(2)));
+  v2s r = {0, 0};
+  if constexpr (BF16) {
+    typedef __bf16 v2b __attribute__((ext_vector_type(2)));
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(r, __builtin_bit_cast(v2b, a), scale, false);
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(r, __builtin_bit_cast(v2b, b), scale, true);
+  } else {
+    typedef _Float16 v2h __attribute__((ext_vector_type(2)));
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp8_f16(r, __builtin_bit_cast(v2h, a), scale, false);
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp8_f16(r, __builtin_bit_cast(v2h, b), scale, true);
+  }
+  return __builtin_bit_cast(unsigned, r);
+}
+// A 16-bit magnitude, of a value that is not finite nothing.
 template <bool BF16> __device__ __forceinline__ unsigned finite_magnitude(unsigned h) {
   constexpr unsigned EXP = BF16 ? 0x7f80 : 0x7c00;
   h &= 0x7fff;
@@ -74,14 +94,24 @@ __global__ void __launch_bounds__(256) k_append(const AppendParams p) {
       }
     }
   }
+  auto of_all = [](unsigned m) { return (unsigned)(int)wave_max((float)max(m & 0xffff, m >> 16)); };
 #pragma unroll
   for (int s = 0; s < STEPS; ++s)
 #pragma unroll
-    for (int y = 0; y < 4; ++y) most = max(most, max(finite_magnitude<BF16>(v[s][y] & 0xffff), finite_magnitude<BF16>(v[s][y] >> 16)));
+    for (int y = 0; y < 4; ++y) most = larger_pair(most, v[s][y] & 0x7fff7fff);
+  most = of_all(most);
+  const bool finite = most < (BF16 ? 0x7f80u : 0x7c00u);
+  if (!finite) {                                   // (the same, of what is finite)
+    most = 0;
 #pragma unroll
-  for (int o = 1; o < 64; o <<= 1) most = max(most, (unsigned)__shfl_xor((int)most, o));
+    for (int s = 0; s < STEPS; ++s)
+#pragma unroll
+      for (int y = 0; y < 4; ++y) most = larger_pair(most, finite_magnitude<BF16>(v[s][y] & 0xffff) | finite_magnitude<BF16>(v[s][y] >> 16) << 16);
+    most = of_all(most);
+  }
   const unsigned bits = __float_as_uint(load16<BF16>((unsigned short)most));
-  int e = min(max((int)(bits >> 23) - 8 + ((bits & 0x7fffff) > 0x600000 ? 1 : 0), 63), p.most);
+  const int fits = max((int)(bits >> 23) - 8 + ((bits & 0x7fffff) > 0x600000 ? 1 : 0), 63);
+  int e = min(fits, p.most);
   unsigned char* codes = (values ? p.c.v : p.c.k) + (size_t)at * (BLOCK * D) + 8 * (lane % L);
   unsigned char* scale = (values ? p.c.vs : p.c.ks) + at;
   if (lo > t0) {                                   // the block holds earlier tokens
@@ -103,23 +133,33 @@ __global__ void __launch_bounds__(256) k_append(const AppendParams p) {
     }
     e = max(e, old);
   }
-  const float inv = e == 255 ? NAN : e == 254 ? 0x1p-127f : __uint_as_float((unsigned)(254 - e) << 23);
-  auto scaled = [&](unsigned u) {
-    const float y = load16<BF16>((unsigned short)u) * inv;
-    const float cut = fminf(fmaxf(y, -E4M3_MAX), E4M3_MAX);      // (of a NaN a number)
-    return (u & 0x7fff) < (BF16 ? 0x7f80u : 0x7c00u) && y == y ? cut : NAN;
-  };
+  if (finite && e >= fits && e < 254) {            // nothing to cut
+    const float two = scale_of((unsigned)e);
 #pragma unroll
-  for (int s = 0; s < STEPS; ++s) {
-    const int r = s * R + lane / L;
-    if (t0 + r < lo || t0 + r >= hi) continue;
-    int u[2];
-#pragma unroll
-    for (int y = 0; y < 2; ++y) {
-      u[y] = __builtin_amdgcn_cvt_pk_fp8_f32(scaled(v[s][2 * y] & 0xffff), scaled(v[s][2 * y] >> 16), 0, false);
-      u[y] = __builtin_amdgcn_cvt_pk_fp8_f32(scaled(v[s][2 * y + 1] & 0xffff), scaled(v[s][2 * y + 1] >> 16), u[y], true);
+    for (int s = 0; s < STEPS; ++s) {
+      const int r = s * R + lane / L;
+      if (t0 + r < lo || t0 + r >= hi) continue;
+      *reinterpret_cast<uint2*>(codes + (size_t)r * D) = make_uint2(codes_of<BF16>(v[s][0], v[s][1], two), codes_of<BF16>(v[s][2], v[s][3], two));
     }
-    *reinterpret_cast<uint2*>(codes + (size_t)r * D) = make_uint2((unsigned)u[0], (unsigned)u[1]);
+  } else {
+    const float inv = e == 255 ? NAN : e == 254 ? 0x1p-127f : __uint_as_float((unsigned)(254 - e) << 23);
+    auto scaled = [&](unsigned u) {
+      const float y = load16<BF16>((unsigned short)u) * inv;
+      const float cut = fminf(fmaxf(y, -E4M3_MAX), E4M3_MAX);      // (of a NaN a number)
+      return (u & 0x7fff) < (BF16 ? 0x7f80u : 0x7c00u) && y == y ? cut : NAN;
+    };
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s) {
+      const int r = s * R + lane / L;
+      if (t0 + r < lo || t0 + r >= hi) continue;
+      int u[2];
+#pragma unroll
+      for (int y = 0; y < 2; ++y) {
+        u[y] = __builtin_amdgcn_cvt_pk_fp8_f32(scaled(v[s][2 * y] & 0xffff), scaled(v[s][2 * y] >> 16), 0, false);
+        u[y] = __builtin_amdgcn_cvt_pk_fp8_f32(scaled(v[s][2 * y + 1] & 0xffff), scaled(v[s][2 * y + 1] >> 16), u[y], true);
+      }
+      *reinterpret_cast<uint2*>(codes + (size_t)r * D) = make_uint2((unsigned)u[0], (unsigned)u[1]);
+    }
   }
   if (lane == 0) *scale = (unsigned char)e;
 }
