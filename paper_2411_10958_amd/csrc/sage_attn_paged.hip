@@ -79,18 +79,37 @@ __device__ __forceinline__ void dma_u8(const void* from, unsigned lds_byte) {
   asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_ubyte %2, off" : "={m0}"(m0_after) : "s"(lds_byte), "v"(from) : "memory");
 }
 
-template <int D> constexpr int paged_occupancy() { return D == 64 ? 3 : 2; }      // wavefronts per SIMD
-// Wavefronts that share their rows' channels: of 256, whose outputs and queries would take all registers of a SIMD, two form the same scores and have half of the outputs each.
-// (One on a SIMD with 512 registers: 6 caches of 5120, 5 queries of 4 heads, window 3001: 30 us.)
-template <int D> constexpr int channel_groups() { return D == 256 ? 2 : 1; }
-template <int D> constexpr int paged_threads() { return 256 * channel_groups<D>(); }
+// Sum / maximum of a value over the four lanes 16 apart, in all of them.
+__device__ __forceinline__ float quarter_sum(float x) {
+  const unsigned u = __float_as_uint(half_sum(x));
+  const auto sw = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  return __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
+}
+__device__ __forceinline__ float quarter_max(float x) {
+  const unsigned u = __float_as_uint(half_max(x));
+  const auto sw = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  return fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
+}
 
-// RG: groups of 32 rows of a workgroup.  Its wavefronts are RG row groups times KG = 4 / RG key groups (which take the blocks kg, kg + KG, .. of a tile) times CG channel groups.
+// Wavefronts that share their rows' channels: of 256, whose outputs and queries would take all registers of a SIMD with 32 rows, two form the same scores and have half of the
+// outputs each.  (One on a SIMD with 512 registers: 6 caches of 5120, 5 queries of 4 heads, window 3001: 30 us.)
+template <int D, int COLS> constexpr int channel_groups() { return D == 256 && COLS == 32 ? 2 : 1; }
+template <int D, int COLS> constexpr int paged_threads() { return 256 * channel_groups<D, COLS>(); }
+template <int D, int COLS> constexpr int paged_occupancy() { return D == 64 ? (COLS == 16 ? 4 : 3) : 2; }   // wavefronts per SIMD
+
+// COLS: rows of a wavefront, the columns of its score tiles: 32 (32 x 32 products, two parts of the lanes with eight tokens a step) or, with few, 16 (16 x 16, four parts), which halves the
+// products, the exponentials and the chain of products that a block's scores are.
+// RG: groups of them in a workgroup.  Its wavefronts are RG row groups times KG = 4 / RG key groups (which take the blocks kg, kg + KG, .. of a tile) times CG channel groups.
 // ONE: a workgroup takes all keys and leaves the output itself.
-template <int D, bool BF16, int RG, bool ONE>
-__global__ void __launch_bounds__(paged_threads<D>(), paged_occupancy<D>()) k_paged(const PagedParams p) {
-  constexpr int CG = channel_groups<D>(), THREADS = paged_threads<D>();
-  constexpr int KS = D / 16, CT = D / 32 / CG, KG = 4 / RG, ROWS = 32 * RG;      // CT: channel tiles of a wavefront
+template <int D, bool BF16, int COLS, int RG, bool ONE>
+__global__ void __launch_bounds__((paged_threads<D, COLS>()), (paged_occupancy<D, COLS>())) k_paged(const PagedParams p) {
+  constexpr int CG = channel_groups<D, COLS>(), THREADS = paged_threads<D, COLS>();
+  constexpr bool WIDE = COLS == 32;
+  constexpr int KS = D / (WIDE ? 16 : 32), KST = WIDE ? 2 : 1;      // contraction steps of the two products
+  constexpr int ST = WIDE ? 1 : 2, NSC = WIDE ? 16 : 8;            // score tiles of a block; scores of a lane
+  constexpr int CT = D / COLS / CG, AV = WIDE ? 16 : 4;            // channel tiles of a wavefront, values of one in a lane
+  constexpr int KG = 4 / RG, ROWS = COLS * RG;
+  typedef typename std::conditional<WIDE, v16f, v4f>::type acc_t;
   constexpr bool SHARED = RG > 1 || CG > 1;       // wavefronts read blocks that others copied
   constexpr unsigned BYTES = BLOCK * D;           // of a block of K or V
   constexpr int COPIES = D / 32;                  // copies of 64 pieces of a block of K (or V)
@@ -98,7 +117,7 @@ __global__ void __launch_bounds__(paged_threads<D>(), paged_occupancy<D>()) k_pa
   __shared__ float s_ml[4 * CG][64];
   __shared__ unsigned s_scale[4 * CG][2][64];     // of the blocks in at_lo, at_hi: K's, V's
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
-  const int col = lane & 31, half = lane >> 5, cg = wave % CG, own = wave / CG, kg = own % KG, rg = own / KG;      // own: the block of a tile that this one copies
+  const int col = lane & (COLS - 1), part = lane / COLS, cg = wave % CG, own = wave / CG, kg = own % KG, rg = own / KG;      // own: the block of a tile that this one copies
 
   // ---- which rows and keys.  The row tiles of the same keys are 8 apart: workgroups go to the 8 XCDs in turn and each has a cache of its own.
   unsigned rt = blockIdx.x;
@@ -131,7 +150,7 @@ __global__ void __launch_bounds__(paged_threads<D>(), paged_occupancy<D>()) k_pa
     j0 = min((int)s * per, tiles);
     j1 = min(j0 + per, tiles);
   }
-  const bool active = rg * 32 < nr;
+  const bool active = rg * COLS < nr;
   const size_t part0 = ((size_t)s * (p.B * p.c.Hkv) + bh) * ((size_t)p.G * p.N) + r0;      // of the partial results' rows
   if (!ONE && j0 >= j1) {                         // no keys: a partial result that the merge skips
     for (int i = t; i < nr; i += THREADS) {
@@ -141,14 +160,14 @@ __global__ void __launch_bounds__(paged_threads<D>(), paged_occupancy<D>()) k_pa
     return;
   }
 
-  // ---- my row's query as the B operand: channels 32 u + 16 half + 0..15 are two steps
-  const int i0 = r0 + min(rg * 32 + col, nr - 1);
+  // ---- my row's query as the B operand: 16 channels of each part are two steps
+  const int i0 = r0 + min(rg * COLS + col, nr - 1);
   unsigned rh = (unsigned)i0;
   const unsigned rn = split_by(rh, p.by_g);
   const size_t qrow = row_offset(p.qm, head_offset_of(p.qm, (int)b, (int)(hkv * p.G + rh)), (int)rn);
   v4i q[KS];
 #pragma unroll
-  for (int st = 0; st < KS; ++st) q[st] = *reinterpret_cast<const v4i*>(p.q + qrow + 32 * (st >> 1) + 16 * half + 8 * (st & 1));
+  for (int st = 0; st < KS; ++st) q[st] = *reinterpret_cast<const v4i*>(p.q + qrow + 16 * ((64 / COLS) * (st >> 1) + part) + 8 * (st & 1));
   const Seen mine = seen_from(p, len, coff + (int)rn);
   // ---- where the next 16 tiles' blocks are in the pool, one block a lane, and their scales, which go to LDS like the blocks do, so that no wait for them is one for what
   // is copied after them.  Half of the lanes are refilled every 8 tiles.
@@ -216,67 +235,86 @@ __global__ void __launch_bounds__(paged_threads<D>(), paged_occupancy<D>()) k_pa
   copy(j0, 0);
   bool next = j0 + 1 < j1 && copy(j0 + 1, 1);     // whether tile j + 1 is on its way
 
-  v16f o[CT];
+  acc_t o[CT];
 #pragma unroll
   for (int c = 0; c < CT; ++c)
 #pragma unroll
-    for (int v = 0; v < 16; ++v) o[c][v] = 0.0f;
-  float mx = -INFINITY, l = 0.0f;                 // running maximum (of both halves; fp16: less 14) and this half's sum
+    for (int v = 0; v < AV; ++v) o[c][v] = 0.0f;
+  float mx = -INFINITY, l = 0.0f;                 // running maximum (of all parts; fp16: less 14) and this part's sum
 
-  // Where my operands start in a block.  K: row of token 16 (g / 2) + 8h + 4 (g % 2) + r for operand row 8g + 4h + r, so that half h of the lanes gets scores of
-  // tokens 8h + 0..7 and 16 + 8h + 0..7, as the second product wants its weights; two pieces' steps are an exclusive or.  V: the transposed read gives lane l channel
-  // l % 16 of the eight tokens whose rows its group of 16 lanes point at, two lanes a row.
+  // Where my operands start in a block; steps to other pieces are exclusive ors.  K: rows in an order that gives each part of the lanes the scores of the tokens whose weights the
+  // second product wants of it: tokens 8 part + 0..7 (32 columns: and 16 on), score i of a lane being token_of(i).  V: the transposed read gives lane l channel l % 16 of the
+  // eight tokens whose rows its group of 16 lanes point at, two lanes a row.
   typedef __attribute__((address_space(3))) const v4i* lds_v4i;
   typedef __attribute__((address_space(3))) v2i* lds_v2i;
-  const int kr = 16 * (col >> 4) + 8 * ((col >> 2) & 1) + 4 * ((col >> 3) & 1) + (col & 3), vr = 8 * half + ((lane & 15) >> 1);
-  const unsigned k_at = (unsigned)(kr * D + (half ^ turn<D>(kr)) * 16);
-  const unsigned v_at = BYTES + ((unsigned)(vr * D + (((lane >> 4) & 1) ^ turn<D>(vr)) * 16 + 8 * (lane & 1)) ^ (unsigned)(32 * CT * cg));
+  unsigned k_at[ST];
+#pragma unroll
+  for (int y = 0; y < ST; ++y) {
+    const int kr = WIDE ? 16 * (col >> 4) + 8 * ((col >> 2) & 1) + 4 * ((col >> 3) & 1) + (col & 3) : 8 * (col >> 2) + 4 * y + (col & 3);
+    k_at[y] = (unsigned)(kr * D + (part ^ turn<D>(kr)) * 16);
+  }
+  const int vr = 8 * part + ((lane & 15) >> 1);
+  const unsigned v_at = BYTES + ((unsigned)(vr * D + ((WIDE ? (lane >> 4) & 1 : 0) ^ turn<D>(vr)) * 16 + 8 * (lane & 1)) ^ (unsigned)(COLS * CT * cg));
+  auto token_of = [&](int i) __attribute__((always_inline)) { return WIDE ? 16 * (i >> 3) + 8 * part + (i & 7) : 8 * part + i; };
+  auto mfma = [](v4i x, v4i y, acc_t c) __attribute__((always_inline)) {
+    if constexpr (WIDE) return mfma16<BF16>(x, y, c);
+    else return mfma16_small<BF16>(x, y, c);
+  };
 
   // One block: scores, weights and their product with V.  PART: some row does not see some token of it.
   constexpr int FITS = BF16 ? 246 : 134;           // 448 2^119 and 448 2^7 are numbers of the type
-  auto attend = [&](auto part, unsigned base, int t0, float kk, int ev) __attribute__((always_inline)) {
-    constexpr bool PART = decltype(part)::value;
+  auto attend = [&](auto partly, unsigned base, int t0, float kk, int ev) __attribute__((always_inline)) {
+    constexpr bool PART = decltype(partly)::value;
     const float vs = scale_of((unsigned)(PART ? min(ev, FITS) : ev));
-    const unsigned ka = base + k_at, va = base + v_at;      // (a block's first byte has its low bits zero: steps to other pieces need no address kept over the loop)
-    v16f sc;
+    const unsigned va = base + v_at;              // (a block's first byte has its low bits zero: steps to other pieces need no address kept over the loop)
+    acc_t tile[ST];
 #pragma unroll
-    for (int v = 0; v < 16; ++v) sc[v] = 0.0f;
-    constexpr int AHEAD = PART ? 1 : KS / 2 < 4 ? KS / 2 : 4;      // reads of K in flight
+    for (int y = 0; y < ST; ++y)
+#pragma unroll
+      for (int v = 0; v < AV; ++v) tile[y][v] = 0.0f;
+    constexpr int AHEAD = PART ? 1 : KS / 2 < 4 / ST ? KS / 2 : 4 / ST;      // reads of K in flight
 #pragma unroll
     for (int u0 = 0; u0 < KS / 2; u0 += AHEAD) {
-      v4i x[AHEAD];
+      v4i x[AHEAD][ST];
 #pragma unroll
-      for (int u = 0; u < AHEAD; ++u) x[u] = *(lds_v4i)(uintptr_t)(ka ^ (32 * (u0 + u)));
+      for (int u = 0; u < AHEAD; ++u)
+#pragma unroll
+        for (int y = 0; y < ST; ++y) x[u][y] = *(lds_v4i)(uintptr_t)((base + k_at[y]) ^ (16 * (64 / COLS) * (u0 + u)));
       if constexpr (!PART) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int u = 0; u < AHEAD; ++u) {
-        sc = mfma16<BF16>(widen<BF16>(x[u][0], x[u][1], 1.0f), q[2 * (u0 + u)], sc);
-        sc = mfma16<BF16>(widen<BF16>(x[u][2], x[u][3], 1.0f), q[2 * (u0 + u) + 1], sc);
+#pragma unroll
+        for (int y = 0; y < ST; ++y) tile[y] = mfma(widen<BF16>(x[u][y][0], x[u][y][1], 1.0f), q[2 * (u0 + u)], tile[y]);
+#pragma unroll
+        for (int y = 0; y < ST; ++y) tile[y] = mfma(widen<BF16>(x[u][y][2], x[u][y][3], 1.0f), q[2 * (u0 + u) + 1], tile[y]);
       }
     }
     // The values are read while the weights are worked out
-    v2i xv[PART ? 1 : 2][CT];
+    v2i xv[PART ? 1 : KST][CT];
     if constexpr (!PART) {
 #pragma unroll
-      for (int ks = 0; ks < 2; ++ks)
+      for (int ks = 0; ks < KST; ++ks)
 #pragma unroll
-        for (int c = 0; c < CT; ++c) xv[ks][c] = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_v2i)(uintptr_t)((va ^ (32 * c)) + ks * 16 * D));
+        for (int c = 0; c < CT; ++c) xv[ks][c] = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_v2i)(uintptr_t)((va ^ (COLS * c)) + ks * 16 * D));
       __builtin_amdgcn_sched_barrier(0);
     }
-    unsigned seen = 0xffff;                       // bit v: my row sees score v's token
+    float sc[NSC];
+#pragma unroll
+    for (int i = 0; i < NSC; ++i) sc[i] = tile[i / AV][i % AV];
+    unsigned seen = 0xffff;                       // bit i: my row sees score i's token
     if constexpr (PART) {
       seen = 0;
 #pragma unroll
-      for (int v = 0; v < 16; ++v) {
-        const bool see = sees(mine, t0 + 16 * (v >> 3) + 8 * half + (v & 7));
-        seen |= (unsigned)see << v;
-        sc[v] = see ? sc[v] : -INFINITY;
+      for (int i = 0; i < NSC; ++i) {
+        const bool see = sees(mine, t0 + token_of(i));
+        seen |= (unsigned)see << i;
+        sc[i] = see ? sc[i] : -INFINITY;
       }
     }
     float top = -INFINITY;
 #pragma unroll
-    for (int v = 0; v < 16; ++v) top = fmaxf(top, sc[v]);
-    top = half_max(top) * kk;
+    for (int i = 0; i < NSC; ++i) top = fmaxf(top, sc[i]);
+    top = (WIDE ? half_max(top) : quarter_max(top)) * kk;
     // (m is a whole step or less off for scores below 2^24, so weights stay below 2^15; beyond, where a step of 14 may be lost, none is taken)
     if (!BF16) top = fabsf(top) < 16777216.0f ? top - 14.0f : top;
     const float m_new = fmaxf(mx, top);
@@ -287,13 +325,13 @@ __global__ void __launch_bounds__(paged_threads<D>(), paged_occupancy<D>()) k_pa
 #pragma unroll
       for (int c = 0; c < CT; ++c)
 #pragma unroll
-        for (int v = 0; v < 16; ++v) o[c][v] *= alpha;
+        for (int v = 0; v < AV; ++v) o[c][v] *= alpha;
       mx = m_new;
     }
     float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    v4i pb[2];
+    v4i pb[KST];
 #pragma unroll
-    for (int v = 0; v < 16; v += 2) {
+    for (int v = 0; v < NSC; v += 2) {
       float e0 = __builtin_amdgcn_exp2f(__fmaf_rn(sc[v], kk, -m)), e1 = __builtin_amdgcn_exp2f(__fmaf_rn(sc[v + 1], kk, -m));
       if constexpr (PART) {                       // (where kk is NaN, or m infinite, a hidden token's weight would not be zero)
         e0 = seen >> v & 1 ? e0 : 0.0f;
@@ -306,24 +344,24 @@ __global__ void __launch_bounds__(paged_threads<D>(), paged_occupancy<D>()) k_pa
     l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
     if constexpr (!PART) {
 #pragma unroll
-      for (int ks = 0; ks < 2; ++ks)
+      for (int ks = 0; ks < KST; ++ks)
 #pragma unroll
-        for (int c = 0; c < CT; ++c) o[c] = mfma16<BF16>(widen<BF16>(xv[ks][c][0], xv[ks][c][1], vs), pb[ks], o[c]);
+        for (int c = 0; c < CT; ++c) o[c] = mfma(widen<BF16>(xv[ks][c][0], xv[ks][c][1], vs), pb[ks], o[c]);
     } else {
       // A NaN among V times a weight of zero would reach rows that do not see it: NaN is taken out before the product.  How many of a channel's a row sees is a product
       // too, of ones; where that is not zero, the output is NaN.  What no row sees counts as zeros.
       constexpr unsigned UNIT = BF16 ? 0x3f80 : 0x3c00;
       const float more = ev <= FITS ? 1.0f : scale_of((unsigned)(127 + ev - FITS));      // what vs leaves out
-      v4i sb[2];
-      unsigned keep[2][2];                        // bytes of tokens that some row sees
+      v4i sb[KST];
+      unsigned keep[KST][2];                      // bytes of tokens that some row sees
 #pragma unroll
-      for (int ks = 0; ks < 2; ++ks)
+      for (int ks = 0; ks < KST; ++ks)
 #pragma unroll
         for (int y = 0; y < 2; ++y) {
           keep[ks][y] = 0;
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const int tok = t0 + 16 * ks + 8 * half + 4 * y + e;
+            const int tok = t0 + token_of(8 * ks + 4 * y + e);
             keep[ks][y] |= tok < last.to && (tok >= first.from || tok < last.sink) ? 0xffu << (8 * e) : 0u;
           }
 #pragma unroll
@@ -334,29 +372,30 @@ __global__ void __launch_bounds__(paged_threads<D>(), paged_occupancy<D>()) k_pa
         }
 #pragma unroll
       for (int c = 0; c < CT; ++c) {
-        unsigned nan[2][2];
-        v16f y16;
+        unsigned nan[KST][2], any = 0;
+        acc_t sum_of;
 #pragma unroll
-        for (int v = 0; v < 16; ++v) y16[v] = 0.0f;
+        for (int v = 0; v < AV; ++v) sum_of[v] = 0.0f;
 #pragma unroll
-        for (int ks = 0; ks < 2; ++ks) {
-          v2i x = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_v2i)(uintptr_t)((va ^ (32 * c)) + ks * 16 * D));
+        for (int ks = 0; ks < KST; ++ks) {
+          v2i x = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_v2i)(uintptr_t)((va ^ (COLS * c)) + ks * 16 * D));
 #pragma unroll
           for (int y = 0; y < 2; ++y) {
             const unsigned u = (unsigned)x[y] & keep[ks][y];
             nan[ks][y] = ((u & 0x7f7f7f7fu) + 0x01010101u) >> 7 & 0x01010101u;      // 0x7f and 0xff
+            any |= nan[ks][y];
             x[y] = (int)(u & ~(nan[ks][y] * 0xffu));
           }
-          y16 = mfma16<BF16>(widen<BF16>(x[0], x[1], vs), pb[ks], y16);
+          sum_of = mfma(widen<BF16>(x[0], x[1], vs), pb[ks], sum_of);
         }
 #pragma unroll
-        for (int v = 0; v < 16; ++v) o[c][v] = __fmaf_rn(y16[v], more, o[c][v]);
-        if (__ballot((nan[0][0] | nan[0][1] | nan[1][0] | nan[1][1]) != 0) != 0) {
-          v16f hits;
+        for (int v = 0; v < AV; ++v) o[c][v] = __fmaf_rn(sum_of[v], more, o[c][v]);
+        if (__ballot(any != 0) != 0) {
+          acc_t hits;
 #pragma unroll
-          for (int v = 0; v < 16; ++v) hits[v] = 0.0f;
+          for (int v = 0; v < AV; ++v) hits[v] = 0.0f;
 #pragma unroll
-          for (int ks = 0; ks < 2; ++ks) {
+          for (int ks = 0; ks < KST; ++ks) {
             v4i a;
 #pragma unroll
             for (int y = 0; y < 2; ++y) {
@@ -364,10 +403,10 @@ __global__ void __launch_bounds__(paged_threads<D>(), paged_occupancy<D>()) k_pa
               a[2 * y] = (int)((n & 1 ? UNIT : 0u) | (n >> 8 & 1 ? UNIT << 16 : 0u));
               a[2 * y + 1] = (int)((n >> 16 & 1 ? UNIT : 0u) | (n >> 24 & 1 ? UNIT << 16 : 0u));
             }
-            hits = mfma16<BF16>(a, sb[ks], hits);
+            hits = mfma(a, sb[ks], hits);
           }
 #pragma unroll
-          for (int v = 0; v < 16; ++v) o[c][v] = hits[v] > 0.0f ? NAN : o[c][v];
+          for (int v = 0; v < AV; ++v) o[c][v] = hits[v] > 0.0f ? NAN : o[c][v];
         }
         __builtin_amdgcn_sched_barrier(0);        // (channel tiles one after the other: side by side they take more registers than there are)
       }
@@ -395,11 +434,11 @@ __global__ void __launch_bounds__(paged_threads<D>(), paged_occupancy<D>()) k_pa
         whole |= (unsigned)(there && all) << x;
         others |= (unsigned)(there && !all) << x;
       }
-      auto block = [&](auto part, int x) __attribute__((always_inline)) {
+      auto block = [&](auto partly, int x) __attribute__((always_inline)) {
         const int i = 4 * j + x;
         const unsigned two = (unsigned)__builtin_amdgcn_readlane((int)scales, ((j - j0) & 15) * 4 + x);
         const bool nan = two >> 8 == 255;         // a NaN among the scales makes the rows NaN that see the block, through kk
-        attend(part, lds0 + (unsigned)(stage * PT_BLOCKS + x) * (2 * BYTES), BLOCK * (i < ns ? i : i - ns + w0), nan ? NAN : p.kappa * scale_of(two & 255),
+        attend(partly, lds0 + (unsigned)(stage * PT_BLOCKS + x) * (2 * BYTES), BLOCK * (i < ns ? i : i - ns + w0), nan ? NAN : p.kappa * scale_of(two & 255),
                nan ? 127 : (int)(two >> 8));
       };
 #pragma unroll 1
@@ -418,23 +457,23 @@ __global__ void __launch_bounds__(paged_threads<D>(), paged_occupancy<D>()) k_pa
       next = false;
     }
   }
-  l = half_sum(l);
+  l = WIDE ? half_sum(l) : quarter_sum(l);
 
-  // ---- the key groups of the same rows into one, each wavefront's share of the channels: units of four of them a lane, unit 4 c + g is channels 32 c + 8 g + 4 half + 0..3
-  constexpr int UN = 4 * CT / KG;
-  const int unit0 = 4 * CT * cg + kg * UN;        // the first that I write
+  // ---- the key groups of the same rows into one, each wavefront's share of the channels: units of four of them a lane, unit u being channels (256 / COLS) u + 4 part + 0..3
+  constexpr int ALL = CT * AV / 4, UN = ALL / KG;
+  const int unit0 = ALL * cg + kg * UN;           // the first that I write
+  auto mine_of = [&](int u) __attribute__((always_inline)) { return v4f{o[4 * u / AV][4 * u % AV], o[4 * u / AV][4 * u % AV + 1], o[4 * u / AV][4 * u % AV + 2], o[4 * u / AV][4 * u % AV + 3]}; };
   v4f res[UN];
   if constexpr (KG == 1) {
 #pragma unroll
-    for (int u = 0; u < UN; ++u) res[u] = v4f{o[u / 4][4 * (u % 4)], o[u / 4][4 * (u % 4) + 1], o[u / 4][4 * (u % 4) + 2], o[u / 4][4 * (u % 4) + 3]};
+    for (int u = 0; u < UN; ++u) res[u] = mine_of(u);
   } else {
     v4f* x = reinterpret_cast<v4f*>(&s_kv[0]);
     __syncthreads();
     if (active) {
 #pragma unroll
-      for (int u = 0; u < 4 * CT; ++u)
-        x[(wave * 4 * CT + u) * 64 + lane] = v4f{o[u / 4][4 * (u % 4)], o[u / 4][4 * (u % 4) + 1], o[u / 4][4 * (u % 4) + 2], o[u / 4][4 * (u % 4) + 3]};
-      if (half == 0) {
+      for (int u = 0; u < ALL; ++u) x[(wave * ALL + u) * 64 + lane] = mine_of(u);
+      if (part == 0) {
         s_ml[wave][2 * col] = mx;
         s_ml[wave][2 * col + 1] = l;
       }
@@ -456,31 +495,31 @@ __global__ void __launch_bounds__(paged_threads<D>(), paged_occupancy<D>()) k_pa
         res[u] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int k = 0; k < KG; ++k) {
-          const v4f y = x[(((rg * KG + k) * CG + cg) * 4 * CT + kg * UN + u) * 64 + lane];
+          const v4f y = x[(((rg * KG + k) * CG + cg) * ALL + kg * UN + u) * 64 + lane];
 #pragma unroll
           for (int e = 0; e < 4; ++e) res[u][e] = __fmaf_rn(a[k], y[e], res[u][e]);
         }
       }
     }
   }
-  if (!active || rg * 32 + col >= nr) return;
+  if (!active || rg * COLS + col >= nr) return;
   if constexpr (ONE) {
     const bool none = mx == -INFINITY && l == 0.0f;      // no token at all: zeros
     const float inv = none ? 0.0f : __fdiv_rn(1.0f, l);
-    if (p.lse && half == 0 && kg == 0 && cg == 0) p.lse[((size_t)b * p.H + hkv * p.G + rh) * p.N + rn] = none ? -INFINITY : LN2 * (mx + __builtin_amdgcn_logf(l));
-    unsigned short* y = p.out + qrow + 4 * half;
+    if (p.lse && part == 0 && kg == 0 && cg == 0) p.lse[((size_t)b * p.H + hkv * p.G + rh) * p.N + rn] = none ? -INFINITY : LN2 * (mx + __builtin_amdgcn_logf(l));
+    unsigned short* y = p.out + qrow + 4 * part;
 #pragma unroll
     for (int u = 0; u < UN; ++u)
-      *reinterpret_cast<uint2*>(y + 8 * (unit0 + u)) = make_uint2(pack16x2<BF16>(res[u][0] * inv, res[u][1] * inv), pack16x2<BF16>(res[u][2] * inv, res[u][3] * inv));
+      *reinterpret_cast<uint2*>(y + (256 / COLS) * (unit0 + u)) = make_uint2(pack16x2<BF16>(res[u][0] * inv, res[u][1] * inv), pack16x2<BF16>(res[u][2] * inv, res[u][3] * inv));
   } else {
-    const size_t pr = part0 + rg * 32 + col;
-    if (half == 0 && kg == 0 && cg == 0) {
+    const size_t pr = part0 + rg * COLS + col;
+    if (part == 0 && kg == 0 && cg == 0) {
       p.part_ml[pr * 2] = mx;
       p.part_ml[pr * 2 + 1] = l;
     }
-    float* po = p.part_o + pr * D + 4 * half;
+    float* po = p.part_o + pr * D + 4 * part;
 #pragma unroll
-    for (int u = 0; u < UN; ++u) *reinterpret_cast<v4f*>(po + 8 * (unit0 + u)) = res[u];
+    for (int u = 0; u < UN; ++u) *reinterpret_cast<v4f*>(po + (256 / COLS) * (unit0 + u)) = res[u];
   }
 }
 
@@ -594,7 +633,8 @@ __global__ void __launch_bounds__(256) k_paged_merge_few(const PagedParams p) {
   *reinterpret_cast<uint2*>(y) = make_uint2(pack16x2<BF16>(acc[0] * inv, acc[1] * inv), pack16x2<BF16>(acc[2] * inv, acc[3] * inv));
 }
 
-int row_groups(const PagedParams& p) { return p.G * p.N <= 32 ? 1 : p.G * p.N <= 64 ? 2 : 4; }
+// Rows of a workgroup.
+int rows_of(const PagedParams& p) { return p.G * p.N <= 16 ? 16 : p.G * p.N <= 32 ? 32 : p.G * p.N <= 64 ? 64 : 128; }
 
 // Key chunks of a row tile, S.  Workgroups beyond one on each CU (two of 64 channels, and where rows are many and products count, but of 256 channels, which fill the LDS) share
 // what the chip reads, so what counts is rounds of them times the tiles of each, two tiles' worth of a start, and, with a merge, some 9 us of a second launch.  Us, sequences x
@@ -602,21 +642,21 @@ int row_groups(const PagedParams& p) { return p.G * p.N <= 32 ? 1 : p.G * p.N <=
 // 69 (3) 64 (6); 1 x 4096, 600 queries 86 (3) 95 (4) 113 (2); 16 heads of 256 over 4 in 4 x 8192 25 (16) 34 (8) 31 (24); 8 heads over 2 in 4 x 1024 15 (1) 19 (8).
 // Lengths that the host does not know are cut finer, 8 tiles or 2048 workgroups, so that the chip stays full up to the end: 8 x 8192 27 (8) 29 (4); 16 x 32768 128 (16) 133 (8) 141 (32).
 void choose_chunks(PagedParams* p, int d) {
-  const int rg = row_groups(*p);
+  const int rows = rows_of(*p);
   const long long gn = (long long)p->G * p->N;
-  p->rt = (int)((gn + 32 * rg - 1) / (32 * rg));
+  p->rt = (int)((gn + rows - 1) / rows);
   long long keys = p->cap, seen = keys;
-  if (p->window > 0) seen = (long long)p->sink + p->window + std::min((long long)p->N, (32LL * rg + p->G - 1) / p->G + 1) + 2 * BLOCK;
+  if (p->window > 0) seen = (long long)p->sink + p->window + std::min((long long)p->N, (long long)(rows + p->G - 1) / p->G + 1) + 2 * BLOCK;
   const bool even = p->B == 1 || 3 * seen < 2 * keys;      // all sequences about as long, as far as is known here
   const long long tiles = (std::min(keys, seen) + BLOCK * PT_BLOCKS - 1) / (BLOCK * PT_BLOCKS);
-  const long long heads = (long long)p->B * p->c.Hkv * p->rt, places = d == 64 || (rg > 1 && d == 128) ? 512 : 256, merge = d == 64 ? 15 : d == 128 ? 8 : 4;
+  const long long heads = (long long)p->B * p->c.Hkv * p->rt, places = d == 64 || (rows > 32 && d == 128) ? 512 : 256, merge = d == 64 ? 15 : d == 128 ? 8 : 4;
   long long best = 0, chosen = 1;
   for (int S : {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 40, 48, 64, 96, 128}) {
     if (S > tiles) break;
     const long long per = (tiles + S - 1) / S, cost = (heads * ((tiles + per - 1) / per) + places - 1) / places * (per + 2) + (S > 1 ? merge : 0);
     if (S == 1 || cost < best) { best = cost; chosen = S; }
   }
-  if (chosen > 1 && rg == 1 && !even) chosen = std::max(chosen, tiles / std::max(8LL, heads * tiles / 2048));
+  if (chosen > 1 && rows <= 32 && !even) chosen = std::max(chosen, tiles / std::max(8LL, heads * tiles / 2048));
   chosen = std::min(chosen, (long long)MAX_PARTS);
   const long long per = (tiles + chosen - 1) / chosen;
   p->S = (int)((tiles + per - 1) / per);
@@ -654,18 +694,20 @@ int paged_params(const sage_attn_paged_args* a, PagedParams* p, bool need_io) {
 size_t part_rows(const PagedParams& p) { return p.S > 1 ? (size_t)p.S * p.B * p.H * p.N : 0; }
 size_t paged_bytes(const PagedParams& p, int d) { return align256(part_rows(p) * 2 * sizeof(float)) + align256(part_rows(p) * d * sizeof(float)); }
 
-template <int D, bool BF16> hipError_t launch(const PagedParams& p, hipStream_t s) {
+template <int D, bool BF16, bool ONE> void launch_rows(const PagedParams& p, hipStream_t s) {
   const unsigned grid = (unsigned)((p.units + 7) / 8 * 8) * p.rt;
-  const int rg = row_groups(p);
+  const int rows = rows_of(p);
+  if (rows == 16) k_paged<D, BF16, 16, 1, ONE><<<grid, paged_threads<D, 16>(), 0, s>>>(p);
+  else if (rows == 32) k_paged<D, BF16, 32, 1, ONE><<<grid, paged_threads<D, 32>(), 0, s>>>(p);
+  else if (rows == 64) k_paged<D, BF16, 32, 2, ONE><<<grid, paged_threads<D, 32>(), 0, s>>>(p);
+  else k_paged<D, BF16, 32, 4, ONE><<<grid, paged_threads<D, 32>(), 0, s>>>(p);
+}
+template <int D, bool BF16> hipError_t launch(const PagedParams& p, hipStream_t s) {
   if (p.S == 1) {
-    if (rg == 1) k_paged<D, BF16, 1, true><<<grid, paged_threads<D>(), 0, s>>>(p);
-    else if (rg == 2) k_paged<D, BF16, 2, true><<<grid, paged_threads<D>(), 0, s>>>(p);
-    else k_paged<D, BF16, 4, true><<<grid, paged_threads<D>(), 0, s>>>(p);
+    launch_rows<D, BF16, true>(p, s);
     return hipGetLastError();
   }
-  if (rg == 1) k_paged<D, BF16, 1, false><<<grid, paged_threads<D>(), 0, s>>>(p);
-  else if (rg == 2) k_paged<D, BF16, 2, false><<<grid, paged_threads<D>(), 0, s>>>(p);
-  else k_paged<D, BF16, 4, false><<<grid, paged_threads<D>(), 0, s>>>(p);
+  launch_rows<D, BF16, false>(p, s);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   if (p.S <= FEW) {
