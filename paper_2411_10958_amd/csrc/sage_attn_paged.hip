@@ -101,6 +101,10 @@ template <int D, int COLS> constexpr int paged_occupancy() { return D == 64 ? (C
 // products, the exponentials and the chain of products that a block's scores are.
 // RG: groups of them in a workgroup.  Its wavefronts are RG row groups times KG = 4 / RG key groups (which take the blocks kg, kg + KG, .. of a tile) times CG channel groups.
 // ONE: a workgroup takes all keys and leaves the output itself.
+// Two tiles are in LDS, the one that is attended to and the next.  (Four, where no other workgroup needs the room: 8 x 8 tiles of 128 channels 12.0 us, with two 11.6; it is a
+// wavefront's chain of instructions, 0.75 us a block, that a tile takes where few are busy.)  They are dynamic LDS: were their size known, the compiler would see one wavefront on a SIMD with 256
+// channels, hence 512 registers, and move outputs to and from the upper ones (4 x 8192 of 16 heads 16.0 us, so 14.6).
+template <int D> constexpr unsigned lds_bytes() { return 2 * PT_BLOCKS * 2 * BLOCK * D; }
 template <int D, bool BF16, int COLS, int RG, bool ONE>
 __global__ void __launch_bounds__((paged_threads<D, COLS>()), (paged_occupancy<D, COLS>())) k_paged(const PagedParams p) {
   constexpr int CG = channel_groups<D, COLS>(), THREADS = paged_threads<D, COLS>();
@@ -113,7 +117,7 @@ __global__ void __launch_bounds__((paged_threads<D, COLS>()), (paged_occupancy<D
   constexpr bool SHARED = RG > 1 || CG > 1;       // wavefronts read blocks that others copied
   constexpr unsigned BYTES = BLOCK * D;           // of a block of K or V
   constexpr int COPIES = D / 32;                  // copies of 64 pieces of a block of K (or V)
-  __shared__ __align__(1024) v4i s_kv[2 * PT_BLOCKS * 2 * BYTES / 16];      // [stage][block][K, V]
+  extern __shared__ __align__(1024) v4i s_kv[];   // [stage][block][K, V]
   __shared__ float s_ml[4 * CG][64];
   __shared__ unsigned s_scale[4 * CG][2][64];     // of the blocks in at_lo, at_hi: K's, V's
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
@@ -697,10 +701,10 @@ size_t paged_bytes(const PagedParams& p, int d) { return align256(part_rows(p) *
 template <int D, bool BF16, bool ONE> void launch_rows(const PagedParams& p, hipStream_t s) {
   const unsigned grid = (unsigned)((p.units + 7) / 8 * 8) * p.rt;
   const int rows = rows_of(p);
-  if (rows == 16) k_paged<D, BF16, 16, 1, ONE><<<grid, paged_threads<D, 16>(), 0, s>>>(p);
-  else if (rows == 32) k_paged<D, BF16, 32, 1, ONE><<<grid, paged_threads<D, 32>(), 0, s>>>(p);
-  else if (rows == 64) k_paged<D, BF16, 32, 2, ONE><<<grid, paged_threads<D, 32>(), 0, s>>>(p);
-  else k_paged<D, BF16, 32, 4, ONE><<<grid, paged_threads<D, 32>(), 0, s>>>(p);
+  if (rows == 16) k_paged<D, BF16, 16, 1, ONE><<<grid, paged_threads<D, 16>(), lds_bytes<D>(), s>>>(p);
+  else if (rows == 32) k_paged<D, BF16, 32, 1, ONE><<<grid, paged_threads<D, 32>(), lds_bytes<D>(), s>>>(p);
+  else if (rows == 64) k_paged<D, BF16, 32, 2, ONE><<<grid, paged_threads<D, 32>(), lds_bytes<D>(), s>>>(p);
+  else k_paged<D, BF16, 32, 4, ONE><<<grid, paged_threads<D, 32>(), lds_bytes<D>(), s>>>(p);
 }
 template <int D, bool BF16> hipError_t launch(const PagedParams& p, hipStream_t s) {
   if (p.S == 1) {
