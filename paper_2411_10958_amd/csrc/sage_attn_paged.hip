@@ -653,15 +653,15 @@ void choose_chunks(PagedParams* p, int d) {
   if (p->window > 0) seen = (long long)p->sink + p->window + std::min((long long)p->N, (long long)(rows + p->G - 1) / p->G + 1) + 2 * BLOCK;
   const bool even = p->B == 1 || 3 * seen < 2 * keys;      // all sequences about as long, as far as is known here
   const long long tiles = (std::min(keys, seen) + BLOCK * PT_BLOCKS - 1) / (BLOCK * PT_BLOCKS);
-  const long long heads = (long long)p->B * p->c.Hkv * p->rt, merge = d == 64 ? 15 : d == 128 ? 8 : 4;
+  const long long heads = (long long)p->B * p->c.Hkv * p->rt, start = rows > 64 ? 1 : 2, merge = (d == 64 ? 15 : d == 128 ? 8 : 4) * 32 / std::max(rows, 32);
   const int places = d == 64 || (rows > 32 && d == 128) ? 9 : 8;      // log2 of them
   auto rounds = [&](unsigned chunks) { return (heads * chunks + (1 << places) - 1) >> places; };
-  long long best = rounds(1) * (tiles + 2), chosen = 1;
-  if (best > merge + 3)
+  long long best = rounds(1) * (tiles + start), chosen = 1;
+  if (best > merge + start + 1)
     for (unsigned S : {2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 40, 48, 64, 96, 128}) {
       if (S > tiles) break;
       const unsigned per = ((unsigned)tiles + S - 1) / S;
-      const long long cost = rounds(((unsigned)tiles + per - 1) / per) * (per + 2) + merge;
+      const long long cost = rounds(((unsigned)tiles + per - 1) / per) * (per + start) + merge;
       if (cost < best) { best = cost; chosen = S; }
     }
   if (chosen > 1 && rows <= 32 && !even) chosen = std::max(chosen, tiles / std::max(8LL, heads * tiles / 2048));
