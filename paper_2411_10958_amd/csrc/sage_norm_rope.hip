@@ -235,7 +235,7 @@ __global__ void __launch_bounds__(256) k_norm_rope(const NormParams p) {
 }
 
 // A workgroup walks over every gridDim.x-th group of tokens, and leaves its sums for the weights' gradients.
-constexpr int BWD_GROUPS = 1024;         // workgroups at most
+constexpr int BWD_GROUPS = 512;          // workgroups at most: two on a CU, what it has registers for
 template <bool BF16, int VW, bool INTER, bool PAST>
 __global__ void __launch_bounds__(256) k_norm_rope_bwd(const NormParams p) {
   __shared__ __align__(16) NormShared sh;
@@ -435,6 +435,11 @@ void plan(NormParams* p, NormLaunch* l, const NormShape& a, const NormView* v, i
   const int heads = a.H + (a.keys ? a.Hkv : 0), rows_of = 256 / p->units;
   p->lanes = 1;
   while (p->lanes * 2 <= rows_of / 4 && p->lanes * 2 <= heads) p->lanes *= 2;
+  // (Backward: half as many where the workgroups' last round would be near empty: 24 x 98 tokens of 60 heads of 128, 588 groups of 4 for 512 workgroups 36.6 us, 1176 of 2 33.8.)
+  if (most > 0) {
+    const long long groups = ((long long)p->tokens * p->lanes + rows_of - 1) / rows_of;
+    if (groups > most && 4 * ((groups + most - 1) / most) * most > 5 * groups && p->lanes * 2 <= rows_of && p->lanes * 2 <= heads) p->lanes *= 2;
+  }
   p->at_once = rows_of / p->lanes;
   // Reads and writes pass the caches by where every access is whole lines of 128 bytes and what is read and written does not fit the 256 MB of the memory-side cache
   // (as sage_rope).
