@@ -123,6 +123,9 @@ __global__ void __launch_bounds__((paged_threads<D, COLS>()), (paged_occupancy<D
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
   const int col = lane & (COLS - 1), part = lane / COLS, cg = wave % CG, own = wave / CG, kg = own % KG, rg = own / KG;      // own: the block of a tile that this one copies
 
+  // The arguments take five cache lines: one wait for all of them, not one for each where its first word is needed
+  asm volatile("" ::"s"(p.c.table), "s"(p.c.by_bpp.m), "s"(p.lens), "s"(p.qm.sn), "s"(p.kappa), "s"(p.by_s.m), "s"(p.by_gn.m));
+
   // ---- which rows and keys.  The row tiles of the same keys are 8 apart: workgroups go to the 8 XCDs in turn and each has a cache of its own.
   unsigned rt = blockIdx.x;
   unsigned unit = split_by(rt, p.by_rt8) * 8 + rt % 8;
@@ -175,13 +178,15 @@ __global__ void __launch_bounds__((paged_threads<D, COLS>()), (paged_occupancy<D
   const Seen mine = seen_from(p, len, coff + (int)rn);
   // ---- where the next 16 tiles' blocks are in the pool, one block a lane, and their scales, which go to LDS like the blocks do, so that no wait for them is one for what
   // is copied after them.  Half of the lanes are refilled every 8 tiles.
-  int at_lo = -1, at_hi = -1;
-  unsigned scales = 0;
+  int at_lo = -1, at_hi = -1, token0 = 0;        // (no page, or past the last block: -1); the block's first token
+  unsigned about = 0;                             // its scales, K's and V's, and from bit 16 on whether there is one and whether all rows see all of it
   auto fetch = [&](int j, int from, int to) __attribute__((always_inline)) {      // lanes from .. to - 1, the first of them tile j's first block
     const int i = 4 * j + lane - from;
     if (lane < from || lane >= to) return;
     long long at = -1;
-    if (i < nb) at = pool_block(p.c, (int)b, (int)hkv, i < ns ? i : i - ns + w0);
+    const int block = i < ns ? i : i - ns + w0;
+    if (i < nb) at = pool_block(p.c, (int)b, (int)hkv, block);
+    token0 = BLOCK * block;
     at_lo = (int)at; at_hi = (int)(at >> 32);
     if (at < 0) return;
     const unsigned dst = (unsigned)(size_t)(__attribute__((address_space(3))) char*)&s_scale[wave][0][0];
@@ -266,10 +271,10 @@ __global__ void __launch_bounds__((paged_threads<D, COLS>()), (paged_occupancy<D
   };
 
   // One block: scores, weights and their product with V.  PART: some row does not see some token of it.
-  constexpr int FITS = BF16 ? 246 : 134;           // 448 2^119 and 448 2^7 are numbers of the type
+  constexpr unsigned FITS = BF16 ? 246 : 134;      // 448 2^119 and 448 2^7 are numbers of the type
   auto attend = [&](auto partly, unsigned base, int t0, float kk, int ev) __attribute__((always_inline)) {
     constexpr bool PART = decltype(partly)::value;
-    const float vs = scale_of((unsigned)(PART ? min(ev, FITS) : ev));
+    const float vs = scale_of(PART ? min((unsigned)ev, FITS) : (unsigned)ev);
     const unsigned va = base + v_at;              // (a block's first byte has its low bits zero: steps to other pieces need no address kept over the loop)
     acc_t tile[ST];
 #pragma unroll
@@ -355,7 +360,7 @@ __global__ void __launch_bounds__((paged_threads<D, COLS>()), (paged_occupancy<D
       // A NaN among V times a weight of zero would reach rows that do not see it: NaN is taken out before the product.  How many of a channel's a row sees is a product
       // too, of ones; where that is not zero, the output is NaN.  What no row sees counts as zeros.
       constexpr unsigned UNIT = BF16 ? 0x3f80 : 0x3c00;
-      const float more = ev <= FITS ? 1.0f : scale_of((unsigned)(127 + ev - FITS));      // what vs leaves out
+      const float more = (unsigned)ev <= FITS ? 1.0f : scale_of(127 + (unsigned)ev - FITS);      // what vs leaves out
       v4i sb[KST];
       unsigned keep[KST][2];                      // bytes of tokens that some row sees
 #pragma unroll
@@ -424,26 +429,26 @@ __global__ void __launch_bounds__((paged_threads<D, COLS>()), (paged_occupancy<D
     else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
     if constexpr (SHARED) __builtin_amdgcn_s_barrier();      // tile j is there
     asm volatile("" ::: "memory");
-    if (((j - j0) & 7) == 0) scales = s_scale[wave][0][lane] | s_scale[wave][1][lane] << 8;
+    if (((j - j0) & 7) == 0) {
+      // Values that may not fit the 16-bit type go the way of partly seen blocks, which scales their product.
+      const unsigned ek = s_scale[wave][0][lane] & 255, ev = s_scale[wave][1][lane] & 255;
+      const bool all = (ev <= FITS || ev == 255) && token0 + BLOCK <= first.to && (token0 >= last.from || token0 + BLOCK <= first.sink);
+      about = at_hi < 0 ? 0 : ek | ev << 8 | 1u << 16 | (unsigned)all << 17;
+    }
     if (active) {
       // Blocks that all rows see whole first, then the others.  (In one loop, or with a way round the products, the outputs are copied from register to register for each block.)
-      // Values that may not fit the 16-bit type go the way of partly seen blocks, which scales their product.
       unsigned whole = 0, others = 0;
 #pragma unroll
       for (int x = kg; x < PT_BLOCKS; x += KG) {
-        const int at_lane = ((j - j0) & 15) * 4 + x, i = 4 * j + x, t0 = BLOCK * (i < ns ? i : i - ns + w0);
-        const bool there = __builtin_amdgcn_readlane(at_hi, at_lane) >= 0;      // (no tokens: past the last, or no page)
-        const unsigned ev = (unsigned)__builtin_amdgcn_readlane((int)scales, at_lane) >> 8;
-        const bool all = (ev <= FITS || ev == 255) && t0 + BLOCK <= first.to && (t0 >= last.from || t0 + BLOCK <= first.sink);
-        whole |= (unsigned)(there && all) << x;
-        others |= (unsigned)(there && !all) << x;
+        const unsigned w = (unsigned)__builtin_amdgcn_readlane((int)about, ((j - j0) & 15) * 4 + x) >> 16;
+        whole |= (w >> 1) << x;
+        others |= (w & ~(w >> 1) & 1) << x;
       }
       auto block = [&](auto partly, int x) __attribute__((always_inline)) {
-        const int i = 4 * j + x;
-        const unsigned two = (unsigned)__builtin_amdgcn_readlane((int)scales, ((j - j0) & 15) * 4 + x);
-        const bool nan = two >> 8 == 255;         // a NaN among the scales makes the rows NaN that see the block, through kk
-        attend(partly, lds0 + (unsigned)(stage * PT_BLOCKS + x) * (2 * BYTES), BLOCK * (i < ns ? i : i - ns + w0), nan ? NAN : p.kappa * scale_of(two & 255),
-               nan ? 127 : (int)(two >> 8));
+        const int at_lane = ((j - j0) & 15) * 4 + x;
+        const unsigned w = (unsigned)__builtin_amdgcn_readlane((int)about, at_lane), ek = w & 255, ev = w >> 8 & 255;
+        const bool nan = ev == 255;               // a NaN among the scales makes the rows NaN that see the block, through kk
+        attend(partly, lds0 + (unsigned)(stage * PT_BLOCKS + x) * (2 * BYTES), __builtin_amdgcn_readlane(token0, at_lane), nan ? NAN : p.kappa * scale_of(ek), nan ? 127 : (int)ev);
       };
 #pragma unroll 1
       for (; whole != 0; whole &= whole - 1) block(std::false_type{}, __builtin_ctz(whole));
