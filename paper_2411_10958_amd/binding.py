@@ -788,13 +788,13 @@ def _check_norm_rope(q, k, inv_freq, q_weight, k_weight, positions, index, packe
             raise ValueError(f"positions must have shape ({N},) or ({B}, {N}), got {tuple(positions.shape)}")
     elif packed and inv_freq is not None:
         raise ValueError("a packed batch needs positions")
-    first = None
-    for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
-        if w is not None:
-            first = w if first is None else first
-            if w.dtype not in (torch.float32, q.dtype) or w.dtype != first.dtype:
-                raise TypeError(f"the weights must both be float32 or both {q.dtype}, got {name} of {w.dtype}")
-            _need(name, w, index, w.dtype, (d,))
+    if q_weight is not None:
+        _need("q_weight", q_weight, index, q_weight.dtype, (d,))
+    if k_weight is not None:
+        _need("k_weight", k_weight, index, k_weight.dtype if q_weight is None else q_weight.dtype, (d,))
+    weight = q_weight if q_weight is not None else k_weight
+    if weight is not None and weight.dtype != torch.float32 and weight.dtype != q.dtype:
+        raise TypeError(f"the weights must both be float32 or both {q.dtype}, got {weight.dtype}")
 
 
 def _norm_rope_sizes(q, layout):
@@ -816,6 +816,24 @@ def _output_like(name, x, y, index, stream):
     if y.get_device() != index or y.dtype != x.dtype or y.shape != x.shape:
         raise ValueError(f"{name} must have the type, shape and device of its input")
     return y
+
+
+def _grad_of(name, x, g, index):
+    """Raises unless g, the gradient of an output, goes with the input x."""
+    if g.get_device() != index or g.dtype != x.dtype or g.shape != x.shape:
+        raise ValueError(f"{name} must have the type, shape and device of its input")
+
+
+def _weight_grad(name, w, g, shape, index, stream):
+    """Room for a weight's gradient, as given or new; None for a weight that is not there."""
+    if w is None:
+        if g is not None:
+            raise ValueError(f"{name} without its weight")
+        return None
+    if g is None:
+        return _new(shape, torch.float32, index, stream)
+    _need(name, g, index, torch.float32, shape)
+    return g
 
 
 def _norm_rope_common(q, k, inv_freq, q_weight, k_weight, eps, positions, offset, interleaved, scale, packed, sizes, nhd, dtype):
@@ -842,9 +860,15 @@ def sage_qk_norm_rope(q, k=None, inv_freq=None, q_weight=None, k_weight=None, ep
     a = sage_qk_norm_rope_args(q.data_ptr(), _address(k), q_out.data_ptr(), _address(k_out), _address(q_weight), _address(k_weight),
                                *_norm_rope_common(q, k, inv_freq, q_weight, k_weight, eps, positions, offset, interleaved, scale, packed, sizes, nhd, dtype))
     a.stream = raw_stream
-    for t, field in ((q, "q_strides"), (k, "k_strides"), (q_out, "q_out_strides"), (k_out, "k_out_strides")):
-        if t is not None and not t.is_contiguous():
-            _set_strides(getattr(a, field), t, packed, nhd)
+    if not q.is_contiguous():
+        _set_strides(a.q_strides, q, packed, nhd)
+    if not q_out.is_contiguous():
+        _set_strides(a.q_out_strides, q_out, packed, nhd)
+    if k is not None:
+        if not k.is_contiguous():
+            _set_strides(a.k_strides, k, packed, nhd)
+        if not k_out.is_contiguous():
+            _set_strides(a.k_out_strides, k_out, packed, nhd)
     _call("sage_qk_norm_rope", a, index)
     return q_out if k is None else (q_out, k_out)
 
@@ -865,31 +889,33 @@ def sage_qk_norm_rope_bwd(dq_out, q, dk_out=None, k=None, inv_freq=None, q_weigh
     _check_norm_rope(q, k, inv_freq, q_weight, k_weight, positions, index, packed, nhd, sizes)
     if (k is None) != (dk_out is None) or (k is None and dk is not None):
         raise ValueError("k, its gradient and that of its output go together")
-    for name, x, g in (("dq_out", q, dq_out), ("dk_out", k, dk_out)):
-        if x is not None and (g.get_device() != index or g.dtype != x.dtype or g.shape != x.shape):
-            raise ValueError(f"{name} must have the type, shape and device of its input")
+    _grad_of("dq_out", q, dq_out, index)
+    if k is not None:
+        _grad_of("dk_out", k, dk_out, index)
     dq, dk = _output_like("dq", q, dq, index, stream), _output_like("dk", k, dk, index, stream)
-    grads = []
-    for name, w, g in (("dq_weight", q_weight, dq_weight), ("dk_weight", k_weight, dk_weight)):
-        if w is None:
-            if g is not None:
-                raise ValueError(f"{name} without its weight")
-        elif g is None:
-            g = _new(sizes[3:], torch.float32, index, stream)
-        else:
-            _need(name, g, index, torch.float32, sizes[3:])
-        grads.append(g)
+    dq_weight = _weight_grad("dq_weight", q_weight, dq_weight, sizes[3:], index, stream)
+    dk_weight = _weight_grad("dk_weight", k_weight, dk_weight, sizes[3:], index, stream)
     a = sage_qk_norm_rope_bwd_args(dq_out.data_ptr(), _address(dk_out), q.data_ptr(), _address(k), dq.data_ptr(), _address(dk), _address(q_weight), _address(k_weight),
-                                   _address(grads[0]), _address(grads[1]),
+                                   _address(dq_weight), _address(dk_weight),
                                    *_norm_rope_common(q, k, inv_freq, q_weight, k_weight, eps, positions, offset, interleaved, scale, packed, sizes, nhd, dtype))
     a.stream = raw_stream
-    for t, field in ((dq_out, "dq_out_strides"), (dk_out, "dk_out_strides"), (q, "q_strides"), (k, "k_strides"), (dq, "dq_strides"), (dk, "dk_strides")):
-        if t is not None and not t.is_contiguous():
-            _set_strides(getattr(a, field), t, packed, nhd)
+    if not dq_out.is_contiguous():
+        _set_strides(a.dq_out_strides, dq_out, packed, nhd)
+    if not q.is_contiguous():
+        _set_strides(a.q_strides, q, packed, nhd)
+    if not dq.is_contiguous():
+        _set_strides(a.dq_strides, dq, packed, nhd)
+    if k is not None:
+        if not dk_out.is_contiguous():
+            _set_strides(a.dk_out_strides, dk_out, packed, nhd)
+        if not k.is_contiguous():
+            _set_strides(a.k_strides, k, packed, nhd)
+        if not dk.is_contiguous():
+            _set_strides(a.dk_strides, dk, packed, nhd)
     keep = _own_workspace("sage_qk_norm_rope_bwd", a, index, workspace, stream)
     _call("sage_qk_norm_rope_bwd", a, index)
     del keep
-    return dq, dk, grads[0], grads[1]
+    return dq, dk, dq_weight, dk_weight
 
 
 _E4M3, _E8M0 = torch.float8_e4m3fn, torch.float8_e8m0fnu
