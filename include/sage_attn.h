@@ -413,7 +413,8 @@ int sage_cache_evict(const sage_cache_evict_args* args);
 /* Norm of every head's queries and keys, and their rotation, in one pass - what models with normalised queries and keys do in front of
  * attention.  Every row x of d channels becomes  R(x / sqrt(mean(x^2) + eps) * weight)  with R the rotation of sage_rope (its positions,
  * frequencies and pairs); rounded once, at the end.  Sums are FP32.  Rows whose squares do not fit it, beyond 1.8e19, become zeros, as the division by
- * infinity says; a value that is not finite reaches its own row only.  In place and views: as sage_rope. */
+ * infinity says; a value that is not finite reaches its own row only, and a row of zeros with eps = 0 is 0 / 0.  B N is 2^26 at most.  In place and views: as sage_rope; outputs that
+ * share a value with a weight, the frequencies or the positions are refused. */
 enum { SAGE_WEIGHT_FP32 = 0, SAGE_WEIGHT_SAME = 1 };
 typedef struct sage_qk_norm_rope_args {
   const void* q;            /* device, [B, H, N, d] or [B, N, H, d]; rows are aligned to 2 bytes at least (16 is fastest) */
@@ -479,7 +480,8 @@ int sage_qk_norm_rope_bwd(const sage_qk_norm_rope_bwd_args* args);
  * 2^-64 at least and at most 2^119 for bf16, 2^7 for fp16 tokens (whose largest values are kept as 448 times that).  A block that holds earlier tokens
  * keeps its scale, or, where the new ones need a larger one, gets that, and the earlier codes are rounded once more: to the same value but for
  * those below 2^-6 of the new scale.  A value that is not finite becomes NaN and does not count for the scale.  Codes behind the last token stay as they were.
- * No page that new tokens go to may belong to another sequence's new tokens too. */
+ * No page that new tokens go to may be that of another sequence's new tokens, or stand twice in its own sequence's row.  The four arrays overlap neither the inputs nor each
+ * other. */
 typedef struct sage_cache_append_args {
   const void* k;            /* device, [B, H_kv, N, d] or [B, N, H_kv, d]; fp16 or bf16; rows are aligned to 2 bytes at least (16 is fastest) */
   const void* v;

@@ -181,6 +181,58 @@ def test_long_caches(B, H, Hkv, cap, N):
     _check(pa, q, c, lens=lens, window=5000, sink=70)
 
 
+@pytest.mark.parametrize("B,H,Hkv,N,cap,d,window,sink", [(64, 4, 4, 1, 4096, 128, 0, 0), (90, 8, 4, 3, 16384, 64, 4000, 40), (16, 16, 16, 140, 3008, 64, 0, 0), (64, 8, 4, 20, 2560, 128, 0, 0)])
+def test_many_tiles_of_one_workgroup(B, H, Hkv, N, cap, d, window, sink):
+    """More than the 16 whose places are looked up at a time: so many sequences that keys are not cut."""
+    pa = _pa()
+    c = pref.filled(B, Hkv, cap, 64, d, torch.bfloat16)
+    c["page_table"][1, 20] = -1
+    q = _q(B, H, N, d, torch.bfloat16, "HND")
+    lens = torch.linspace(cap, cap // 3, B).to(torch.int32).cuda()
+    some = [0, 1, B // 2, B - 1]                           # (every sequence is its own: the reference is asked for a few)
+    out, lse = pa.sage_attn_paged(q, **c, kv_lens=lens, window=window, sink=sink, return_lse=True)
+    few = dict(c, page_table=c["page_table"][some])
+    want, wl, ob, lb = pref.paged(q[some], few, lens[some], None, True, window, sink, 0.0, "HND")
+    ref.check("lse", lse[some], wl, lb)
+    ref.check("out", out[some], want, ob)
+    alone = pa.sage_attn_paged(q, **c, kv_lens=lens, window=window, sink=sink)
+    assert torch.equal(alone, out)
+
+
+@pytest.mark.parametrize("N,G", [(1, 4), (6, 4), (70, 2)])
+def test_scales_that_are_not_numbers(N, G):
+    """A scale byte of 255, K's or V's: NaN in the rows that see its block, and in no others."""
+    pa = _pa()
+    for d in (64, 256):
+        for x in ("k_scale", "v_scale"):
+            c = pref.filled(2, 2, 320, 64, d, torch.bfloat16, seed=3)
+            q = _q(2, 2 * G, N, d, torch.bfloat16, "HND")
+            lens = _int([300, 200])
+            clean = pa.sage_attn_paged(q, **c, kv_lens=lens, window=90, sink=3, return_lse=True)
+            # block 8 (tokens 256 ..) of sequence 0, KV head 1
+            c[x].view(torch.uint8)[int(c["page_table"][0, 4]), 1, 0] = 255
+            got = pa.sage_attn_paged(q, **c, kv_lens=lens, window=90, sink=3, return_lse=True)
+            pos = 300 - N + torch.arange(N, device="cuda")
+            hit = torch.zeros((2, 2 * G, N), dtype=torch.bool, device="cuda")
+            hit[0, G:] = (pos >= 256) & (pos - 90 < 287)
+            assert hit.any() and (N < 50 or not hit[0, G].all())
+            assert got[0][hit].isnan().all() and got[1][hit].isnan().all()
+            assert torch.equal(got[0][~hit], clean[0][~hit]) and torch.equal(got[1][~hit], clean[1][~hit])
+
+
+def test_values_beyond_fp16_with_small_weights():
+    """A cache filled from bf16 tokens, read with fp16 queries: values far beyond 65504 whose weighted mean is within."""
+    pa = _pa()
+    for N in (1, 40):
+        c = pref.filled(1, 1, 256, 32, 64, torch.float16, seed=8)
+        e = c["v_scale"].view(torch.uint8)
+        e[int(c["page_table"][0, 2])] = 127 + 14            # values of up to 448 2^14 in the block of tokens 64 .. 95
+        c["v_cache"].view(torch.uint8)[int(c["page_table"][0, 2]), 0, 1:] = 0
+        q = _q(1, 2, N, 64, torch.float16, "HND", std=0.02)      # (nearly equal weights: the one large token has some 2^-8)
+        out, _ = _check(pa, q, c)
+        assert out.isfinite().all() and out[:, :, -1].abs().max() > 5000
+
+
 def test_rows_behind_the_last_query_stay():
     pa = _pa()
     for layout in ("HND", "NHD"):
