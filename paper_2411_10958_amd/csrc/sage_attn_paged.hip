@@ -8,7 +8,9 @@
 // are in the sum all the same: there m is kept 14 below the maximum, so that weights are up to 2^14 and vanish from 2^-39 of the largest on.
 //
 // With few queries it reads the cache and nothing else should bound it.  A block's K (or V) is 32 d contiguous bytes whatever the size of a page; each wavefront copies its own blocks
-// into LDS, two tiles ahead.  Where all queries of a KV head are 32 rows at most, it also attends to just those blocks, with no barrier; more rows are divided over the wavefronts.
+// into LDS, two tiles ahead.  Where all queries of a KV head are 32 rows at most (256 channels: 16), it also attends to just those blocks, with no barrier; more rows are divided over the wavefronts.
+// 32 heads of 128 over 8: 16 sequences of up to 32768 tokens 123 us (5.7 TB/s), 32 in a window of 4096 47 us (5.8 TB/s).  Chunks of 512 queries over 2 x 16384 tokens 266 us (0.82 PFLOP/s), bound by
+// vector issue: of some 180 instructions of a block 64 widen its codes.  A lone workgroup takes 5 us to its first tile and from its last, and 0.65 us a tile.
 #include "sage_paged.h"
 
 #include <algorithm>
@@ -92,7 +94,7 @@ __device__ __forceinline__ float quarter_max(float x) {
 }
 
 // Wavefronts that share their rows' channels: of 256, whose outputs and queries would take all registers of a SIMD with 32 rows, two form the same scores and have half of the
-// outputs each.  (One on a SIMD with 512 registers: 6 caches of 5120, 5 queries of 4 heads, window 3001: 30 us.)
+// outputs each.  (One on a SIMD with 512 registers: 6 caches of 5120, 5 queries of 4 heads, window 3001: 30 us, so 20.)
 template <int D, int COLS> constexpr int channel_groups() { return D == 256 && COLS == 32 ? 2 : 1; }
 template <int D, int COLS> constexpr int paged_threads() { return 256 * channel_groups<D, COLS>(); }
 template <int D, int COLS> constexpr int paged_occupancy() { return D == 64 ? (COLS == 16 ? 4 : 3) : 2; }   // wavefronts per SIMD
@@ -207,7 +209,7 @@ __global__ void __launch_bounds__((paged_threads<D, COLS>()), (paged_occupancy<D
     const int pc = x * 64 + lane, r = pc / (D / 16);
     offs[x] = (unsigned)(r * D + ((pc % (D / 16)) ^ turn<D>(r)) * 16);
   }
-  const bool once = p.rt == 1;                    // what one workgroup alone reads passes the caches by
+  const bool once = p.rt == 1;                    // what one workgroup alone reads passes the caches by (16 x 32768: 123 us, through them 135)
   auto copy = [&](int j, int stage) __attribute__((always_inline)) -> bool {      // my block of tile j; whether there is one
     const int at_lane = ((j - j0) & 15) * 4 + own;
     const int hi = __builtin_amdgcn_readlane(at_hi, at_lane);
@@ -601,7 +603,7 @@ __global__ void __launch_bounds__(256) k_paged_merge(const PagedParams p) {
   *reinterpret_cast<uint2*>(y) = make_uint2(pack16x2<BF16>(acc[0] * inv, acc[1] * inv), pack16x2<BF16>(acc[2] * inv, acc[3] * inv));
 }
 
-// The same of up to FEW partial results: a thread has four channels of a row and all of their loads in flight.
+// The same of up to FEW partial results: a thread has four channels of a row and all of their loads in flight (32768 rows of two: 8.3 us, a wavefront per row 18).
 constexpr int FEW = 8;
 template <int D, bool BF16>
 __global__ void __launch_bounds__(256) k_paged_merge_few(const PagedParams p) {
@@ -646,10 +648,11 @@ __global__ void __launch_bounds__(256) k_paged_merge_few(const PagedParams p) {
 int rows_of(const PagedParams& p) { return p.G * p.N <= 16 ? 16 : p.G * p.N <= 32 ? 32 : p.G * p.N <= 64 ? 64 : 128; }
 
 // Key chunks of a row tile, S.  Workgroups beyond one on each CU (two of 64 channels, and where rows are many and products count, but of 256 channels, which fill the LDS) share
-// what the chip reads, so what counts is rounds of them times the tiles of each, two tiles' worth of a start, and, with a merge, some 9 us of a second launch.  Us, sequences x
-// tokens of 8 KV heads of 128 channels, 32 heads, chunks in parentheses: 32 in a window of 4096 50 (1) 54 (2) 57 (4); 1 x 32768 21 (32) 23 (64) 28 (16); 8 x 4096, 40 queries 62 (4)
-// 69 (3) 64 (6); 1 x 4096, 600 queries 86 (3) 95 (4) 113 (2); 16 heads of 256 over 4 in 4 x 8192 25 (16) 34 (8) 31 (24); 8 heads over 2 in 4 x 1024 15 (1) 19 (8).
-// Lengths that the host does not know are cut finer, 8 tiles or 2048 workgroups, so that the chip stays full up to the end: 8 x 8192 27 (8) 29 (4); 16 x 32768 128 (16) 133 (8) 141 (32).
+// what the chip reads, so what counts is rounds of them times the tiles of each, a tile's or two's worth of a start, and, with a merge, some 9 us of a second launch.  (A tile takes a
+// wavefront of many rows as long as four of few.)  Us, sequences x tokens of 8 KV heads of 128 channels, 32 heads, chunks in parentheses: 32 in a window of 4096 48 (1) 49 (2) 52 (4);
+// 1 x 32768 20 (32) 21 (64) 23 (16); 8 x 4096, 40 queries 51 (4) 56 (3) 54 (6); 1 x 4096, 600 queries 68 (3) 78 (4) 87 (2); 16 heads of 256 over 4 in 4 x 8192 18 (16) 21 (8) 23 (24); 8 heads
+// over 2 in 4 x 1024 13 (1) 18 (8).
+// Lengths that the host does not know are cut finer, 8 tiles or 2048 workgroups, so that the chip stays full up to the end: 8 x 8192 23 (8) 24 (4); 16 x 32768 125 (16) 127 (8) 132 (32).
 void choose_chunks(PagedParams* p, int d) {
   const int rows = rows_of(*p);
   const long long gn = (long long)p->G * p->N;

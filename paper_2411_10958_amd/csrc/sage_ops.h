@@ -1,4 +1,5 @@
-// Shared by the operators around attention (sage_rope.hip, sage_attn_shared.hip, sage_key_weights.hip, sage_cache.hip).
+// Shared by the operators around attention (sage_rope.hip, sage_attn_shared.hip, sage_key_weights.hip, sage_cache.hip, sage_norm_rope.hip, sage_cache_append.hip,
+// sage_attn_paged.hip).
 #pragma once
 #include "sage_attn_core.h"
 
