@@ -375,7 +375,8 @@ int check_shape(const NormShape& a) {
   if (a.dtype != SAGE_DT_FP16 && a.dtype != SAGE_DT_BF16) return SAGE_ERR_UNSUPPORTED;
   if (a.layout != SAGE_LAYOUT_HND && a.layout != SAGE_LAYOUT_NHD) return SAGE_ERR_UNSUPPORTED;
   if (a.weight_type != SAGE_WEIGHT_FP32 && a.weight_type != SAGE_WEIGHT_SAME) return SAGE_ERR_UNSUPPORTED;
-  if (a.N > MAX_TOKENS || a.B > 65535 || a.H > 65535 || (a.keys && a.Hkv > 65535) || (long long)a.B * a.N > 1LL << 26) return SAGE_ERR_UNSUPPORTED;
+  if (a.N > MAX_TOKENS || a.B > 65535 || a.H > 65535 || (a.keys && a.Hkv > 65535)) return SAGE_ERR_UNSUPPORTED;
+  if (((long long)a.B * a.N + 3) / 4 * 256 > MAX_THREADS) return SAGE_ERR_UNSUPPORTED;      // (a workgroup takes four tokens at least)
   if ((a.interleaved & ~1) != 0) return SAGE_ERR_UNSUPPORTED;
   return SAGE_OK;
 }

@@ -60,6 +60,21 @@ def test_norm_bwd(kw, status):
     assert _status(pa, lib, "sage_qk_norm_rope_bwd", BWD, **kw) == status
 
 
+@pytest.mark.parametrize("B,N", [(4, 1 << 24), (16, 1 << 22), (5, 13421772 + 1), (4 * 5, (1 << 24) // 5 + 1)])
+def test_norms_of_more_tokens_than_a_launch_counts(B, N):
+    """A workgroup of 256 threads takes four tokens at least, and a launch counts its threads in 32 bits: 2^26 - 4 tokens."""
+    pa, lib = _pa()
+    assert B * N > (1 << 26) - 4
+    assert _status(pa, lib, "sage_qk_norm_rope", NORM, B=B, N=N, H=16, q_out=P, k=0, k_out=0, k_weight=0, rot_dim=0, inv_freq=0, q_weight=0) == -2
+    assert _status(pa, lib, "sage_qk_norm_rope_bwd", BWD, B=B, N=N) == -2
+    a = pa.sage_qk_norm_rope_bwd_args()
+    for n, x in {**BWD, "B": 4, "N": (1 << 24) - 1}.items():
+        setattr(a, n, x)
+    assert pa.sage_qk_norm_rope_bwd_workspace_bytes(a) > 0
+    a.N = 1 << 24
+    assert pa.sage_qk_norm_rope_bwd_workspace_bytes(a) == 0
+
+
 def test_norm_bwd_workspace():
     pa, _ = _pa()
     def size(**kw):
