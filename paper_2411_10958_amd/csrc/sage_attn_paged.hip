@@ -200,6 +200,23 @@ __global__ void __launch_bounds__((paged_threads<D, COLS>()), (paged_occupancy<D
   for (int st = 0; st < KS; ++st)                 // (the queries are there with the page numbers: no wait for them is one for a copy)
 #pragma unroll
     for (int x = 0; x < 4; ++x) use_now(q[st][x]);
+  // What a score (to the base 2) of these rows may reach, for a K scale of 1: the largest magnitude of a query times 448, d of them.  Infinities and NaN make their own scores whatever they make.
+  // (32 caches in a window of 4096 take 0.3 us more for it; the far scores looked for block by block, 512 queries 2 x 16384 tokens 4.)
+  unsigned most = 0;
+#pragma unroll
+  for (int st = 0; st < KS; ++st)
+#pragma unroll
+    for (int x = 0; x < 4; ++x) most = larger_pair(most, (unsigned)q[st][x] & 0x7fff7fff);
+  most = largest_of_all(most);
+  if (most >= (BF16 ? 0x7f80u : 0x7c00u)) {
+    most = 0;
+#pragma unroll
+    for (int st = 0; st < KS; ++st)
+#pragma unroll
+      for (int x = 0; x < 4; ++x) most = larger_pair(most, finite_pair<BF16>((unsigned)q[st][x]));
+    most = largest_of_all(most);
+  }
+  const float reach = load16<BF16>((unsigned short)most) * (448.0f * D) * p.kappa;
 
   // ---- copies
   const unsigned lds0 = (unsigned)(size_t)(__attribute__((address_space(3))) char*)&s_kv[0];
@@ -272,8 +289,9 @@ __global__ void __launch_bounds__((paged_threads<D, COLS>()), (paged_occupancy<D
     else return mfma16_small<BF16>(x, y, c);
   };
 
-  // One block: scores, weights and their product with V.  PART: some row does not see some token of it.
+  // One block: scores, weights and their product with V.  PART: some row does not see some token of it, its values may not fit the 16-bit type or its scores may be FAR from zero.
   constexpr unsigned FITS = BF16 ? 246 : 134;      // 448 2^119 and 448 2^7 are numbers of the type
+  constexpr float FAR = 16777216.0f;              // 2^24
   auto attend = [&](auto partly, unsigned base, int t0, float kk, int ev) __attribute__((always_inline)) {
     constexpr bool PART = decltype(partly)::value;
     const float vs = scale_of(PART ? min((unsigned)ev, FITS) : (unsigned)ev);
@@ -326,8 +344,8 @@ __global__ void __launch_bounds__((paged_threads<D, COLS>()), (paged_occupancy<D
 #pragma unroll
     for (int i = 0; i < NSC; ++i) top = fmaxf(top, sc[i]);
     top = (WIDE ? half_max(top) : quarter_max(top)) * kk;
-    // (m is a whole step or less off for scores below 2^24, so weights stay below 2^15; beyond, where a step of 14 may be lost, none is taken)
-    if (!BF16) top = fabsf(top) < 16777216.0f ? top - 14.0f : top;
+    // (Up to a score of 2^24 m is a whole step or less off, so weights stay below 2^15; beyond, where a step of 14 may be lost, none is taken)
+    if (!BF16) top = PART && fabsf(top) >= FAR ? top : top - 14.0f;
     const float m_new = fmaxf(mx, top);
     const float m = m_new == -INFINITY ? 0.0f : m_new;          // (no token seen yet: every weight 2^-inf)
     if (__ballot(m_new > mx) != 0) {
@@ -339,11 +357,22 @@ __global__ void __launch_bounds__((paged_threads<D, COLS>()), (paged_occupancy<D
         for (int v = 0; v < AV; ++v) o[c][v] *= alpha;
       mx = m_new;
     }
+    // m is a rounded product and a weight's exponent is formed from the exact one, so the largest weight is 2^(that rounding): as good as 1, but from 2^24 on a whole step and soon anything.
+    // There the products are rounded like m, and the largest weight is 1.
+    float by = kk;
+    if constexpr (PART) {
+      const bool is_far = fabsf(m) >= FAR;
+      if (__ballot(is_far) != 0) {
+#pragma unroll
+        for (int i = 0; i < NSC; ++i) sc[i] = is_far ? sc[i] * kk : sc[i];
+        by = is_far ? 1.0f : kk;
+      }
+    }
     float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
     v4i pb[KST];
 #pragma unroll
     for (int v = 0; v < NSC; v += 2) {
-      float e0 = __builtin_amdgcn_exp2f(__fmaf_rn(sc[v], kk, -m)), e1 = __builtin_amdgcn_exp2f(__fmaf_rn(sc[v + 1], kk, -m));
+      float e0 = __builtin_amdgcn_exp2f(__fmaf_rn(sc[v], by, -m)), e1 = __builtin_amdgcn_exp2f(__fmaf_rn(sc[v + 1], by, -m));
       if constexpr (PART) {                       // (where kk is NaN, or m infinite, a hidden token's weight would not be zero)
         e0 = seen >> v & 1 ? e0 : 0.0f;
         e1 = seen >> (v + 1) & 1 ? e1 : 0.0f;
@@ -432,9 +461,9 @@ __global__ void __launch_bounds__((paged_threads<D, COLS>()), (paged_occupancy<D
     if constexpr (SHARED) __builtin_amdgcn_s_barrier();      // tile j is there
     asm volatile("" ::: "memory");
     if (((j - j0) & 7) == 0) {
-      // Values that may not fit the 16-bit type go the way of partly seen blocks, which scales their product.
+      // Values that may not fit the 16-bit type, and scores that may be far from zero, go the way of partly seen blocks.
       const unsigned ek = s_scale[wave][0][lane] & 255, ev = s_scale[wave][1][lane] & 255;
-      const bool all = (ev <= FITS || ev == 255) && token0 + BLOCK <= first.to && (token0 >= last.from || token0 + BLOCK <= first.sink);
+      const bool all = (ev <= FITS || ev == 255) && !(reach * scale_of(ek) >= 0.5f * FAR) && token0 + BLOCK <= first.to && (token0 >= last.from || token0 + BLOCK <= first.sink);
       about = at_hi < 0 ? 0 : ek | ev << 8 | 1u << 16 | (unsigned)all << 17;
     }
     if (active) {

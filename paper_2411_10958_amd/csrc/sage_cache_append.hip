@@ -28,11 +28,6 @@ struct AppendParams {
   FastDiv by_hkv, by_blocks;
 };
 
-// Larger of two pairs of 16-bit magnitudes, as numbers of the same order.
-__device__ __forceinline__ unsigned larger_pair(unsigned a, unsigned b) {
-  typedef unsigned short v2u __attribute__((ext_vector_type(2)));
-  return __builtin_bit_cast(unsigned, __builtin_elementwise_max(__builtin_bit_cast(v2u, a), __builtin_bit_cast(v2u, b)));
-}
 // Four values (two dwords) as codes: divided by the scale, rounded to the nearest, all in one instruction for two.
 template <bool BF16> __device__ __forceinline__ unsigned codes_of(unsigned a, unsigned b, float scale) {
   typedef short v2s __attribute__((ext_vector_type(2)));
@@ -47,12 +42,6 @@ template <bool BF16> __device__ __forceinline__ unsigned codes_of(unsigned a, un
     r = __builtin_amdgcn_cvt_scalef32_pk_fp8_f16(r, __builtin_bit_cast(v2h, b), scale, true);
   }
   return __builtin_bit_cast(unsigned, r);
-}
-// A 16-bit magnitude, of a value that is not finite nothing.
-template <bool BF16> __device__ __forceinline__ unsigned finite_magnitude(unsigned h) {
-  constexpr unsigned EXP = BF16 ? 0x7f80 : 0x7c00;
-  h &= 0x7fff;
-  return h < EXP ? h : 0;
 }
 
 template <bool BF16, int D, bool WIDE>
@@ -95,20 +84,19 @@ __global__ void __launch_bounds__(256) k_append(const AppendParams p) {
       }
     }
   }
-  auto of_all = [](unsigned m) { return (unsigned)(int)wave_max((float)max(m & 0xffff, m >> 16)); };
 #pragma unroll
   for (int s = 0; s < STEPS; ++s)
 #pragma unroll
     for (int y = 0; y < 4; ++y) most = larger_pair(most, v[s][y] & 0x7fff7fff);
-  most = of_all(most);
+  most = largest_of_all(most);
   const bool finite = most < (BF16 ? 0x7f80u : 0x7c00u);
   if (!finite) {                                   // (the same, of what is finite)
     most = 0;
 #pragma unroll
     for (int s = 0; s < STEPS; ++s)
 #pragma unroll
-      for (int y = 0; y < 4; ++y) most = larger_pair(most, finite_magnitude<BF16>(v[s][y] & 0xffff) | finite_magnitude<BF16>(v[s][y] >> 16) << 16);
-    most = of_all(most);
+      for (int y = 0; y < 4; ++y) most = larger_pair(most, finite_pair<BF16>(v[s][y]));
+    most = largest_of_all(most);
   }
   const unsigned bits = __float_as_uint(load16<BF16>((unsigned short)most));
   const int fits = max((int)(bits >> 23) - 8 + ((bits & 0x7fffff) > 0x600000 ? 1 : 0), 63);

@@ -2,6 +2,7 @@
 #pragma once
 #include "sage_attn.h"
 #include "sage_ops.h"
+#include "sage_quant.h"
 
 #include <cmath>
 
@@ -25,6 +26,18 @@ __device__ __forceinline__ long long pool_block(const PagedCache& c, int b, int 
 }
 // A scale byte as the FP32 number 2^(byte - 127); 255 is NaN.
 __device__ __forceinline__ float scale_of(unsigned byte) { return byte == 0 ? 0x1p-127f : byte == 255 ? NAN : __uint_as_float(byte << 23); }
+
+// Magnitudes of 16-bit values are numbers of the same order.  The larger of two pairs; a pair without what is not finite; the largest of all lanes' pairs.
+__device__ __forceinline__ unsigned larger_pair(unsigned a, unsigned b) {
+  typedef unsigned short v2u __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(unsigned, __builtin_elementwise_max(__builtin_bit_cast(v2u, a), __builtin_bit_cast(v2u, b)));
+}
+template <bool BF16> __device__ __forceinline__ unsigned finite_pair(unsigned two) {
+  constexpr unsigned EXP = BF16 ? 0x7f80 : 0x7c00;
+  const unsigned lo = two & 0x7fff, hi = two >> 16 & 0x7fff;
+  return (lo < EXP ? lo : 0) | (hi < EXP ? hi : 0) << 16;
+}
+__device__ __forceinline__ unsigned largest_of_all(unsigned two) { return (unsigned)(int)wave_max((float)max(two & 0xffff, two >> 16)); }
 
 // The shape of a cache, checked; every offset into it stays within 48 bits.
 inline int cache_shape(PagedCache* c, int B, int Hkv, int d, int n_pages, int page, int max_pages) {
