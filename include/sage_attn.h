@@ -523,7 +523,7 @@ typedef struct sage_attn_paged_args {
   int B, H, H_kv, N, d;
   int n_pages, page, max_pages;
   int causal, window, sink; /* window 0: none; sink counts only with a window */
-  float sm_scale;           /* <= 0 means 1/sqrt(d) */
+  float sm_scale;           /* <= 0 means 1/sqrt(d); 2.3e38 at most */
   int dtype, layout;
   int clear;                /* SAGE_CLEAR_OUT, SAGE_CLEAR_LSE: places behind q_lens are set to zeros there instead of staying as they were */
   void* workspace;          /* device, 256-byte aligned; may be NULL where the size is 0 */

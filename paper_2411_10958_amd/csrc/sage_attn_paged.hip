@@ -182,6 +182,7 @@ __global__ void __launch_bounds__((paged_threads<D, COLS>()), (paged_occupancy<D
   // is copied after them.  Half of the lanes are refilled every 8 tiles.
   int at_lo = -1, at_hi = -1, token0 = 0;        // (no page, or past the last block: -1); the block's first token
   unsigned about = 0;                             // its scales, K's and V's, and from bit 16 on whether there is one and whether all rows see all of it
+  float factor = 0.0f;                            // kappa times K's
   auto fetch = [&](int j, int from, int to) __attribute__((always_inline)) {      // lanes from .. to - 1, the first of them tile j's first block
     const int i = 4 * j + lane - from;
     if (lane < from || lane >= to) return;
@@ -289,10 +290,11 @@ __global__ void __launch_bounds__((paged_threads<D, COLS>()), (paged_occupancy<D
     else return mfma16_small<BF16>(x, y, c);
   };
 
-  // One block: scores, weights and their product with V.  PART: some row does not see some token of it, its values may not fit the 16-bit type or its scores may be FAR from zero.
+  // One block: scores, weights and their product with V.  PART: some row does not see some token of it, its values may not fit the 16-bit type, its scores may be FAR from zero or kappa times
+  // its K scale is beyond FP32 (then kk is kappa and lift the scale).
   constexpr unsigned FITS = BF16 ? 246 : 134;      // 448 2^119 and 448 2^7 are numbers of the type
   constexpr float FAR = 16777216.0f;              // 2^24
-  auto attend = [&](auto partly, unsigned base, int t0, float kk, int ev) __attribute__((always_inline)) {
+  auto attend = [&](auto partly, unsigned base, int t0, float kk, float lift, int ev) __attribute__((always_inline)) {
     constexpr bool PART = decltype(partly)::value;
     const float vs = scale_of(PART ? min((unsigned)ev, FITS) : (unsigned)ev);
     const unsigned va = base + v_at;              // (a block's first byte has its low bits zero: steps to other pieces need no address kept over the loop)
@@ -332,6 +334,9 @@ __global__ void __launch_bounds__((paged_threads<D, COLS>()), (paged_occupancy<D
     for (int i = 0; i < NSC; ++i) sc[i] = tile[i / AV][i % AV];
     unsigned seen = 0xffff;                       // bit i: my row sees score i's token
     if constexpr (PART) {
+      if (lift != 1.0f)
+#pragma unroll
+        for (int i = 0; i < NSC; ++i) sc[i] *= lift;
       seen = 0;
 #pragma unroll
       for (int i = 0; i < NSC; ++i) {
@@ -461,10 +466,12 @@ __global__ void __launch_bounds__((paged_threads<D, COLS>()), (paged_occupancy<D
     if constexpr (SHARED) __builtin_amdgcn_s_barrier();      // tile j is there
     asm volatile("" ::: "memory");
     if (((j - j0) & 7) == 0) {
-      // Values that may not fit the 16-bit type, and scores that may be far from zero, go the way of partly seen blocks.
+      // Values that may not fit the 16-bit type, scores that may be far from zero and factors beyond FP32 go the way of partly seen blocks.
       const unsigned ek = s_scale[wave][0][lane] & 255, ev = s_scale[wave][1][lane] & 255;
-      const bool all = (ev <= FITS || ev == 255) && !(reach * scale_of(ek) >= 0.5f * FAR) && token0 + BLOCK <= first.to && (token0 >= last.from || token0 + BLOCK <= first.sink);
-      about = at_hi < 0 ? 0 : ek | ev << 8 | 1u << 16 | (unsigned)all << 17;
+      const bool all = (ev <= FITS || ev == 255) && !(reach * scale_of(ek) >= 0.5f * FAR) && p.kappa * scale_of(ek) != INFINITY && token0 + BLOCK <= first.to && (token0 >= last.from || token0 + BLOCK <= first.sink);
+      const float by_scale = p.kappa * scale_of(ek);
+      about = at_hi < 0 ? 0 : ek | (ev == 255 ? 127 : ev) << 8 | 1u << 16 | (unsigned)all << 17;
+      factor = ev == 255 ? NAN : by_scale == INFINITY ? p.kappa : by_scale;      // a NaN among the scales makes the rows NaN that see the block, through kk
     }
     if (active) {
       // Blocks that all rows see whole first, then the others.  (In one loop, or with a way round the products, the outputs are copied from register to register for each block.)
@@ -477,9 +484,10 @@ __global__ void __launch_bounds__((paged_threads<D, COLS>()), (paged_occupancy<D
       }
       auto block = [&](auto partly, int x) __attribute__((always_inline)) {
         const int at_lane = ((j - j0) & 15) * 4 + x;
-        const unsigned w = (unsigned)__builtin_amdgcn_readlane((int)about, at_lane), ek = w & 255, ev = w >> 8 & 255;
-        const bool nan = ev == 255;               // a NaN among the scales makes the rows NaN that see the block, through kk
-        attend(partly, lds0 + (unsigned)(stage * PT_BLOCKS + x) * (2 * BYTES), __builtin_amdgcn_readlane(token0, at_lane), nan ? NAN : p.kappa * scale_of(ek), nan ? 127 : (int)ev);
+        const unsigned w = (unsigned)__builtin_amdgcn_readlane((int)about, at_lane);
+        const float kk = __uint_as_float((unsigned)__builtin_amdgcn_readlane((int)__float_as_uint(factor), at_lane));
+        const float lift = decltype(partly)::value && p.kappa * scale_of(w & 255) == INFINITY ? scale_of(w & 255) : 1.0f;
+        attend(partly, lds0 + (unsigned)(stage * PT_BLOCKS + x) * (2 * BYTES), __builtin_amdgcn_readlane(token0, at_lane), kk, lift, (int)(w >> 8 & 255));
       };
 #pragma unroll 1
       for (; whole != 0; whole &= whole - 1) block(std::false_type{}, __builtin_ctz(whole));
@@ -729,6 +737,7 @@ int paged_params(const sage_attn_paged_args* a, PagedParams* p, bool need_io) {
   p->clear = a->q_lens ? a->clear : 0;
   p->causal = a->causal; p->window = std::min(a->window, MAX_TOKENS * 2); p->sink = std::min(a->sink, MAX_TOKENS);
   p->kappa = (a->sm_scale > 0.0f ? a->sm_scale : (float)(1.0 / std::sqrt((double)a->d))) * LOG2E;
+  if (!std::isfinite(p->kappa)) return SAGE_ERR_INVALID_ARG;
   choose_chunks(p, a->d);
   if (((long long)p->units + 7) / 8 * 8 * p->rt * 512 > MAX_THREADS) return SAGE_ERR_UNSUPPORTED;
   p->by_rt8 = fast_div(8u * p->rt); p->by_s = fast_div(p->S); p->by_hkv = fast_div(a->H_kv); p->by_g = fast_div(p->G);
