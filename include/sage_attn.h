@@ -506,7 +506,7 @@ int sage_cache_append(const sage_cache_append_args* args);
  * those behind are not read and their places in out and lse stay as they were.  Query r stands at p = max(len - q_len, 0) + r.  causal: it
  * sees the tokens t <= p; with window > 0, of these, t > p - window and, whatever the window, the first `sink` of the sequence.  Without causal it sees all
  * len (and window must be 0).  What no query sees is not read: a sequence's pages behind its window can be given back.  A query that sees no token gets zeros
- * and lse = -inf; a NaN reaches only queries that see its token.
+ * and lse = -inf; one whose scores are all -inf gets NaN, as 0 / 0 says, and lse = -inf.  A NaN reaches only queries that see its token.
  * out may be q; other overlaps of out, lse or the workspace are refused. */
 enum { SAGE_CLEAR_OUT = 1, SAGE_CLEAR_LSE = 2 };
 typedef struct sage_attn_paged_args {

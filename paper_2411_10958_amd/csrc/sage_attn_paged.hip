@@ -270,6 +270,7 @@ __global__ void __launch_bounds__((paged_threads<D, COLS>()), (paged_occupancy<D
 #pragma unroll
     for (int v = 0; v < AV; ++v) o[c][v] = 0.0f;
   float mx = -INFINITY, l = 0.0f;                 // running maximum (of all parts; fp16: less 14) and this part's sum
+  unsigned long long saw = 0;                     // lanes that have seen a token, whatever its score
 
   // Where my operands start in a block; steps to other pieces are exclusive ors.  K: rows in an order that gives each part of the lanes the scores of the tokens whose weights the
   // second product wants of it: tokens 8 part + 0..7 (32 columns: and 16 on), score i of a lane being token_of(i).  V: the transposed read gives lane l channel l % 16 of the
@@ -344,6 +345,7 @@ __global__ void __launch_bounds__((paged_threads<D, COLS>()), (paged_occupancy<D
         seen |= (unsigned)see << i;
         sc[i] = see ? sc[i] : -INFINITY;
       }
+      saw |= __ballot(seen != 0);
     }
     float top = -INFINITY;
 #pragma unroll
@@ -489,6 +491,7 @@ __global__ void __launch_bounds__((paged_threads<D, COLS>()), (paged_occupancy<D
         const float lift = decltype(partly)::value && p.kappa * scale_of(w & 255) == INFINITY ? scale_of(w & 255) : 1.0f;
         attend(partly, lds0 + (unsigned)(stage * PT_BLOCKS + x) * (2 * BYTES), __builtin_amdgcn_readlane(token0, at_lane), kk, lift, (int)(w >> 8 & 255));
       };
+      if (whole != 0) saw = ~0ull;
 #pragma unroll 1
       for (; whole != 0; whole &= whole - 1) block(std::false_type{}, __builtin_ctz(whole));
 #pragma unroll 1
@@ -506,6 +509,10 @@ __global__ void __launch_bounds__((paged_threads<D, COLS>()), (paged_occupancy<D
     }
   }
   l = WIDE ? half_sum(l) : quarter_sum(l);
+  // Scores of minus infinity alone: the sum of 1 tells them from no token at all, and goes with a weight of zero beside a finite maximum
+  saw |= saw >> 32 | saw << 32;
+  if constexpr (!WIDE) saw |= saw >> 16 | saw << 48;
+  if (mx == -INFINITY && l == 0.0f && (saw >> lane & 1)) l = 1.0f;
 
   // ---- the key groups of the same rows into one, each wavefront's share of the channels: units of four of them a lane, unit u being channels (256 / COLS) u + 4 part + 0..3
   constexpr int ALL = CT * AV / 4, UN = ALL / KG;
@@ -534,7 +541,7 @@ __global__ void __launch_bounds__((paged_threads<D, COLS>()), (paged_occupancy<D
       l = 0.0f;
 #pragma unroll
       for (int k = 0; k < KG; ++k) {
-        a[k] = __builtin_amdgcn_exp2f(s_ml[(rg * KG + k) * CG + cg][2 * col] - (m == -INFINITY ? 0.0f : m));
+        a[k] = m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(s_ml[(rg * KG + k) * CG + cg][2 * col] - m);
         l = __fmaf_rn(a[k], s_ml[(rg * KG + k) * CG + cg][2 * col + 1], l);
       }
       mx = m;
@@ -553,7 +560,7 @@ __global__ void __launch_bounds__((paged_threads<D, COLS>()), (paged_occupancy<D
   if (!active || rg * COLS + col >= nr) return;
   if constexpr (ONE) {
     const bool none = mx == -INFINITY && l == 0.0f;      // no token at all: zeros
-    const float inv = none ? 0.0f : __fdiv_rn(1.0f, l);
+    const float inv = none ? 0.0f : mx == -INFINITY ? NAN : __fdiv_rn(1.0f, l);
     if (p.lse && part == 0 && kg == 0 && cg == 0) p.lse[((size_t)b * p.H + hkv * p.G + rh) * p.N + rn] = none ? -INFINITY : LN2 * (mx + __builtin_amdgcn_logf(l));
     unsigned short* y = p.out + qrow + 4 * part;
 #pragma unroll
@@ -602,7 +609,7 @@ __global__ void __launch_bounds__(256) k_paged_merge(const PagedParams p) {
 #pragma unroll
   for (int x = 0; x < MERGE_PER_LANE; ++x) {
     const float ls = w[x];
-    w[x] = ms[x] == -INFINITY && ls == 0.0f ? -1.0f : __builtin_amdgcn_exp2f(ms[x] - m);    // (-1: no token is seen: O may not even be there)
+    w[x] = ms[x] == -INFINITY && ls == 0.0f ? -1.0f : m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(ms[x] - m);    // (-1: no token is seen: O may not even be there)
     if (w[x] != -1.0f) l = __fmaf_rn(w[x], ls, l);
   }
 #pragma unroll
@@ -634,7 +641,7 @@ __global__ void __launch_bounds__(256) k_paged_merge(const PagedParams p) {
   if (grp != 0) return;
   const unsigned h = hkv * p.G + g;
   const bool none = m == -INFINITY && l == 0.0f;  // no token at all: zeros
-  const float inv = none ? 0.0f : __fdiv_rn(1.0f, l);
+  const float inv = none ? 0.0f : m == -INFINITY ? NAN : __fdiv_rn(1.0f, l);
   if (p.lse && c == 0) p.lse[((size_t)b * p.H + h) * p.N + n] = none ? -INFINITY : LN2 * (m + __builtin_amdgcn_logf(l));
   unsigned short* y = p.out + row_offset(p.qm, head_offset_of(p.qm, (int)b, (int)h), (int)n) + c;
   *reinterpret_cast<uint2*>(y) = make_uint2(pack16x2<BF16>(acc[0] * inv, acc[1] * inv), pack16x2<BF16>(acc[2] * inv, acc[3] * inv));
@@ -668,14 +675,14 @@ __global__ void __launch_bounds__(256) k_paged_merge_few(const PagedParams p) {
 #pragma unroll
   for (int s = 0; s < FEW; ++s) {
     if (ml[s].x == -INFINITY && ml[s].y == 0.0f) continue;      // (no token is seen: O may not even be there)
-    const float w = __builtin_amdgcn_exp2f(ml[s].x - m);
+    const float w = m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(ml[s].x - m);
     l = __fmaf_rn(w, ml[s].y, l);
 #pragma unroll
     for (int y = 0; y < 4; ++y) acc[y] = __fmaf_rn(w, o4[s][y], acc[y]);
   }
   const unsigned h = hkv * p.G + g;
   const bool none = m == -INFINITY && l == 0.0f;  // no token at all: zeros
-  const float inv = none ? 0.0f : __fdiv_rn(1.0f, l);
+  const float inv = none ? 0.0f : m == -INFINITY ? NAN : __fdiv_rn(1.0f, l);
   if (p.lse && c == 0) p.lse[((size_t)b * p.H + h) * p.N + n] = none ? -INFINITY : LN2 * (m + __builtin_amdgcn_logf(l));
   unsigned short* y = p.out + row_offset(p.qm, head_offset_of(p.qm, (int)b, (int)h), (int)n) + c;
   *reinterpret_cast<uint2*>(y) = make_uint2(pack16x2<BF16>(acc[0] * inv, acc[1] * inv), pack16x2<BF16>(acc[2] * inv, acc[3] * inv));
