@@ -174,14 +174,19 @@ template <bool INTER> __device__ __forceinline__ bool angles_of(const NormParams
   }
   return any;
 }
-// A thread's pairs turned, or turned back.  (A value that is not finite makes its neighbour NaN where nothing is turned: the row has a NaN or zeros in all other
-// places anyway.)
+// A product that is zero where a factor is, whatever the other one; else the ordinary one, small results included.
+__device__ __forceinline__ float product_or_zero(float x, float y) {
+  float r;
+  asm("v_mul_legacy_f32 %0, %1, %2" : "=v"(r) : "v"(x), "v"(y));
+  return r;
+}
+// A thread's pairs turned, or turned back.  Where nothing is turned the sine is zero, and a partner that is not finite has no part in the result.
 template <bool INTER, bool BACK> __device__ __forceinline__ void turn(float (&x)[16], const float (&c)[8], const float (&s)[8]) {
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const float f = x[first_of<INTER>(i)], g = x[second_of<INTER>(i)], t = BACK ? -s[i] : s[i];
-    x[first_of<INTER>(i)] = __fmaf_rn(f, c[i], -__fmul_rn(g, t));
-    x[second_of<INTER>(i)] = __fmaf_rn(g, c[i], __fmul_rn(f, t));
+    const float f = x[first_of<INTER>(i)], g = x[second_of<INTER>(i)], fs = product_or_zero(f, s[i]), gs = product_or_zero(g, s[i]);
+    x[first_of<INTER>(i)] = __fmaf_rn(f, c[i], BACK ? gs : -gs);
+    x[second_of<INTER>(i)] = __fmaf_rn(g, c[i], BACK ? -fs : fs);
   }
 }
 
