@@ -414,7 +414,7 @@ int sage_cache_evict(const sage_cache_evict_args* args);
  * attention.  Every row x of d channels becomes  R(x / sqrt(mean(x^2) + eps) * weight)  with R the rotation of sage_rope (its positions,
  * frequencies and pairs); rounded once, at the end.  Sums are FP32, of rows brought into its range by a power of two where their squares
  * leave it: rows of the smallest and the largest values are normed like others, here and in the gradient.  A value that is not finite reaches its own row only, and a row of zeros with
- * eps = 0 is 0 / 0.  B N is 2^26 - 4 at most.  In place and views: as sage_rope; outputs that
+ * eps = 0 is 0 / 0.  N is 2^24 at most, B N 2^26 - 4, B, H and H_kv 65535.  In place and views: as sage_rope; outputs that
  * share a value with a weight, the frequencies or the positions are refused. */
 enum { SAGE_WEIGHT_FP32 = 0, SAGE_WEIGHT_SAME = 1 };
 typedef struct sage_qk_norm_rope_args {
@@ -474,6 +474,7 @@ int sage_qk_norm_rope_bwd(const sage_qk_norm_rope_bwd_args* args);
  * its block's scale.  E4M3's step is relative, so powers of two lose nothing to finer scales, and dividing by them is exact: a code is its value
  * correctly rounded.  kv_lens counts the tokens of each sequence, up to max_pages * page.  A number that is no page of the pool (-1, say: a page that was
  * given back) stands for no page: its tokens are not there - never written, and seen by no query.  Sequences may share pages.
+ * max_pages * page and N are 2^24 at most, B H_kv 65535, n_pages * H_kv * page * d 2^47.
  *
  * The append of a call's new tokens: of the N rows of sequence b in k and v the first new_lens[b] (NULL: N) are new; they are the
  * last of the kv_lens[b] tokens that the sequence has WITH them (kv_lens as the attention call after it takes it; more new than that: the first ones are left out).
@@ -507,7 +508,8 @@ int sage_cache_append(const sage_cache_append_args* args);
  * sees the tokens t <= p; with window > 0, of these, t > p - window and, whatever the window, the first `sink` of the sequence.  Without causal it sees all
  * len (and window must be 0).  What no query sees is not read: a sequence's pages behind its window can be given back.  A query that sees no token gets zeros
  * and lse = -inf; one whose scores are all -inf gets NaN, as 0 / 0 says, and lse = -inf.  A NaN reaches only queries that see its token.
- * out may be q; other overlaps of out, lse or the workspace are refused. */
+ * FP32 is also what limits them: sums of q times codes (before K's scale), scores, and sums of weights (of which the largest is 1; fp16: 2^14 to 2^15) times values are infinite beyond 3.4e38.
+ * B H N is 2^24 at most, B H 65535.  out may be q; other overlaps of out, lse or the workspace are refused. */
 enum { SAGE_CLEAR_OUT = 1, SAGE_CLEAR_LSE = 2 };
 typedef struct sage_attn_paged_args {
   const void* q;            /* device, [B, H, N, d] or [B, N, H, d] */
