@@ -9,8 +9,8 @@
 //
 // With few queries it reads the cache and nothing else should bound it.  A block's K (or V) is 32 d contiguous bytes whatever the size of a page; each wavefront copies its own blocks
 // into LDS, two tiles ahead.  Where all queries of a KV head are 32 rows at most (256 channels: 16), it also attends to just those blocks, with no barrier; more rows are divided over the wavefronts.
-// 32 heads of 128 over 8: 16 sequences of up to 32768 tokens 123 us (5.7 TB/s), 32 in a window of 4096 47 us (5.8 TB/s).  Chunks of 512 queries over 2 x 16384 tokens 266 us (0.82 PFLOP/s), bound by
-// vector issue: of some 180 instructions of a block 64 widen its codes.  A lone workgroup takes 5 us to its first tile and from its last, and 0.65 us a tile.
+// 32 heads of 128 over 8: 16 sequences of up to 32768 tokens 115 to 124 us by card (5.7 to 6.0 TB/s), 32 in a window of 4096 47.6 us (5.7 TB/s).  Chunks of 512 queries over 2 x 16384 tokens 263 to 285 us
+// (0.77 to 0.83 PFLOP/s), bound by vector issue: of some 170 instructions of a block 64 widen its codes.  A lone workgroup takes 5 us to its first tile and from its last, and 0.65 us a tile.
 #include "sage_paged.h"
 
 #include <algorithm>
@@ -202,7 +202,8 @@ __global__ void __launch_bounds__((paged_threads<D, COLS>()), (paged_occupancy<D
 #pragma unroll
     for (int x = 0; x < 4; ++x) use_now(q[st][x]);
   // What a score (to the base 2) of these rows may reach, for a K scale of 1: the largest magnitude of a query times 448, d of them.  Infinities and NaN make their own scores whatever they make.
-  // (32 caches in a window of 4096 take 0.3 us more for it; the far scores looked for block by block, 512 queries 2 x 16384 tokens 4.)
+  // (32 caches in a window of 4096 take 0.3 us more for it.  Looked for block by block instead, far scores cost chunks of 512 queries 2 %.  Where all blocks are such, these take 675 us for 285, a step over
+  // 32768 tokens 147 for 126.)
   unsigned most = 0;
 #pragma unroll
   for (int st = 0; st < KS; ++st)

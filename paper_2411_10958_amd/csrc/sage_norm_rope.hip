@@ -5,7 +5,7 @@
 // in one go, so every value is read once.
 // A row is d / 16 neighbouring threads, each with 8 pairs of channels in registers.  A workgroup takes the heads of a few tokens: it works their angles out
 // once, an angle a thread, and leaves them and the weights in LDS (each thread with its own angles, and one row in flight: 77 and 115 us where this takes 62 and 53).  Only bytes bound
-// it, 4 a value forward and 6 backward: 4 x 4096 tokens of 40 heads of 128 62 us (5.4 TB/s), the gradient of 2 x 4096 53 us (5.0 TB/s in its first kernel).
+// it, 4 a value forward and 6 backward: 4 x 4096 tokens of 40 heads of 128 62 us (5.4 TB/s), the gradient of 2 x 4096 54 us (4.9 TB/s in its first kernel).
 #include "sage_attn.h"
 #include "sage_quant.h"
 #include "sage_rows.h"
