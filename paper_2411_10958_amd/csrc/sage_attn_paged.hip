@@ -181,7 +181,8 @@ __global__ void __launch_bounds__((paged_threads<D, COLS>()), (paged_occupancy<D
   // ---- where the next 16 tiles' blocks are in the pool, one block a lane, and their scales, which go to LDS like the blocks do, so that no wait for them is one for what
   // is copied after them.  Half of the lanes are refilled every 8 tiles.
   int at_lo = -1, at_hi = -1, token0 = 0;        // (no page, or past the last block: -1); the block's first token
-  unsigned about = 0;                             // its scales, K's and V's, and from bit 16 on whether there is one and whether all rows see all of it
+  unsigned about = 0;                             // its scales, K's and V's, and from bit 16 on whether there is one, whether all rows see all of it and
+  constexpr unsigned OUTER = 1u << 18;            // whether its scores may be FAR from zero, or kappa times K's scale is beyond FP32
   float factor = 0.0f;                            // kappa times K's
   auto fetch = [&](int j, int from, int to) __attribute__((always_inline)) {      // lanes from .. to - 1, the first of them tile j's first block
     const int i = 4 * j + lane - from;
@@ -264,7 +265,6 @@ __global__ void __launch_bounds__((paged_threads<D, COLS>()), (paged_occupancy<D
   };
   copy(j0, 0);
   bool next = j0 + 1 < j1 && copy(j0 + 1, 1);     // whether tile j + 1 is on its way
-
   acc_t o[CT];
 #pragma unroll
   for (int c = 0; c < CT; ++c)
@@ -292,12 +292,13 @@ __global__ void __launch_bounds__((paged_threads<D, COLS>()), (paged_occupancy<D
     else return mfma16_small<BF16>(x, y, c);
   };
 
-  // One block: scores, weights and their product with V.  PART: some row does not see some token of it, its values may not fit the 16-bit type, its scores may be FAR from zero or kappa times
-  // its K scale is beyond FP32 (then kk is kappa and lift the scale).
+  // One block: scores, weights and their product with V.  w: its `about`.  PART: some row does not see some token of it, its values may not fit the 16-bit type or it is OUTER; kk: kappa times
+  // K's scale, or where that is beyond FP32 kappa alone, and the products are multiplied by the scale first.
   constexpr unsigned FITS = BF16 ? 246 : 134;      // 448 2^119 and 448 2^7 are numbers of the type
   constexpr float FAR = 16777216.0f;              // 2^24
-  auto attend = [&](auto partly, unsigned base, int t0, float kk, float lift, int ev) __attribute__((always_inline)) {
+  auto attend = [&](auto partly, unsigned base, int t0, float kk, unsigned w) __attribute__((always_inline)) {
     constexpr bool PART = decltype(partly)::value;
+    const int ev = (int)(w >> 8 & 255);
     const float vs = scale_of(PART ? min((unsigned)ev, FITS) : (unsigned)ev);
     const unsigned va = base + v_at;              // (a block's first byte has its low bits zero: steps to other pieces need no address kept over the loop)
     acc_t tile[ST];
@@ -336,9 +337,11 @@ __global__ void __launch_bounds__((paged_threads<D, COLS>()), (paged_occupancy<D
     for (int i = 0; i < NSC; ++i) sc[i] = tile[i / AV][i % AV];
     unsigned seen = 0xffff;                       // bit i: my row sees score i's token
     if constexpr (PART) {
-      if (lift != 1.0f)
+      if (w & OUTER) {
+        const float first_by = p.kappa * scale_of(w & 255) == INFINITY ? scale_of(w & 255) : 1.0f;
 #pragma unroll
-        for (int i = 0; i < NSC; ++i) sc[i] *= lift;
+        for (int i = 0; i < NSC; ++i) sc[i] *= first_by;
+      }
       seen = 0;
 #pragma unroll
       for (int i = 0; i < NSC; ++i) {
@@ -366,11 +369,11 @@ __global__ void __launch_bounds__((paged_threads<D, COLS>()), (paged_occupancy<D
       mx = m_new;
     }
     // m is a rounded product and a weight's exponent is formed from the exact one, so the largest weight is 2^(that rounding): as good as 1, but from 2^24 on a whole step and soon anything.
-    // There the products are rounded like m, and the largest weight is 1.
+    // There the products are rounded like m, and the largest weight is 1.  (Under such an m of another block all weights of this one are zero.)
     float by = kk;
     if constexpr (PART) {
-      const bool is_far = fabsf(m) >= FAR;
-      if (__ballot(is_far) != 0) {
+      if (w & OUTER) {
+        const bool is_far = fabsf(m) >= FAR;
 #pragma unroll
         for (int i = 0; i < NSC; ++i) sc[i] = is_far ? sc[i] * kk : sc[i];
         by = is_far ? 1.0f : kk;
@@ -471,9 +474,10 @@ __global__ void __launch_bounds__((paged_threads<D, COLS>()), (paged_occupancy<D
     if (((j - j0) & 7) == 0) {
       // Values that may not fit the 16-bit type, scores that may be far from zero and factors beyond FP32 go the way of partly seen blocks.
       const unsigned ek = s_scale[wave][0][lane] & 255, ev = s_scale[wave][1][lane] & 255;
-      const bool all = (ev <= FITS || ev == 255) && !(reach * scale_of(ek) >= 0.5f * FAR) && p.kappa * scale_of(ek) != INFINITY && token0 + BLOCK <= first.to && (token0 >= last.from || token0 + BLOCK <= first.sink);
       const float by_scale = p.kappa * scale_of(ek);
-      about = at_hi < 0 ? 0 : ek | (ev == 255 ? 127 : ev) << 8 | 1u << 16 | (unsigned)all << 17;
+      const bool outer = reach * scale_of(ek) >= 0.5f * FAR || by_scale == INFINITY;
+      const bool all = (ev <= FITS || ev == 255) && !outer && token0 + BLOCK <= first.to && (token0 >= last.from || token0 + BLOCK <= first.sink);
+      about = at_hi < 0 ? 0 : ek | (ev == 255 ? 127 : ev) << 8 | 1u << 16 | (unsigned)all << 17 | (outer ? OUTER : 0);
       factor = ev == 255 ? NAN : by_scale == INFINITY ? p.kappa : by_scale;      // a NaN among the scales makes the rows NaN that see the block, through kk
     }
     if (active) {
@@ -482,15 +486,14 @@ __global__ void __launch_bounds__((paged_threads<D, COLS>()), (paged_occupancy<D
 #pragma unroll
       for (int x = kg; x < PT_BLOCKS; x += KG) {
         const unsigned w = (unsigned)__builtin_amdgcn_readlane((int)about, ((j - j0) & 15) * 4 + x) >> 16;
-        whole |= (w >> 1) << x;
+        whole |= (w >> 1 & 1) << x;
         others |= (w & ~(w >> 1) & 1) << x;
       }
       auto block = [&](auto partly, int x) __attribute__((always_inline)) {
         const int at_lane = ((j - j0) & 15) * 4 + x;
         const unsigned w = (unsigned)__builtin_amdgcn_readlane((int)about, at_lane);
         const float kk = __uint_as_float((unsigned)__builtin_amdgcn_readlane((int)__float_as_uint(factor), at_lane));
-        const float lift = decltype(partly)::value && p.kappa * scale_of(w & 255) == INFINITY ? scale_of(w & 255) : 1.0f;
-        attend(partly, lds0 + (unsigned)(stage * PT_BLOCKS + x) * (2 * BYTES), __builtin_amdgcn_readlane(token0, at_lane), kk, lift, (int)(w >> 8 & 255));
+        attend(partly, lds0 + (unsigned)(stage * PT_BLOCKS + x) * (2 * BYTES), __builtin_amdgcn_readlane(token0, at_lane), kk, w);
       };
       if (whole != 0) saw = ~0ull;
 #pragma unroll 1
