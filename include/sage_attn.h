@@ -413,7 +413,7 @@ int sage_cache_evict(const sage_cache_evict_args* args);
 /* Norm of every head's queries and keys, and their rotation, in one pass - what models with normalised queries and keys do in front of
  * attention.  Every row x of d channels becomes  R(x / sqrt(mean(x^2) + eps) * weight)  with R the rotation of sage_rope (its positions,
  * frequencies and pairs); rounded once, at the end.  Sums are FP32, of rows brought into its range by a power of two where their squares
- * leave it: rows of the smallest and the largest values are normed like others, here and in the gradient.  A value that is not finite reaches its own row only, and a row of zeros with
+ * leave it: rows of the smallest and the largest values are normed like others, here and in the gradient (whose products g w x are FP32).  A value that is not finite reaches its own row only, and a row of zeros with
  * eps = 0 is 0 / 0.  N is 2^24 at most, B N 2^26 - 4, B, H and H_kv 65535.  In place and views: as sage_rope; outputs that
  * share a value with a weight, the frequencies or the positions are refused. */
 enum { SAGE_WEIGHT_FP32 = 0, SAGE_WEIGHT_SAME = 1 };

@@ -9,8 +9,8 @@
 //
 // With few queries it reads the cache and nothing else should bound it.  A block's K (or V) is 32 d contiguous bytes whatever the size of a page; each wavefront copies its own blocks
 // into LDS, two tiles ahead.  Where all queries of a KV head are 32 rows at most (256 channels: 16), it also attends to just those blocks, with no barrier; more rows are divided over the wavefronts.
-// 32 heads of 128 over 8: 16 sequences of up to 32768 tokens 115 to 124 us by card (5.7 to 6.0 TB/s), 32 in a window of 4096 47.6 us (5.7 TB/s).  Chunks of 512 queries over 2 x 16384 tokens 263 to 285 us
-// (0.77 to 0.83 PFLOP/s), bound by vector issue: of some 170 instructions of a block 64 widen its codes.  A lone workgroup takes 5 us to its first tile and from its last, and 0.65 us a tile.
+// 32 heads of 128 over 8: 16 sequences of up to 32768 tokens 115 to 124 us by card (5.7 to 6.0 TB/s), 32 in a window of 4096 47.6 us (5.7 TB/s).  Chunks of 512 queries over 2 x 16384 tokens 263 to 288 us
+// (0.76 to 0.83 PFLOP/s), bound by vector issue: of some 170 instructions of a block 64 widen its codes.  A lone workgroup takes 5 us to its first tile and from its last, and 0.65 us a tile.
 #include "sage_paged.h"
 
 #include <algorithm>
